@@ -50,7 +50,10 @@ enum {
     BIRKHOFF4_ERR_LAUNCH = -10,   /* kernel launch failed (hipGetLastError) */
     BIRKHOFF4_ERR_VARIANT = -11,  /* unknown forward variant */
     BIRKHOFF4_ERR_ETA = -12,      /* eta not positive and finite */
-    BIRKHOFF4_ERR_CHANNELS = -13  /* stream width C negative or not a whole number of 16-byte chunks */
+    BIRKHOFF4_ERR_CHANNELS = -13, /* stream width C negative or not a whole number of 16-byte chunks */
+    BIRKHOFF4_ERR_EPS = -14,      /* eps negative, infinite or NaN */
+    BIRKHOFF4_ERR_WORK = -15,     /* the workspace is smaller than birkhoff*_pre_work says */
+    BIRKHOFF4_ERR_DROP = -16      /* dropout probability outside [0, 1) */
 };
 
 /* Forward kernel variants (birkhoff4_fwd_ex2). Both compute the same projection to the
@@ -285,6 +288,52 @@ int birkhoff8_mix_bwd(const float* P, const void* X, const void* dY, int x_dtype
  * anything otherwise. */
 int birkhoff8_mix_bwd_ex(const float* P, const void* X, const void* dY, int x_dtype, void* dX, float* dP, void* dH,
                          int dh_dtype, int64_t B, int64_t C, hipStream_t stream);
+
+/* How the layer reads its streams (Sec. 2.1: x <- H^res x + (H^post)^T F(H^pre x)): the
+ * coefficients of a token from its streams, and the branch's input U = H^pre x. With v the token's
+ * K = n C values (n = 4 here), N = n^2 + 2 n, r = (|v|^2 / K + eps)^(-1/2):
+ *   q = r W v,  l_j = alpha_g q_j + bias_j with g = 0 for rows j < n, 1 for n <= j < 2 n, else 2,
+ *   h^pre = sigmoid(l_0 .. l_{n-1}),  h = 2 sigmoid(l_n .. l_{2n-1}),  H = the other n^2 (row-major),
+ *   U = sum_i h^pre_i X_i.
+ *
+ * X      [B][n][C] streams in x_dtype (F32 or BF16); W [N][n C] in x_dtype too.
+ * alpha  [3] fp32, bias [N] fp32; eps >= 0 and finite (BIRKHOFF4_ERR_EPS).
+ * U      [B][C] output in x_dtype (bf16 rounded to nearest even); sums are fp32 throughout.
+ * h, H   [B][n], [B][n][n] fp32 outputs: what birkhoff4_post_fwd takes.
+ * q, rms [B][N], [B] fp32 outputs: q and r, which the backward needs.
+ * work   workspace of work_bytes >= birkhoff4_pre_work(B, C, x_dtype, 0) bytes, in use until the
+ *        call's work on `stream` has ended; its contents before and after mean nothing.
+ * C      > 0, a multiple of 8 for BF16 or 4 for F32, at most 2^24 (BIRKHOFF4_ERR_CHANNELS, _SIZE);
+ *        B at most 2^26.
+ * A token with a NaN or infinite value has NaN (or infinite) outputs; the others are not touched
+ * by it. The result does not depend on timing: no atomics, fixed orders of sums. */
+int birkhoff4_pre_fwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, float eps, void* U,
+                      float* h, float* H, float* q, float* rms, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream);
+
+/* Backward of birkhoff4_pre_fwd: from its inputs, q and rms, and the gradients dU [B][C] (x_dtype),
+ * dh [B][n], dH [B][n][n] (fp32) and E [B][n][C] (x_dtype; a gradient of the streams from
+ * elsewhere, added to dX), each of which may be NULL for zero, writes dX [B][n][C] and dW [N][n C]
+ * (x_dtype), dalpha [3] and dbias [N] (fp32). With B = 0 these sums are written as zeros, and only
+ * dW, dalpha and dbias need be there. work as above, of birkhoff4_pre_work(B, C, x_dtype, 1) bytes. */
+int birkhoff4_pre_bwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, const float* q,
+                      const float* rms, const void* dU, const float* dh, const float* dH, const void* E, void* dX,
+                      void* dW, float* dalpha, float* dbias, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream);
+
+/* Bytes of workspace of the forward (backward = 0) or the backward (1); a negative return code for
+ * sizes or a dtype that those calls refuse. */
+int64_t birkhoff4_pre_work(int64_t B, int64_t C, int x_dtype, int backward);
+
+/* The same for n = 8 streams: N = 80, H and dH [B][8][8]. */
+int birkhoff8_pre_fwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, float eps, void* U,
+                      float* h, float* H, float* q, float* rms, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream);
+int birkhoff8_pre_bwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, const float* q,
+                      const float* rms, const void* dU, const float* dh, const float* dH, const void* E, void* dX,
+                      void* dW, float* dalpha, float* dbias, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream);
+int64_t birkhoff8_pre_work(int64_t B, int64_t C, int x_dtype, int backward);
 
 /* Human-readable text for a return code (static storage). */
 const char* birkhoff4_strerror(int code);

@@ -17,6 +17,8 @@ a GPU, the calls raise.
     Y, P, _, _ = mix_fwd(H, X); dX, dH = mix_bwd(P, X, dY)  # residual mixing Y = P X (Sec. 2.1)
     Y = mix(H, X)                     # autograd-aware, gradients for H and X (4 or 8 streams)
     Y, P, _, _ = mix8_fwd(H8, X8); dX, dH = mix8_bwd(P, X8, dY)  # 8 streams per token
+    U, h, H, q, rms = pre_fwd(X, W, alpha, bias)  # the streams' coefficients and the branch's input
+    U, h, H, X = pre(X, W, alpha, bias)  # autograd-aware, gradients for all four (4 or 8 streams)
 """
 from __future__ import annotations
 
@@ -33,6 +35,7 @@ AUTO, THROUGHPUT, LATENCY = 0, 1, 2
 NOT_CONVERGED, NON_FINITE = -1, -2
 DEFAULT_TOL = 1e-6
 DEFAULT_MAX_ITER = 64
+DEFAULT_EPS = 1e-6
 
 _lib = None
 
@@ -77,10 +80,17 @@ def _load():
         "birkhoff8_mix_bwd": [vp, vp, vp, i32, vp, vp, i64, i64, st],
         "birkhoff4_version": [],
     }
+    for n in (4, 8):
+        sigs[f"birkhoff{n}_pre_fwd"] = [vp, vp, i32, vp, vp, f32, vp, vp, vp, vp, vp, vp, i64, i64, i64, st]
+        sigs[f"birkhoff{n}_pre_bwd"] = [vp, vp, i32] + [vp] * 13 + [i64, i64, i64, st]
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = ctypes.c_int
+    for n in (4, 8):
+        fn = getattr(lib, f"birkhoff{n}_pre_work")
+        fn.argtypes = [i64, i64, i32, i32]
+        fn.restype = i64
     lib.birkhoff4_strerror.argtypes = [ctypes.c_int]
     lib.birkhoff4_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -515,6 +525,105 @@ def mix(H: torch.Tensor, X: torch.Tensor, tol: float = DEFAULT_TOL, max_iter: in
     if H.dim() < 2 or H.shape[-1] not in (4, 8):
         raise ValueError(f"H must have shape [..., 4, 4] or [..., 8, 8], got {tuple(H.shape)}")
     return MixFn.apply(H, X, tol, max_iter)
+
+
+def _params(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor):
+    """Checks pre's streams [..., n, C] and parameters; returns (n, tokens, C)."""
+    n = X.shape[-2] if X.dim() >= 2 else 0
+    if n not in (4, 8):
+        raise ValueError(f"X must have shape [..., 4, C] or [..., 8, C], got {tuple(X.shape)}")
+    C = _streams(X, X.shape[:-2], "X", n)
+    rows = n * n + 2 * n
+    for t, name, shape, dtype in ((W, "W", (rows, n * C), X.dtype), (alpha, "alpha", (3,), torch.float32),
+                                  (bias, "bias", (rows,), torch.float32)):
+        _dense(t, name, shape, dtype, X)
+    return n, X.numel() // (n * C) if C else 0, C
+
+
+def _dense(t: torch.Tensor, name: str, shape, dtype: torch.dtype, like: torch.Tensor) -> None:
+    if not t.is_cuda:
+        raise Birkhoff4Error(f"{name} must be a GPU tensor (no CPU path)")
+    if t.dtype != dtype:
+        raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+    if tuple(t.shape) != tuple(shape) or not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous with shape {tuple(shape)}, got {tuple(t.shape)}")
+    _same_device(like, t)
+
+
+def _work(n: int, tokens: int, C: int, X: torch.Tensor, backward: bool) -> torch.Tensor:
+    """The call's own workspace: another call, or a captured graph, has another."""
+    size = getattr(_load(), f"birkhoff{n}_pre_work")(tokens, C, _dtype_code(X), int(backward))
+    if size < 0:
+        _check(size)
+    return torch.empty(size, dtype=torch.uint8, device=X.device)
+
+
+def pre_fwd(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, eps: float = DEFAULT_EPS):
+    """How a hyper-connection layer reads its streams, per token: with v the token's n C values
+    and r = (mean(v^2) + eps)^(-1/2), q = r W v and l = alpha_g q + bias (g: rows 0..n-1, n..2n-1,
+    the n^2 others), U = sum_i sigmoid(l_i) X_i is the branch's input, h = 2 sigmoid(l_n..) what
+    its output is written back with, and H = the last n^2 of l the logits of the residual mixing.
+
+    X: [..., n, C] float32 or bfloat16 streams, n = 4 or 8 (C a multiple of 8 for bfloat16, of 4
+    for float32); W: [n^2 + 2 n, n C] of X's dtype; alpha [3] and bias [n^2 + 2 n] float32.
+    Returns (U [..., C] like X, h [..., n], H [..., n, n], q [..., n^2 + 2 n], rms [...]), all but U
+    float32; q and rms are for pre_bwd."""
+    n, tokens, C = _params(X, W, alpha, bias)
+    lead = X.shape[:-2]
+    work = _work(n, tokens, C, X, False)
+    U = torch.empty(*lead, C, dtype=X.dtype, device=X.device)
+    h, H, q, rms = (torch.empty(*lead, *k, dtype=torch.float32, device=X.device)
+                    for k in ((n,), (n, n), (n * n + 2 * n,), ()))
+    _call(f"birkhoff{n}_pre_fwd", X, _ptr(X), _ptr(W), _dtype_code(X), _ptr(alpha), _ptr(bias), float(eps), _ptr(U),
+          _ptr(h), _ptr(H), _ptr(q), _ptr(rms), _ptr(work), work.numel(), tokens, C)
+    return U, h, H, q, rms
+
+
+def pre_bwd(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, q: torch.Tensor,
+            rms: torch.Tensor, dU: torch.Tensor | None, dh: torch.Tensor | None, dH: torch.Tensor | None,
+            dX: torch.Tensor | None = None):
+    """Backward of pre_fwd: (dX, dW like X, dalpha, dbias float32) from its inputs, q and rms, and
+    the gradients of its outputs, each None for zero. dX: a gradient of the streams from elsewhere
+    (like X), added in the same pass."""
+    n, tokens, C = _params(X, W, alpha, bias)
+    lead = X.shape[:-2]
+    _dense(q, "q", (*lead, n * n + 2 * n), torch.float32, X)
+    _dense(rms, "rms", lead, torch.float32, X)
+    for t, name, shape, dtype in ((dU, "dU", (*lead, C), X.dtype), (dh, "dh", (*lead, n), torch.float32),
+                                  (dH, "dH", (*lead, n, n), torch.float32), (dX, "dX", X.shape, X.dtype)):
+        if t is not None:
+            _dense(t, name, shape, dtype, X)
+    work = _work(n, tokens, C, X, True)
+    out, dW = torch.empty_like(X), torch.empty_like(W)
+    dalpha, dbias = torch.empty_like(alpha), torch.empty_like(bias)
+    _call(f"birkhoff{n}_pre_bwd", X, _ptr(X), _ptr(W), _dtype_code(X), _ptr(alpha), _ptr(bias), _ptr(q), _ptr(rms),
+          _ptr(dU), _ptr(dh), _ptr(dH), _ptr(dX), _ptr(out), _ptr(dW), _ptr(dalpha), _ptr(dbias), _ptr(work),
+          work.numel(), tokens, C)
+    return out, dW, dalpha, dbias
+
+
+class PreFn(torch.autograd.Function):
+    """pre_fwd that hands the streams on, so that the gradient they get from what follows is added
+    by the backward's own pass over them."""
+
+    @staticmethod
+    def forward(ctx, X, W, alpha, bias, eps=DEFAULT_EPS):
+        ctx.set_materialize_grads(False)
+        Xc, W, alpha, bias = X.contiguous(), W.contiguous(), alpha.contiguous(), bias.contiguous()
+        U, h, H, q, rms = pre_fwd(Xc, W, alpha, bias, eps)
+        ctx.save_for_backward(Xc, W, alpha, bias, q, rms)
+        return U, h, H, Xc.view_as(Xc)
+
+    @staticmethod
+    def backward(ctx, dU, dh, dH, dX):
+        grads = [None if g is None else g.contiguous() for g in (dU, dh, dH, dX)]
+        return (*pre_bwd(*ctx.saved_tensors, *grads), None)
+
+
+def pre(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, eps: float = DEFAULT_EPS):
+    """pre_fwd with gradients for X, W, alpha and bias: (U, h, H, X). The X returned is the X
+    given; give it to what uses the streams next, and their gradient costs no pass of its own."""
+    return PreFn.apply(X, W, alpha, bias, eps)
 
 
 def version() -> int:

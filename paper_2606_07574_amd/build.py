@@ -10,13 +10,13 @@ import subprocess
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRC = os.path.join(PKG, "csrc", "birkhoff4.hip")
+SOURCES = [os.path.join(PKG, "csrc", f) for f in ("birkhoff4.hip", "pre.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libbirkhoff4.so")
 ARCH = "gfx950"
 
 FLAGS = [
-    "-O3", "-std=c++17", "-fPIC", "-shared", f"--offload-arch={ARCH}",
+    "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
     # keep packed-fp32 instructions out of the generated code
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     # fp32 denormals flush to zero (the forward kernel relies on it, see csrc)
@@ -33,13 +33,25 @@ def hipcc() -> str:
 
 
 def build(extra_flags: list[str] | None = None, out: str = LIB, verbose: bool = False) -> str:
-    """Compile csrc/birkhoff4.hip into ``out`` (always recompiles)."""
+    """Compile the sources in csrc/ and link them into ``out`` (always recompiles)."""
+    objs = [out + ".%s.tmp%d.o" % (os.path.basename(s), os.getpid()) for s in SOURCES]
     tmp = out + ".tmp%d" % os.getpid()
-    cmd = [hipcc(), *FLAGS, *(extra_flags or []), "-I", INCLUDE, "-o", tmp, SRC]
+    cmds = [[hipcc(), *FLAGS, *(extra_flags or []), "-I", INCLUDE, "-c", "-o", o, s] for s, o in zip(SOURCES, objs)]
+    link = [hipcc(), "-shared", "-fPIC", f"--offload-arch={ARCH}", "-o", tmp, *objs]
     if verbose:
-        print(" ".join(cmd), flush=True)
-    subprocess.check_call(cmd)
-    os.replace(tmp, out)
+        print("\n".join(" ".join(c) for c in (*cmds, link)), flush=True)
+    try:
+        jobs = [subprocess.Popen(c) for c in cmds]
+        codes = [j.wait() for j in jobs]  # every compiler has ended before any error is raised
+        for c, code in zip(cmds, codes):
+            if code:
+                raise subprocess.CalledProcessError(code, c)
+        subprocess.check_call(link)
+        os.replace(tmp, out)
+    finally:
+        for f in (*objs, tmp):
+            if os.path.exists(f):
+                os.remove(f)
     return out
 
 

@@ -1,0 +1,928 @@
+// pre.hip -- how a hyper-connection layer reads its streams (Sec. 2.1), for gfx950 (MI355X).
+//
+// The layer's update is x <- H^res x + (H^post)^T F(H^pre x) with x a token's n = 4 or 8 streams
+// of C channels. Its coefficients come from the streams themselves: with v the token's K = n C
+// values, r = (|v|^2 / K + eps)^(-1/2) and W of N = n^2 + 2 n rows,
+//     q = r W v,   l = alpha_g q + bias   (g: rows 0..n-1, n..2n-1 and the n^2 others)
+//     h^pre = sigmoid(l_pre),   h = 2 sigmoid(l_post),   H = l_res,   U = sum_i h^pre_i X_i
+// H are the logits of the residual mixing and U is the branch's input. The backward, from
+// dU, dh, dH and optionally E, a gradient of the streams from elsewhere:
+//     dl_pre,i = h^pre_i (1 - h^pre_i) <dU, X_i>,  dl_post = dh h (1 - h / 2),  dl_res = dH
+//     dbias = sum over tokens of dl,   dalpha_g = sum over tokens and rows of g of dl q
+//     G = r alpha_g dl,   dW = sum over tokens of G v^T,   s = (r / K) sum_j G_j q_j
+//     dX_i = E_i + h^pre_i dU + (G W)_i - s X_i
+//
+// Both are bound by HBM: with n = 4 a token of 2-byte values is 2 N operations per 2 bytes, a
+// tenth of what the matrix cores do in that time. W (N rows) is used by every token and stays in
+// L2; the products run on the matrix cores with the tokens as one side of the tile.
+
+#include "common.h"
+
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+
+template <int N>
+struct Gates {
+    static constexpr int rows = N * N + 2 * N;        // 24 or 80: rows of W, coefficients of a token
+    static constexpr int tiles = (rows + 15) / 16;    // 16-row tiles of a product
+    static constexpr int stride = rows + 4;           // floats per token of the partial sums: rows, |v|^2, 0, 0, 0
+    static constexpr int ksteps = (rows + 31) / 32;   // 32-row steps of a product over the rows
+};
+
+__device__ __forceinline__ v4f mfma_bf16(const v4u a, const v4u b, const v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0,
+                                                   0);
+}
+
+__device__ __forceinline__ v4f mfma_f32(float a, float b, const v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x4f32(a, b, c, 0, 0, 0);
+}
+
+// c += a b over 64 bytes of sixteen rows of each side, lane l holding 16-byte chunk l / 16 of row
+// l % 16: one product of 32 bf16 values, or four of 4 fp32 values (values m of the four chunks).
+template <int DX>
+__device__ __forceinline__ v4f mfma_chunks(const v4u a, const v4u b, v4f c) {
+    if constexpr (DX == BIRKHOFF4_BF16) {
+        return mfma_bf16(a, b, c);
+    } else {
+#pragma unroll
+        for (int m = 0; m < 4; ++m) c = mfma_f32(__uint_as_float(a[m]), __uint_as_float(b[m]), c);
+        return c;
+    }
+}
+
+__device__ __forceinline__ float sigmoid(float x) { return rcp(1.0f + ex2(-kLog2e * x)); }
+
+// alpha's entry for row j of W.
+template <int N>
+__device__ __forceinline__ float row_scale(const float* __restrict__ alpha, int j) {
+    return alpha[j < N ? 0 : j < 2 * N ? 1 : 2];
+}
+
+// ---------------------------------------------------------------------------
+// Forward: the products W v and |v|^2 of every token
+// ---------------------------------------------------------------------------
+// A block takes 16 TT tokens and a share of the row, in steps of 64 bytes; its four waves take the
+// steps in pairs (a 128-byte line of each token) in turn. Tokens are the columns of the tile, rows
+// of W its rows, both loaded straight into the operands' layout; |v|^2 is the diagonal of the
+// product of the tokens' operand with itself (fp32: plain sums, as the fp32 matrix rate is nearer
+// to what HBM delivers). The waves' sums are added in LDS in wave order, the shares' by the
+// reader: no atomics, so a token's result does not depend on timing.
+constexpr int kGateWaves = 4;
+
+template <int DX, int N, int TT>
+__global__ __launch_bounds__(64 * kGateWaves, 2) void pre_gate_kernel(const v4u* __restrict__ X,
+                                                                      const v4u* __restrict__ W,
+                                                                      float* __restrict__ part, int64_t B, int64_t steps,
+                                                                      int64_t per) {
+    constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4;
+    __shared__ v4f red[kGateWaves / 2][16 * TT][S4];
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int64_t first = static_cast<int64_t>(blockIdx.x) * 16 * TT;
+    const int64_t s0 = blockIdx.y * per, s1 = s0 + per < steps ? s0 + per : steps;
+    const v4u *x[TT], *wr[RT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {  // past the last token: that token again, its sums not stored
+        const int64_t tok = first + 16 * t + c;
+        x[t] = X + 4 * steps * (tok < B ? tok : B - 1) + g;
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) wr[r] = W + 4 * steps * (16 * r + c < R ? 16 * r + c : R - 1) + g;
+    v4f acc[TT][RT], gram[TT];
+    float ss[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        gram[t] = v4f{0.f, 0.f, 0.f, 0.f};
+        ss[t] = 0.f;
+#pragma unroll
+        for (int r = 0; r < RT; ++r) acc[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
+    }
+    for (int64_t s = s0 + 2 * w; s < s1; s += 2 * kGateWaves) {
+        v4u xv[2][TT], wv[2][RT];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            if (s + u < s1) {  // uniform
+#pragma unroll
+                for (int t = 0; t < TT; ++t) xv[u][t] = x[t][4 * (s + u)];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) wv[u][r] = wr[r][4 * (s + u)];
+            } else {
+#pragma unroll
+                for (int t = 0; t < TT; ++t) xv[u][t] = v4u{0u, 0u, 0u, 0u};
+#pragma unroll
+                for (int r = 0; r < RT; ++r) wv[u][r] = v4u{0u, 0u, 0u, 0u};
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int t = 0; t < TT; ++t) {
+#pragma unroll
+                for (int r = 0; r < RT; ++r) acc[t][r] = mfma_chunks<DX>(wv[u][r], xv[u][t], acc[t][r]);
+                if constexpr (DX == BIRKHOFF4_BF16) {
+                    gram[t] = mfma_bf16(xv[u][t], xv[u][t], gram[t]);
+                } else {
+#pragma unroll
+                    for (int m = 0; m < 4; ++m) {
+                        const float v = __uint_as_float(xv[u][t][m]);
+                        ss[t] = __builtin_fmaf(v, v, ss[t]);
+                    }
+                }
+            }
+    }
+    // lane (g, c) holds rows 16 r + 4 g .. + 3 of token 16 t + c, and a lane group each token's |v|^2
+    v4f norm[TT];
+#pragma unroll
+    for (int t = 0; t < TT; ++t) {
+        float sum;
+        if constexpr (DX == BIRKHOFF4_BF16) {
+            sum = (c & 3) == 0 ? gram[t].x : (c & 3) == 1 ? gram[t].y : (c & 3) == 2 ? gram[t].z : gram[t].w;
+        } else {
+            sum = ss[t];
+            sum += __shfl_xor(sum, 16);
+            sum += __shfl_xor(sum, 32);
+        }
+        norm[t] = v4f{sum, 0.f, 0.f, 0.f};
+    }
+    auto each = [&](auto&& f) {  // this lane's quads: f(token of the block, quad of the token, value)
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                if (16 * r + 4 * g < R) f(16 * t + c, 4 * r + g, acc[t][r]);
+            if (g == c >> 2) f(16 * t + c, S4 - 1, norm[t]);
+        }
+    };
+    auto put = [&](int k) { each([&](int t, int q, v4f& v) { red[k][t][q] = v; }); };
+    auto add = [&](int k) { each([&](int t, int q, v4f& v) { v += red[k][t][q]; }); };
+    // waves 1 and 3 to 0 and 2, then 2 to 0
+    if (w & 1) put(w >> 1);
+    __syncthreads();
+    if (!(w & 1)) add(w >> 1);
+    __syncthreads();
+    if (w == 2) put(0);
+    __syncthreads();
+    if (w == 0) {
+        add(0);
+        v4f* dst = reinterpret_cast<v4f*>(part) + (blockIdx.y * B + first) * S4;
+        each([&](int t, int q, v4f& v) {
+            if (first + t < B) dst[t * S4 + q] = v;
+        });
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Forward: the coefficients, and U = sum_i h^pre_i X_i
+// ---------------------------------------------------------------------------
+// Lanes take 16-byte chunks of the rows, L lanes a token and 64 / L tokens a wave; a wave adds its
+// tokens' partial sums itself (lane j row j), while its part of the streams is on the way.
+template <int DX, int N, int L>
+__global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__ part, const v4u* __restrict__ X,
+                                                       const float* __restrict__ alpha, const float* __restrict__ bias,
+                                                       float eps, float inv_k, v4u* __restrict__ U,
+                                                       float* __restrict__ h, float* __restrict__ H,
+                                                       float* __restrict__ Q, float* __restrict__ rms, int64_t B,
+                                                       int64_t nc, int splits) {
+    constexpr int R = Gates<N>::rows, S = Gates<N>::stride, J = (S + 63) / 64, TW = 64 / L, E = MixChunk<DX>::E;
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int W = blockDim.x >> 6;
+    // blocks from the last token back: the last ones that the products read are still in the cache
+    const int64_t t0 = (gridDim.x - 1 - static_cast<int64_t>(blockIdx.x)) * TW;
+    const int64_t tok = t0 + lane / L;
+    const int64_t first = L == 64 ? 64 * (static_cast<int64_t>(blockIdx.y) * W + w) : 0;  // this wave's column
+    const int64_t col = first + lane % L;
+    v4u x[N];
+    const v4u* row = X + N * nc * (tok < B ? tok : B - 1);
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = v4u{0u, 0u, 0u, 0u};
+    if (col < nc) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) x[i] = row[i * nc + col];
+    }
+    float hp[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) hp[i] = 0.f;
+#pragma unroll
+    for (int k = 0; k < TW; ++k) {
+        const int64_t t = t0 + k;
+        if (t >= B) break;  // uniform
+        float sum[J], l[J], gate[J];
+#pragma unroll
+        for (int m = 0; m < J; ++m) sum[m] = 0.f;
+        for (int s = 0; s < splits; ++s) {
+            const float* p = part + (s * B + t) * S;
+#pragma unroll
+            for (int m = 0; m < J; ++m)
+                if (64 * m + lane < S) sum[m] += p[64 * m + lane];
+        }
+        const float norm2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum[R / 64]), R % 64));
+        const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(norm2, inv_k, eps));
+#pragma unroll
+        for (int m = 0; m < J; ++m) {
+            const int j = 64 * m + lane < R ? 64 * m + lane : R - 1;
+            sum[m] *= r;  // q
+            l[m] = __builtin_fmaf(row_scale<N>(alpha, j), sum[m], bias[j]);
+            gate[m] = sigmoid(l[m]);
+        }
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float v = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(gate[0]), i));
+            if (lane / L == k) hp[i] = v;
+        }
+        if (first == 0) {  // the token's first wave
+            if (lane == 0) rms[t] = r;
+            if (lane >= N && lane < 2 * N) h[N * t + lane - N] = 2.0f * gate[0];
+#pragma unroll
+            for (int m = 0; m < J; ++m) {
+                const int j = 64 * m + lane;
+                if (j < R) Q[R * t + j] = sum[m];
+                if (j >= 2 * N && j < R) H[N * N * t + j - 2 * N] = l[m];
+            }
+        }
+    }
+    if (col < nc && tok < B) {
+        float u[E];
+#pragma unroll
+        for (int e = 0; e < E; ++e) u[e] = 0.f;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            float v[E];
+            unpack_chunk<DX>(x[i], v);
+#pragma unroll
+            for (int e = 0; e < E; ++e) u[e] = __builtin_fmaf(hp[i], v[e], u[e]);
+        }
+        U[nc * tok + col] = pack_chunk<DX>(u);
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Backward: <dU, X_i> and the coefficients' gradients
+// ---------------------------------------------------------------------------
+// Tokens are padded to whole steps of 32 (Bp), whose G, h^pre and s are zero, for the products
+// below. A token has `share` waves of the block, which take its columns in turn; its first wave
+// forms G. A block takes `turns` times 8 / share consecutive tokens and leaves one row of sums for
+// dbias and dalpha.
+constexpr int kTokenStep = 32;
+constexpr int kDotWaves = 8;
+
+template <int DX, int N>
+__device__ __forceinline__ float add_dot(const v4u a, const v4u b, float acc) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        if constexpr (DX == BIRKHOFF4_BF16)  // products of bf16 values are exact in fp32
+            acc = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, static_cast<uint32_t>(a[k])),
+                                                  __builtin_bit_cast(bf16x2, static_cast<uint32_t>(b[k])), acc, false);
+        else
+            acc = __builtin_fmaf(__uint_as_float(a[k]), __uint_as_float(b[k]), acc);
+    }
+    return acc;
+}
+
+// Sum over the 64 / N lanes that lane_sums leaves of one of N values, in all of them.
+template <int N>
+__device__ __forceinline__ float rest_sum(float x) {
+    x = gsum_lanes<8>(x);
+    if constexpr (N == 4)
+        x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));  // row_ror:8
+    return x;
+}
+
+__device__ __forceinline__ float wave_sum(float x) {
+    x = rest_sum<4>(x);
+    x += __shfl_xor(x, 16);
+    return x + __shfl_xor(x, 32);
+}
+
+template <int DX, int N>
+__global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
+    const v4u* __restrict__ X, const v4u* __restrict__ dU, const float* __restrict__ Q, const float* __restrict__ rms,
+    const float* __restrict__ alpha, const float* __restrict__ bias, const float* __restrict__ dh,
+    const float* __restrict__ dH, float* __restrict__ G, float* __restrict__ GT, float* __restrict__ coef,
+    float* __restrict__ sums, int64_t B, int64_t Bp, int64_t nc, float inv_k, int share, int turns) {
+    constexpr int R = Gates<N>::rows, S = Gates<N>::stride, J = (R + 63) / 64;
+    __shared__ float dots[kDotWaves][N];
+    __shared__ float total[kDotWaves][S];
+    const int lane = threadIdx.x & 63;
+    const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int per = kDotWaves / share, sub = w / share, part = w % share;  // share: a power of two
+    float sum_dl[J], sum_dq[3] = {0.f, 0.f, 0.f};
+#pragma unroll
+    for (int m = 0; m < J; ++m) sum_dl[m] = 0.f;
+    for (int k = 0; k < turns; ++k) {
+        const int64_t t = (static_cast<int64_t>(blockIdx.x) * turns + k) * per + sub;
+        float d[N], out[1];
+#pragma unroll
+        for (int i = 0; i < N; ++i) d[i] = 0.f;
+        if (dU && t < B) {  // uniform over the wave
+            for (int64_t col = 64 * part + lane; col < nc; col += 64 * share) {
+                const v4u u = dU[nc * t + col];
+                v4u x[N];
+#pragma unroll
+                for (int i = 0; i < N; ++i) x[i] = X[nc * (N * t + i) + col];
+#pragma unroll
+                for (int i = 0; i < N; ++i) d[i] = add_dot<DX, N>(u, x[i], d[i]);
+            }
+        }
+        lane_sums<32, N>(d, out, lane);
+        float dot = rest_sum<N>(out[0]);  // lane: value lane N / 64
+        if (share > 1) {  // uniform over the block
+            if (lane % (64 / N) == 0) dots[w][lane / (64 / N)] = dot;
+            __syncthreads();
+            if (part == 0) {
+                dot = dots[w][lane / (64 / N)];
+                for (int q = 1; q < share; ++q) dot += dots[w + q][lane / (64 / N)];
+            }
+            __syncthreads();
+        }
+        if (part == 0 && t < Bp) {
+            // lane j < N takes <dU, X_j>
+            dot = __int_as_float(
+                __builtin_amdgcn_ds_bpermute(4 * (lane < N ? lane * (64 / N) : 0), __float_as_int(dot)));
+            const float r = t < B ? rms[t] : 0.f;
+            float s = 0.f;
+#pragma unroll
+            for (int m = 0; m < J; ++m) {
+                const int j = 64 * m + lane;
+                if (j >= R) continue;
+                float dl = 0.f, q = 0.f, gate = 0.f;
+                const float a = row_scale<N>(alpha, j);
+                if (t < B) {
+                    q = Q[R * t + j];
+                    if (j < 2 * N) {
+                        gate = sigmoid(__builtin_fmaf(a, q, bias[j]));
+                        const float up = j < N ? dot : dh ? 2.0f * dh[N * t + j - N] : 0.f;
+                        dl = up * gate * (1.0f - gate);
+                    } else if (dH) {
+                        dl = dH[N * N * t + j - 2 * N];
+                    }
+                }
+                const float gj = r * a * dl, dq = dl * q;
+                s = __builtin_fmaf(gj, q, s);
+                G[R * t + j] = gj;
+                GT[j * Bp + t] = gj;
+                if (j < N) coef[j * Bp + t] = gate;
+                sum_dl[m] += dl;
+                sum_dq[0] += j < N ? dq : 0.f;
+                sum_dq[1] += j >= N && j < 2 * N ? dq : 0.f;
+                sum_dq[2] += j >= 2 * N ? dq : 0.f;
+            }
+            s = wave_sum(s);
+            if (lane == 0) coef[N * Bp + t] = s * r * inv_k;
+        }
+    }
+    // a row of sums for the block: dl's, then the three groups' dl q
+#pragma unroll
+    for (int m = 0; m < J; ++m)
+        if (64 * m + lane < R) total[w][64 * m + lane] = sum_dl[m];
+#pragma unroll
+    for (int q = 0; q < 3; ++q) {
+        const float v = wave_sum(sum_dq[q]);
+        if (lane == 0) total[w][R + q] = v;
+    }
+    if (lane == 0) total[w][R + 3] = 0.f;
+    __syncthreads();
+    for (int j = threadIdx.x; j < S; j += 64 * kDotWaves) {
+        float v = 0.f;
+        for (int q = 0; q < kDotWaves; q += share) v += total[q][j];
+        sums[static_cast<int64_t>(blockIdx.x) * S + j] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Backward: dX and partial sums of dW
+// ---------------------------------------------------------------------------
+// Wave w of a block takes stream w's channels CW chunk .. + CW, CE of them per lane (lane l: group
+// g = l / 16 of tokens, channels CE (l % 16) .. + CE), over the steps of 32 tokens of its share, of
+// which lane group g has tokens 8 g .. 8 g + 7. The same registers serve everything:
+//  * dW: tile of 16 rows of W (G transposed, tokens along k) times the tokens' values, one product
+//    per channel c of the lanes: column l % 16 is channel CE (l % 16) + c, and k runs over the
+//    tokens in the order in which the lanes hold them, 8 per lane group.
+//  * dX: rows of a product are tokens; product a in {0, 1} has token 8 (i / 4) + 4 a + i % 4 as row
+//    i, so that its result lands in the lane that holds the token's values.
+// bf16: G enters as the sum of two bf16 values (the upper 16 bits, and the rest rounded), 2^-16 off
+// at most, since one alone (2^-8) would be as coarse as the result's own rounding; W and X are
+// exact. Sums are fp32. Rows of W stay in registers throughout.
+template <int DX, int N>
+struct Back {
+    // bf16 with n = 8: half as many channels, as the sums of 5 row tiles fill the registers
+    static constexpr int CE = DX == BIRKHOFF4_BF16 && N == 4 ? 8 : 4;
+    static constexpr int CW = 16 * CE;
+    static constexpr int words = CE * (DX == BIRKHOFF4_BF16 ? 2 : 4) / 4;  // of a lane's channels
+};
+
+template <int WORDS>
+struct Words {
+    uint32_t v[WORDS];
+};
+
+template <int WORDS>
+__device__ __forceinline__ Words<WORDS> load_words(const void* base, int64_t byte) {
+    Words<WORDS> r;
+    const char* p = static_cast<const char*>(base) + byte;
+    if constexpr (WORDS == 4) {
+        const v4u q = *reinterpret_cast<const v4u*>(p);
+        r.v[0] = q.x; r.v[1] = q.y; r.v[2] = q.z; r.v[3] = q.w;
+    } else {
+        const uint2 q = *reinterpret_cast<const uint2*>(p);
+        r.v[0] = q.x; r.v[1] = q.y;
+    }
+    return r;
+}
+
+template <int WORDS>
+__device__ __forceinline__ void store_words(void* base, int64_t byte, const Words<WORDS>& r) {
+    char* p = static_cast<char*>(base) + byte;
+    if constexpr (WORDS == 4)
+        __builtin_nontemporal_store(v4u{r.v[0], r.v[1], r.v[2], r.v[3]}, reinterpret_cast<v4u*>(p));
+    else
+        __builtin_nontemporal_store(static_cast<uint64_t>(r.v[1]) << 32 | r.v[0], reinterpret_cast<uint64_t*>(p));
+}
+
+// Channel c of a lane's words.
+template <int DX, int WORDS>
+__device__ __forceinline__ float channel(const Words<WORDS>& r, int c) {
+    if constexpr (DX == BIRKHOFF4_BF16)
+        return __uint_as_float(c & 1 ? r.v[c / 2] & 0xffff0000u : r.v[c / 2] << 16);
+    else
+        return __uint_as_float(r.v[c]);
+}
+
+// bf16 channel c of eight rows, in order.
+template <int WORDS>
+__device__ __forceinline__ v4u column_of(const Words<WORDS> r[8], int c) {
+    v4u out;
+#pragma unroll
+    for (int k = 0; k < 4; ++k)  // bytes 0..3 of the selector's operand 1, 4..7 of operand 0
+        out[k] = __builtin_amdgcn_perm(r[2 * k + 1].v[c / 2], r[2 * k].v[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+    return out;
+}
+
+// Eight fp32 values as the sum of two bf16 ones each: the upper half of the bits (no rounding, so
+// a large value does not overflow) and the rest (nothing where the value is not finite).
+__device__ __forceinline__ void split8(const v4f a, const v4f b, v4u& hi, v4u& lo) {
+    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
+    float rest[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+        const float up = __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u);
+        rest[k] = __builtin_fabsf(v[k]) < __builtin_inff() ? v[k] - up : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        hi[k] = __builtin_amdgcn_perm(__float_as_uint(v[2 * k + 1]), __float_as_uint(v[2 * k]), 0x07060302u);
+        lo[k] = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+    }
+}
+
+template <int DX, int N>
+__global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restrict__ X, const void* __restrict__ W,
+                                                             const void* __restrict__ dU, const void* __restrict__ E,
+                                                             const float* __restrict__ G, const float* __restrict__ GT,
+                                                             const float* __restrict__ coef, void* __restrict__ dX,
+                                                             float* __restrict__ dWp, int64_t B, int64_t Bp, int64_t C) {
+    constexpr bool H16 = DX == BIRKHOFF4_BF16;
+    constexpr int R = Gates<N>::rows, RT = Gates<N>::tiles, KS = H16 ? Gates<N>::ksteps : R / 4;
+    constexpr int CE = Back<DX, N>::CE, WO = Back<DX, N>::words, SZ = H16 ? 2 : 4;
+    const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
+    const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));  // the stream
+    const int64_t ch = static_cast<int64_t>(blockIdx.x) * Back<DX, N>::CW + CE * c16;
+    const bool own = ch < C;
+    const int64_t at = own ? ch : 0;  // lanes past the end of the row read its start and store nothing
+    const int64_t K = N * C;
+
+    // W's rows: operand of the dX products, for each channel c of the lane
+    v4u wb[H16 ? KS : 1][CE];
+    float wf[H16 ? 1 : KS][CE];
+    if constexpr (H16) {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {
+            Words<WO> rows[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {  // past the last row: that row, which meets zeros of G
+                const int row = 32 * k + 8 * g + j;
+                rows[j] = load_words<WO>(W, (K * (row < R ? row : R - 1) + w * C + at) * SZ);
+            }
+#pragma unroll
+            for (int c = 0; c < CE; ++c) wb[k][c] = column_of<WO>(rows, c);
+        }
+    } else {
+#pragma unroll
+        for (int k = 0; k < KS; ++k) {  // lane group g has rows g R / 4 ..
+            const Words<WO> row = load_words<WO>(W, (K * (g * KS + k) + w * C + at) * SZ);
+#pragma unroll
+            for (int c = 0; c < CE; ++c) wf[k][c] = __uint_as_float(row.v[c]);
+        }
+    }
+    v4f acc[RT][CE];
+#pragma unroll
+    for (int r = 0; r < RT; ++r)
+#pragma unroll
+        for (int c = 0; c < CE; ++c) acc[r][c] = v4f{0.f, 0.f, 0.f, 0.f};
+
+    const int64_t nsteps = Bp / kTokenStep;
+    // the last steps first: their streams are still in the cache from the dot products
+    for (int64_t st = nsteps - 1 - blockIdx.y; st >= 0; st -= gridDim.y) {
+        const int64_t t0 = st * kTokenStep + 8 * g;  // this lane's eight tokens
+        const bool whole = (st + 1) * kTokenStep <= B;
+        Words<WO> x[8], e[8], u[8];
+        int64_t tok[8];
+#pragma unroll
+        for (int k = 0; k < 8; ++k) tok[k] = whole || t0 + k < B ? t0 + k : B - 1;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = load_words<WO>(X, (K * tok[k] + w * C + at) * SZ);
+        if (E) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e[k] = load_words<WO>(E, (K * tok[k] + w * C + at) * SZ);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) e[k] = Words<WO>{};
+        }
+        if (dU) {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[k] = load_words<WO>(dU, (C * tok[k] + at) * SZ);
+        } else {
+#pragma unroll
+            for (int k = 0; k < 8; ++k) u[k] = Words<WO>{};
+        }
+        if (!whole) {  // tokens past the last one add nothing to dW: zeros, as 0 times their G
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                if (t0 + k >= B) x[k] = Words<WO>{};
+        }
+
+        // dW += G^T X
+        {
+            v4f ga[RT], gb[RT];
+#pragma unroll
+            for (int r = 0; r < RT; ++r) {
+                const int j = 16 * r + c16 < R ? 16 * r + c16 : R - 1;
+                const v4f* p = reinterpret_cast<const v4f*>(GT + j * Bp + t0);
+                ga[r] = p[0];
+                gb[r] = p[1];
+            }
+            if constexpr (H16) {
+                v4u hi[RT], lo[RT];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) split8(ga[r], gb[r], hi[r], lo[r]);
+#pragma unroll
+                for (int c = 0; c < CE; ++c) {
+                    const v4u b = column_of<WO>(x, c);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) acc[r][c] = mfma_bf16(lo[r], b, mfma_bf16(hi[r], b, acc[r][c]));
+                }
+            } else {
+#pragma unroll
+                for (int k = 0; k < 8; ++k)
+#pragma unroll
+                    for (int r = 0; r < RT; ++r)
+#pragma unroll
+                        for (int c = 0; c < CE; ++c)
+                            acc[r][c] = mfma_f32(k < 4 ? ga[r][k & 3] : gb[r][k & 3], __uint_as_float(x[k].v[c]), acc[r][c]);
+            }
+        }
+        // dX = E + h^pre dU + G W - s X, four tokens of the lane at a time
+#pragma unroll
+        for (int a = 0; a < 2; ++a) {
+            const int64_t gt = st * kTokenStep + 8 * (c16 >> 2) + 4 * a + (c16 & 3);  // row c16's token
+            v4f d[CE];
+#pragma unroll
+            for (int c = 0; c < CE; ++c) d[c] = v4f{0.f, 0.f, 0.f, 0.f};
+            if constexpr (H16) {
+#pragma unroll
+                for (int k = 0; k < KS; ++k) {
+                    v4u hi = {0u, 0u, 0u, 0u}, lo = {0u, 0u, 0u, 0u};
+                    if (32 * k + 8 * g < R) {
+                        const v4f* p = reinterpret_cast<const v4f*>(G + R * gt + 32 * k + 8 * g);
+                        split8(p[0], p[1], hi, lo);
+                    }
+#pragma unroll
+                    for (int c = 0; c < CE; ++c) d[c] = mfma_bf16(lo, wb[k][c], mfma_bf16(hi, wb[k][c], d[c]));
+                }
+            } else {
+                float gv[KS];
+#pragma unroll
+                for (int k = 0; k < KS; ++k) gv[k] = G[R * gt + g * KS + k];
+#pragma unroll
+                for (int k = 0; k < KS; ++k)
+#pragma unroll
+                    for (int c = 0; c < CE; ++c) d[c] = mfma_f32(gv[k], wf[k][c], d[c]);
+            }
+            const v4f hp = *reinterpret_cast<const v4f*>(coef + w * Bp + t0 + 4 * a);
+            const v4f sv = *reinterpret_cast<const v4f*>(coef + N * Bp + t0 + 4 * a);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int k = 4 * a + i;
+                float o[CE];
+#pragma unroll
+                for (int c = 0; c < CE; ++c) {
+                    o[c] = __builtin_fmaf(hp[i], channel<DX, WO>(u[k], c), channel<DX, WO>(e[k], c) + d[c][i]);
+                    o[c] = __builtin_fmaf(-sv[i], channel<DX, WO>(x[k], c), o[c]);
+                }
+                Words<WO> r;
+#pragma unroll
+                for (int q = 0; q < WO; ++q) {
+                    if constexpr (H16)
+                        r.v[q] = pack_bf16(o[2 * q], o[2 * q + 1]);
+                    else
+                        r.v[q] = __float_as_uint(o[q]);
+                }
+                if (own && t0 + k < B) store_words<WO>(dX, (K * (t0 + k) + w * C + ch) * SZ, r);
+            }
+        }
+    }
+    if (own) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int j = 16 * r + 4 * g + i;
+                if (j >= R) continue;
+                v4f* p = reinterpret_cast<v4f*>(dWp + (static_cast<int64_t>(blockIdx.y) * R + j) * K + w * C + ch);
+#pragma unroll
+                for (int q = 0; q < CE / 4; ++q)
+                    p[q] = v4f{acc[r][4 * q][i], acc[r][4 * q + 1][i], acc[r][4 * q + 2][i], acc[r][4 * q + 3][i]};
+            }
+    }
+}
+
+// The shares' sums added in order: dW, and in the grid's last blocks dbias and dalpha, sixteen
+// entries a block.
+constexpr int kJoinBlock = 1024;
+
+template <int N, bool DW16>
+__global__ __launch_bounds__(kJoinBlock) void pre_join_kernel(const v4f* __restrict__ dWp, const float* __restrict__ sums,
+                                                              void* __restrict__ dW, float* __restrict__ dalpha,
+                                                              float* __restrict__ dbias, int64_t quads, int shares,
+                                                              int64_t rows, unsigned wblocks) {
+    constexpr int R = Gates<N>::rows, S = Gates<N>::stride;
+    if (blockIdx.x < wblocks) {
+        for (int64_t q = static_cast<int64_t>(blockIdx.x) * kJoinBlock + threadIdx.x; q < quads;
+             q += static_cast<int64_t>(wblocks) * kJoinBlock) {
+            v4f v = {0.f, 0.f, 0.f, 0.f};
+            for (int k = 0; k < shares; ++k) v += dWp[k * quads + q];
+            if constexpr (DW16)
+                static_cast<uint2*>(dW)[q] = uint2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
+            else
+                static_cast<v4f*>(dW)[q] = v;
+        }
+        return;
+    }
+    __shared__ float red[kJoinBlock / 16][16];
+    const int c = threadIdx.x & 15, part = threadIdx.x >> 4;
+    const int j = 16 * static_cast<int>(blockIdx.x - wblocks) + c;
+    float v = 0.f;
+    if (j < S)
+        for (int64_t k = part; k < rows; k += kJoinBlock / 16) v += sums[k * S + j];
+    red[part][c] = v;
+    __syncthreads();
+    if (part == 0) {
+        v = red[0][c];
+        for (int k = 1; k < kJoinBlock / 16; ++k) v += red[k][c];
+        if (j < R)
+            dbias[j] = v;
+        else if (j < R + 3)
+            dalpha[j - R] = v;
+    }
+}
+
+// ---------------------------------------------------------------------------
+// Host side
+// ---------------------------------------------------------------------------
+int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct PreShape {
+    int64_t B, C, nc, steps;  // nc: 16-byte chunks of a stream's row; steps: 64 bytes of a token
+};
+
+struct GateLaunch {
+    int tt;                      // 16-token tiles per block
+    int64_t tiles, splits, per;  // blocks over tokens, shares of the row, steps per share
+};
+
+constexpr int64_t kGateBlocks = 1024;
+constexpr int64_t kGateMaxSplits = 64;
+
+GateLaunch gate_launch(const PreShape& s) {
+    GateLaunch l;
+    l.tt = s.B <= 16 ? 1 : s.B <= 32 ? 2 : 4;
+    l.tiles = cdiv(s.B, 16 * l.tt);
+    const int64_t most = cdiv(s.steps, 2 * kGateWaves);
+    int64_t want = cdiv(kGateBlocks, l.tiles);
+    if (want > most) want = most;
+    if (want > kGateMaxSplits) want = kGateMaxSplits;
+    l.per = 2 * cdiv(cdiv(s.steps, want), 2);
+    l.splits = cdiv(s.steps, l.per);
+    return l;
+}
+
+struct BackLaunch {
+    int64_t Bp;                    // tokens in whole steps
+    int share, turns;              // of pre_dot_kernel
+    int64_t dot_blocks;
+    int64_t chunks, token_shares;  // of pre_back_kernel
+    int64_t g, gt, coef, sums, dw, bytes;  // the workspace's parts: offsets in bytes, and its size
+};
+
+constexpr int64_t kDotBlocks = 2048;
+constexpr int64_t kBackWaves = 2048;  // two per SIMD
+
+BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
+    BackLaunch l;
+    const int64_t rows = n * n + 2 * n;
+    l.Bp = cdiv(s.B, kTokenStep) * kTokenStep;
+    l.share = 1;
+    while (l.share < kDotWaves && l.share < cdiv(s.nc, 64) && l.Bp * l.share < 8192) l.share *= 2;
+    const int64_t groups = cdiv(l.Bp, kDotWaves / l.share);
+    const int64_t turns = cdiv(groups, kDotBlocks);
+    l.turns = turns > 1 ? static_cast<int>(turns) : 1;
+    l.dot_blocks = cdiv(groups, l.turns);
+    const int cw = bf16 ? (n == 4 ? Back<BIRKHOFF4_BF16, 4>::CW : Back<BIRKHOFF4_BF16, 8>::CW) : Back<BIRKHOFF4_F32, 4>::CW;
+    l.chunks = cdiv(s.C, cw);
+    const int64_t steps = l.Bp / kTokenStep;
+    int64_t shares = kBackWaves / (n * l.chunks);
+    if (shares < 1) shares = 1;
+    l.token_shares = shares < steps ? shares : steps;
+    int64_t at = 0;
+    auto take = [&](int64_t floats) {
+        const int64_t was = at;
+        at += cdiv(4 * floats, 256) * 256;
+        return was;
+    };
+    l.g = take(l.Bp * rows);
+    l.gt = take(l.Bp * rows);
+    l.coef = take(l.Bp * (n + 1));
+    l.sums = take(l.dot_blocks * (rows + 4));
+    l.dw = take(l.token_shares * rows * n * s.C);
+    l.bytes = at;
+    return l;
+}
+
+constexpr int64_t kPreMaxTokens = int64_t(1) << 26;  // a launch's lanes over tokens stay 32-bit
+constexpr int64_t kPreMaxValues = int64_t(1) << 46;
+constexpr int64_t kPreMaxChannels = int64_t(1) << 24;
+
+// The checks that both directions and the workspace's size share.
+int pre_shape(int n, int64_t B, int64_t C, int x_dtype, PreShape* s) {
+    if (B < 0 || B > kPreMaxTokens) return BIRKHOFF4_ERR_SIZE;
+    if (!dtype_ok(x_dtype)) return BIRKHOFF4_ERR_DTYPE;
+    const int64_t e = x_dtype == BIRKHOFF4_BF16 ? 8 : 4;
+    if (C <= 0 || C % e != 0) return BIRKHOFF4_ERR_CHANNELS;
+    if (C > kPreMaxChannels || (B > 0 && n * C > kPreMaxValues / B)) return BIRKHOFF4_ERR_SIZE;
+    *s = {B, C, C / e, n * (C / e) / 4};
+    return BIRKHOFF4_OK;
+}
+
+bool eps_ok(float eps) { return eps >= 0.f && eps < __builtin_inff(); }
+
+struct Span {
+    const void* p;
+    size_t bytes;
+};
+
+// No output overlaps another output or an input.
+bool disjoint(const Span* outs, int no, const Span* ins, int ni) {
+    for (int a = 0; a < no; ++a) {
+        for (int b = a + 1; b < no; ++b)
+            if (overlaps(outs[a].p, outs[a].bytes, outs[b].p, outs[b].bytes)) return false;
+        for (int b = 0; b < ni; ++b)
+            if (overlaps(outs[a].p, outs[a].bytes, ins[b].p, ins[b].bytes)) return false;
+    }
+    return true;
+}
+
+template <int DX, int N>
+int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float* alpha, const float* bias, float eps,
+                   void* U, float* h, float* H, float* q, float* rms, float* part, hipStream_t stream) {
+    const GateLaunch l = gate_launch(s);
+    const v4u *x = static_cast<const v4u*>(X), *w = static_cast<const v4u*>(W);
+    auto gate = l.tt == 1 ? pre_gate_kernel<DX, N, 1> : l.tt == 2 ? pre_gate_kernel<DX, N, 2> : pre_gate_kernel<DX, N, 4>;
+    launch_kernel(gate, dim3(static_cast<unsigned>(l.tiles), static_cast<unsigned>(l.splits)), dim3(64 * kGateWaves), 0,
+                  stream, x, w, part, s.B, s.steps, l.per);
+    const int L = s.nc <= 8 ? 8 : s.nc <= 16 ? 16 : s.nc <= 32 ? 32 : 64;
+    auto read = L == 8 ? pre_read_kernel<DX, N, 8> : L == 16 ? pre_read_kernel<DX, N, 16>
+                : L == 32 ? pre_read_kernel<DX, N, 32> : pre_read_kernel<DX, N, 64>;
+    const int64_t cols = cdiv(s.nc, L), shares = cdiv(cols, 8), waves = cdiv(cols, shares);
+    launch_kernel(read, dim3(static_cast<unsigned>(cdiv(s.B, 64 / L)), static_cast<unsigned>(shares)),
+                  dim3(static_cast<unsigned>(64 * waves)), 0, stream, part, x, alpha, bias, eps,
+                  static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), static_cast<v4u*>(U), h, H, q, rms, s.B, s.nc,
+                  static_cast<int>(l.splits));
+    return launch_status();
+}
+
+template <int DX, int N>
+int launch_pre_bwd(const PreShape& s, const void* X, const void* W, const float* alpha, const float* bias, const float* q,
+                   const float* rms, const void* dU, const float* dh, const float* dH, const void* E, void* dX, void* dW,
+                   float* dalpha, float* dbias, char* work, hipStream_t stream) {
+    const BackLaunch l = back_launch(s, N, DX == BIRKHOFF4_BF16);
+    auto at = [&](int64_t o) { return reinterpret_cast<float*>(work + o); };
+    if (s.B > 0) {
+        launch_kernel((pre_dot_kernel<DX, N>), dim3(static_cast<unsigned>(l.dot_blocks)), dim3(64 * kDotWaves), 0, stream,
+                      static_cast<const v4u*>(X), static_cast<const v4u*>(dU), q, rms, alpha, bias, dh, dH, at(l.g),
+                      at(l.gt), at(l.coef), at(l.sums), s.B, l.Bp, s.nc,
+                      static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), l.share, l.turns);
+        launch_kernel((pre_back_kernel<DX, N>), dim3(static_cast<unsigned>(l.chunks), static_cast<unsigned>(l.token_shares)),
+                      dim3(64 * N), 0, stream, X, W, dU, E, at(l.g), at(l.gt), at(l.coef), dX, at(l.dw), s.B, l.Bp, s.C);
+    }
+    // without tokens the sums are empty: zeros
+    const int64_t quads = Gates<N>::rows * N * s.C / 4;
+    const int64_t want = cdiv(quads, kJoinBlock);
+    const unsigned wblocks = static_cast<unsigned>(want < 4096 ? want : 4096);
+    launch_kernel((pre_join_kernel<N, DX == BIRKHOFF4_BF16>), dim3(wblocks + (Gates<N>::stride + 15) / 16),
+                  dim3(kJoinBlock), 0, stream, reinterpret_cast<const v4f*>(at(l.dw)), at(l.sums), dW, dalpha, dbias,
+                  quads, static_cast<int>(l.token_shares), l.dot_blocks, wblocks);
+    return launch_status();
+}
+
+int64_t pre_work(int n, int64_t B, int64_t C, int x_dtype, int backward) {
+    PreShape s;
+    if (int e = pre_shape(n, B, C, x_dtype, &s)) return e;
+    if (B == 0) return 0;
+    if (backward) return back_launch(s, n, x_dtype == BIRKHOFF4_BF16).bytes;
+    const GateLaunch l = gate_launch(s);
+    return l.splits * B * (n * n + 2 * n + 4) * 4;
+}
+
+template <int N>
+int pre_fwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, float eps, void* U, float* h,
+            float* H, float* q, float* rms, void* work, int64_t work_bytes, int64_t B, int64_t C, hipStream_t stream) {
+    PreShape s;
+    if (int e = pre_shape(N, B, C, x_dtype, &s)) return e;
+    if (!eps_ok(eps)) return BIRKHOFF4_ERR_EPS;
+    if (B == 0) return BIRKHOFF4_OK;
+    if (!X || !W || !alpha || !bias || !U || !h || !H || !q || !rms || !work) return BIRKHOFF4_ERR_NULL;
+    const int64_t need = pre_work(N, B, C, x_dtype, 0);
+    if (work_bytes < need) return BIRKHOFF4_ERR_WORK;
+    const void* all[] = {X, W, alpha, bias, U, h, H, q, rms, work};
+    for (const void* p : all)
+        if (misaligned(p)) return BIRKHOFF4_ERR_ALIGN;
+    const size_t row = static_cast<size_t>(C) * dtype_bytes(x_dtype), b = static_cast<size_t>(B), R = Gates<N>::rows;
+    const Span ins[] = {{X, b * N * row}, {W, R * N * row}, {alpha, 12}, {bias, 4 * R}};
+    const Span outs[] = {{U, b * row}, {h, b * N * 4}, {H, b * N * N * 4}, {q, b * R * 4}, {rms, b * 4},
+                         {work, static_cast<size_t>(need)}};
+    if (!disjoint(outs, 6, ins, 4)) return BIRKHOFF4_ERR_OVERLAP;
+    auto launch = x_dtype == BIRKHOFF4_BF16 ? launch_pre_fwd<BIRKHOFF4_BF16, N> : launch_pre_fwd<BIRKHOFF4_F32, N>;
+    return launch(s, X, W, alpha, bias, eps, U, h, H, q, rms, static_cast<float*>(work), stream);
+}
+
+template <int N>
+int pre_bwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, const float* q,
+            const float* rms, const void* dU, const float* dh, const float* dH, const void* E, void* dX, void* dW,
+            float* dalpha, float* dbias, void* work, int64_t work_bytes, int64_t B, int64_t C, hipStream_t stream) {
+    PreShape s;
+    if (int e = pre_shape(N, B, C, x_dtype, &s)) return e;
+    if (!dW || !dalpha || !dbias) return BIRKHOFF4_ERR_NULL;
+    if (B > 0 && (!X || !W || !alpha || !bias || !q || !rms || !dX || !work)) return BIRKHOFF4_ERR_NULL;
+    const int64_t need = pre_work(N, B, C, x_dtype, 1);
+    if (work_bytes < need) return BIRKHOFF4_ERR_WORK;
+    const void* all[] = {X, W, alpha, bias, q, rms, dU, dh, dH, E, dX, dW, dalpha, dbias, work};
+    for (const void* p : all)
+        if (misaligned(p)) return BIRKHOFF4_ERR_ALIGN;
+    const size_t row = static_cast<size_t>(C) * dtype_bytes(x_dtype), b = static_cast<size_t>(B), R = Gates<N>::rows;
+    const Span ins[] = {{X, b * N * row}, {W, R * N * row}, {alpha, 12}, {bias, 4 * R}, {q, b * R * 4}, {rms, b * 4},
+                        {dU, b * row}, {dh, b * N * 4}, {dH, b * N * N * 4}, {E, b * N * row}};
+    const Span outs[] = {{dX, b * N * row}, {dW, R * N * row}, {dalpha, 12}, {dbias, 4 * R},
+                         {work, static_cast<size_t>(need)}};
+    if (!disjoint(outs, 5, ins, 10)) return BIRKHOFF4_ERR_OVERLAP;
+    auto launch = x_dtype == BIRKHOFF4_BF16 ? launch_pre_bwd<BIRKHOFF4_BF16, N> : launch_pre_bwd<BIRKHOFF4_F32, N>;
+    return launch(s, X, W, alpha, bias, q, rms, dU, dh, dH, E, dX, dW, dalpha, dbias, static_cast<char*>(work), stream);
+}
+
+}  // namespace
+
+extern "C" {
+
+int64_t birkhoff4_pre_work(int64_t B, int64_t C, int x_dtype, int backward) { return pre_work(4, B, C, x_dtype, backward); }
+int64_t birkhoff8_pre_work(int64_t B, int64_t C, int x_dtype, int backward) { return pre_work(8, B, C, x_dtype, backward); }
+
+int birkhoff4_pre_fwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, float eps, void* U,
+                      float* h, float* H, float* q, float* rms, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream) {
+    return pre_fwd<4>(X, W, x_dtype, alpha, bias, eps, U, h, H, q, rms, work, work_bytes, B, C, stream);
+}
+
+int birkhoff8_pre_fwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, float eps, void* U,
+                      float* h, float* H, float* q, float* rms, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream) {
+    return pre_fwd<8>(X, W, x_dtype, alpha, bias, eps, U, h, H, q, rms, work, work_bytes, B, C, stream);
+}
+
+int birkhoff4_pre_bwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, const float* q,
+                      const float* rms, const void* dU, const float* dh, const float* dH, const void* E, void* dX,
+                      void* dW, float* dalpha, float* dbias, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream) {
+    return pre_bwd<4>(X, W, x_dtype, alpha, bias, q, rms, dU, dh, dH, E, dX, dW, dalpha, dbias, work, work_bytes, B, C,
+                      stream);
+}
+
+int birkhoff8_pre_bwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, const float* q,
+                      const float* rms, const void* dU, const float* dh, const float* dH, const void* E, void* dX,
+                      void* dW, float* dalpha, float* dbias, void* work, int64_t work_bytes, int64_t B, int64_t C,
+                      hipStream_t stream) {
+    return pre_bwd<8>(X, W, x_dtype, alpha, bias, q, rms, dU, dh, dH, E, dX, dW, dalpha, dbias, work, work_bytes, B, C,
+                      stream);
+}
+
+}  // extern "C"
