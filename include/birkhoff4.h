@@ -335,6 +335,37 @@ int birkhoff8_pre_bwd(const void* X, const void* W, int x_dtype, const float* al
                       hipStream_t stream);
 int64_t birkhoff8_pre_work(int64_t B, int64_t C, int x_dtype, int backward);
 
+/* How the layer writes its streams (Sec. 2.1): the residual mixing of birkhoff4_mix_fwd plus the
+ * branch's output Z, weighted by h and with dropout,
+ *   Y_i = sum_j P_ij X_j + h_i D,  P = proj(exp(H)),  D = Z / (1 - p) where kept, else 0.
+ *
+ * h    [B][n] fp32 (n = 4 here), Z [B][C] in x_dtype (NULL allowed when C = 0).
+ * p    dropout probability, 0 <= p < 1 (BIRKHOFF4_ERR_DROP). rng is two 64-bit words in device
+ *      memory, seed and offset; NULL allowed with p = 0. Element e of Z (counted over the whole
+ *      array) is kept where word e mod 4 of the Philox 4x32-10 block with counter (e div 4, offset)
+ *      and key seed is at least floor(p 2^32); no mask is stored. Neither n, the dtype nor the
+ *      launch changes it. The words are read when the work runs: a replayed graph takes what they
+ *      are by then, and the backward must find what the forward found.
+ * The other arguments as in birkhoff4_mix_fwd; sums are fp32, bf16 results rounded once. */
+int birkhoff4_post_fwd(const void* H, int h_dtype, const void* X, const float* h, const void* Z, int x_dtype, double p,
+                       const int64_t* rng, void* Y, float* P, float* dual, int32_t* iters, int64_t B, int64_t C,
+                       float tol, int max_iter, hipStream_t stream);
+
+/* Backward of birkhoff4_post_fwd: from its P, X, h, Z, p and rng, and dY [B][n][C] (x_dtype), writes
+ * dX and dH as birkhoff4_mix_bwd_ex does, dZ [B][C] (x_dtype) and dh [B][n] (fp32), in one pass over
+ * X, Z and dY. Outputs must not overlap each other or any input. */
+int birkhoff4_post_bwd(const float* P, const void* X, const float* h, const void* Z, const void* dY, int x_dtype, double p,
+                       const int64_t* rng, void* dX, void* dZ, float* dh, void* dH, int dh_dtype, int64_t B, int64_t C,
+                       hipStream_t stream);
+
+/* The same with n = 8 streams per token; dP [B][8][8] fp32 as in birkhoff8_mix_bwd_ex. */
+int birkhoff8_post_fwd(const void* H, int h_dtype, const void* X, const float* h, const void* Z, int x_dtype, double p,
+                       const int64_t* rng, void* Y, float* P, float* dual, int32_t* iters, int64_t B, int64_t C,
+                       float tol, int max_iter, hipStream_t stream);
+int birkhoff8_post_bwd(const float* P, const void* X, const float* h, const void* Z, const void* dY, int x_dtype, double p,
+                       const int64_t* rng, void* dX, void* dZ, float* dh, float* dP, void* dH, int dh_dtype, int64_t B,
+                       int64_t C, hipStream_t stream);
+
 /* Human-readable text for a return code (static storage). */
 const char* birkhoff4_strerror(int code);
 

@@ -19,6 +19,9 @@ a GPU, the calls raise.
     Y, P, _, _ = mix8_fwd(H8, X8); dX, dH = mix8_bwd(P, X8, dY)  # 8 streams per token
     U, h, H, q, rms = pre_fwd(X, W, alpha, bias)  # the streams' coefficients and the branch's input
     U, h, H, X = pre(X, W, alpha, bias)  # autograd-aware, gradients for all four (4 or 8 streams)
+    Y, P, _, _ = post_fwd(H, X, h, Z, p, rng); dX, dH, dh, dZ = post_bwd(P, X, h, Z, dY, p, rng)
+    Y = post(H, X, h, Z, p, rng)      # autograd-aware: Y = P X + h drop(Z), the branch written back
+    Y = connect(X, W, alpha, bias, branch)  # pre, the caller's branch, post: a whole layer's update
 """
 from __future__ import annotations
 
@@ -54,6 +57,7 @@ def _load():
             "(or __graft_entry__.build())")
     lib = ctypes.CDLL(LIB_PATH)
     vp, i64, f32, i32, st = ctypes.c_void_p, ctypes.c_int64, ctypes.c_float, ctypes.c_int, ctypes.c_void_p
+    f64 = ctypes.c_double
     sigs = {
         "birkhoff4_fwd": [vp, vp, vp, i64, f32, i32, st],
         "birkhoff4_bwd": [vp, vp, vp, vp, i64, st],
@@ -83,6 +87,8 @@ def _load():
     for n in (4, 8):
         sigs[f"birkhoff{n}_pre_fwd"] = [vp, vp, i32, vp, vp, f32, vp, vp, vp, vp, vp, vp, i64, i64, i64, st]
         sigs[f"birkhoff{n}_pre_bwd"] = [vp, vp, i32] + [vp] * 13 + [i64, i64, i64, st]
+        sigs[f"birkhoff{n}_post_fwd"] = [vp, i32, vp, vp, vp, i32, f64, vp, vp, vp, vp, vp, i64, i64, f32, i32, st]
+        sigs[f"birkhoff{n}_post_bwd"] = [vp] * 5 + [i32, f64] + [vp] * (n // 4 + 4) + [i32, i64, i64, st]
     for name, args in sigs.items():
         fn = getattr(lib, name)
         fn.argtypes = args
@@ -624,6 +630,112 @@ def pre(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tenso
     """pre_fwd with gradients for X, W, alpha and bias: (U, h, H, X). The X returned is the X
     given; give it to what uses the streams next, and their gradient costs no pass of its own."""
     return PreFn.apply(X, W, alpha, bias, eps)
+
+
+def _written(lead, n: int, C: int, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: float,
+             rng: torch.Tensor | None) -> None:
+    _dense(h, "h", (*lead, n), torch.float32, X)
+    _dense(Z, "Z", (*lead, C), X.dtype, X)
+    if rng is not None:
+        _dense(rng, "rng", (2,), torch.int64, X)
+    elif p != 0.0:
+        raise ValueError("dropout needs rng, an int64 tensor (seed, offset) on the GPU")
+
+
+def _side(H: torch.Tensor, name: str) -> int:
+    n = H.shape[-1] if H.dim() >= 2 else 0
+    if n not in (4, 8):
+        raise ValueError(f"{name} must have shape [..., 4, 4] or [..., 8, 8], got {tuple(H.shape)}")
+    return n
+
+
+def post_fwd(H: torch.Tensor, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: float = 0.0,
+             rng: torch.Tensor | None = None, tol: float = DEFAULT_TOL, max_iter: int = DEFAULT_MAX_ITER,
+             want_dual: bool = False, want_iters: bool = False):
+    """How a hyper-connection layer writes its streams: mix_fwd (mix8_fwd) plus the branch's output,
+    Y_i = sum_j P_ij X_j + h_i drop(Z) per token.
+
+    H: [..., n, n] float32 or bfloat16 logits, X: [..., n, C] streams, h: [..., n] float32,
+    Z: [..., C] of X's dtype. p: dropout probability of Z's elements, 0 <= p < 1, whose mask is a
+    function of rng, an int64 tensor (seed, offset) on the GPU, and the element's index, and is
+    never stored: change rng from call to call, on the device where a captured graph replays it.
+    Returns (Y like X, P float32, dual or None, iters or None)."""
+    n = _side(H, "H")
+    B = _batch(H, "H", n)
+    lead = H.shape[:-2]
+    C = _streams(X, lead, "X", n)
+    _same_device(H, X)
+    _written(lead, n, C, X, h, Z, p, rng)
+    Y = torch.empty_like(X)
+    P = torch.empty(H.shape, dtype=torch.float32, device=H.device)
+    dual = torch.empty(*lead, 2 * n, dtype=torch.float32, device=H.device) if want_dual else None
+    iters = torch.empty(lead, dtype=torch.int32, device=H.device) if want_iters else None
+    _call(f"birkhoff{n}_post_fwd", H, _ptr(H), _dtype_code(H), _ptr(X), _ptr(h), _ptr(Z), _dtype_code(X), float(p),
+          _ptr(rng), _ptr(Y), _ptr(P), _ptr(dual), _ptr(iters), B, C, float(tol), int(max_iter))
+    return Y, P, dual, iters
+
+
+def _post_bwd(P, X, h, Z, dY, p, rng, dtype=torch.float32):
+    """(dX, dH stored as dtype, dh, dZ)."""
+    n = _side(P, "P")
+    B = _batch(P, "P", n)
+    if P.dtype != torch.float32:
+        raise TypeError("P must be float32")
+    lead = P.shape[:-2]
+    C = _streams(X, lead, "X", n)
+    if _streams(dY, lead, "dY", n) != C or dY.dtype != X.dtype:
+        raise ValueError("dY must have the shape and dtype of X")
+    _same_device(P, X, dY)
+    _written(lead, n, C, X, h, Z, p, rng)
+    dX, dZ, dh = torch.empty_like(X), torch.empty_like(Z), torch.empty_like(h)
+    dH = torch.empty(P.shape, dtype=dtype, device=P.device)
+    places = [dH]
+    if n == 8:  # dL/dP in fp32 on the way, in dH's own memory if that is fp32
+        places.insert(0, dH if dtype == torch.float32 else torch.empty(P.shape, dtype=torch.float32, device=P.device))
+    _call(f"birkhoff{n}_post_bwd", P, _ptr(P), _ptr(X), _ptr(h), _ptr(Z), _ptr(dY), _dtype_code(X), float(p), _ptr(rng),
+          _ptr(dX), _ptr(dZ), _ptr(dh), *(_ptr(t) for t in places), _dtype_code(dH), B, C)
+    return dX, dH, dh, dZ
+
+
+def post_bwd(P: torch.Tensor, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, dY: torch.Tensor, p: float = 0.0,
+             rng: torch.Tensor | None = None):
+    """Backward of post_fwd from its P and inputs (rng unchanged) and dY (like X): (dX, dH, dh, dZ),
+    dH and dh float32, the others like X."""
+    return _post_bwd(P, X, h, Z, dY, p, rng)
+
+
+class PostFn(torch.autograd.Function):
+    """post_fwd with gradients for H, X, h and Z; the backward is one pass over X, Z and dY."""
+
+    @staticmethod
+    def forward(ctx, H, X, h, Z, p=0.0, rng=None, tol=DEFAULT_TOL, max_iter=DEFAULT_MAX_ITER):
+        X, h, Z = X.contiguous(), h.contiguous(), Z.contiguous()
+        Y, P, _, _ = post_fwd(H.contiguous(), X, h, Z, p, rng, tol, max_iter)
+        # rng is saved too: changed in place before the backward, it raises there
+        ctx.save_for_backward(P, X, h, Z, rng)
+        ctx.p, ctx.h_dtype = p, H.dtype
+        return Y
+
+    @staticmethod
+    def backward(ctx, dY):
+        P, X, h, Z, rng = ctx.saved_tensors
+        dX, dH, dh, dZ = _post_bwd(P, X, h, Z, dY.contiguous(), ctx.p, rng, ctx.h_dtype)
+        return dH, dX, dh, dZ, None, None, None, None
+
+
+def post(H: torch.Tensor, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: float = 0.0,
+         rng: torch.Tensor | None = None, tol: float = DEFAULT_TOL, max_iter: int = DEFAULT_MAX_ITER) -> torch.Tensor:
+    """post_fwd under autograd: Y alone, with gradients for H, X, h and Z."""
+    return PostFn.apply(H, X, h, Z, p, rng, tol, max_iter)
+
+
+def connect(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, branch, p: float = 0.0,
+            rng: torch.Tensor | None = None, eps: float = DEFAULT_EPS, tol: float = DEFAULT_TOL,
+            max_iter: int = DEFAULT_MAX_ITER) -> torch.Tensor:
+    """A hyper-connection layer around `branch` (Sec. 2.1: x <- H^res x + (H^post)^T F(H^pre x)):
+    pre, Z = branch(U) with U and Z [..., C], post. Under autograd or without."""
+    U, h, H, X = pre(X, W, alpha, bias, eps)
+    return post(H, X, h, branch(U), p, rng, tol, max_iter)
 
 
 def version() -> int:

@@ -1081,9 +1081,10 @@ __device__ __forceinline__ void unpack_word(const v4u c, int w, float v[MixChunk
 
 // out_i = sum_j m_ij in_j over the E channels of one chunk of each of the N rows (TRANS:
 // m_ji, the transpose, read in place), one 32-bit word of the chunk at a time so that only
-// that word's channels are unpacked at once.
-template <int DX, int N, bool TRANS = false>
-__device__ __forceinline__ void mix_chunk(const float m[N * N], const v4u in[N], v4u out[N]) {
+// that word's channels are unpacked at once. POST: plus hs_i z, rounded once.
+template <int DX, int N, bool TRANS = false, bool POST = false>
+__device__ __forceinline__ void mix_chunk(const float m[N * N], const v4u in[N], v4u out[N], const float* hs = nullptr,
+                                          const v4u z = v4u{0u, 0u, 0u, 0u}) {
     constexpr int EW = MixChunk<DX>::E / 4;
     uint32_t o[N][4];
 #pragma unroll
@@ -1091,12 +1092,15 @@ __device__ __forceinline__ void mix_chunk(const float m[N * N], const v4u in[N],
         float x[N][EW];
 #pragma unroll
         for (int j = 0; j < N; ++j) unpack_word<DX>(in[j], w, x[j]);
+        float d[EW];
+        if constexpr (POST) unpack_word<DX>(z, w, d);
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float y[EW];
 #pragma unroll
             for (int e = 0; e < EW; ++e) {
                 y[e] = m[TRANS ? i : N * i] * x[0][e];
+                if constexpr (POST) y[e] = __builtin_fmaf(hs[i], d[e], y[e]);
 #pragma unroll
                 for (int j = 1; j < N; ++j) y[e] = __builtin_fmaf(m[TRANS ? N * j + i : N * i + j], x[j][e], y[e]);
             }
@@ -1108,6 +1112,78 @@ __device__ __forceinline__ void mix_chunk(const float m[N * N], const v4u in[N],
     }
 #pragma unroll
     for (int i = 0; i < N; ++i) out[i] = v4u{o[i][0], o[i][1], o[i][2], o[i][3]};
+}
+
+// What the layer's write (post) adds to the mixing: Y_i += h_i drop(Z), Z [B][C] the branch's
+// output. drop keeps an element where its word of the counter-based generator is at least `least`
+// and scales by 1 / (1 - p); the words are drawn again in the backward, no mask is stored.
+template <bool POST>
+struct Write {};
+
+template <>
+struct Write<true> {
+    const float* h;       // [B][N]
+    const v4u* Z;
+    const uint64_t* rng;  // seed and offset, in device memory: a replayed graph reads what they are then
+    uint32_t least;       // floor(p 2^32); 0 keeps everything
+    float scale;          // 1 / (1 - p)
+};
+
+// And its gradients' places.
+template <bool POST>
+struct WriteBack {};
+
+template <>
+struct WriteBack<true> {
+    v4u* dZ;
+    float* dh;  // [B][N]
+};
+
+// Philox 4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011): four words
+// for each value of a counter of four words under a key of two; ten rounds are the authors' own
+// choice.
+__device__ __forceinline__ v4u philox(uint64_t index, uint64_t offset, uint64_t seed) {
+    uint32_t c0 = static_cast<uint32_t>(index), c1 = static_cast<uint32_t>(index >> 32);
+    uint32_t c2 = static_cast<uint32_t>(offset), c3 = static_cast<uint32_t>(offset >> 32);
+    uint32_t k0 = static_cast<uint32_t>(seed), k1 = static_cast<uint32_t>(seed >> 32);
+#pragma unroll
+    for (int r = 0; r < 10; ++r) {
+        const uint64_t a = static_cast<uint64_t>(0xD2511F53u) * c0, b = static_cast<uint64_t>(0xCD9E8D57u) * c2;
+        c0 = static_cast<uint32_t>(b >> 32) ^ c1 ^ k0;
+        c1 = static_cast<uint32_t>(b);
+        c2 = static_cast<uint32_t>(a >> 32) ^ c3 ^ k1;
+        c3 = static_cast<uint32_t>(a);
+        k0 += 0x9E3779B9u;
+        k1 += 0xBB67AE85u;
+    }
+    return v4u{c0, c1, c2, c3};
+}
+
+// Ones where chunk `index` of Z ([B][nc], counted over the whole array) keeps its elements:
+// element e's word is word e % 4 of block e / 4.
+template <int DX>
+__device__ __forceinline__ v4u keep_mask(const Write<true>& wr, int64_t index) {
+    const uint64_t seed = wr.rng[0], offset = wr.rng[1];
+    if constexpr (DX == BIRKHOFF4_F32) {
+        const v4u r = philox(index, offset, seed);
+        v4u m;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) m[k] = r[k] >= wr.least ? 0xffffffffu : 0u;
+        return m;
+    } else {
+        const v4u r = philox(2 * index, offset, seed), q = philox(2 * index + 1, offset, seed);
+        auto pair = [&](uint32_t a, uint32_t b) {
+            return (a >= wr.least ? 0x0000ffffu : 0u) | (b >= wr.least ? 0xffff0000u : 0u);
+        };
+        return v4u{pair(r.x, r.y), pair(r.z, r.w), pair(q.x, q.y), pair(q.z, q.w)};
+    }
+}
+
+// h_i / (1 - p) of token t: what the kept elements are multiplied by.
+template <int N>
+__device__ __forceinline__ void load_gates(const Write<true>& wr, int64_t t, float hs[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) hs[i] = wr.h[N * t + i] * wr.scale;
 }
 
 // P of token t (N x N), uniform over the wave.
@@ -1140,10 +1216,10 @@ __device__ __forceinline__ int64_t mix_token(int64_t k, int64_t count, int win) 
 // (4 x 1000: 93 and 127 us) or the same.
 constexpr int kMixMaxWaves = 16;
 
-template <int DX, int N>
+template <int DX, int N, bool POST>
 __global__ __launch_bounds__(64 * kMixMaxWaves) void mix_fwd_kernel(const float* __restrict__ P,
                                                                     const v4u* __restrict__ X, v4u* __restrict__ Y,
-                                                                    int64_t B, int64_t nc, int win) {
+                                                                    int64_t B, int64_t nc, int win, Write<POST> wr) {
     const unsigned lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int ty = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.y));
@@ -1157,15 +1233,19 @@ __global__ __launch_bounds__(64 * kMixMaxWaves) void mix_fwd_kernel(const float*
              col += 64 * static_cast<int64_t>(gridDim.y) * W) {
             const int64_t off = N * nc * t + col;  // uniform: scalar row addresses, the lane a 32-bit offset
             const bool own = lane < nc - col;
-            v4u x[N], y[N];
+            v4u x[N], y[N], z = {0u, 0u, 0u, 0u};
             if (own) {
 #pragma unroll
                 for (int j = 0; j < N; ++j) x[j] = __builtin_nontemporal_load(X + (off + j * nc) + lane);
+                if constexpr (POST) z = __builtin_nontemporal_load(wr.Z + (nc * t + col) + lane);
             }
-            float p[N * N];
+            float p[N * N], hs[N];
             load_token_matrix<N>(P, t, p);
+            if constexpr (POST) load_gates<N>(wr, t, hs);
             if (own) {
-                mix_chunk<DX, N>(p, x, y);
+                if constexpr (POST)
+                    if (wr.least) z &= keep_mask<DX>(wr, nc * t + col + lane);
+                mix_chunk<DX, N, false, POST>(p, x, y, hs, z);
 #pragma unroll
                 for (int j = 0; j < N; ++j) __builtin_nontemporal_store(y[j], Y + (off + j * nc) + lane);
             }
@@ -1206,6 +1286,37 @@ __device__ __forceinline__ void add_outer(const v4u x[N], const v4u g[N], float 
     }
 }
 
+// acc_i += sum_c z[c] g_i[c] over one chunk, as in add_outer.
+template <int DX, int N>
+__device__ __forceinline__ void add_inner(const v4u z, const v4u g[N], float acc[N]) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w)
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            if constexpr (DX == BIRKHOFF4_BF16)
+                acc[i] = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, static_cast<uint32_t>(z[w])),
+                                                         __builtin_bit_cast(bf16x2, static_cast<uint32_t>(g[i][w])), acc[i],
+                                                         false);
+            else
+                acc[i] = __builtin_fmaf(__uint_as_float(z[w]), __uint_as_float(g[i][w]), acc[i]);
+        }
+}
+
+// sum_i hs_i g_i over one chunk of each row.
+template <int DX, int N>
+__device__ __forceinline__ v4u combine_chunk(const float hs[N], const v4u g[N]) {
+    constexpr int E = MixChunk<DX>::E;
+    float sum[E];
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        float v[E];
+        unpack_chunk<DX>(g[i], v);
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] = i == 0 ? hs[0] * v[e] : __builtin_fmaf(hs[i], v[e], sum[e]);
+    }
+    return pack_chunk<DX>(sum);
+}
+
 // Row `i` (a lane index) of token t's 4 x 4 dH, which the lane holds whole, stored as fp32 or
 // rounded to nearest even as bf16.
 __device__ __forceinline__ void store_dh_row(void* dH, bool h16, int64_t t, int i, const float m[16]) {
@@ -1224,30 +1335,37 @@ __device__ __forceinline__ void store_dh_row(void* dH, bool h16, int64_t t, int 
 // sums its lanes' parts; with W > 1 the waves leave them in LDS and the first one adds them
 // in wave order, so the result does not depend on timing. For n = 4 it then forms dH; for n =
 // 8 it writes dP, lane L entry L, for the 8 x 8 backward to take over.
-constexpr int mix_bwd_max_waves(int n) { return n == 8 ? 8 : kMixMaxWaves; }
+constexpr int mix_bwd_max_waves(int n, bool post) { return n == 8 || post ? 8 : kMixMaxWaves; }
 
-template <int DX, int N>
-__global__ __launch_bounds__(64 * mix_bwd_max_waves(N)) void mix_bwd_kernel(const float* __restrict__ P,
+//
+// POST: dh_i = sum_c dY_i[c] drop(Z)[c] goes the way of dP, and dZ = drop(sum_i h_i dY_i) is
+// written beside dX.
+template <int DX, int N, bool POST>
+__global__ __launch_bounds__(64 * mix_bwd_max_waves(N, POST)) void mix_bwd_kernel(const float* __restrict__ P,
                                                                            const v4u* __restrict__ X,
                                                                            const v4u* __restrict__ dY,
                                                                            v4u* __restrict__ dX, void* __restrict__ dH,
-                                                                           int64_t B, int64_t nc, int win, bool h16) {
+                                                                           int64_t B, int64_t nc, int win, bool h16,
+                                                                           Write<POST> wr, WriteBack<POST> wb) {
     constexpr int NN = N * N;
-    __shared__ float part[mix_bwd_max_waves(N) * NN];  // [wave][entry]
+    __shared__ float part[mix_bwd_max_waves(N, POST) * NN];  // [wave][entry]
+    __shared__ float part_h[POST ? mix_bwd_max_waves(N, POST) * N : 1];
     const unsigned lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int W = blockDim.x >> 6;
     for (int64_t k = blockIdx.x; k < B; k += gridDim.x) {
         const int64_t t = mix_token(k, B, win);
-        float p[NN], acc[NN];
+        float p[NN], acc[NN], hacc[N];
 #pragma unroll
         for (int q = 0; q < NN; ++q) acc[q] = 0.f;
+#pragma unroll
+        for (int q = 0; q < N; ++q) hacc[q] = 0.f;
         for (int64_t col = 64 * w; col < nc; col += 64 * W) {
             const int64_t off = N * nc * t + col;  // uniform: scalar row addresses, the lane a 32-bit offset
             const bool own = lane < nc - col;
             int64_t nr = nc;  // opaque: rows are stepped to here, not kept as 3 N addresses over the loop
             asm volatile("" : "+s"(nr));
-            v4u x[N], g[N], o[N];
+            v4u x[N], g[N], o[N], z = {0u, 0u, 0u, 0u};
 #pragma unroll
             for (int j = 0; j < N; ++j) x[j] = g[j] = v4u{0u, 0u, 0u, 0u};
             if (own) {
@@ -1255,11 +1373,21 @@ __global__ __launch_bounds__(64 * mix_bwd_max_waves(N)) void mix_bwd_kernel(cons
                 for (int j = 0; j < N; ++j) x[j] = __builtin_nontemporal_load(X + (off + j * nr) + lane);
 #pragma unroll
                 for (int j = 0; j < N; ++j) g[j] = __builtin_nontemporal_load(dY + (off + j * nr) + lane);
+                if constexpr (POST) z = __builtin_nontemporal_load(wr.Z + (nc * t + col) + lane);
             }
             load_token_matrix<N>(P, t, p);
             // dP first: X's registers are then free for dX (three waves per SIMD with n = 8)
             add_outer<DX, N>(x, g, acc);
             __builtin_amdgcn_sched_barrier(0);
+            if constexpr (POST) {
+                v4u keep = {~0u, ~0u, ~0u, ~0u};
+                if (wr.least) keep = keep_mask<DX>(wr, nc * t + col + lane);
+                add_inner<DX, N>(z & keep, g, hacc);
+                float hs[N];
+                load_gates<N>(wr, t, hs);
+                const v4u dz = combine_chunk<DX, N>(hs, g) & keep;
+                if (own) __builtin_nontemporal_store(dz, wb.dZ + (nc * t + col) + lane);
+            }
             mix_chunk<DX, N, true>(p, g, o);
             if (own) {
 #pragma unroll
@@ -1270,16 +1398,28 @@ __global__ __launch_bounds__(64 * mix_bwd_max_waves(N)) void mix_bwd_kernel(cons
         const int entry = N == 4 ? lane >> 2 : lane;
         float own_sum[1];
         lane_sums<32, NN>(acc, own_sum, lane);
-        float sum = N == 4 ? qsum(own_sum[0]) : own_sum[0];
+        float sum = N == 4 ? qsum(own_sum[0]) : own_sum[0], hsum = 0.f;
+        const int gate = lane / (64 / N);  // dh's entry of this lane
+        if constexpr (POST) {
+            lane_sums<32, N>(hacc, own_sum, lane);
+            hsum = rest_sum<N>(own_sum[0]);
+        }
         if (W > 1) {  // uniform over the block
             part[NN * w + entry] = sum;
+            if constexpr (POST) part_h[N * w + gate] = hsum;
             __syncthreads();
             if (w == 0) {
                 sum = part[entry];
                 for (int q = 1; q < W; ++q) sum += part[NN * q + entry];
+                if constexpr (POST) {
+                    hsum = part_h[gate];
+                    for (int q = 1; q < W; ++q) hsum += part_h[N * q + gate];
+                }
             }
         }
         if (w == 0) {
+            if constexpr (POST)
+                if (lane % (64 / N) == 0) wb.dh[N * t + gate] = hsum * wr.scale;
             if constexpr (N == 8) {
                 static_cast<float*>(dH)[64 * t + lane] = sum;
             } else {
@@ -1312,33 +1452,40 @@ __device__ __forceinline__ void load_lane_matrix(const float* __restrict__ P, in
     }
 }
 
-template <int DX, int N, int L>
+template <int DX, int N, int L, bool POST>
 __global__ __launch_bounds__(mix_short_block(L)) void mix_fwd_short_kernel(const float* __restrict__ P,
                                                                            const v4u* __restrict__ X,
-                                                                           v4u* __restrict__ Y, int64_t B, int nc) {
+                                                                           v4u* __restrict__ Y, int64_t B, int nc,
+                                                                           Write<POST> wr) {
     constexpr int T = mix_short_block(L) / L;  // tokens per block
     const int c = threadIdx.x % L;
     for (int64_t t = static_cast<int64_t>(blockIdx.x) * T + threadIdx.x / L; t < B;
          t += static_cast<int64_t>(gridDim.x) * T) {
         if (c >= nc) return;
         const int64_t off = static_cast<int64_t>(N) * nc * t + c;
-        v4u x[N], y[N];
+        v4u x[N], y[N], z = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = __builtin_nontemporal_load(X + off + j * nc);
-        float p[N * N];
+        if constexpr (POST) z = __builtin_nontemporal_load(wr.Z + nc * t + c);
+        float p[N * N], hs[N];
         load_lane_matrix<N>(P, t, p);
-        mix_chunk<DX, N>(p, x, y);
+        if constexpr (POST) {
+            load_gates<N>(wr, t, hs);
+            if (wr.least) z &= keep_mask<DX>(wr, nc * t + c);
+        }
+        mix_chunk<DX, N, false, POST>(p, x, y, hs, z);
 #pragma unroll
         for (int j = 0; j < N; ++j) __builtin_nontemporal_store(y[j], Y + off + j * nc);
     }
 }
 
-template <int DX, int N, int L>
+template <int DX, int N, int L, bool POST>
 __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const float* __restrict__ P,
                                                                            const v4u* __restrict__ X,
                                                                            const v4u* __restrict__ dY,
                                                                            v4u* __restrict__ dX, void* __restrict__ dH,
-                                                                           int64_t B, int nc, bool h16) {
+                                                                           int64_t B, int nc, bool h16, Write<POST> wr,
+                                                                           WriteBack<POST> wb) {
     constexpr int NN = N * N, T = mix_short_block(L) / L;  // T: tokens per block
     const int c = threadIdx.x % L;
     const int64_t first = static_cast<int64_t>(blockIdx.x) * T;
@@ -1347,7 +1494,7 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const
         const int64_t t = base + threadIdx.x / L;
         const bool valid = t < B, own = valid && c < nc;
         const int64_t off = static_cast<int64_t>(N) * nc * t + c;
-        v4u x[N], g[N], o[N];
+        v4u x[N], g[N], o[N], z = {0u, 0u, 0u, 0u};
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = g[j] = v4u{0u, 0u, 0u, 0u};
         if (own) {
@@ -1355,6 +1502,7 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const
             for (int j = 0; j < N; ++j) x[j] = __builtin_nontemporal_load(X + off + j * nc);
 #pragma unroll
             for (int j = 0; j < N; ++j) g[j] = __builtin_nontemporal_load(dY + off + j * nc);
+            if constexpr (POST) z = __builtin_nontemporal_load(wr.Z + nc * t + c);
         }
         float p[NN], acc[NN];
 #pragma unroll
@@ -1366,6 +1514,34 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const
             for (int j = 0; j < N; ++j) __builtin_nontemporal_store(o[j], dX + off + j * nc);
         }
         add_outer<DX, N>(x, g, acc);
+        // the sum over the token's L lanes, in all of them
+        auto total = [&](float v) {
+            float s = gsum_lanes<8>(v);
+            if constexpr (L >= 16)
+                s += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(s), 0x128, 0xF, 0xF, true));  // row_ror:8
+            if constexpr (L >= 32) {
+                const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
+                s = __uint_as_float(r[0]) + __uint_as_float(r[1]);
+            }
+            return s;
+        };
+        if constexpr (POST) {
+            v4u keep = {~0u, ~0u, ~0u, ~0u};
+            if (wr.least) keep = keep_mask<DX>(wr, nc * t + c);
+            float hacc[N], hs[N], mine = 0.f;
+#pragma unroll
+            for (int i = 0; i < N; ++i) hacc[i] = hs[i] = 0.f;
+            add_inner<DX, N>(z & keep, g, hacc);
+            if (valid) load_gates<N>(wr, t, hs);
+            const v4u dz = combine_chunk<DX, N>(hs, g) & keep;
+            if (own) __builtin_nontemporal_store(dz, wb.dZ + nc * t + c);
+#pragma unroll
+            for (int i = 0; i < N; ++i) {
+                const float s = total(hacc[i]);
+                if (c == i) mine = s;
+            }
+            if (valid && c < N) wb.dh[N * t + c] = mine * wr.scale;
+        }
         if constexpr (N == 8) {
             constexpr int NE = 64 / L;  // entries of dP per lane
             float d[NE];
@@ -1378,16 +1554,7 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const
             // every lane of the token needs the sixteen sums: butterflies over its L lanes
             float G[16], out[16];
 #pragma unroll
-            for (int q = 0; q < 16; ++q) {
-                float s = gsum_lanes<8>(acc[q]);
-                if constexpr (L >= 16)
-                    s += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(s), 0x128, 0xF, 0xF, true));  // row_ror:8
-                if constexpr (L >= 32) {
-                    const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(s), __float_as_uint(s), false, false);
-                    s = __uint_as_float(r[0]) + __uint_as_float(r[1]);
-                }
-                G[q] = s;
-            }
+            for (int q = 0; q < 16; ++q) G[q] = total(acc[q]);
             implicit_vjp(p, G, out);
             if (valid && c < 4) store_dh_row(dH, h16, t, c, out);
         }
@@ -2592,11 +2759,11 @@ __global__ __launch_bounds__(kGrp8Block) void newton8_fwd_group_kernel(const voi
 // column's loads are in flight; the column-0 wave writes P, dual and status. While the waves
 // are few the repeated projections cost nothing and a launch is saved: 96 tokens of 4 x 4096
 // bf16 channels, N(0,1) logits, 7.3 us as two launches, 4.6 as one.
-template <int DX, int DT, int N, bool WRITE_DUAL, bool WRITE_ITERS>
+template <int DX, int DT, int N, bool WRITE_DUAL, bool WRITE_ITERS, bool POST>
 __global__ __launch_bounds__(64) void mix_small_kernel(const void* __restrict__ H, const v4u* __restrict__ X,
                                                        v4u* __restrict__ Y, float* __restrict__ P,
                                                        float* __restrict__ dual, int32_t* __restrict__ iters, int64_t nc,
-                                                       float tol, int max_iter) {
+                                                       float tol, int max_iter, Write<POST> wr) {
     const int64_t t = blockIdx.x, col = 64 * static_cast<int64_t>(blockIdx.y);
     const unsigned lane = threadIdx.x;
     const int q = lane % N;  // this lane's row
@@ -2613,6 +2780,13 @@ __global__ __launch_bounds__(64) void mix_small_kernel(const void* __restrict__ 
     if (own) {
 #pragma unroll
         for (int j = 0; j < N; ++j) x[j] = __builtin_nontemporal_load(X + (off + j * nc) + lane);
+    }
+    v4u z = {0u, 0u, 0u, 0u};
+    float hs[N];
+    if constexpr (POST) {
+        if (own) z = __builtin_nontemporal_load(wr.Z + (nc * t + col) + lane);
+        load_gates<N>(wr, t, hs);
+        if (wr.least) z &= keep_mask<DX>(wr, nc * t + col + lane);
     }
     float p[N * N];  // row i from lane i, uniform
     auto gather = [&](const float T[N]) {
@@ -2631,7 +2805,7 @@ __global__ __launch_bounds__(64) void mix_small_kernel(const void* __restrict__ 
         if (col == 0 && lane < 8) store_group8<1, WRITE_DUAL, WRITE_ITERS, false>(P, dual, iters, t, q, r, ma, 1.f);
         gather(r.T[0]);
     }
-    mix_chunk<DX, N>(p, x, y);
+    mix_chunk<DX, N, false, POST>(p, x, y, hs, z);
     if (own) {
 #pragma unroll
         for (int j = 0; j < N; ++j) __builtin_nontemporal_store(y[j], Y + (off + j * nc) + lane);
@@ -3596,12 +3770,12 @@ struct MixLaunch {
     int win;  // tokens in an XCD's window
 };
 
-MixLaunch mix_launch(int64_t B, int64_t nc, int n, bool backward, bool bf16) {
+MixLaunch mix_launch(int64_t B, int64_t nc, int n, bool backward, bool bf16, bool post) {
     const int64_t cols = nc > 0 ? (nc + 63) / 64 : 1;
     const bool wide8 = n == 8 && cols > 8, alone = B <= 256;  // alone: no second block on a CU
     int64_t most = n == 4 ? kMixMaxWaves : wide8 ? 4 : 8;
     if (backward && n == 4) {
-        const bool whole = cols > 14 && cols <= kMixMaxWaves && (!bf16 || alone || (cols == 15 && B >= 8192));
+        const bool whole = !post && cols > 14 && cols <= kMixMaxWaves && (!bf16 || alone || (cols == 15 && B >= 8192));
         most = whole ? kMixMaxWaves : 8;
     }
     if (backward && n == 8) {
@@ -3624,8 +3798,9 @@ unsigned mix_short_grid(int64_t B, int lanes) {
     return static_cast<unsigned>(want < kMixMaxGrid ? want : kMixMaxGrid);
 }
 
-template <int DX, int N = 4>
-int launch_mix_fwd(const float* P, const void* X, void* Y, int64_t B, int64_t nc, hipStream_t stream) {
+template <int DX, int N = 4, bool POST = false>
+int launch_mix_fwd(const float* P, const void* X, void* Y, int64_t B, int64_t nc, hipStream_t stream,
+                   const Write<POST>& wr = {}) {
     const v4u* x = static_cast<const v4u*>(X);
     v4u* y = static_cast<v4u*>(Y);
     // (The 64 entries of P that each lane of an 8-stream token reads cost more than idle lanes
@@ -3635,15 +3810,15 @@ int launch_mix_fwd(const float* P, const void* X, void* Y, int64_t B, int64_t nc
     constexpr int64_t kShort = N == 4 && DX == BIRKHOFF4_BF16 ? kMixShortRow : 16;
     if (nc <= kShort) {
         const int L = nc <= 8 ? 8 : nc <= 16 ? 16 : 32;
-        auto kern = L == 8 ? mix_fwd_short_kernel<DX, N, 8> : mix_fwd_short_kernel<DX, N, 16>;
+        auto kern = L == 8 ? mix_fwd_short_kernel<DX, N, 8, POST> : mix_fwd_short_kernel<DX, N, 16, POST>;
         if constexpr (kShort > 16)
-            if (L == 32) kern = mix_fwd_short_kernel<DX, N, 32>;
+            if (L == 32) kern = mix_fwd_short_kernel<DX, N, 32, POST>;
         launch_kernel(kern, dim3(mix_short_grid(B, L)), dim3(mix_short_block(L)), 0, stream, P, x, y, B,
-                      static_cast<int>(nc));
+                      static_cast<int>(nc), wr);
         return launch_status();
     }
-    const MixLaunch l = mix_launch(B, nc, N, false, DX == BIRKHOFF4_BF16);
-    launch_kernel((mix_fwd_kernel<DX, N>), l.grid, l.block, 0, stream, P, x, y, B, nc, l.win);
+    const MixLaunch l = mix_launch(B, nc, N, false, DX == BIRKHOFF4_BF16, POST);
+    launch_kernel((mix_fwd_kernel<DX, N, POST>), l.grid, l.block, 0, stream, P, x, y, B, nc, l.win, wr);
     return launch_status();
 }
 
@@ -3661,41 +3836,118 @@ bool mix_small(int64_t B, int64_t nc) {
     return nc > 0 && B <= most && cols <= most && B * cols <= most;
 }
 
-template <int N, int DX, int DT>
+template <int N, int DX, int DT, bool POST>
 int launch_mix_small(const void* H, const void* X, void* Y, float* P, float* dual, int32_t* iters, int64_t B,
-                     int64_t nc, float tol, int max_iter, hipStream_t stream) {
-    auto kern = dual ? (iters ? mix_small_kernel<DX, DT, N, true, true> : mix_small_kernel<DX, DT, N, true, false>)
-                     : (iters ? mix_small_kernel<DX, DT, N, false, true> : mix_small_kernel<DX, DT, N, false, false>);
+                     int64_t nc, float tol, int max_iter, hipStream_t stream, const Write<POST>& wr) {
+    auto kern = dual ? (iters ? mix_small_kernel<DX, DT, N, true, true, POST> : mix_small_kernel<DX, DT, N, true, false, POST>)
+                     : (iters ? mix_small_kernel<DX, DT, N, false, true, POST>
+                              : mix_small_kernel<DX, DT, N, false, false, POST>);
     launch_kernel(kern, dim3(static_cast<unsigned>(B), static_cast<unsigned>((nc + 63) / 64)), dim3(64), 0, stream, H,
-                  static_cast<const v4u*>(X), static_cast<v4u*>(Y), P, dual, iters, nc, tol, max_iter);
+                  static_cast<const v4u*>(X), static_cast<v4u*>(Y), P, dual, iters, nc, tol, max_iter, wr);
     return launch_status();
 }
 
-template <int N>
+template <int N, bool POST = false>
 int launch_mix_small(const void* H, int h_dtype, const void* X, int x_dtype, void* Y, float* P, float* dual,
-                     int32_t* iters, int64_t B, int64_t nc, float tol, int max_iter, hipStream_t stream) {
+                     int32_t* iters, int64_t B, int64_t nc, float tol, int max_iter, hipStream_t stream,
+                     const Write<POST>& wr = {}) {
     constexpr int F = BIRKHOFF4_F32, S = BIRKHOFF4_BF16;
-    auto launch = x_dtype == S ? (h_dtype == S ? launch_mix_small<N, S, S> : launch_mix_small<N, S, F>)
-                               : (h_dtype == S ? launch_mix_small<N, F, S> : launch_mix_small<N, F, F>);
-    return launch(H, X, Y, P, dual, iters, B, nc, tol, max_iter, stream);
+    auto launch = x_dtype == S ? (h_dtype == S ? launch_mix_small<N, S, S, POST> : launch_mix_small<N, S, F, POST>)
+                               : (h_dtype == S ? launch_mix_small<N, F, S, POST> : launch_mix_small<N, F, F, POST>);
+    return launch(H, X, Y, P, dual, iters, B, nc, tol, max_iter, stream, wr);
 }
 
-template <int DX, int N = 4>
+template <int DX, int N = 4, bool POST = false>
 int launch_mix_bwd(const float* P, const void* X, const void* dY, void* dX, void* dH, bool h16, int64_t B, int64_t nc,
-                   hipStream_t stream) {
+                   hipStream_t stream, const Write<POST>& wr = {}, const WriteBack<POST>& wb = {}) {
     const v4u *x = static_cast<const v4u*>(X), *dy = static_cast<const v4u*>(dY);
     v4u* dx = static_cast<v4u*>(dX);
     if (nc <= kMixShortRow) {  // nc = 0 too: dP = 0
         const int L = nc <= 8 ? 8 : nc <= 16 ? 16 : 32;
-        auto kern = L == 8 ? mix_bwd_short_kernel<DX, N, 8>
-                           : L == 16 ? mix_bwd_short_kernel<DX, N, 16> : mix_bwd_short_kernel<DX, N, 32>;
+        auto kern = L == 8 ? mix_bwd_short_kernel<DX, N, 8, POST>
+                           : L == 16 ? mix_bwd_short_kernel<DX, N, 16, POST> : mix_bwd_short_kernel<DX, N, 32, POST>;
         launch_kernel(kern, dim3(mix_short_grid(B, L)), dim3(mix_short_block(L)), 0, stream, P, x, dy, dx, dH, B,
-                      static_cast<int>(nc), h16);
+                      static_cast<int>(nc), h16, wr, wb);
         return launch_status();
     }
-    const MixLaunch l = mix_launch(B, nc, N, true, DX == BIRKHOFF4_BF16);
-    launch_kernel((mix_bwd_kernel<DX, N>), l.grid, l.block, 0, stream, P, x, dy, dx, dH, B, nc, l.win, h16);
+    const MixLaunch l = mix_launch(B, nc, N, true, DX == BIRKHOFF4_BF16, POST);
+    launch_kernel((mix_bwd_kernel<DX, N, POST>), l.grid, l.block, 0, stream, P, x, dy, dx, dH, B, nc, l.win, h16, wr, wb);
     return launch_status();
+}
+
+bool drop_ok(double p) { return p >= 0.0 && p < 1.0; }
+
+Write<true> write_args(const float* h, const void* Z, double p, const void* rng) {
+    return {h, static_cast<const v4u*>(Z), static_cast<const uint64_t*>(rng), static_cast<uint32_t>(p * 4294967296.0),
+            static_cast<float>(1.0 / (1.0 - p))};
+}
+
+template <int N>
+int post_fwd(const void* H, int h_dtype, const void* X, const float* h, const void* Z, int x_dtype, double p,
+             const void* rng, void* Y, float* P, float* dual, int32_t* iters, int64_t B, int64_t C, float tol,
+             int max_iter, hipStream_t stream) {
+    if (B < 0 || B > (INT64_MAX / (16 * N * N))) return BIRKHOFF4_ERR_SIZE;
+    if (!dtype_ok(h_dtype) || !dtype_ok(x_dtype)) return BIRKHOFF4_ERR_DTYPE;
+    const int64_t E = x_dtype == BIRKHOFF4_BF16 ? 8 : 4;
+    if (C < 0 || C % E != 0) return BIRKHOFF4_ERR_CHANNELS;
+    const int64_t nc = C / E;  // 16-byte chunks per row
+    if (B > 0 && nc > INT64_MAX / (16 * N) / B) return BIRKHOFF4_ERR_SIZE;
+    if (!(tol >= 0.f)) return BIRKHOFF4_ERR_TOL;
+    if (max_iter < 0 || max_iter > kMaxIterCap) return BIRKHOFF4_ERR_MAX_ITER;
+    if (!drop_ok(p)) return BIRKHOFF4_ERR_DROP;
+    if (B == 0) return BIRKHOFF4_OK;
+    if (!H || !P || !h || (nc > 0 && (!X || !Z || !Y)) || (p > 0.0 && !rng)) return BIRKHOFF4_ERR_NULL;
+    const void* all[] = {H, X, h, Z, rng, Y, P, dual, iters};
+    for (const void* a : all)
+        if (misaligned(a)) return BIRKHOFF4_ERR_ALIGN;
+    const size_t b = static_cast<size_t>(B), row = static_cast<size_t>(nc) * 16;
+    const Span ins[] = {{H, b * N * N * dtype_bytes(h_dtype)}, {X, b * N * row}, {h, b * N * 4}, {Z, b * row}, {rng, 16}};
+    const Span outs[] = {{Y, b * N * row}, {P, b * N * N * 4}, {dual, b * N * 8}, {iters, b * 4}};
+    if (!disjoint(outs, 4, ins, 5)) return BIRKHOFF4_ERR_OVERLAP;
+    const Write<true> wr = write_args(h, Z, p, rng);
+    if (mix_small<N>(B, nc))
+        return launch_mix_small<N, true>(H, h_dtype, X, x_dtype, Y, P, dual, iters, B, nc, tol, max_iter, stream, wr);
+    // the projection checks and queues P first; the mixing kernel then reads it
+    const int e = N == 4 ? birkhoff4_fwd_ex2(H, h_dtype, P, dual, iters, B, tol, max_iter, BIRKHOFF4_AUTO, stream)
+                         : birkhoff8_fwd(H, h_dtype, P, dual, iters, B, tol, max_iter, stream);
+    if (e || nc == 0) return e;
+    if (x_dtype == BIRKHOFF4_BF16) return launch_mix_fwd<BIRKHOFF4_BF16, N, true>(P, X, Y, B, nc, stream, wr);
+    return launch_mix_fwd<BIRKHOFF4_F32, N, true>(P, X, Y, B, nc, stream, wr);
+}
+
+// dP: with n = 8 the place of dL/dP (dH's own memory if that is fp32, or not overlapping it); with
+// n = 4 dL/dP stays in registers.
+template <int N>
+int post_bwd(const float* P, const void* X, const float* h, const void* Z, const void* dY, int x_dtype, double p,
+             const void* rng, void* dX, void* dZ, float* dh, float* dP, void* dH, int dh_dtype, int64_t B, int64_t C,
+             hipStream_t stream) {
+    if (B < 0 || B > (INT64_MAX / (16 * N * N))) return BIRKHOFF4_ERR_SIZE;
+    if (!dtype_ok(x_dtype) || !dtype_ok(dh_dtype)) return BIRKHOFF4_ERR_DTYPE;
+    const int64_t E = x_dtype == BIRKHOFF4_BF16 ? 8 : 4;
+    if (C < 0 || C % E != 0) return BIRKHOFF4_ERR_CHANNELS;
+    const int64_t nc = C / E;
+    if (B > 0 && nc > INT64_MAX / (16 * N) / B) return BIRKHOFF4_ERR_SIZE;
+    if (!drop_ok(p)) return BIRKHOFF4_ERR_DROP;
+    if (B == 0) return BIRKHOFF4_OK;
+    if (!P || !h || !dh || !dP || !dH || (nc > 0 && (!X || !Z || !dY || !dX || !dZ)) || (p > 0.0 && !rng))
+        return BIRKHOFF4_ERR_NULL;
+    const void* all[] = {P, X, h, Z, dY, rng, dX, dZ, dh, dP, dH};
+    for (const void* a : all)
+        if (misaligned(a)) return BIRKHOFF4_ERR_ALIGN;
+    const size_t b = static_cast<size_t>(B), row = static_cast<size_t>(nc) * 16, nh = b * N * N * dtype_bytes(dh_dtype);
+    const bool in_place = dh_dtype == BIRKHOFF4_F32 && dH == static_cast<void*>(dP);
+    const Span ins[] = {{P, b * N * N * 4}, {X, b * N * row}, {h, b * N * 4}, {Z, b * row}, {dY, b * N * row}, {rng, 16}};
+    const Span outs[] = {{dX, b * N * row}, {dZ, b * row}, {dh, b * N * 4}, {dH, nh},
+                         {dP, N == 4 || in_place ? 0 : b * N * N * 4}};
+    if (!disjoint(outs, 5, ins, 6)) return BIRKHOFF4_ERR_OVERLAP;
+    constexpr int F = BIRKHOFF4_F32, S = BIRKHOFF4_BF16;
+    const Write<true> wr = write_args(h, Z, p, rng);
+    const WriteBack<true> wb = {static_cast<v4u*>(dZ), dh};
+    auto launch = x_dtype == S ? launch_mix_bwd<S, N, true> : launch_mix_bwd<F, N, true>;
+    const int e = launch(P, X, dY, dX, N == 4 ? dH : dP, N == 4 && dh_dtype == S, B, nc, stream, wr, wb);
+    if (e || N == 4) return e;
+    if (in_place) return launch_bwd8<F, F, false, true>(P, dP, dH, B, stream);
+    return dh_dtype == S ? launch_bwd8<F, S, false>(P, dP, dH, B, stream) : launch_bwd8<F, F, false>(P, dP, dH, B, stream);
 }
 
 }  // namespace
@@ -4100,6 +4352,30 @@ int birkhoff8_mix_bwd_ex(const float* P, const void* X, const void* dY, int x_dt
 int birkhoff8_mix_bwd(const float* P, const void* X, const void* dY, int x_dtype, void* dX, float* dH, int64_t B,
                       int64_t C, hipStream_t stream) {
     return birkhoff8_mix_bwd_ex(P, X, dY, x_dtype, dX, dH, dH, BIRKHOFF4_F32, B, C, stream);
+}
+
+int birkhoff4_post_fwd(const void* H, int h_dtype, const void* X, const float* h, const void* Z, int x_dtype, double p,
+                       const int64_t* rng, void* Y, float* P, float* dual, int32_t* iters, int64_t B, int64_t C,
+                       float tol, int max_iter, hipStream_t stream) {
+    return post_fwd<4>(H, h_dtype, X, h, Z, x_dtype, p, rng, Y, P, dual, iters, B, C, tol, max_iter, stream);
+}
+
+int birkhoff8_post_fwd(const void* H, int h_dtype, const void* X, const float* h, const void* Z, int x_dtype, double p,
+                       const int64_t* rng, void* Y, float* P, float* dual, int32_t* iters, int64_t B, int64_t C,
+                       float tol, int max_iter, hipStream_t stream) {
+    return post_fwd<8>(H, h_dtype, X, h, Z, x_dtype, p, rng, Y, P, dual, iters, B, C, tol, max_iter, stream);
+}
+
+int birkhoff4_post_bwd(const float* P, const void* X, const float* h, const void* Z, const void* dY, int x_dtype, double p,
+                       const int64_t* rng, void* dX, void* dZ, float* dh, void* dH, int dh_dtype, int64_t B, int64_t C,
+                       hipStream_t stream) {
+    return post_bwd<4>(P, X, h, Z, dY, x_dtype, p, rng, dX, dZ, dh, static_cast<float*>(dH), dH, dh_dtype, B, C, stream);
+}
+
+int birkhoff8_post_bwd(const float* P, const void* X, const float* h, const void* Z, const void* dY, int x_dtype, double p,
+                       const int64_t* rng, void* dX, void* dZ, float* dh, float* dP, void* dH, int dh_dtype, int64_t B,
+                       int64_t C, hipStream_t stream) {
+    return post_bwd<8>(P, X, h, Z, dY, x_dtype, p, rng, dX, dZ, dh, dP, dH, dh_dtype, B, C, stream);
 }
 
 const char* birkhoff4_strerror(int code) {

@@ -133,6 +133,15 @@ __device__ __forceinline__ void lane_sums(const float (&v)[NV], float (&out)[NV 
     }
 }
 
+// Sum over the 64 / N lanes that lane_sums leaves of one of N values, in all of them.
+template <int N>
+__device__ __forceinline__ float rest_sum(float x) {
+    x = gsum_lanes<8>(x);
+    if constexpr (N == 4)
+        x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));  // row_ror:8
+    return x;
+}
+
 // ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
@@ -161,6 +170,22 @@ bool overlaps(const void* a, size_t na, const void* b, size_t nb) {
     if (!a || !b || na == 0 || nb == 0) return false;
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return x < y + nb && y < x + na;
+}
+
+struct Span {
+    const void* p;
+    size_t bytes;
+};
+
+// No output overlaps another output or an input.
+bool disjoint(const Span* outs, int no, const Span* ins, int ni) {
+    for (int a = 0; a < no; ++a) {
+        for (int b = a + 1; b < no; ++b)
+            if (overlaps(outs[a].p, outs[a].bytes, outs[b].p, outs[b].bytes)) return false;
+        for (int b = 0; b < ni; ++b)
+            if (overlaps(outs[a].p, outs[a].bytes, ins[b].p, ins[b].bytes)) return false;
+    }
+    return true;
 }
 
 size_t dtype_bytes(int dt) { return dt == BIRKHOFF4_BF16 ? 2 : 4; }

@@ -281,15 +281,6 @@ __device__ __forceinline__ float add_dot(const v4u a, const v4u b, float acc) {
     return acc;
 }
 
-// Sum over the 64 / N lanes that lane_sums leaves of one of N values, in all of them.
-template <int N>
-__device__ __forceinline__ float rest_sum(float x) {
-    x = gsum_lanes<8>(x);
-    if constexpr (N == 4)
-        x += __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), 0x128, 0xF, 0xF, true));  // row_ror:8
-    return x;
-}
-
 __device__ __forceinline__ float wave_sum(float x) {
     x = rest_sum<4>(x);
     x += __shfl_xor(x, 16);
@@ -776,22 +767,6 @@ int pre_shape(int n, int64_t B, int64_t C, int x_dtype, PreShape* s) {
 }
 
 bool eps_ok(float eps) { return eps >= 0.f && eps < __builtin_inff(); }
-
-struct Span {
-    const void* p;
-    size_t bytes;
-};
-
-// No output overlaps another output or an input.
-bool disjoint(const Span* outs, int no, const Span* ins, int ni) {
-    for (int a = 0; a < no; ++a) {
-        for (int b = a + 1; b < no; ++b)
-            if (overlaps(outs[a].p, outs[a].bytes, outs[b].p, outs[b].bytes)) return false;
-        for (int b = 0; b < ni; ++b)
-            if (overlaps(outs[a].p, outs[a].bytes, ins[b].p, ins[b].bytes)) return false;
-    }
-    return true;
-}
 
 template <int DX, int N>
 int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float* alpha, const float* bias, float eps,

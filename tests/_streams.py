@@ -106,3 +106,49 @@ def within(got, ref, err, label, tiny=1e-30):
     worst = ((g - ref).abs() / slack).max().item() if g.numel() else 0.0
     print(f"  {label}: worst error / bound {worst:.3f}", flush=True)
     assert not bad.any(), f"{label}: {int(bad.sum())} of {bad.numel()} outside, worst {worst}"
+
+
+def philox(counter, key):
+    """One block of Philox 4x32-10 (Salmon et al. 2011) in Python's integers: counter of four
+    words, key of two."""
+    c, k = list(counter), list(key)
+    for _ in range(10):
+        a, b = 0xD2511F53 * c[0], 0xCD9E8D57 * c[2]
+        c = [b >> 32 ^ c[1] ^ k[0], b & 0xFFFFFFFF, a >> 32 ^ c[3] ^ k[1], a & 0xFFFFFFFF]
+        k = [(k[0] + 0x9E3779B9) & 0xFFFFFFFF, (k[1] + 0xBB67AE85) & 0xFFFFFFFF]
+    return c
+
+
+def kept(shape, p, seed, offset):
+    """Which elements of Z stay: a bool tensor on the CPU."""
+    numel = 1
+    for s in shape:
+        numel *= s
+    words = []
+    lo = lambda v: v & 0xFFFFFFFF
+    for g in range((numel + 3) // 4):
+        words += philox((lo(g), g >> 32, lo(offset), lo(offset >> 32)), (lo(seed), lo(seed >> 32)))
+    return (torch.tensor(words[:numel], dtype=torch.int64) >= int(p * 2 ** 32)).reshape(shape)
+
+
+def post_ref(P, X, h, Z, keep, p, dY=None):
+    """Y in float64 from the projected P (its own errors are the projection's), or with dY the
+    gradients (dX, dP, dh, dZ), each with its bound."""
+    n, C = X.shape[-2:]
+    P, X, h, Z = (t.double() for t in (P, X, h, Z))
+    mult = keep.to(X.device).double() / (1.0 - p)
+    # masked values do not count, whatever they are
+    D = torch.where(mult > 0, Z * mult, torch.zeros_like(Z))
+    if dY is None:
+        Y = P @ X + h[:, :, None] * D[:, None]
+        mag = P.abs() @ X.abs() + (h[:, :, None] * D[:, None]).abs()
+        return Y, (2 * n + 4) * U32 * mag  # n + 1 terms; scale and its product with h rounded
+    dY = dY.double()
+    Pt = P.transpose(1, 2).contiguous()
+    dX, e_dX = Pt @ dY, 2 * n * U32 * (Pt.abs() @ dY.abs())
+    Xt = X.transpose(1, 2).contiguous()
+    dP = dY @ Xt
+    dh, dh_abs = (dY * D[:, None]).sum(2), (dY * D[:, None]).abs().sum(2)
+    dZ = (h[:, :, None] * dY).sum(1) * mult
+    e_dZ = (h[:, :, None] * dY).abs().sum(1) * mult * (2 * n + 4) * U32
+    return (dX, dP, dh, dZ), (e_dX, None, (depth(C) + 4) * U32 * dh_abs, e_dZ)
