@@ -16,6 +16,8 @@
 // tenth of what the matrix cores do in that time. W (N rows) is used by every token and stays in
 // L2; the products run on the matrix cores with the tokens as one side of the tile.
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
@@ -265,7 +267,8 @@ __global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__
 // below. A token has `share` waves of the block, which take its columns in turn; its first wave
 // forms G. A block takes `turns` times 8 / share consecutive tokens and leaves one row of sums for
 // dbias and dalpha.
-constexpr int kTokenStep = 32;
+constexpr int kTokenStep = 32;  // tokens of a stage of the products over tokens
+constexpr int kHalf = 16;
 constexpr int kDotWaves = 8;
 
 template <int DX, int N>
@@ -291,7 +294,7 @@ template <int DX, int N>
 __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
     const v4u* __restrict__ X, const v4u* __restrict__ dU, const float* __restrict__ Q, const float* __restrict__ rms,
     const float* __restrict__ alpha, const float* __restrict__ bias, const float* __restrict__ dh,
-    const float* __restrict__ dH, float* __restrict__ G, float* __restrict__ GT, float* __restrict__ coef,
+    const float* __restrict__ dH, float* __restrict__ G, float* __restrict__ coef,
     float* __restrict__ sums, int64_t B, int64_t Bp, int64_t nc, float inv_k, int share, int turns) {
     constexpr int R = Gates<N>::rows, S = Gates<N>::stride, J = (R + 63) / 64;
     __shared__ float dots[kDotWaves][N];
@@ -353,15 +356,14 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
                 const float gj = r * a * dl, dq = dl * q;
                 s = __builtin_fmaf(gj, q, s);
                 G[R * t + j] = gj;
-                GT[j * Bp + t] = gj;
-                if (j < N) coef[j * Bp + t] = gate;
+                if (j < N) coef[(N + 1) * t + j] = gate;
                 sum_dl[m] += dl;
                 sum_dq[0] += j < N ? dq : 0.f;
                 sum_dq[1] += j >= N && j < 2 * N ? dq : 0.f;
                 sum_dq[2] += j >= 2 * N ? dq : 0.f;
             }
             s = wave_sum(s);
-            if (lane == 0) coef[N * Bp + t] = s * r * inv_k;
+            if (lane == 0) coef[(N + 1) * t + N] = s * r * inv_k;
         }
     }
     // a row of sums for the block: dl's, then the three groups' dl q
@@ -386,16 +388,18 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 // Backward: dX and partial sums of dW
 // ---------------------------------------------------------------------------
 // Wave w of a block takes stream w's channels CW chunk .. + CW, CE of them per lane (lane l: group
-// g = l / 16 of tokens, channels CE (l % 16) .. + CE), over the steps of 32 tokens of its share, of
-// which lane group g has tokens 8 g .. 8 g + 7. The same registers serve everything:
+// g = l / 16, channels CE (l % 16) .. + CE), over the stages of 32 tokens of its share, in halves of
+// 16 of which lane group g has tokens 4 g .. 4 g + 3. The same registers serve everything:
 //  * dW: tile of 16 rows of W (G transposed, tokens along k) times the tokens' values, one product
 //    per channel c of the lanes: column l % 16 is channel CE (l % 16) + c, and k runs over the
-//    tokens in the order in which the lanes hold them, 8 per lane group.
-//  * dX: rows of a product are tokens; product a in {0, 1} has token 8 (i / 4) + 4 a + i % 4 as row
-//    i, so that its result lands in the lane that holds the token's values.
+//    tokens as the lanes hold them.
+//  * dX: the rows of a product are the half's tokens, so that row 4 g + i, which lane group g gets,
+//    is the token whose values it holds.
 // bf16: G enters as the sum of two bf16 values (the upper 16 bits, and the rest rounded), 2^-16 off
 // at most, since one alone (2^-8) would be as coarse as the result's own rounding; W and X are
-// exact. Sums are fp32. Rows of W stay in registers throughout.
+// exact. Sums are fp32. W's rows stay in registers throughout; G is brought into the operands'
+// layout in LDS once for all waves of a block, a stage ahead, and a half's streams are loaded while
+// the other half is worked on.
 template <int DX, int N>
 struct Back {
     // bf16 with n = 8: half as many channels, as the sums of 5 row tiles fill the registers
@@ -409,27 +413,25 @@ struct Words {
     uint32_t v[WORDS];
 };
 
-template <int WORDS>
-__device__ __forceinline__ Words<WORDS> load_words(const void* base, int64_t byte) {
+// ONCE: a byte that no other wave reads (non-temporal).
+template <int WORDS, bool ONCE = false, typename I>
+__device__ __forceinline__ Words<WORDS> load_words(const void* base, I byte) {
+    typedef uint32_t vec __attribute__((ext_vector_type(WORDS)));
+    const vec* p = reinterpret_cast<const vec*>(static_cast<const char*>(base) + byte);
+    const vec q = ONCE ? __builtin_nontemporal_load(p) : *p;
     Words<WORDS> r;
-    const char* p = static_cast<const char*>(base) + byte;
-    if constexpr (WORDS == 4) {
-        const v4u q = *reinterpret_cast<const v4u*>(p);
-        r.v[0] = q.x; r.v[1] = q.y; r.v[2] = q.z; r.v[3] = q.w;
-    } else {
-        const uint2 q = *reinterpret_cast<const uint2*>(p);
-        r.v[0] = q.x; r.v[1] = q.y;
-    }
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) r.v[k] = q[k];
     return r;
 }
 
-template <int WORDS>
-__device__ __forceinline__ void store_words(void* base, int64_t byte, const Words<WORDS>& r) {
-    char* p = static_cast<char*>(base) + byte;
-    if constexpr (WORDS == 4)
-        __builtin_nontemporal_store(v4u{r.v[0], r.v[1], r.v[2], r.v[3]}, reinterpret_cast<v4u*>(p));
-    else
-        __builtin_nontemporal_store(static_cast<uint64_t>(r.v[1]) << 32 | r.v[0], reinterpret_cast<uint64_t*>(p));
+template <int WORDS, typename I>
+__device__ __forceinline__ void store_words(void* base, I byte, const Words<WORDS>& r) {
+    typedef uint32_t vec __attribute__((ext_vector_type(WORDS)));
+    vec q;
+#pragma unroll
+    for (int k = 0; k < WORDS; ++k) q[k] = r.v[k];
+    __builtin_nontemporal_store(q, reinterpret_cast<vec*>(static_cast<char*>(base) + byte));
 }
 
 // Channel c of a lane's words.
@@ -441,42 +443,85 @@ __device__ __forceinline__ float channel(const Words<WORDS>& r, int c) {
         return __uint_as_float(r.v[c]);
 }
 
-// bf16 channel c of eight rows, in order.
+// bf16 channel c of eight (four) rows, in order.
 template <int WORDS>
-__device__ __forceinline__ v4u column_of(const Words<WORDS> r[8], int c) {
-    v4u out;
-#pragma unroll
-    for (int k = 0; k < 4; ++k)  // bytes 0..3 of the selector's operand 1, 4..7 of operand 0
-        out[k] = __builtin_amdgcn_perm(r[2 * k + 1].v[c / 2], r[2 * k].v[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
-    return out;
+__device__ __forceinline__ uint32_t column_pair(const Words<WORDS>& a, const Words<WORDS>& b, int c) {
+    // selector bytes 0..3: second operand, 4..7: first
+    return __builtin_amdgcn_perm(b.v[c / 2], a.v[c / 2], c & 1 ? 0x07060302u : 0x05040100u);
 }
 
-// Eight fp32 values as the sum of two bf16 ones each: the upper half of the bits (no rounding, so
-// a large value does not overflow) and the rest (nothing where the value is not finite).
-__device__ __forceinline__ void split8(const v4f a, const v4f b, v4u& hi, v4u& lo) {
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    float rest[8];
-#pragma unroll
-    for (int k = 0; k < 8; ++k) {
-        const float up = __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u);
-        rest[k] = __builtin_fabsf(v[k]) < __builtin_inff() ? v[k] - up : 0.f;
-    }
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-        hi[k] = __builtin_amdgcn_perm(__float_as_uint(v[2 * k + 1]), __float_as_uint(v[2 * k]), 0x07060302u);
-        lo[k] = pack_bf16(rest[2 * k], rest[2 * k + 1]);
-    }
+template <int WORDS>
+__device__ __forceinline__ v4u column8(const Words<WORDS> r[8], int c) {
+    return v4u{column_pair(r[0], r[1], c), column_pair(r[2], r[3], c), column_pair(r[4], r[5], c),
+               column_pair(r[6], r[7], c)};
 }
+
+typedef short short4v __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ v4f mfma_bf16_16(const v2u a, const v2u b, const v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4v, a), __builtin_bit_cast(short4v, b), c, 0,
+                                                     0, 0);
+}
+
+// A stage of G in LDS, by halves, in the operands' layouts, and the tokens' h^pre and s.
+template <int DX, int N>
+struct Stage {
+    static constexpr bool H16 = DX == BIRKHOFF4_BF16;
+    static constexpr int R = Gates<N>::rows, RT = Gates<N>::tiles, KS = H16 ? Gates<N>::ksteps : R / 4;
+    static constexpr int parts = H16 ? 2 : 1;  // upper and lower bf16 values
+    using T = std::conditional_t<H16, uint16_t, float>;
+    static constexpr int KE = H16 ? 8 : KS;               // values per lane of a dX operand
+    static constexpr int KO = H16 ? KS : 1;               // dX operands per half
+    alignas(16) T w[2][parts][RT][64][4];                 // dW: lane (g, j): row j's tokens 4 g .. + 3
+    alignas(16) T x[2][parts][KO][64][KE];                // dX: lane (g, t): token t's rows KE g .. of the operand
+    alignas(16) float coef[N + 1][kTokenStep];
+
+    __device__ __forceinline__ void put(int t, int j, float v) {
+        const int half = t >> 4, tt = t & 15;
+        const int wl = (tt >> 2) * 16 + (j & 15), xl = (j / KE % 4) * 16 + tt;
+        if constexpr (H16) {
+            // the upper half of the bits (no rounding, so a large value does not overflow) and the
+            // rest (nothing where the value is not finite)
+            const uint32_t up = __float_as_uint(v) & 0xffff0000u;
+            const float rest = __builtin_fabsf(v) < __builtin_inff() ? v - __uint_as_float(up) : 0.f;
+            const uint16_t hi = static_cast<uint16_t>(up >> 16), lo = static_cast<uint16_t>(pack_bf16(rest, 0.f));
+            w[half][0][j >> 4][wl][tt & 3] = hi;
+            w[half][1][j >> 4][wl][tt & 3] = lo;
+            x[half][0][j >> 5][xl][j & 7] = hi;
+            x[half][1][j >> 5][xl][j & 7] = lo;
+        } else {
+            w[half][0][j >> 4][wl][tt & 3] = v;
+            x[half][0][0][xl][j % KE] = v;
+        }
+    }
+};
+
+// W's rows in the dX products' layout: in LDS, or, where it does not fit beside the stages (fp32
+// with n = 8: 160 KB), in registers; and whether E and dU are loaded a half ahead too.
+template <int DX, int N>
+struct BackPlan {
+    static constexpr bool H16 = DX == BIRKHOFF4_BF16;
+    static constexpr bool w_lds = H16 || N == 4, ahead = w_lds;
+};
 
 template <int DX, int N>
 __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restrict__ X, const void* __restrict__ W,
                                                              const void* __restrict__ dU, const void* __restrict__ E,
-                                                             const float* __restrict__ G, const float* __restrict__ GT,
-                                                             const float* __restrict__ coef, void* __restrict__ dX,
-                                                             float* __restrict__ dWp, int64_t B, int64_t Bp, int64_t C) {
-    constexpr bool H16 = DX == BIRKHOFF4_BF16;
-    constexpr int R = Gates<N>::rows, RT = Gates<N>::tiles, KS = H16 ? Gates<N>::ksteps : R / 4;
+                                                             const float* __restrict__ G, const float* __restrict__ coef,
+                                                             void* __restrict__ dX, float* __restrict__ dWp, int64_t B,
+                                                             int64_t stages, int64_t C) {
+    using St = Stage<DX, N>;
+    constexpr bool H16 = St::H16;
+    constexpr int R = St::R, RT = St::RT, KS = St::KS;
     constexpr int CE = Back<DX, N>::CE, WO = Back<DX, N>::words, SZ = H16 ? 2 : 4;
+    constexpr int kThreads = 64 * N, GQ = (kTokenStep * R + kThreads - 1) / kThreads;
+    static_assert(kTokenStep * (N + 1) <= kThreads, "one coefficient per thread");
+    constexpr bool kLds = BackPlan<DX, N>::w_lds, kAhead = BackPlan<DX, N>::ahead;
+    using Row = Words<WO>;
+    __shared__ St lds[2];
+    // [operand][channel][lane]: of bf16 eight rows, of fp32 one
+    __shared__ std::conditional_t<H16, v4u, float> wlds[kLds ? N : 1][kLds ? KS : 1][CE][64];
     const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));  // the stream
     const int64_t ch = static_cast<int64_t>(blockIdx.x) * Back<DX, N>::CW + CE * c16;
@@ -484,9 +529,83 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
     const int64_t at = own ? ch : 0;  // lanes past the end of the row read its start and store nothing
     const int64_t K = N * C;
 
+    // operand rows past the last row of W stay zero
+    for (unsigned q = threadIdx.x; q < sizeof(lds) / 4; q += kThreads) reinterpret_cast<uint32_t*>(lds)[q] = 0;
+    float gq[GQ], cq = 0.f;
+    auto fetch = [&](int64_t st) {
+#pragma unroll
+        for (int q = 0; q < GQ; ++q) {
+            const int k = static_cast<int>(threadIdx.x) + kThreads * q;
+            if (k < kTokenStep * R) gq[q] = G[st * kTokenStep * R + k];
+        }
+        if (threadIdx.x < kTokenStep * (N + 1)) cq = coef[st * kTokenStep * (N + 1) + threadIdx.x];
+    };
+    auto put = [&](St& to) {
+#pragma unroll
+        for (int q = 0; q < GQ; ++q) {
+            const int k = static_cast<int>(threadIdx.x) + kThreads * q;
+            if (k < kTokenStep * R) to.put(k / R, k % R, gq[q]);
+        }
+        if (threadIdx.x < kTokenStep * (N + 1)) to.coef[threadIdx.x % (N + 1)][threadIdx.x / (N + 1)] = cq;
+    };
+    // a half's rows start at a uniform address, the lane's four at 32-bit offsets from it; past the
+    // last token: that token again
+    auto rows_of = [&](int64_t t0, uint32_t off[4], int64_t stride) {
+        const int last = B - t0 < kHalf ? static_cast<int>(B - t0) - 1 : kHalf - 1;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            off[k] = static_cast<uint32_t>(4 * g + k < last ? 4 * g + k : last) * static_cast<uint32_t>(stride * SZ) +
+                     static_cast<uint32_t>(at * SZ);
+    };
+    auto load_x = [&](Row (&x)[4], int64_t t0) {
+        uint32_t off[4];
+        rows_of(t0, off, K);
+        const char* base = static_cast<const char*>(X) + (K * t0 + w * C) * SZ;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) x[k] = load_words<WO, true>(base, off[k]);
+    };
+    auto load_eu = [&](Row (&e)[4], Row (&u)[4], int64_t t0) {
+        uint32_t off[4];
+        if (E) {
+            rows_of(t0, off, K);
+            const char* base = static_cast<const char*>(E) + (K * t0 + w * C) * SZ;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) e[k] = load_words<WO, true>(base, off[k]);
+        }
+        if (dU) {
+            rows_of(t0, off, C);
+            const char* base = static_cast<const char*>(dU) + C * t0 * SZ;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) u[k] = load_words<WO>(base, off[k]);
+        }
+    };
+
+    int64_t st = blockIdx.y;
+    fetch(st);
+    Row x[2][4], e[kAhead ? 2 : 1][4] = {}, u[kAhead ? 2 : 1][4] = {};
+    // a stage has two halves also where the last one is past the end
+    auto load = [&](int hf, int64_t t0) {
+        if (t0 >= B) return;  // uniform
+        load_x(x[hf], t0);
+        if constexpr (kAhead) load_eu(e[hf], u[hf], t0);
+    };
+    load(0, st * kTokenStep);
+    load(1, st * kTokenStep + kHalf);
+
     // W's rows: operand of the dX products, for each channel c of the lane
-    v4u wb[H16 ? KS : 1][CE];
-    float wf[H16 ? 1 : KS][CE];
+    std::conditional_t<H16, v4u, float> wreg[kLds ? 1 : KS][CE];
+    auto keep = [&](int k, int c, auto v) {
+        if constexpr (kLds)
+            wlds[w][k][c][lane] = v;
+        else
+            wreg[k][c] = v;
+    };
+    auto wop = [&](int k, int c) {
+        if constexpr (kLds)
+            return wlds[w][k][c][lane];
+        else
+            return wreg[k][c];
+    };
     if constexpr (H16) {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {
@@ -497,14 +616,14 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
                 rows[j] = load_words<WO>(W, (K * (row < R ? row : R - 1) + w * C + at) * SZ);
             }
 #pragma unroll
-            for (int c = 0; c < CE; ++c) wb[k][c] = column_of<WO>(rows, c);
+            for (int c = 0; c < CE; ++c) keep(k, c, column8<WO>(rows, c));
         }
     } else {
 #pragma unroll
         for (int k = 0; k < KS; ++k) {  // lane group g has rows g R / 4 ..
             const Words<WO> row = load_words<WO>(W, (K * (g * KS + k) + w * C + at) * SZ);
 #pragma unroll
-            for (int c = 0; c < CE; ++c) wf[k][c] = __uint_as_float(row.v[c]);
+            for (int c = 0; c < CE; ++c) keep(k, c, __uint_as_float(row.v[c]));
         }
     }
     v4f acc[RT][CE];
@@ -513,115 +632,98 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
 #pragma unroll
         for (int c = 0; c < CE; ++c) acc[r][c] = v4f{0.f, 0.f, 0.f, 0.f};
 
-    const int64_t nsteps = Bp / kTokenStep;
-    // the last steps first: their streams are still in the cache from the dot products
-    for (int64_t st = nsteps - 1 - blockIdx.y; st >= 0; st -= gridDim.y) {
-        const int64_t t0 = st * kTokenStep + 8 * g;  // this lane's eight tokens
-        const bool whole = (st + 1) * kTokenStep <= B;
-        Words<WO> x[8], e[8], u[8];
-        int64_t tok[8];
+    auto work = [&](Row (&x)[4], Row (&e)[4], Row (&u)[4], const St& s, int hf, int64_t t0) {
+        if (t0 >= B) return;  // uniform
+        if constexpr (!kAhead) load_eu(e, u, t0);
+        if (t0 + kHalf > B) {  // tokens past the last one add nothing to dW: zeros, as 0 times their G
 #pragma unroll
-        for (int k = 0; k < 8; ++k) tok[k] = whole || t0 + k < B ? t0 + k : B - 1;
-#pragma unroll
-        for (int k = 0; k < 8; ++k) x[k] = load_words<WO>(X, (K * tok[k] + w * C + at) * SZ);
-        if (E) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = load_words<WO>(E, (K * tok[k] + w * C + at) * SZ);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) e[k] = Words<WO>{};
+            for (int k = 0; k < 4; ++k)
+                if (t0 + 4 * g + k >= B) x[k] = Row{};
         }
-        if (dU) {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] = load_words<WO>(dU, (C * tok[k] + at) * SZ);
-        } else {
-#pragma unroll
-            for (int k = 0; k < 8; ++k) u[k] = Words<WO>{};
-        }
-        if (!whole) {  // tokens past the last one add nothing to dW: zeros, as 0 times their G
-#pragma unroll
-            for (int k = 0; k < 8; ++k)
-                if (t0 + k >= B) x[k] = Words<WO>{};
-        }
-
         // dW += G^T X
-        {
-            v4f ga[RT], gb[RT];
+        if constexpr (H16) {
+            v2u hi[RT], lo[RT];
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
-                const int j = 16 * r + c16 < R ? 16 * r + c16 : R - 1;
-                const v4f* p = reinterpret_cast<const v4f*>(GT + j * Bp + t0);
-                ga[r] = p[0];
-                gb[r] = p[1];
+                hi[r] = *reinterpret_cast<const v2u*>(s.w[hf][0][r][lane]);
+                lo[r] = *reinterpret_cast<const v2u*>(s.w[hf][St::parts - 1][r][lane]);
             }
-            if constexpr (H16) {
-                v4u hi[RT], lo[RT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) split8(ga[r], gb[r], hi[r], lo[r]);
+            for (int c = 0; c < CE; ++c) {
+                const v2u b = {column_pair(x[0], x[1], c), column_pair(x[2], x[3], c)};
 #pragma unroll
-                for (int c = 0; c < CE; ++c) {
-                    const v4u b = column_of<WO>(x, c);
+                for (int r = 0; r < RT; ++r) acc[r][c] = mfma_bf16_16(lo[r], b, mfma_bf16_16(hi[r], b, acc[r][c]));
+            }
+        } else {
 #pragma unroll
-                    for (int r = 0; r < RT; ++r) acc[r][c] = mfma_bf16(lo[r], b, mfma_bf16(hi[r], b, acc[r][c]));
-                }
-            } else {
+            for (int r = 0; r < RT; ++r) {
+                const v4f gr = *reinterpret_cast<const v4f*>(s.w[hf][0][r][lane]);
 #pragma unroll
-                for (int k = 0; k < 8; ++k)
+                for (int k = 0; k < 4; ++k)
 #pragma unroll
-                    for (int r = 0; r < RT; ++r)
-#pragma unroll
-                        for (int c = 0; c < CE; ++c)
-                            acc[r][c] = mfma_f32(k < 4 ? ga[r][k & 3] : gb[r][k & 3], __uint_as_float(x[k].v[c]), acc[r][c]);
+                    for (int c = 0; c < CE; ++c) acc[r][c] = mfma_f32(gr[k], __uint_as_float(x[k].v[c]), acc[r][c]);
             }
         }
-        // dX = E + h^pre dU + G W - s X, four tokens of the lane at a time
+        // dX = E + h^pre dU + G W - s X
+        v4f d[CE];
 #pragma unroll
-        for (int a = 0; a < 2; ++a) {
-            const int64_t gt = st * kTokenStep + 8 * (c16 >> 2) + 4 * a + (c16 & 3);  // row c16's token
-            v4f d[CE];
+        for (int c = 0; c < CE; ++c) d[c] = v4f{0.f, 0.f, 0.f, 0.f};
+        if constexpr (H16) {
 #pragma unroll
-            for (int c = 0; c < CE; ++c) d[c] = v4f{0.f, 0.f, 0.f, 0.f};
-            if constexpr (H16) {
-#pragma unroll
-                for (int k = 0; k < KS; ++k) {
-                    v4u hi = {0u, 0u, 0u, 0u}, lo = {0u, 0u, 0u, 0u};
-                    if (32 * k + 8 * g < R) {
-                        const v4f* p = reinterpret_cast<const v4f*>(G + R * gt + 32 * k + 8 * g);
-                        split8(p[0], p[1], hi, lo);
-                    }
-#pragma unroll
-                    for (int c = 0; c < CE; ++c) d[c] = mfma_bf16(lo, wb[k][c], mfma_bf16(hi, wb[k][c], d[c]));
-                }
-            } else {
-                float gv[KS];
-#pragma unroll
-                for (int k = 0; k < KS; ++k) gv[k] = G[R * gt + g * KS + k];
-#pragma unroll
-                for (int k = 0; k < KS; ++k)
-#pragma unroll
-                    for (int c = 0; c < CE; ++c) d[c] = mfma_f32(gv[k], wf[k][c], d[c]);
-            }
-            const v4f hp = *reinterpret_cast<const v4f*>(coef + w * Bp + t0 + 4 * a);
-            const v4f sv = *reinterpret_cast<const v4f*>(coef + N * Bp + t0 + 4 * a);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int k = 4 * a + i;
-                float o[CE];
+            for (int k = 0; k < KS; ++k) {
+                const v4u hi = *reinterpret_cast<const v4u*>(s.x[hf][0][k][lane]);
+                const v4u lo = *reinterpret_cast<const v4u*>(s.x[hf][St::parts - 1][k][lane]);
 #pragma unroll
                 for (int c = 0; c < CE; ++c) {
-                    o[c] = __builtin_fmaf(hp[i], channel<DX, WO>(u[k], c), channel<DX, WO>(e[k], c) + d[c][i]);
-                    o[c] = __builtin_fmaf(-sv[i], channel<DX, WO>(x[k], c), o[c]);
+                    const v4u b = wop(k, c);
+                    d[c] = mfma_bf16(lo, b, mfma_bf16(hi, b, d[c]));
                 }
-                Words<WO> r;
-#pragma unroll
-                for (int q = 0; q < WO; ++q) {
-                    if constexpr (H16)
-                        r.v[q] = pack_bf16(o[2 * q], o[2 * q + 1]);
-                    else
-                        r.v[q] = __float_as_uint(o[q]);
-                }
-                if (own && t0 + k < B) store_words<WO>(dX, (K * (t0 + k) + w * C + ch) * SZ, r);
             }
+        } else {
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int c = 0; c < CE; ++c) d[c] = mfma_f32(s.x[hf][0][0][lane][k], wop(k, c), d[c]);
+        }
+        uint32_t off[4];
+        rows_of(t0, off, K);
+        char* out = static_cast<char*>(dX) + (K * t0 + w * C) * SZ;
+        const v4f hp = *reinterpret_cast<const v4f*>(&s.coef[w][kHalf * hf + 4 * g]);
+        const v4f sv = *reinterpret_cast<const v4f*>(&s.coef[N][kHalf * hf + 4 * g]);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            float o[CE];
+#pragma unroll
+            for (int c = 0; c < CE; ++c) {
+                o[c] = __builtin_fmaf(hp[k], channel<DX, WO>(u[k], c), channel<DX, WO>(e[k], c) + d[c][k]);
+                o[c] = __builtin_fmaf(-sv[k], channel<DX, WO>(x[k], c), o[c]);
+            }
+            Words<WO> r;
+#pragma unroll
+            for (int q = 0; q < WO; ++q) {
+                if constexpr (H16)
+                    r.v[q] = pack_bf16(o[2 * q], o[2 * q + 1]);
+                else
+                    r.v[q] = __float_as_uint(o[q]);
+            }
+            if (own && t0 + 4 * g + k < B) store_words<WO>(out, off[k], r);
+        }
+    };
+
+    __syncthreads();  // the zeros
+    put(lds[0]);
+    for (int cur = 0; st < stages; cur ^= 1) {
+        const int64_t t0 = st * kTokenStep;
+        st += gridDim.y;
+        const bool more = st < stages;  // uniform over the block
+        __syncthreads();                // this stage's G is there, and nobody reads the other's any more
+        if (more) fetch(st);
+        work(x[0], e[0], u[0], lds[cur], 0, t0);
+        if (more) load(0, st * kTokenStep);
+        work(x[1], e[kAhead ? 1 : 0], u[kAhead ? 1 : 0], lds[cur], 1, t0 + kHalf);
+        if (more) {
+            load(1, st * kTokenStep + kHalf);
+            put(lds[cur ^ 1]);
         }
     }
     if (own) {
@@ -714,7 +816,7 @@ struct BackLaunch {
     int share, turns;              // of pre_dot_kernel
     int64_t dot_blocks;
     int64_t chunks, token_shares;  // of pre_back_kernel
-    int64_t g, gt, coef, sums, dw, bytes;  // the workspace's parts: offsets in bytes, and its size
+    int64_t g, coef, sums, dw, bytes;  // the workspace's parts: offsets in bytes, and its size
 };
 
 constexpr int64_t kDotBlocks = 2048;
@@ -743,7 +845,6 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
         return was;
     };
     l.g = take(l.Bp * rows);
-    l.gt = take(l.Bp * rows);
     l.coef = take(l.Bp * (n + 1));
     l.sums = take(l.dot_blocks * (rows + 4));
     l.dw = take(l.token_shares * rows * n * s.C);
@@ -753,7 +854,7 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
 
 constexpr int64_t kPreMaxTokens = int64_t(1) << 26;  // a launch's lanes over tokens stay 32-bit
 constexpr int64_t kPreMaxValues = int64_t(1) << 46;
-constexpr int64_t kPreMaxChannels = int64_t(1) << 24;
+constexpr int64_t kPreMaxChannels = int64_t(1) << 22;  // sixteen tokens within 32-bit offsets
 
 // The checks that both directions and the workspace's size share.
 int pre_shape(int n, int64_t B, int64_t C, int x_dtype, PreShape* s) {
@@ -796,10 +897,10 @@ int launch_pre_bwd(const PreShape& s, const void* X, const void* W, const float*
     if (s.B > 0) {
         launch_kernel((pre_dot_kernel<DX, N>), dim3(static_cast<unsigned>(l.dot_blocks)), dim3(64 * kDotWaves), 0, stream,
                       static_cast<const v4u*>(X), static_cast<const v4u*>(dU), q, rms, alpha, bias, dh, dH, at(l.g),
-                      at(l.gt), at(l.coef), at(l.sums), s.B, l.Bp, s.nc,
+                      at(l.coef), at(l.sums), s.B, l.Bp, s.nc,
                       static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), l.share, l.turns);
         launch_kernel((pre_back_kernel<DX, N>), dim3(static_cast<unsigned>(l.chunks), static_cast<unsigned>(l.token_shares)),
-                      dim3(64 * N), 0, stream, X, W, dU, E, at(l.g), at(l.gt), at(l.coef), dX, at(l.dw), s.B, l.Bp, s.C);
+                      dim3(64 * N), 0, stream, X, W, dU, E, at(l.g), at(l.coef), dX, at(l.dw), s.B, l.Bp / kTokenStep, s.C);
     }
     // without tokens the sums are empty: zeros
     const int64_t quads = Gates<N>::rows * N * s.C / 4;
