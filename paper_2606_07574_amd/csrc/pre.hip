@@ -65,30 +65,38 @@ __device__ __forceinline__ float row_scale(const float* __restrict__ alpha, int 
 // ---------------------------------------------------------------------------
 // Forward: the products W v and |v|^2 of every token
 // ---------------------------------------------------------------------------
-// A block takes 16 TT tokens and a share of the row, in steps of 64 bytes; its four waves take the
+// A block takes 16 TT tokens and a share of the row, in steps of 64 bytes; its waves take the
 // steps in pairs (a 128-byte line of each token) in turn. Tokens are the columns of the tile, rows
 // of W its rows, both loaded straight into the operands' layout; |v|^2 is the diagonal of the
 // product of the tokens' operand with itself (fp32: plain sums, as the fp32 matrix rate is nearer
 // to what HBM delivers). The waves' sums are added in LDS in wave order, the shares' by the
 // reader: no atomics, so a token's result does not depend on timing.
-constexpr int kGateWaves = 4;
-
-template <int DX, int N, int TT>
-__global__ __launch_bounds__(64 * kGateWaves, 2) void pre_gate_kernel(const v4u* __restrict__ X,
+template <int DX, int N, int TT, int GW>
+__global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(const v4u* __restrict__ X,
                                                                       const v4u* __restrict__ W,
                                                                       float* __restrict__ part, int64_t B, int64_t steps,
                                                                       int64_t per) {
     constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4;
-    __shared__ v4f red[kGateWaves / 2][16 * TT][S4];
+    // a wave's rows on their way into the operands' layout: 128 bytes and 16 that keep the lanes that
+    // read one chunk of sixteen rows on different banks
+    __shared__ union {
+        v4u rows[GW][16 * TT][9];
+        v4f red[GW / 2][16 * TT][S4];
+    } lds;
+    auto& rows = lds.rows;
+    auto& red = lds.red;
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int64_t first = static_cast<int64_t>(blockIdx.x) * 16 * TT;
     const int64_t s0 = blockIdx.y * per, s1 = s0 + per < steps ? s0 + per : steps;
-    const v4u *x[TT], *wr[RT];
+    const int64_t row_bytes = 64 * steps;
+    const char* base = reinterpret_cast<const char*>(X) + row_bytes * first;
+    uint32_t off[2 * TT];  // of the rows that the lane loads: eight lanes a row, eight rows at a time
+    const v4u* wr[RT];
 #pragma unroll
-    for (int t = 0; t < TT; ++t) {  // past the last token: that token again, its sums not stored
-        const int64_t tok = first + 16 * t + c;
-        x[t] = X + 4 * steps * (tok < B ? tok : B - 1) + g;
+    for (int t = 0; t < 2 * TT; ++t) {  // past the last token: that token again, its sums not stored
+        const int64_t row = 8 * t + (lane >> 3), last = B - 1 - first;
+        off[t] = static_cast<uint32_t>(row_bytes * (row < last ? row : last)) + 16 * (lane & 7);
     }
 #pragma unroll
     for (int r = 0; r < RT; ++r) wr[r] = W + 4 * steps * (16 * r + c < R ? 16 * r + c : R - 1) + g;
@@ -101,21 +109,41 @@ __global__ __launch_bounds__(64 * kGateWaves, 2) void pre_gate_kernel(const v4u*
 #pragma unroll
         for (int r = 0; r < RT; ++r) acc[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
     }
-    for (int64_t s = s0 + 2 * w; s < s1; s += 2 * kGateWaves) {
+    const int64_t turns = (s1 - s0 + 2 * GW - 1) / (2 * GW);
+    int64_t turn = (blockIdx.x >> 3) % turns, next = s0 + 2 * GW * turn + 2 * w;
+    v4u xr[2 * TT];
+    auto load_x = [&](int64_t s) {
+        const char* p = base + 64 * s;
+        if (s + 1 < s1) {  // uniform
+#pragma unroll
+            for (int t = 0; t < 2 * TT; ++t) xr[t] = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p + off[t]));
+        } else {
+#pragma unroll
+            for (int t = 0; t < 2 * TT; ++t) {
+                xr[t] = v4u{0u, 0u, 0u, 0u};
+                if (s < s1 && (lane & 7) < 4) xr[t] = *reinterpret_cast<const v4u*>(p + off[t]);
+            }
+        }
+    };
+    load_x(next);
+    for (int64_t k = 0; k < turns; ++k) {
+        const int64_t s = next;
         v4u xv[2][TT], wv[2][RT];
 #pragma unroll
+        for (int t = 0; t < 2 * TT; ++t) rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
+        turn = turn + 1 < turns ? turn + 1 : 0;
+        next = s0 + 2 * GW * turn + 2 * w;
+        if (k + 1 < turns) load_x(next);
+#pragma unroll
         for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) wv[u][r] = v4u{0u, 0u, 0u, 0u};
             if (s + u < s1) {  // uniform
 #pragma unroll
-                for (int t = 0; t < TT; ++t) xv[u][t] = x[t][4 * (s + u)];
-#pragma unroll
                 for (int r = 0; r < RT; ++r) wv[u][r] = wr[r][4 * (s + u)];
-            } else {
-#pragma unroll
-                for (int t = 0; t < TT; ++t) xv[u][t] = v4u{0u, 0u, 0u, 0u};
-#pragma unroll
-                for (int r = 0; r < RT; ++r) wv[u][r] = v4u{0u, 0u, 0u, 0u};
             }
+#pragma unroll
+            for (int t = 0; t < TT; ++t) xv[u][t] = rows[w][16 * t + c][4 * u + g];
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u)
@@ -159,15 +187,15 @@ __global__ __launch_bounds__(64 * kGateWaves, 2) void pre_gate_kernel(const v4u*
     };
     auto put = [&](int k) { each([&](int t, int q, v4f& v) { red[k][t][q] = v; }); };
     auto add = [&](int k) { each([&](int t, int q, v4f& v) { v += red[k][t][q]; }); };
-    // waves 1 and 3 to 0 and 2, then 2 to 0
-    if (w & 1) put(w >> 1);
     __syncthreads();
-    if (!(w & 1)) add(w >> 1);
-    __syncthreads();
-    if (w == 2) put(0);
-    __syncthreads();
+#pragma unroll
+    for (int half = GW / 2; half >= 1; half /= 2) {  // the upper half of the waves to the lower
+        if (w >= half && w < 2 * half) put(w - half);
+        __syncthreads();
+        if (w < half) add(w);
+        __syncthreads();
+    }
     if (w == 0) {
-        add(0);
         v4f* dst = reinterpret_cast<v4f*>(part) + (blockIdx.y * B + first) * S4;
         each([&](int t, int q, v4f& v) {
             if (first + t < B) dst[t * S4 + q] = v;
@@ -202,7 +230,7 @@ __global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__
     for (int i = 0; i < N; ++i) x[i] = v4u{0u, 0u, 0u, 0u};
     if (col < nc) {
 #pragma unroll
-        for (int i = 0; i < N; ++i) x[i] = row[i * nc + col];
+        for (int i = 0; i < N; ++i) x[i] = __builtin_nontemporal_load(row + (i * nc + col));
     }
     float hp[N];
 #pragma unroll
@@ -214,6 +242,7 @@ __global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__
         float sum[J], l[J], gate[J];
 #pragma unroll
         for (int m = 0; m < J; ++m) sum[m] = 0.f;
+#pragma unroll 16
         for (int s = 0; s < splits; ++s) {
             const float* p = part + (s * B + t) * S;
 #pragma unroll
@@ -263,10 +292,10 @@ __global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__
 // ---------------------------------------------------------------------------
 // Backward: <dU, X_i> and the coefficients' gradients
 // ---------------------------------------------------------------------------
-// Tokens are padded to whole steps of 32 (Bp), whose G, h^pre and s are zero, for the products
-// below. A token has `share` waves of the block, which take its columns in turn; its first wave
-// forms G. A block takes `turns` times 8 / share consecutive tokens and leaves one row of sums for
-// dbias and dalpha.
+// Tokens are padded to whole stages of 32 (Bp), whose G, h^pre and s are zero, for the products
+// below. `share` waves of the block take four consecutive tokens, one after the other, sharing
+// their columns; the first of these waves forms G. A block leaves one row of sums for dbias and
+// dalpha.
 constexpr int kTokenStep = 32;  // tokens of a stage of the products over tokens
 constexpr int kHalf = 16;
 constexpr int kDotWaves = 8;
@@ -290,23 +319,104 @@ __device__ __forceinline__ float wave_sum(float x) {
     return x + __shfl_xor(x, 32);
 }
 
+// A stage of G in the operands' layouts, with the tokens' h^pre and s: written by pre_dot_kernel,
+// copied to LDS as it is by pre_back_kernel. bf16: G as the sum of two bf16 values (the upper 16
+// bits, and the rest rounded), 2^-16 off at most, since one alone (2^-8) would be as coarse as the
+// result's own rounding. Operand rows past the last row of W are zeros.
+template <int DX, int N>
+struct Stage {
+    static constexpr bool H16 = DX == BIRKHOFF4_BF16;
+    static constexpr int R = Gates<N>::rows, RT = Gates<N>::tiles, KS = H16 ? Gates<N>::ksteps : R / 4;
+    static constexpr int parts = H16 ? 2 : 1;  // upper and lower bf16 values
+    static constexpr int rows = H16 ? 32 * KS : 16 * RT;  // rows that have a place
+    using T = std::conditional_t<H16, uint16_t, float>;
+    static constexpr int KE = H16 ? 8 : KS;  // values per lane of a dX operand
+    static constexpr int KO = H16 ? KS : 1;  // dX operands per half
+    alignas(16) T w[parts][RT][2][64][4];    // dW: lane (g, j): row j's tokens 4 g .. + 3 of each half
+    alignas(16) T x[2][parts][KO][64][KE];   // dX: by halves; lane (g, t): token t's rows KE g .. of the operand
+    alignas(16) float coef[N + 1][kTokenStep];
+};
+
+// Eight fp32 values as two bf16 ones each: the upper half of the bits (no rounding, so a large
+// value does not overflow) and the rest, rounded (nothing where the value is not finite).
+template <int NV>
+__device__ __forceinline__ void split_bf16(const float (&v)[NV], uint32_t (&hi)[NV / 2], uint32_t (&lo)[NV / 2]) {
+    float rest[NV];
+#pragma unroll
+    for (int k = 0; k < NV; ++k) {
+        const float up = __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u);
+        rest[k] = __builtin_fabsf(v[k]) < __builtin_inff() ? v[k] - up : 0.f;
+    }
+#pragma unroll
+    for (int k = 0; k < NV / 2; ++k) {
+        hi[k] = __builtin_amdgcn_perm(__float_as_uint(v[2 * k + 1]), __float_as_uint(v[2 * k]), 0x07060302u);
+        lo[k] = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+    }
+}
+
+// Four tokens' rows (G, then h^pre and s) from a wave's LDS to their places in the stage, in pieces
+// of 8 and 16 bytes that lie together (single values written as they come cost 45 of 280 us at
+// 2^15 tokens of 4 x 4096). t: the first of them in the stage.
+template <int DX, int N, int LEN>
+__device__ __forceinline__ void store_stage(Stage<DX, N>& to, const float (&row)[4][LEN], int t, int lane) {
+    using St = Stage<DX, N>;
+    const int half = t >> 4, g = (t >> 2) & 3;
+    for (int j = lane; j < 16 * St::RT; j += 64) {
+        const float v[4] = {row[0][j], row[1][j], row[2][j], row[3][j]};
+        const int at = 16 * g + (j & 15);
+        if constexpr (St::H16) {
+            uint32_t hi[2], lo[2];
+            split_bf16<4>(v, hi, lo);
+            *reinterpret_cast<uint2*>(to.w[0][j >> 4][half][at]) = uint2{hi[0], hi[1]};
+            *reinterpret_cast<uint2*>(to.w[1][j >> 4][half][at]) = uint2{lo[0], lo[1]};
+        } else {
+            *reinterpret_cast<v4f*>(to.w[0][j >> 4][half][at]) = v4f{v[0], v[1], v[2], v[3]};
+        }
+    }
+    if constexpr (St::H16) {
+        const int k = lane & 3, j8 = lane >> 2;
+        if (j8 < St::rows / 8) {
+            float v[8];
+            uint32_t hi[4], lo[4];
+#pragma unroll
+            for (int q = 0; q < 8; ++q) v[q] = row[k][8 * j8 + q];
+            split_bf16<8>(v, hi, lo);
+            const int at = 16 * (j8 & 3) + (t & 15) + k;
+            *reinterpret_cast<v4u*>(to.x[half][0][j8 >> 2][at]) = v4u{hi[0], hi[1], hi[2], hi[3]};
+            *reinterpret_cast<v4u*>(to.x[half][1][j8 >> 2][at]) = v4u{lo[0], lo[1], lo[2], lo[3]};
+        }
+    } else {
+        for (int q = lane; q < 2 * St::R; q += 64) {  // pairs of rows
+            const int k = q / (St::R / 2), j = 2 * (q % (St::R / 2));
+            *reinterpret_cast<f32x2*>(&to.x[half][0][0][16 * (j / St::KS) + (t & 15) + k][j % St::KS]) =
+                f32x2{row[k][j], row[k][j + 1]};
+        }
+    }
+    if (lane <= N) {
+        const int j = St::rows + lane;
+        *reinterpret_cast<v4f*>(&to.coef[lane][t]) = v4f{row[0][j], row[1][j], row[2][j], row[3][j]};
+    }
+}
+
 template <int DX, int N>
 __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
     const v4u* __restrict__ X, const v4u* __restrict__ dU, const float* __restrict__ Q, const float* __restrict__ rms,
     const float* __restrict__ alpha, const float* __restrict__ bias, const float* __restrict__ dh,
-    const float* __restrict__ dH, float* __restrict__ G, float* __restrict__ coef,
-    float* __restrict__ sums, int64_t B, int64_t Bp, int64_t nc, float inv_k, int share, int turns) {
-    constexpr int R = Gates<N>::rows, S = Gates<N>::stride, J = (R + 63) / 64;
+    const float* __restrict__ dH, Stage<DX, N>* __restrict__ G,
+    float* __restrict__ sums, int64_t B, int64_t Bp, int64_t nc, float inv_k, int share) {
+    constexpr int R = Gates<N>::rows, S = Gates<N>::stride, P = Stage<DX, N>::rows, J = (P + 63) / 64;
     __shared__ float dots[kDotWaves][N];
     __shared__ float total[kDotWaves][S];
+    __shared__ float row[kDotWaves][4][P + N + 1];
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int per = kDotWaves / share, sub = w / share, part = w % share;  // share: a power of two
     float sum_dl[J], sum_dq[3] = {0.f, 0.f, 0.f};
 #pragma unroll
     for (int m = 0; m < J; ++m) sum_dl[m] = 0.f;
-    for (int k = 0; k < turns; ++k) {
-        const int64_t t = (static_cast<int64_t>(blockIdx.x) * turns + k) * per + sub;
+    const int64_t t0 = 4 * (static_cast<int64_t>(blockIdx.x) * per + sub);
+    for (int k = 0; k < 4; ++k) {
+        const int64_t t = t0 + k;
         float d[N], out[1];
 #pragma unroll
         for (int i = 0; i < N; ++i) d[i] = 0.f;
@@ -315,7 +425,7 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
                 const v4u u = dU[nc * t + col];
                 v4u x[N];
 #pragma unroll
-                for (int i = 0; i < N; ++i) x[i] = X[nc * (N * t + i) + col];
+                for (int i = 0; i < N; ++i) x[i] = __builtin_nontemporal_load(X + (nc * (N * t + i) + col));
 #pragma unroll
                 for (int i = 0; i < N; ++i) d[i] = add_dot<DX, N>(u, x[i], d[i]);
             }
@@ -331,7 +441,7 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
             }
             __syncthreads();
         }
-        if (part == 0 && t < Bp) {
+        if (part == 0) {
             // lane j < N takes <dU, X_j>
             dot = __int_as_float(
                 __builtin_amdgcn_ds_bpermute(4 * (lane < N ? lane * (64 / N) : 0), __float_as_int(dot)));
@@ -340,10 +450,10 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 #pragma unroll
             for (int m = 0; m < J; ++m) {
                 const int j = 64 * m + lane;
-                if (j >= R) continue;
+                if (j >= P) continue;
                 float dl = 0.f, q = 0.f, gate = 0.f;
                 const float a = row_scale<N>(alpha, j);
-                if (t < B) {
+                if (t < B && j < R) {
                     q = Q[R * t + j];
                     if (j < 2 * N) {
                         gate = sigmoid(__builtin_fmaf(a, q, bias[j]));
@@ -355,17 +465,18 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
                 }
                 const float gj = r * a * dl, dq = dl * q;
                 s = __builtin_fmaf(gj, q, s);
-                G[R * t + j] = gj;
-                if (j < N) coef[(N + 1) * t + j] = gate;
+                row[w][k][j] = gj;
+                if (j < N) row[w][k][P + j] = gate;
                 sum_dl[m] += dl;
                 sum_dq[0] += j < N ? dq : 0.f;
                 sum_dq[1] += j >= N && j < 2 * N ? dq : 0.f;
                 sum_dq[2] += j >= 2 * N ? dq : 0.f;
             }
             s = wave_sum(s);
-            if (lane == 0) coef[(N + 1) * t + N] = s * r * inv_k;
+            if (lane == 0) row[w][k][P + N] = s * r * inv_k;
         }
     }
+    if (part == 0 && t0 < Bp) store_stage<DX, N>(G[t0 / kTokenStep], row[w], static_cast<int>(t0 % kTokenStep), lane);
     // a row of sums for the block: dl's, then the three groups' dl q
 #pragma unroll
     for (int m = 0; m < J; ++m)
@@ -392,14 +503,12 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 // 16 of which lane group g has tokens 4 g .. 4 g + 3. The same registers serve everything:
 //  * dW: tile of 16 rows of W (G transposed, tokens along k) times the tokens' values, one product
 //    per channel c of the lanes: column l % 16 is channel CE (l % 16) + c, and k runs over the
-//    tokens as the lanes hold them.
+//    stage's tokens as the lanes hold them, four of each half.
 //  * dX: the rows of a product are the half's tokens, so that row 4 g + i, which lane group g gets,
 //    is the token whose values it holds.
-// bf16: G enters as the sum of two bf16 values (the upper 16 bits, and the rest rounded), 2^-16 off
-// at most, since one alone (2^-8) would be as coarse as the result's own rounding; W and X are
-// exact. Sums are fp32. W's rows stay in registers throughout; G is brought into the operands'
-// layout in LDS once for all waves of a block, a stage ahead, and a half's streams are loaded while
-// the other half is worked on.
+// W and X are exact in bf16, sums are fp32. W's rows stay in LDS or registers throughout; a stage of
+// G is copied to LDS once for all waves of a block, a stage ahead, and a half's streams are loaded
+// while the other half is worked on.
 template <int DX, int N>
 struct Back {
     // bf16 with n = 8: half as many channels, as the sums of 5 row tiles fill the registers
@@ -456,46 +565,7 @@ __device__ __forceinline__ v4u column8(const Words<WORDS> r[8], int c) {
                column_pair(r[6], r[7], c)};
 }
 
-typedef short short4v __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
-
-__device__ __forceinline__ v4f mfma_bf16_16(const v2u a, const v2u b, const v4f c) {
-    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(__builtin_bit_cast(short4v, a), __builtin_bit_cast(short4v, b), c, 0,
-                                                     0, 0);
-}
-
-// A stage of G in LDS, by halves, in the operands' layouts, and the tokens' h^pre and s.
-template <int DX, int N>
-struct Stage {
-    static constexpr bool H16 = DX == BIRKHOFF4_BF16;
-    static constexpr int R = Gates<N>::rows, RT = Gates<N>::tiles, KS = H16 ? Gates<N>::ksteps : R / 4;
-    static constexpr int parts = H16 ? 2 : 1;  // upper and lower bf16 values
-    using T = std::conditional_t<H16, uint16_t, float>;
-    static constexpr int KE = H16 ? 8 : KS;               // values per lane of a dX operand
-    static constexpr int KO = H16 ? KS : 1;               // dX operands per half
-    alignas(16) T w[2][parts][RT][64][4];                 // dW: lane (g, j): row j's tokens 4 g .. + 3
-    alignas(16) T x[2][parts][KO][64][KE];                // dX: lane (g, t): token t's rows KE g .. of the operand
-    alignas(16) float coef[N + 1][kTokenStep];
-
-    __device__ __forceinline__ void put(int t, int j, float v) {
-        const int half = t >> 4, tt = t & 15;
-        const int wl = (tt >> 2) * 16 + (j & 15), xl = (j / KE % 4) * 16 + tt;
-        if constexpr (H16) {
-            // the upper half of the bits (no rounding, so a large value does not overflow) and the
-            // rest (nothing where the value is not finite)
-            const uint32_t up = __float_as_uint(v) & 0xffff0000u;
-            const float rest = __builtin_fabsf(v) < __builtin_inff() ? v - __uint_as_float(up) : 0.f;
-            const uint16_t hi = static_cast<uint16_t>(up >> 16), lo = static_cast<uint16_t>(pack_bf16(rest, 0.f));
-            w[half][0][j >> 4][wl][tt & 3] = hi;
-            w[half][1][j >> 4][wl][tt & 3] = lo;
-            x[half][0][j >> 5][xl][j & 7] = hi;
-            x[half][1][j >> 5][xl][j & 7] = lo;
-        } else {
-            w[half][0][j >> 4][wl][tt & 3] = v;
-            x[half][0][0][xl][j % KE] = v;
-        }
-    }
-};
 
 // W's rows in the dX products' layout: in LDS, or, where it does not fit beside the stages (fp32
 // with n = 8: 160 KB), in registers; and whether E and dU are loaded a half ahead too.
@@ -503,50 +573,52 @@ template <int DX, int N>
 struct BackPlan {
     static constexpr bool H16 = DX == BIRKHOFF4_BF16;
     static constexpr bool w_lds = H16 || N == 4, ahead = w_lds;
+    static constexpr int waves = 4;  // of a block
+    static constexpr int adj = 512 / (Back<DX, N>::CW * (H16 ? 2 : 4));  // neighbouring chunks of a stream in it
+    static constexpr int stages = H16 && N == 8 ? 1 : 2;  // of G in LDS
 };
 
 template <int DX, int N>
-__global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restrict__ X, const void* __restrict__ W,
+__global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_kernel(const void* __restrict__ X, const void* __restrict__ W,
                                                              const void* __restrict__ dU, const void* __restrict__ E,
-                                                             const float* __restrict__ G, const float* __restrict__ coef,
-                                                             void* __restrict__ dX, float* __restrict__ dWp, int64_t B,
-                                                             int64_t stages, int64_t C) {
+                                                             const Stage<DX, N>* __restrict__ G, void* __restrict__ dX,
+                                                             float* __restrict__ dWp, int64_t B, int64_t stages,
+                                                             int64_t C) {
     using St = Stage<DX, N>;
     constexpr bool H16 = St::H16;
     constexpr int R = St::R, RT = St::RT, KS = St::KS;
     constexpr int CE = Back<DX, N>::CE, WO = Back<DX, N>::words, SZ = H16 ? 2 : 4;
-    constexpr int kThreads = 64 * N, GQ = (kTokenStep * R + kThreads - 1) / kThreads;
-    static_assert(kTokenStep * (N + 1) <= kThreads, "one coefficient per thread");
+    constexpr int NW = BackPlan<DX, N>::waves, NS = BackPlan<DX, N>::stages;
+    constexpr int kThreads = 64 * NW, kQuads = sizeof(St) / 16, GQ = (kQuads + kThreads - 1) / kThreads;
+    static_assert(sizeof(St) % 16 == 0, "copied in 16-byte pieces");
     constexpr bool kLds = BackPlan<DX, N>::w_lds, kAhead = BackPlan<DX, N>::ahead;
     using Row = Words<WO>;
-    __shared__ St lds[2];
+    __shared__ St lds[NS];
     // [operand][channel][lane]: of bf16 eight rows, of fp32 one
-    __shared__ std::conditional_t<H16, v4u, float> wlds[kLds ? N : 1][kLds ? KS : 1][CE][64];
+    __shared__ std::conditional_t<H16, v4u, float> wlds[kLds ? NW : 1][kLds ? KS : 1][CE][64];
     const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
-    const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));  // the stream
-    const int64_t ch = static_cast<int64_t>(blockIdx.x) * Back<DX, N>::CW + CE * c16;
+    const int ww = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    constexpr int ADJ = BackPlan<DX, N>::adj;
+    const int w = static_cast<int>(blockIdx.z) * (BackPlan<DX, N>::waves / ADJ) + ww / ADJ;  // the stream
+    const int64_t ch = (static_cast<int64_t>(blockIdx.x) * ADJ + ww % ADJ) * Back<DX, N>::CW + CE * c16;
     const bool own = ch < C;
     const int64_t at = own ? ch : 0;  // lanes past the end of the row read its start and store nothing
     const int64_t K = N * C;
 
-    // operand rows past the last row of W stay zero
-    for (unsigned q = threadIdx.x; q < sizeof(lds) / 4; q += kThreads) reinterpret_cast<uint32_t*>(lds)[q] = 0;
-    float gq[GQ], cq = 0.f;
+    v4u gq[GQ];
     auto fetch = [&](int64_t st) {
 #pragma unroll
         for (int q = 0; q < GQ; ++q) {
             const int k = static_cast<int>(threadIdx.x) + kThreads * q;
-            if (k < kTokenStep * R) gq[q] = G[st * kTokenStep * R + k];
+            if (k < kQuads) gq[q] = reinterpret_cast<const v4u*>(G + st)[k];
         }
-        if (threadIdx.x < kTokenStep * (N + 1)) cq = coef[st * kTokenStep * (N + 1) + threadIdx.x];
     };
     auto put = [&](St& to) {
 #pragma unroll
         for (int q = 0; q < GQ; ++q) {
             const int k = static_cast<int>(threadIdx.x) + kThreads * q;
-            if (k < kTokenStep * R) to.put(k / R, k % R, gq[q]);
+            if (k < kQuads) reinterpret_cast<v4u*>(&to)[k] = gq[q];
         }
-        if (threadIdx.x < kTokenStep * (N + 1)) to.coef[threadIdx.x % (N + 1)][threadIdx.x / (N + 1)] = cq;
     };
     // a half's rows start at a uniform address, the lane's four at 32-bit offsets from it; past the
     // last token: that token again
@@ -582,7 +654,7 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
 
     int64_t st = blockIdx.y;
     fetch(st);
-    Row x[2][4], e[kAhead ? 2 : 1][4] = {}, u[kAhead ? 2 : 1][4] = {};
+    Row x[2][4] = {}, e[kAhead ? 2 : 1][4] = {}, u[kAhead ? 2 : 1][4] = {};
     // a stage has two halves also where the last one is past the end
     auto load = [&](int hf, int64_t t0) {
         if (t0 >= B) return;  // uniform
@@ -596,13 +668,13 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
     std::conditional_t<H16, v4u, float> wreg[kLds ? 1 : KS][CE];
     auto keep = [&](int k, int c, auto v) {
         if constexpr (kLds)
-            wlds[w][k][c][lane] = v;
+            wlds[ww][k][c][lane] = v;
         else
             wreg[k][c] = v;
     };
     auto wop = [&](int k, int c) {
         if constexpr (kLds)
-            return wlds[w][k][c][lane];
+            return wlds[ww][k][c][lane];
         else
             return wreg[k][c];
     };
@@ -632,38 +704,41 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
 #pragma unroll
         for (int c = 0; c < CE; ++c) acc[r][c] = v4f{0.f, 0.f, 0.f, 0.f};
 
+    // dW += G^T X
+    auto sum_w = [&](const St& s) {
+        if constexpr (H16) {
+            v4u b[CE];
+#pragma unroll
+            for (int c = 0; c < CE; ++c)
+                b[c] = v4u{column_pair(x[0][0], x[0][1], c), column_pair(x[0][2], x[0][3], c),
+                           column_pair(x[1][0], x[1][1], c), column_pair(x[1][2], x[1][3], c)};
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) {
+                    const v2u a0 = *reinterpret_cast<const v2u*>(s.w[p][r][0][lane]);
+                    const v2u a1 = *reinterpret_cast<const v2u*>(s.w[p][r][1][lane]);
+                    const v4u a = {a0.x, a0.y, a1.x, a1.y};
+#pragma unroll
+                    for (int c = 0; c < CE; ++c) acc[r][c] = mfma_bf16(a, b[c], acc[r][c]);
+                }
+        } else {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int hf = 0; hf < 2; ++hf) {
+                    const v4f gr = *reinterpret_cast<const v4f*>(s.w[0][r][hf][lane]);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+#pragma unroll
+                        for (int c = 0; c < CE; ++c)
+                            acc[r][c] = mfma_f32(gr[k], __uint_as_float(x[hf][k].v[c]), acc[r][c]);
+                }
+        }
+    };
     auto work = [&](Row (&x)[4], Row (&e)[4], Row (&u)[4], const St& s, int hf, int64_t t0) {
         if (t0 >= B) return;  // uniform
         if constexpr (!kAhead) load_eu(e, u, t0);
-        if (t0 + kHalf > B) {  // tokens past the last one add nothing to dW: zeros, as 0 times their G
-#pragma unroll
-            for (int k = 0; k < 4; ++k)
-                if (t0 + 4 * g + k >= B) x[k] = Row{};
-        }
-        // dW += G^T X
-        if constexpr (H16) {
-            v2u hi[RT], lo[RT];
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                hi[r] = *reinterpret_cast<const v2u*>(s.w[hf][0][r][lane]);
-                lo[r] = *reinterpret_cast<const v2u*>(s.w[hf][St::parts - 1][r][lane]);
-            }
-#pragma unroll
-            for (int c = 0; c < CE; ++c) {
-                const v2u b = {column_pair(x[0], x[1], c), column_pair(x[2], x[3], c)};
-#pragma unroll
-                for (int r = 0; r < RT; ++r) acc[r][c] = mfma_bf16_16(lo[r], b, mfma_bf16_16(hi[r], b, acc[r][c]));
-            }
-        } else {
-#pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                const v4f gr = *reinterpret_cast<const v4f*>(s.w[hf][0][r][lane]);
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-#pragma unroll
-                    for (int c = 0; c < CE; ++c) acc[r][c] = mfma_f32(gr[k], __uint_as_float(x[k].v[c]), acc[r][c]);
-            }
-        }
         // dX = E + h^pre dU + G W - s X
         v4f d[CE];
 #pragma unroll
@@ -710,20 +785,28 @@ __global__ __launch_bounds__(64 * N, 2) void pre_back_kernel(const void* __restr
         }
     };
 
-    __syncthreads();  // the zeros
     put(lds[0]);
-    for (int cur = 0; st < stages; cur ^= 1) {
+    for (int cur = 0; st < stages; cur ^= NS - 1) {
         const int64_t t0 = st * kTokenStep;
         st += gridDim.y;
         const bool more = st < stages;  // uniform over the block
         __syncthreads();                // this stage's G is there, and nobody reads the other's any more
         if (more) fetch(st);
+        if (t0 + kTokenStep > B) {  // tokens past the last one add nothing to dW: zeros, as 0 times their G
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    if (t0 + kHalf * hf + 4 * g + k >= B) x[hf][k] = Row{};
+        }
+        sum_w(lds[cur]);
         work(x[0], e[0], u[0], lds[cur], 0, t0);
         if (more) load(0, st * kTokenStep);
         work(x[1], e[kAhead ? 1 : 0], u[kAhead ? 1 : 0], lds[cur], 1, t0 + kHalf);
         if (more) {
             load(1, st * kTokenStep + kHalf);
-            put(lds[cur ^ 1]);
+            if constexpr (NS == 1) __syncthreads();
+            put(lds[NS == 2 ? cur ^ 1 : 0]);
         }
     }
     if (own) {
@@ -768,6 +851,7 @@ __global__ __launch_bounds__(kJoinBlock) void pre_join_kernel(const v4f* __restr
     const int j = 16 * static_cast<int>(blockIdx.x - wblocks) + c;
     float v = 0.f;
     if (j < S)
+#pragma unroll 8
         for (int64_t k = part; k < rows; k += kJoinBlock / 16) v += sums[k * S + j];
     red[part][c] = v;
     __syncthreads();
@@ -791,18 +875,19 @@ struct PreShape {
 };
 
 struct GateLaunch {
-    int tt;                      // 16-token tiles per block
+    int tt, waves;               // 16-token tiles and waves of a block
     int64_t tiles, splits, per;  // blocks over tokens, shares of the row, steps per share
 };
 
 constexpr int64_t kGateBlocks = 1024;
-constexpr int64_t kGateMaxSplits = 64;
+constexpr int64_t kGateMaxSplits = 16;
 
 GateLaunch gate_launch(const PreShape& s) {
     GateLaunch l;
-    l.tt = s.B <= 16 ? 1 : s.B <= 32 ? 2 : 4;
+    l.tt = s.B <= 16 ? 1 : s.B <= 512 ? 2 : 4;
+    l.waves = s.B <= 512 ? 16 : 4;
     l.tiles = cdiv(s.B, 16 * l.tt);
-    const int64_t most = cdiv(s.steps, 2 * kGateWaves);
+    const int64_t most = cdiv(s.steps, 2 * l.waves);
     int64_t want = cdiv(kGateBlocks, l.tiles);
     if (want > most) want = most;
     if (want > kGateMaxSplits) want = kGateMaxSplits;
@@ -813,25 +898,24 @@ GateLaunch gate_launch(const PreShape& s) {
 
 struct BackLaunch {
     int64_t Bp;                    // tokens in whole steps
-    int share, turns;              // of pre_dot_kernel
+    int share;                     // of pre_dot_kernel
     int64_t dot_blocks;
     int64_t chunks, token_shares;  // of pre_back_kernel
-    int64_t g, coef, sums, dw, bytes;  // the workspace's parts: offsets in bytes, and its size
+    int64_t g, sums, dw, bytes;  // the workspace's parts: offsets in bytes, and its size
 };
 
-constexpr int64_t kDotBlocks = 2048;
 constexpr int64_t kBackWaves = 2048;  // two per SIMD
 
 BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
     BackLaunch l;
     const int64_t rows = n * n + 2 * n;
+    constexpr int F = BIRKHOFF4_F32, S = BIRKHOFF4_BF16;
+    const int64_t stage_bytes = n == 4 ? (bf16 ? sizeof(Stage<S, 4>) : sizeof(Stage<F, 4>))
+                                       : (bf16 ? sizeof(Stage<S, 8>) : sizeof(Stage<F, 8>));
     l.Bp = cdiv(s.B, kTokenStep) * kTokenStep;
     l.share = 1;
-    while (l.share < kDotWaves && l.share < cdiv(s.nc, 64) && l.Bp * l.share < 8192) l.share *= 2;
-    const int64_t groups = cdiv(l.Bp, kDotWaves / l.share);
-    const int64_t turns = cdiv(groups, kDotBlocks);
-    l.turns = turns > 1 ? static_cast<int>(turns) : 1;
-    l.dot_blocks = cdiv(groups, l.turns);
+    while (l.share < kDotWaves && l.share < cdiv(s.nc, 64)) l.share *= 2;
+    l.dot_blocks = cdiv(l.Bp / 4, kDotWaves / l.share);
     const int cw = bf16 ? (n == 4 ? Back<BIRKHOFF4_BF16, 4>::CW : Back<BIRKHOFF4_BF16, 8>::CW) : Back<BIRKHOFF4_F32, 4>::CW;
     l.chunks = cdiv(s.C, cw);
     const int64_t steps = l.Bp / kTokenStep;
@@ -844,8 +928,7 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
         at += cdiv(4 * floats, 256) * 256;
         return was;
     };
-    l.g = take(l.Bp * rows);
-    l.coef = take(l.Bp * (n + 1));
+    l.g = take(l.Bp / kTokenStep * (stage_bytes / 4));
     l.sums = take(l.dot_blocks * (rows + 4));
     l.dw = take(l.token_shares * rows * n * s.C);
     l.bytes = at;
@@ -854,7 +937,7 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
 
 constexpr int64_t kPreMaxTokens = int64_t(1) << 26;  // a launch's lanes over tokens stay 32-bit
 constexpr int64_t kPreMaxValues = int64_t(1) << 46;
-constexpr int64_t kPreMaxChannels = int64_t(1) << 22;  // sixteen tokens within 32-bit offsets
+constexpr int64_t kPreMaxChannels = int64_t(1) << 20;  // 64 tokens lie within 32-bit offsets
 
 // The checks that both directions and the workspace's size share.
 int pre_shape(int n, int64_t B, int64_t C, int x_dtype, PreShape* s) {
@@ -874,8 +957,9 @@ int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float*
                    void* U, float* h, float* H, float* q, float* rms, float* part, hipStream_t stream) {
     const GateLaunch l = gate_launch(s);
     const v4u *x = static_cast<const v4u*>(X), *w = static_cast<const v4u*>(W);
-    auto gate = l.tt == 1 ? pre_gate_kernel<DX, N, 1> : l.tt == 2 ? pre_gate_kernel<DX, N, 2> : pre_gate_kernel<DX, N, 4>;
-    launch_kernel(gate, dim3(static_cast<unsigned>(l.tiles), static_cast<unsigned>(l.splits)), dim3(64 * kGateWaves), 0,
+    auto gate = l.tt == 1 ? pre_gate_kernel<DX, N, 1, 16>
+                          : l.tt == 2 ? pre_gate_kernel<DX, N, 2, 16> : pre_gate_kernel<DX, N, 4, 4>;
+    launch_kernel(gate, dim3(static_cast<unsigned>(l.tiles), static_cast<unsigned>(l.splits)), dim3(64 * l.waves), 0,
                   stream, x, w, part, s.B, s.steps, l.per);
     const int L = s.nc <= 8 ? 8 : s.nc <= 16 ? 16 : s.nc <= 32 ? 32 : 64;
     auto read = L == 8 ? pre_read_kernel<DX, N, 8> : L == 16 ? pre_read_kernel<DX, N, 16>
@@ -894,13 +978,14 @@ int launch_pre_bwd(const PreShape& s, const void* X, const void* W, const float*
                    float* dalpha, float* dbias, char* work, hipStream_t stream) {
     const BackLaunch l = back_launch(s, N, DX == BIRKHOFF4_BF16);
     auto at = [&](int64_t o) { return reinterpret_cast<float*>(work + o); };
+    Stage<DX, N>* stage = reinterpret_cast<Stage<DX, N>*>(at(l.g));
     if (s.B > 0) {
         launch_kernel((pre_dot_kernel<DX, N>), dim3(static_cast<unsigned>(l.dot_blocks)), dim3(64 * kDotWaves), 0, stream,
-                      static_cast<const v4u*>(X), static_cast<const v4u*>(dU), q, rms, alpha, bias, dh, dH, at(l.g),
-                      at(l.coef), at(l.sums), s.B, l.Bp, s.nc,
-                      static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), l.share, l.turns);
-        launch_kernel((pre_back_kernel<DX, N>), dim3(static_cast<unsigned>(l.chunks), static_cast<unsigned>(l.token_shares)),
-                      dim3(64 * N), 0, stream, X, W, dU, E, at(l.g), at(l.coef), dX, at(l.dw), s.B, l.Bp / kTokenStep, s.C);
+                      static_cast<const v4u*>(X), static_cast<const v4u*>(dU), q, rms, alpha, bias, dh, dH, stage,
+                      at(l.sums), s.B, l.Bp, s.nc,
+                      static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), l.share);
+        launch_kernel((pre_back_kernel<DX, N>), dim3(static_cast<unsigned>(cdiv(l.chunks, BackPlan<DX, N>::adj)), static_cast<unsigned>(l.token_shares), N * BackPlan<DX, N>::adj / BackPlan<DX, N>::waves),
+                      dim3(64 * BackPlan<DX, N>::waves), 0, stream, X, W, dU, E, stage, dX, at(l.dw), s.B, l.Bp / kTokenStep, s.C);
     }
     // without tokens the sums are empty: zeros
     const int64_t quads = Gates<N>::rows * N * s.C / 4;
