@@ -206,10 +206,13 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
 // ---------------------------------------------------------------------------
 // Forward: the coefficients, and U = sum_i h^pre_i X_i
 // ---------------------------------------------------------------------------
-// Lanes take 16-byte chunks of the rows, L lanes a token and 64 / L tokens a wave; a wave adds its
-// tokens' partial sums itself (lane j row j), while its part of the streams is on the way.
+// Lanes take 16-byte chunks of the rows, L lanes a token and 64 / L tokens a wave. The tokens' partial
+// sums are added (lane j row j) while the streams are on the way; the waves of a block of one token
+// take shares in turn (added by each of its waves: 32 tokens of 8 x 4096 with 32 shares 17 us).
+constexpr int kReadWaves = 8;
+
 template <int DX, int N, int L>
-__global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__ part, const v4u* __restrict__ X,
+__global__ __launch_bounds__(64 * kReadWaves) void pre_read_kernel(const float* __restrict__ part, const v4u* __restrict__ X,
                                                        const float* __restrict__ alpha, const float* __restrict__ bias,
                                                        float eps, float inv_k, v4u* __restrict__ U,
                                                        float* __restrict__ h, float* __restrict__ H,
@@ -232,6 +235,7 @@ __global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__
 #pragma unroll
         for (int i = 0; i < N; ++i) x[i] = __builtin_nontemporal_load(row + (i * nc + col));
     }
+    __shared__ float psum[L == 64 ? kReadWaves : 1][64 * J];
     float hp[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) hp[i] = 0.f;
@@ -242,12 +246,27 @@ __global__ __launch_bounds__(512) void pre_read_kernel(const float* __restrict__
         float sum[J], l[J], gate[J];
 #pragma unroll
         for (int m = 0; m < J; ++m) sum[m] = 0.f;
-#pragma unroll 16
-        for (int s = 0; s < splits; ++s) {
+#pragma unroll 8
+        for (int s = L == 64 ? w : 0; s < splits; s += L == 64 ? W : 1) {
             const float* p = part + (s * B + t) * S;
 #pragma unroll
             for (int m = 0; m < J; ++m)
                 if (64 * m + lane < S) sum[m] += p[64 * m + lane];
+        }
+        if (L == 64 && W > 1 && splits > 1) {  // uniform over the block
+#pragma unroll
+            for (int m = 0; m < J; ++m) psum[w][64 * m + lane] = sum[m];
+            __syncthreads();
+            const int most = splits < W ? splits : W;
+#pragma unroll
+            for (int m = 0; m < J; ++m) {
+                sum[m] = psum[0][64 * m + lane];
+                for (int q = 1; q < most; ++q) sum[m] += psum[q][64 * m + lane];
+            }
+        } else if (L == 64 && W > 1 && w > 0) {  // one share: the other waves read it too
+#pragma unroll
+            for (int m = 0; m < J; ++m)
+                if (64 * m + lane < S) sum[m] = part[t * S + 64 * m + lane];
         }
         const float norm2 = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(sum[R / 64]), R % 64));
         const float r = __builtin_amdgcn_rsqf(__builtin_fmaf(norm2, inv_k, eps));
@@ -879,18 +898,31 @@ struct GateLaunch {
     int64_t tiles, splits, per;  // blocks over tokens, shares of the row, steps per share
 };
 
-constexpr int64_t kGateBlocks = 1024;
-constexpr int64_t kGateMaxSplits = 16;
+// Tokens of a block and its waves, and shares of the row, us of the whole forward:
+//  * up to 16 tokens one tile and 16 waves: 1 token of 4 x 4096 bf16 8.1, of 8 x 4096 13.7.
+//  * n = 4 up to 512 two tiles and 16 waves: 96 tokens of 4 x 4096 11.5, four tiles and 4 waves 12.4; 300
+//    13.8 and 14.8; 600 23 and 19.3. n = 8 up to 64 two tiles and 8 waves (more do not fit the
+//    registers): 32 tokens of 8 x 4096 16.6, four tiles 19.2; 100 of 8 x 2048 18.1 and 17.5.
+//  * else four tiles, each row of W read once for 64 tokens, and 4 waves: 32 K tokens of 4 x 4096
+//    442 (two tiles 488).
+//  * shares until 2048 waves (4097 tokens of 4 x 1000 fp32 45.0; 4096 waves 47.6), each wave with a
+//    whole line of every token at least; at most 16, as each costs a read of the sums (600 tokens of 8 x
+//    4096 33.9, with 32 37.3; 1023 of 8 x 2052 fp32 61.7 and 73.3), 32 where there are few blocks
+//    (32 tokens of 8 x 4096 16.9, with 16 28).
+constexpr int64_t kGateWant = 2048;
 
-GateLaunch gate_launch(const PreShape& s) {
+template <int N>
+constexpr int gate_waves(int tiles) { return tiles == 1 ? 16 : tiles == 2 ? (N == 4 ? 16 : 8) : 4; }
+
+GateLaunch gate_launch(const PreShape& s, int n) {
     GateLaunch l;
-    l.tt = s.B <= 16 ? 1 : s.B <= 512 ? 2 : 4;
-    l.waves = s.B <= 512 ? 16 : 4;
+    l.tt = s.B <= 16 ? 1 : s.B <= (n == 4 ? 512 : 64) ? 2 : 4;
+    l.waves = n == 4 ? gate_waves<4>(l.tt) : gate_waves<8>(l.tt);
     l.tiles = cdiv(s.B, 16 * l.tt);
-    const int64_t most = cdiv(s.steps, 2 * l.waves);
-    int64_t want = cdiv(kGateBlocks, l.tiles);
+    const int64_t most = cdiv(s.steps, 2 * l.waves), cap = l.tiles <= 4 ? 32 : 16;
+    int64_t want = cdiv(kGateWant, l.waves * l.tiles);
     if (want > most) want = most;
-    if (want > kGateMaxSplits) want = kGateMaxSplits;
+    if (want > cap) want = cap;
     l.per = 2 * cdiv(cdiv(s.steps, want), 2);
     l.splits = cdiv(s.steps, l.per);
     return l;
@@ -955,16 +987,16 @@ bool eps_ok(float eps) { return eps >= 0.f && eps < __builtin_inff(); }
 template <int DX, int N>
 int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float* alpha, const float* bias, float eps,
                    void* U, float* h, float* H, float* q, float* rms, float* part, hipStream_t stream) {
-    const GateLaunch l = gate_launch(s);
+    const GateLaunch l = gate_launch(s, N);
     const v4u *x = static_cast<const v4u*>(X), *w = static_cast<const v4u*>(W);
-    auto gate = l.tt == 1 ? pre_gate_kernel<DX, N, 1, 16>
-                          : l.tt == 2 ? pre_gate_kernel<DX, N, 2, 16> : pre_gate_kernel<DX, N, 4, 4>;
+    auto gate = l.tt == 1   ? pre_gate_kernel<DX, N, 1, gate_waves<N>(1)>
+                : l.tt == 2 ? pre_gate_kernel<DX, N, 2, gate_waves<N>(2)> : pre_gate_kernel<DX, N, 4, gate_waves<N>(4)>;
     launch_kernel(gate, dim3(static_cast<unsigned>(l.tiles), static_cast<unsigned>(l.splits)), dim3(64 * l.waves), 0,
                   stream, x, w, part, s.B, s.steps, l.per);
     const int L = s.nc <= 8 ? 8 : s.nc <= 16 ? 16 : s.nc <= 32 ? 32 : 64;
     auto read = L == 8 ? pre_read_kernel<DX, N, 8> : L == 16 ? pre_read_kernel<DX, N, 16>
                 : L == 32 ? pre_read_kernel<DX, N, 32> : pre_read_kernel<DX, N, 64>;
-    const int64_t cols = cdiv(s.nc, L), shares = cdiv(cols, 8), waves = cdiv(cols, shares);
+    const int64_t cols = cdiv(s.nc, L), shares = cdiv(cols, kReadWaves), waves = cdiv(cols, shares);
     launch_kernel(read, dim3(static_cast<unsigned>(cdiv(s.B, 64 / L)), static_cast<unsigned>(shares)),
                   dim3(static_cast<unsigned>(64 * waves)), 0, stream, part, x, alpha, bias, eps,
                   static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), static_cast<v4u*>(U), h, H, q, rms, s.B, s.nc,
@@ -1002,7 +1034,7 @@ int64_t pre_work(int n, int64_t B, int64_t C, int x_dtype, int backward) {
     if (int e = pre_shape(n, B, C, x_dtype, &s)) return e;
     if (B == 0) return 0;
     if (backward) return back_launch(s, n, x_dtype == BIRKHOFF4_BF16).bytes;
-    const GateLaunch l = gate_launch(s);
+    const GateLaunch l = gate_launch(s, n);
     return l.splits * B * (n * n + 2 * n + 4) * 4;
 }
 
