@@ -530,8 +530,8 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 // while the other half is worked on.
 template <int DX, int N>
 struct Back {
-    // bf16 with n = 8: half as many channels, as the sums of 5 row tiles fill the registers
-    static constexpr int CE = DX == BIRKHOFF4_BF16 && N == 4 ? 8 : 4;
+    // n = 8: half as many channels, as the sums of 5 row tiles fill the registers
+    static constexpr int CE = (DX == BIRKHOFF4_BF16 ? 8 : 4) / (N == 8 ? 2 : 1);
     static constexpr int CW = 16 * CE;
     static constexpr int words = CE * (DX == BIRKHOFF4_BF16 ? 2 : 4) / 4;  // of a lane's channels
 };
@@ -586,12 +586,12 @@ __device__ __forceinline__ v4u column8(const Words<WORDS> r[8], int c) {
 
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 
-// W's rows in the dX products' layout: in LDS, or, where it does not fit beside the stages (fp32
-// with n = 8: 160 KB), in registers; and whether E and dU are loaded a half ahead too.
+// W's rows in the dX products' layout are in LDS, or, where they would leave a CU one block (fp32
+// with n = 8), in registers.
 template <int DX, int N>
 struct BackPlan {
     static constexpr bool H16 = DX == BIRKHOFF4_BF16;
-    static constexpr bool w_lds = H16 || N == 4, ahead = w_lds;
+    static constexpr bool w_lds = H16 || N == 4;
     static constexpr int waves = 4;  // of a block
     static constexpr int adj = 512 / (Back<DX, N>::CW * (H16 ? 2 : 4));  // neighbouring chunks of a stream in it
     static constexpr int stages = H16 && N == 8 ? 1 : 2;  // of G in LDS
@@ -610,7 +610,7 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
     constexpr int NW = BackPlan<DX, N>::waves, NS = BackPlan<DX, N>::stages;
     constexpr int kThreads = 64 * NW, kQuads = sizeof(St) / 16, GQ = (kQuads + kThreads - 1) / kThreads;
     static_assert(sizeof(St) % 16 == 0, "copied in 16-byte pieces");
-    constexpr bool kLds = BackPlan<DX, N>::w_lds, kAhead = BackPlan<DX, N>::ahead;
+    constexpr bool kLds = BackPlan<DX, N>::w_lds;
     using Row = Words<WO>;
     __shared__ St lds[NS];
     // [operand][channel][lane]: of bf16 eight rows, of fp32 one
@@ -673,12 +673,12 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
 
     int64_t st = blockIdx.y;
     fetch(st);
-    Row x[2][4] = {}, e[kAhead ? 2 : 1][4] = {}, u[kAhead ? 2 : 1][4] = {};
+    Row x[2][4] = {}, e[2][4] = {}, u[2][4] = {};
     // a stage has two halves also where the last one is past the end
     auto load = [&](int hf, int64_t t0) {
         if (t0 >= B) return;  // uniform
         load_x(x[hf], t0);
-        if constexpr (kAhead) load_eu(e[hf], u[hf], t0);
+        load_eu(e[hf], u[hf], t0);
     };
     load(0, st * kTokenStep);
     load(1, st * kTokenStep + kHalf);
@@ -757,7 +757,6 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
     };
     auto work = [&](Row (&x)[4], Row (&e)[4], Row (&u)[4], const St& s, int hf, int64_t t0) {
         if (t0 >= B) return;  // uniform
-        if constexpr (!kAhead) load_eu(e, u, t0);
         // dX = E + h^pre dU + G W - s X
         v4f d[CE];
 #pragma unroll
@@ -821,7 +820,7 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
         sum_w(lds[cur]);
         work(x[0], e[0], u[0], lds[cur], 0, t0);
         if (more) load(0, st * kTokenStep);
-        work(x[1], e[kAhead ? 1 : 0], u[kAhead ? 1 : 0], lds[cur], 1, t0 + kHalf);
+        work(x[1], e[1], u[1], lds[cur], 1, t0 + kHalf);
         if (more) {
             load(1, st * kTokenStep + kHalf);
             if constexpr (NS == 1) __syncthreads();
@@ -836,9 +835,13 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
                 const int j = 16 * r + 4 * g + i;
                 if (j >= R) continue;
                 v4f* p = reinterpret_cast<v4f*>(dWp + (static_cast<int64_t>(blockIdx.y) * R + j) * K + w * C + ch);
+                if constexpr (CE == 2) {
+                    *reinterpret_cast<f32x2*>(p) = f32x2{acc[r][0][i], acc[r][1][i]};
+                } else {
 #pragma unroll
-                for (int q = 0; q < CE / 4; ++q)
-                    p[q] = v4f{acc[r][4 * q][i], acc[r][4 * q + 1][i], acc[r][4 * q + 2][i], acc[r][4 * q + 3][i]};
+                    for (int q = 0; q < CE / 4; ++q)
+                        p[q] = v4f{acc[r][4 * q][i], acc[r][4 * q + 1][i], acc[r][4 * q + 2][i], acc[r][4 * q + 3][i]};
+                }
             }
     }
 }
@@ -948,7 +951,7 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
     l.share = 1;
     while (l.share < kDotWaves && l.share < cdiv(s.nc, 64)) l.share *= 2;
     l.dot_blocks = cdiv(l.Bp / 4, kDotWaves / l.share);
-    const int cw = bf16 ? (n == 4 ? Back<BIRKHOFF4_BF16, 4>::CW : Back<BIRKHOFF4_BF16, 8>::CW) : Back<BIRKHOFF4_F32, 4>::CW;
+    const int cw = n == 4 ? (bf16 ? Back<S, 4>::CW : Back<F, 4>::CW) : (bf16 ? Back<S, 8>::CW : Back<F, 8>::CW);
     l.chunks = cdiv(s.C, cw);
     const int64_t steps = l.Bp / kTokenStep;
     int64_t shares = kBackWaves / (n * l.chunks);
