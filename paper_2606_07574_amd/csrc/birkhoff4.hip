@@ -1081,10 +1081,11 @@ __device__ __forceinline__ void unpack_word(const v4u c, int w, float v[MixChunk
 
 // out_i = sum_j m_ij in_j over the E channels of one chunk of each of the N rows (TRANS:
 // m_ji, the transpose, read in place), one 32-bit word of the chunk at a time so that only
-// that word's channels are unpacked at once. POST: plus hs_i z, rounded once.
+// that word's channels are unpacked at once. POST: plus hs_i z, rounded once; TRANS: and z = sum_i
+// hs_i in_i as one more output.
 template <int DX, int N, bool TRANS = false, bool POST = false>
 __device__ __forceinline__ void mix_chunk(const float m[N * N], const v4u in[N], v4u out[N], const float* hs = nullptr,
-                                          const v4u z = v4u{0u, 0u, 0u, 0u}) {
+                                          v4u* z = nullptr) {
     constexpr int EW = MixChunk<DX>::E / 4;
     uint32_t o[N][4];
 #pragma unroll
@@ -1093,14 +1094,26 @@ __device__ __forceinline__ void mix_chunk(const float m[N * N], const v4u in[N],
 #pragma unroll
         for (int j = 0; j < N; ++j) unpack_word<DX>(in[j], w, x[j]);
         float d[EW];
-        if constexpr (POST) unpack_word<DX>(z, w, d);
+        if constexpr (POST && !TRANS) unpack_word<DX>(*z, w, d);
+        if constexpr (POST && TRANS) {
+#pragma unroll
+            for (int e = 0; e < EW; ++e) {
+                d[e] = hs[0] * x[0][e];
+#pragma unroll
+                for (int j = 1; j < N; ++j) d[e] = __builtin_fmaf(hs[j], x[j][e], d[e]);
+            }
+            if constexpr (DX == BIRKHOFF4_BF16)
+                (*z)[w] = pack_bf16(d[0], d[1]);
+            else
+                (*z)[w] = __float_as_uint(d[0]);
+        }
 #pragma unroll
         for (int i = 0; i < N; ++i) {
             float y[EW];
 #pragma unroll
             for (int e = 0; e < EW; ++e) {
                 y[e] = m[TRANS ? i : N * i] * x[0][e];
-                if constexpr (POST) y[e] = __builtin_fmaf(hs[i], d[e], y[e]);
+                if constexpr (POST && !TRANS) y[e] = __builtin_fmaf(hs[i], d[e], y[e]);
 #pragma unroll
                 for (int j = 1; j < N; ++j) y[e] = __builtin_fmaf(m[TRANS ? N * j + i : N * i + j], x[j][e], y[e]);
             }
@@ -1139,6 +1152,13 @@ struct WriteBack<true> {
     float* dh;  // [B][N]
 };
 
+// A value at an address that is uniform over the wave and that the launch does not write, through
+// the scalar cache (behind a structure's pointer the compiler cannot tell that it may).
+template <typename T>
+__device__ __forceinline__ T scalar_load(const T* p) {
+    return *(const __attribute__((address_space(4))) T*)(p);
+}
+
 // Philox 4x32-10 (Salmon et al., "Parallel random numbers: as easy as 1, 2, 3", 2011): four words
 // for each value of a counter of four words under a key of two; ten rounds are the authors' own
 // choice.
@@ -1163,7 +1183,7 @@ __device__ __forceinline__ v4u philox(uint64_t index, uint64_t offset, uint64_t 
 // element e's word is word e % 4 of block e / 4.
 template <int DX>
 __device__ __forceinline__ v4u keep_mask(const Write<true>& wr, int64_t index) {
-    const uint64_t seed = wr.rng[0], offset = wr.rng[1];
+    const uint64_t seed = scalar_load(wr.rng), offset = scalar_load(wr.rng + 1);
     if constexpr (DX == BIRKHOFF4_F32) {
         const v4u r = philox(index, offset, seed);
         v4u m;
@@ -1179,11 +1199,11 @@ __device__ __forceinline__ v4u keep_mask(const Write<true>& wr, int64_t index) {
     }
 }
 
-// h_i / (1 - p) of token t: what the kept elements are multiplied by.
-template <int N>
+// h_i / (1 - p) of token t: what the kept elements are multiplied by. UNIFORM: t is, over the wave.
+template <int N, bool UNIFORM>
 __device__ __forceinline__ void load_gates(const Write<true>& wr, int64_t t, float hs[N]) {
 #pragma unroll
-    for (int i = 0; i < N; ++i) hs[i] = wr.h[N * t + i] * wr.scale;
+    for (int i = 0; i < N; ++i) hs[i] = (UNIFORM ? scalar_load(wr.h + (N * t + i)) : wr.h[N * t + i]) * wr.scale;
 }
 
 // P of token t (N x N), uniform over the wave.
@@ -1241,11 +1261,11 @@ __global__ __launch_bounds__(64 * kMixMaxWaves) void mix_fwd_kernel(const float*
             }
             float p[N * N], hs[N];
             load_token_matrix<N>(P, t, p);
-            if constexpr (POST) load_gates<N>(wr, t, hs);
+            if constexpr (POST) load_gates<N, true>(wr, t, hs);
             if (own) {
                 if constexpr (POST)
                     if (wr.least) z &= keep_mask<DX>(wr, nc * t + col + lane);
-                mix_chunk<DX, N, false, POST>(p, x, y, hs, z);
+                mix_chunk<DX, N, false, POST>(p, x, y, hs, &z);
 #pragma unroll
                 for (int j = 0; j < N; ++j) __builtin_nontemporal_store(y[j], Y + (off + j * nc) + lane);
             }
@@ -1302,21 +1322,6 @@ __device__ __forceinline__ void add_inner(const v4u z, const v4u g[N], float acc
         }
 }
 
-// sum_i hs_i g_i over one chunk of each row.
-template <int DX, int N>
-__device__ __forceinline__ v4u combine_chunk(const float hs[N], const v4u g[N]) {
-    constexpr int E = MixChunk<DX>::E;
-    float sum[E];
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-        float v[E];
-        unpack_chunk<DX>(g[i], v);
-#pragma unroll
-        for (int e = 0; e < E; ++e) sum[e] = i == 0 ? hs[0] * v[e] : __builtin_fmaf(hs[i], v[e], sum[e]);
-    }
-    return pack_chunk<DX>(sum);
-}
-
 // Row `i` (a lane index) of token t's 4 x 4 dH, which the lane holds whole, stored as fp32 or
 // rounded to nearest even as bf16.
 __device__ __forceinline__ void store_dh_row(void* dH, bool h16, int64_t t, int i, const float m[16]) {
@@ -1335,21 +1340,21 @@ __device__ __forceinline__ void store_dh_row(void* dH, bool h16, int64_t t, int 
 // sums its lanes' parts; with W > 1 the waves leave them in LDS and the first one adds them
 // in wave order, so the result does not depend on timing. For n = 4 it then forms dH; for n =
 // 8 it writes dP, lane L entry L, for the 8 x 8 backward to take over.
-constexpr int mix_bwd_max_waves(int n, bool post) { return n == 8 || post ? 8 : kMixMaxWaves; }
+constexpr int mix_bwd_max_waves(int n) { return n == 8 ? 8 : kMixMaxWaves; }
 
 //
 // POST: dh_i = sum_c dY_i[c] drop(Z)[c] goes the way of dP, and dZ = drop(sum_i h_i dY_i) is
 // written beside dX.
 template <int DX, int N, bool POST>
-__global__ __launch_bounds__(64 * mix_bwd_max_waves(N, POST)) void mix_bwd_kernel(const float* __restrict__ P,
+__global__ __launch_bounds__(64 * mix_bwd_max_waves(N)) void mix_bwd_kernel(const float* __restrict__ P,
                                                                            const v4u* __restrict__ X,
                                                                            const v4u* __restrict__ dY,
                                                                            v4u* __restrict__ dX, void* __restrict__ dH,
                                                                            int64_t B, int64_t nc, int win, bool h16,
                                                                            Write<POST> wr, WriteBack<POST> wb) {
     constexpr int NN = N * N;
-    __shared__ float part[mix_bwd_max_waves(N, POST) * NN];  // [wave][entry]
-    __shared__ float part_h[POST ? mix_bwd_max_waves(N, POST) * N : 1];
+    __shared__ float part[mix_bwd_max_waves(N) * NN];  // [wave][entry]
+    __shared__ float part_h[POST ? mix_bwd_max_waves(N) * N : 1];
     const unsigned lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int W = blockDim.x >> 6;
@@ -1379,17 +1384,25 @@ __global__ __launch_bounds__(64 * mix_bwd_max_waves(N, POST)) void mix_bwd_kerne
             // dP first: X's registers are then free for dX (three waves per SIMD with n = 8)
             add_outer<DX, N>(x, g, acc);
             __builtin_amdgcn_sched_barrier(0);
+            float hs[N];
+            v4u keep = {~0u, ~0u, ~0u, ~0u};
             if constexpr (POST) {
-                v4u keep = {~0u, ~0u, ~0u, ~0u};
+                // opaque: dP is summed before the generator's branch and dh right after it; moved to where
+                // they are used they would keep X (bf16, n = 4: 147 registers and one block of eight
+                // waves a CU, with them here 117 and two; 2^15 tokens of 4 x 4096 692 -> 604 us with dropout,
+                // 657 -> 600 without)
+#pragma unroll
+                for (int q = 0; q < NN; ++q) asm volatile("" : "+v"(acc[q]));
                 if (wr.least) keep = keep_mask<DX>(wr, nc * t + col + lane);
                 add_inner<DX, N>(z & keep, g, hacc);
-                float hs[N];
-                load_gates<N>(wr, t, hs);
-                const v4u dz = combine_chunk<DX, N>(hs, g) & keep;
-                if (own) __builtin_nontemporal_store(dz, wb.dZ + (nc * t + col) + lane);
+#pragma unroll
+                for (int q = 0; q < N; ++q) asm volatile("" : "+v"(hacc[q]));
+                load_gates<N, true>(wr, t, hs);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            mix_chunk<DX, N, true>(p, g, o);
+            mix_chunk<DX, N, true, POST>(p, g, o, hs, &z);
             if (own) {
+                if constexpr (POST) __builtin_nontemporal_store(z & keep, wb.dZ + (nc * t + col) + lane);
 #pragma unroll
                 for (int j = 0; j < N; ++j) __builtin_nontemporal_store(o[j], dX + (off + j * nr) + lane);
             }
@@ -1470,10 +1483,10 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_fwd_short_kernel(const
         float p[N * N], hs[N];
         load_lane_matrix<N>(P, t, p);
         if constexpr (POST) {
-            load_gates<N>(wr, t, hs);
+            load_gates<N, false>(wr, t, hs);
             if (wr.least) z &= keep_mask<DX>(wr, nc * t + c);
         }
-        mix_chunk<DX, N, false, POST>(p, x, y, hs, z);
+        mix_chunk<DX, N, false, POST>(p, x, y, hs, &z);
 #pragma unroll
         for (int j = 0; j < N; ++j) __builtin_nontemporal_store(y[j], Y + off + j * nc);
     }
@@ -1507,13 +1520,30 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const
         float p[NN], acc[NN];
 #pragma unroll
         for (int q = 0; q < NN; ++q) p[q] = acc[q] = 0.f;
+        if constexpr (POST) {  // first, and here (as in mix_bwd_kernel): X's registers are then free
+            add_outer<DX, N>(x, g, acc);
+#pragma unroll
+            for (int q = 0; q < NN; ++q) asm volatile("" : "+v"(acc[q]));
+        }
         if (valid) load_lane_matrix<N>(P, t, p);
-        mix_chunk<DX, N, true>(p, g, o);
+        v4u keep = {~0u, ~0u, ~0u, ~0u};
+        float hacc[N], hs[N];
+        if constexpr (POST) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) hacc[i] = hs[i] = 0.f;
+            if (wr.least) keep = keep_mask<DX>(wr, nc * t + c);
+            add_inner<DX, N>(z & keep, g, hacc);
+#pragma unroll
+            for (int q = 0; q < N; ++q) asm volatile("" : "+v"(hacc[q]));
+            if (valid) load_gates<N, false>(wr, t, hs);
+        }
+        mix_chunk<DX, N, true, POST>(p, g, o, hs, &z);
         if (own) {
+            if constexpr (POST) __builtin_nontemporal_store(z & keep, wb.dZ + nc * t + c);
 #pragma unroll
             for (int j = 0; j < N; ++j) __builtin_nontemporal_store(o[j], dX + off + j * nc);
         }
-        add_outer<DX, N>(x, g, acc);
+        if constexpr (!POST) add_outer<DX, N>(x, g, acc);
         // the sum over the token's L lanes, in all of them
         auto total = [&](float v) {
             float s = gsum_lanes<8>(v);
@@ -1526,15 +1556,7 @@ __global__ __launch_bounds__(mix_short_block(L)) void mix_bwd_short_kernel(const
             return s;
         };
         if constexpr (POST) {
-            v4u keep = {~0u, ~0u, ~0u, ~0u};
-            if (wr.least) keep = keep_mask<DX>(wr, nc * t + c);
-            float hacc[N], hs[N], mine = 0.f;
-#pragma unroll
-            for (int i = 0; i < N; ++i) hacc[i] = hs[i] = 0.f;
-            add_inner<DX, N>(z & keep, g, hacc);
-            if (valid) load_gates<N>(wr, t, hs);
-            const v4u dz = combine_chunk<DX, N>(hs, g) & keep;
-            if (own) __builtin_nontemporal_store(dz, wb.dZ + nc * t + c);
+            float mine = 0.f;
 #pragma unroll
             for (int i = 0; i < N; ++i) {
                 const float s = total(hacc[i]);
@@ -2785,7 +2807,7 @@ __global__ __launch_bounds__(64) void mix_small_kernel(const void* __restrict__ 
     float hs[N];
     if constexpr (POST) {
         if (own) z = __builtin_nontemporal_load(wr.Z + (nc * t + col) + lane);
-        load_gates<N>(wr, t, hs);
+        load_gates<N, true>(wr, t, hs);
         if (wr.least) z &= keep_mask<DX>(wr, nc * t + col + lane);
     }
     float p[N * N];  // row i from lane i, uniform
@@ -2805,7 +2827,7 @@ __global__ __launch_bounds__(64) void mix_small_kernel(const void* __restrict__ 
         if (col == 0 && lane < 8) store_group8<1, WRITE_DUAL, WRITE_ITERS, false>(P, dual, iters, t, q, r, ma, 1.f);
         gather(r.T[0]);
     }
-    mix_chunk<DX, N, false, POST>(p, x, y, hs, z);
+    mix_chunk<DX, N, false, POST>(p, x, y, hs, &z);
     if (own) {
 #pragma unroll
         for (int j = 0; j < N; ++j) __builtin_nontemporal_store(y[j], Y + (off + j * nc) + lane);
@@ -3770,12 +3792,12 @@ struct MixLaunch {
     int win;  // tokens in an XCD's window
 };
 
-MixLaunch mix_launch(int64_t B, int64_t nc, int n, bool backward, bool bf16, bool post) {
+MixLaunch mix_launch(int64_t B, int64_t nc, int n, bool backward, bool bf16) {
     const int64_t cols = nc > 0 ? (nc + 63) / 64 : 1;
     const bool wide8 = n == 8 && cols > 8, alone = B <= 256;  // alone: no second block on a CU
     int64_t most = n == 4 ? kMixMaxWaves : wide8 ? 4 : 8;
     if (backward && n == 4) {
-        const bool whole = !post && cols > 14 && cols <= kMixMaxWaves && (!bf16 || alone || (cols == 15 && B >= 8192));
+        const bool whole = cols > 14 && cols <= kMixMaxWaves && (!bf16 || alone || (cols == 15 && B >= 8192));
         most = whole ? kMixMaxWaves : 8;
     }
     if (backward && n == 8) {
@@ -3817,7 +3839,7 @@ int launch_mix_fwd(const float* P, const void* X, void* Y, int64_t B, int64_t nc
                       static_cast<int>(nc), wr);
         return launch_status();
     }
-    const MixLaunch l = mix_launch(B, nc, N, false, DX == BIRKHOFF4_BF16, POST);
+    const MixLaunch l = mix_launch(B, nc, N, false, DX == BIRKHOFF4_BF16);
     launch_kernel((mix_fwd_kernel<DX, N, POST>), l.grid, l.block, 0, stream, P, x, y, B, nc, l.win, wr);
     return launch_status();
 }
@@ -3870,7 +3892,7 @@ int launch_mix_bwd(const float* P, const void* X, const void* dY, void* dX, void
                       static_cast<int>(nc), h16, wr, wb);
         return launch_status();
     }
-    const MixLaunch l = mix_launch(B, nc, N, true, DX == BIRKHOFF4_BF16, POST);
+    const MixLaunch l = mix_launch(B, nc, N, true, DX == BIRKHOFF4_BF16);
     launch_kernel((mix_bwd_kernel<DX, N, POST>), l.grid, l.block, 0, stream, P, x, dy, dx, dH, B, nc, l.win, h16, wr, wb);
     return launch_status();
 }
