@@ -65,75 +65,146 @@ __device__ __forceinline__ float row_scale(const float* __restrict__ alpha, int 
 // ---------------------------------------------------------------------------
 // Forward: the products W v and |v|^2 of every token
 // ---------------------------------------------------------------------------
-// A block takes 16 TT tokens and a share of the row, in steps of 64 bytes; its waves take the
-// steps in pairs (a 128-byte line of each token) in turn. Tokens are the columns of the tile, rows
-// of W its rows, both loaded straight into the operands' layout; |v|^2 is the diagonal of the
-// product of the tokens' operand with itself (fp32: plain sums, as the fp32 matrix rate is nearer
-// to what HBM delivers). The waves' sums are added in LDS in wave order, the shares' by the
-// reader: no atomics, so a token's result does not depend on timing.
+// Blocks take some tokens and a share of the row, in steps of 64 bytes, two steps (a 128-byte line of
+// each token) at a time. Tokens are the columns of the products' tiles, rows of W the rows; |v|^2 is
+// the diagonal of the product of the tokens' operand with itself (fp32: plain sums, as the fp32
+// matrix rate is nearer to what HBM delivers). A wave loads whole lines, eight lanes a row, and takes
+// them to the operands' layout (a lane row's chunk) through LDS of its own while the next are on
+// the way: loaded in that layout, sixteen rows of 64 bytes at a time, 32 K tokens of 4 x 4096 bf16 took
+// 225 us instead of 195. The shares' sums are added by the reader, in order: no atomics, so a
+// token's result does not depend on timing.
+template <int DX, int N, int TT>
+struct GateSums {  // of a wave's 16 TT tokens: lane (g, c) has rows 16 r + 4 g .. + 3 of token 16 t + c
+    static constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows;
+    v4f acc[TT][RT], norm[TT];
+    float ss[TT];
+
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            norm[t] = v4f{0.f, 0.f, 0.f, 0.f};
+            ss[t] = 0.f;
+#pragma unroll
+            for (int r = 0; r < RT; ++r) acc[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // One step: chunk g of row 16 r + c of W, and of token 16 t + c.
+    __device__ __forceinline__ void step(const v4u (&wv)[RT], const v4u (&xv)[TT]) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) acc[t][r] = mfma_chunks<DX>(wv[r], xv[t], acc[t][r]);
+            if constexpr (DX == BIRKHOFF4_BF16) {
+                norm[t] = mfma_bf16(xv[t], xv[t], norm[t]);
+            } else {
+#pragma unroll
+                for (int m = 0; m < 4; ++m) {
+                    const float v = __uint_as_float(xv[t][m]);
+                    ss[t] = __builtin_fmaf(v, v, ss[t]);
+                }
+            }
+        }
+    }
+
+    // After the last step: token 16 t + c's |v|^2 is the diagonal's value in lane group c / 4.
+    __device__ __forceinline__ void finish(int c) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+            float sum;
+            if constexpr (DX == BIRKHOFF4_BF16) {
+                sum = (c & 3) == 0 ? norm[t].x : (c & 3) == 1 ? norm[t].y : (c & 3) == 2 ? norm[t].z : norm[t].w;
+            } else {
+                sum = ss[t];
+                sum += __shfl_xor(sum, 16);
+                sum += __shfl_xor(sum, 32);
+            }
+            norm[t] = v4f{sum, 0.f, 0.f, 0.f};
+        }
+    }
+
+    // This lane's quads of the tokens' rows of sums: f(token, quad, value).
+    template <typename F>
+    __device__ __forceinline__ void each(int g, int c, F&& f) {
+#pragma unroll
+        for (int t = 0; t < TT; ++t) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+                if (16 * r + 4 * g < R) f(16 * t + c, 4 * r + g, acc[t][r]);
+            if (g == c >> 2) f(16 * t + c, Gates<N>::stride / 4 - 1, norm[t]);
+        }
+    }
+};
+
+// Offsets of the rows that a lane loads, eight rows at a time, from the wave's first token; past the
+// last token: that token again, its sums not stored.
+template <int TT>
+__device__ __forceinline__ void line_offsets(uint32_t (&off)[2 * TT], int lane, int64_t row_bytes, int64_t last) {
+#pragma unroll
+    for (int t = 0; t < 2 * TT; ++t) {
+        const int64_t row = 8 * t + (lane >> 3);
+        off[t] = static_cast<uint32_t>(row_bytes * (row < last ? row : last)) + 16 * (lane & 7);
+    }
+}
+
+// The lane's chunks of the lines at p: of both steps, or, with the row's end between them, of the first.
+template <int TT>
+__device__ __forceinline__ void load_lines(v4u (&xr)[2 * TT], const char* p, const uint32_t (&off)[2 * TT], bool two,
+                                           int lane) {
+    const bool mine = two || (lane & 7) < 4;
+#pragma unroll
+    for (int t = 0; t < 2 * TT; ++t) {
+        xr[t] = v4u{0u, 0u, 0u, 0u};
+        if (mine) xr[t] = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p + off[t]));
+    }
+}
+
+// A block's GW waves share its 16 TT tokens and take the lines of its share of the row in turn; their
+// sums are added in LDS, the upper half of the waves to the lower.
 template <int DX, int N, int TT, int GW>
 __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(const v4u* __restrict__ X,
                                                                       const v4u* __restrict__ W,
                                                                       float* __restrict__ part, int64_t B, int64_t steps,
                                                                       int64_t per) {
     constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4;
-    // a wave's rows on their way into the operands' layout: 128 bytes and 16 that keep the lanes that
-    // read one chunk of sixteen rows on different banks
+    // 128 bytes of a row and 16 that keep the lanes that read one chunk of sixteen rows on different banks
     __shared__ union {
         v4u rows[GW][16 * TT][9];
         v4f red[GW / 2][16 * TT][S4];
     } lds;
-    auto& rows = lds.rows;
-    auto& red = lds.red;
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int64_t first = static_cast<int64_t>(blockIdx.x) * 16 * TT;
     const int64_t s0 = blockIdx.y * per, s1 = s0 + per < steps ? s0 + per : steps;
-    const int64_t row_bytes = 64 * steps;
-    const char* base = reinterpret_cast<const char*>(X) + row_bytes * first;
-    uint32_t off[2 * TT];  // of the rows that the lane loads: eight lanes a row, eight rows at a time
-    const v4u* wr[RT];
-#pragma unroll
-    for (int t = 0; t < 2 * TT; ++t) {  // past the last token: that token again, its sums not stored
-        const int64_t row = 8 * t + (lane >> 3), last = B - 1 - first;
-        off[t] = static_cast<uint32_t>(row_bytes * (row < last ? row : last)) + 16 * (lane & 7);
-    }
+    const char* base = reinterpret_cast<const char*>(X) + 64 * steps * first;
+    uint32_t off[2 * TT];
+    line_offsets<TT>(off, lane, 64 * steps, B - 1 - first);
+    const v4u* wr[RT];  // past the last row: that row, its sums not stored
 #pragma unroll
     for (int r = 0; r < RT; ++r) wr[r] = W + 4 * steps * (16 * r + c < R ? 16 * r + c : R - 1) + g;
-    v4f acc[TT][RT], gram[TT];
-    float ss[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        gram[t] = v4f{0.f, 0.f, 0.f, 0.f};
-        ss[t] = 0.f;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) acc[t][r] = v4f{0.f, 0.f, 0.f, 0.f};
-    }
+    GateSums<DX, N, TT> sums;
+    sums.clear();
+    // blocks begin at different places of the row: begun together, 249 us instead of 235 at 32 K tokens of 4 x 4096
     const int64_t turns = (s1 - s0 + 2 * GW - 1) / (2 * GW);
     int64_t turn = (blockIdx.x >> 3) % turns, next = s0 + 2 * GW * turn + 2 * w;
     v4u xr[2 * TT];
-    auto load_x = [&](int64_t s) {
-        const char* p = base + 64 * s;
-        if (s + 1 < s1) {  // uniform
-#pragma unroll
-            for (int t = 0; t < 2 * TT; ++t) xr[t] = __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p + off[t]));
+    auto load = [&](int64_t s) {
+        if (s < s1) {  // uniform
+            load_lines<TT>(xr, base + 64 * s, off, s + 1 < s1, lane);
         } else {
 #pragma unroll
-            for (int t = 0; t < 2 * TT; ++t) {
-                xr[t] = v4u{0u, 0u, 0u, 0u};
-                if (s < s1 && (lane & 7) < 4) xr[t] = *reinterpret_cast<const v4u*>(p + off[t]);
-            }
+            for (int t = 0; t < 2 * TT; ++t) xr[t] = v4u{0u, 0u, 0u, 0u};
         }
     };
-    load_x(next);
+    load(next);
     for (int64_t k = 0; k < turns; ++k) {
         const int64_t s = next;
-        v4u xv[2][TT], wv[2][RT];
 #pragma unroll
-        for (int t = 0; t < 2 * TT; ++t) rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
+        for (int t = 0; t < 2 * TT; ++t) lds.rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
         turn = turn + 1 < turns ? turn + 1 : 0;
         next = s0 + 2 * GW * turn + 2 * w;
-        if (k + 1 < turns) load_x(next);
+        if (k + 1 < turns) load(next);
+        v4u xv[2][TT], wv[2][RT];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -143,53 +214,17 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
                 for (int r = 0; r < RT; ++r) wv[u][r] = wr[r][4 * (s + u)];
             }
 #pragma unroll
-            for (int t = 0; t < TT; ++t) xv[u][t] = rows[w][16 * t + c][4 * u + g];
+            for (int t = 0; t < TT; ++t) xv[u][t] = lds.rows[w][16 * t + c][4 * u + g];
         }
 #pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int t = 0; t < TT; ++t) {
-#pragma unroll
-                for (int r = 0; r < RT; ++r) acc[t][r] = mfma_chunks<DX>(wv[u][r], xv[u][t], acc[t][r]);
-                if constexpr (DX == BIRKHOFF4_BF16) {
-                    gram[t] = mfma_bf16(xv[u][t], xv[u][t], gram[t]);
-                } else {
-#pragma unroll
-                    for (int m = 0; m < 4; ++m) {
-                        const float v = __uint_as_float(xv[u][t][m]);
-                        ss[t] = __builtin_fmaf(v, v, ss[t]);
-                    }
-                }
-            }
+        for (int u = 0; u < 2; ++u) sums.step(wv[u], xv[u]);
     }
-    // lane (g, c) holds rows 16 r + 4 g .. + 3 of token 16 t + c, and a lane group each token's |v|^2
-    v4f norm[TT];
-#pragma unroll
-    for (int t = 0; t < TT; ++t) {
-        float sum;
-        if constexpr (DX == BIRKHOFF4_BF16) {
-            sum = (c & 3) == 0 ? gram[t].x : (c & 3) == 1 ? gram[t].y : (c & 3) == 2 ? gram[t].z : gram[t].w;
-        } else {
-            sum = ss[t];
-            sum += __shfl_xor(sum, 16);
-            sum += __shfl_xor(sum, 32);
-        }
-        norm[t] = v4f{sum, 0.f, 0.f, 0.f};
-    }
-    auto each = [&](auto&& f) {  // this lane's quads: f(token of the block, quad of the token, value)
-#pragma unroll
-        for (int t = 0; t < TT; ++t) {
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-                if (16 * r + 4 * g < R) f(16 * t + c, 4 * r + g, acc[t][r]);
-            if (g == c >> 2) f(16 * t + c, S4 - 1, norm[t]);
-        }
-    };
-    auto put = [&](int k) { each([&](int t, int q, v4f& v) { red[k][t][q] = v; }); };
-    auto add = [&](int k) { each([&](int t, int q, v4f& v) { v += red[k][t][q]; }); };
+    sums.finish(c);
+    auto put = [&](int k) { sums.each(g, c, [&](int t, int q, v4f& v) { lds.red[k][t][q] = v; }); };
+    auto add = [&](int k) { sums.each(g, c, [&](int t, int q, v4f& v) { v += lds.red[k][t][q]; }); };
     __syncthreads();
 #pragma unroll
-    for (int half = GW / 2; half >= 1; half /= 2) {  // the upper half of the waves to the lower
+    for (int half = GW / 2; half >= 1; half /= 2) {
         if (w >= half && w < 2 * half) put(w - half);
         __syncthreads();
         if (w < half) add(w);
@@ -197,10 +232,83 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
     }
     if (w == 0) {
         v4f* dst = reinterpret_cast<v4f*>(part) + (blockIdx.y * B + first) * S4;
-        each([&](int t, int q, v4f& v) {
+        sums.each(g, c, [&](int t, int q, v4f& v) {
             if (first + t < B) dst[t * S4 + q] = v;
         });
     }
+}
+
+// Many tokens: a block's waves have 64 tokens each and go along the row together, so that a line of
+// W is brought to LDS once for all of them. With n = 4 from 20 K tokens on, eight waves: 32 K tokens of
+// 4 x 4096 bf16 forward 443 -> 418 us (8 K tokens 105 and 108, 16 K about 220 and 233); with n = 8,
+// whose W is as much as the streams of 80 tokens, from 2 K on, four: 8000 tokens of 8 x 1024 fp32 223 ->
+// 176.
+template <int N>
+constexpr int gate_wide_waves() { return N == 4 ? 8 : 4; }
+
+template <int DX, int N>
+__global__ __launch_bounds__((64 * gate_wide_waves<N>()), 2) void pre_gate_wide_kernel(const v4u* __restrict__ X,
+                                                                                       const v4u* __restrict__ W,
+                                                                                       float* __restrict__ part,
+                                                                                       int64_t B, int64_t steps,
+                                                                                       int64_t per) {
+    constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4, TT = 4, GW = gate_wide_waves<N>();
+    constexpr int kThreads = 64 * GW, WQ = (8 * R + kThreads - 1) / kThreads;
+    __shared__ v4u rows[GW][16 * TT][9];
+    __shared__ v4u wrow[2][R][9];
+    const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
+    const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
+    const int64_t first = (static_cast<int64_t>(blockIdx.x) * GW + w) * 16 * TT;
+    const int64_t s0 = blockIdx.y * per, s1 = s0 + per < steps ? s0 + per : steps;
+    const int64_t start = first < B ? first : B - 1;  // a wave without tokens goes along on the last one's values
+    const char* base = reinterpret_cast<const char*>(X) + 64 * steps * start;
+    uint32_t off[2 * TT];
+    line_offsets<TT>(off, lane, 64 * steps, B - 1 - start);
+    GateSums<DX, N, TT> sums;
+    sums.clear();
+    const int64_t turns = (s1 - s0 + 1) / 2;
+    int64_t turn = (blockIdx.x >> 3) % turns;
+    v4u xr[2 * TT], wq[WQ];
+    auto load = [&](int64_t s) {
+        const bool two = s + 1 < s1;  // uniform
+        load_lines<TT>(xr, base + 64 * s, off, two, lane);
+#pragma unroll
+        for (int q = 0; q < WQ; ++q) {
+            const int k = static_cast<int>(threadIdx.x) + kThreads * q;
+            wq[q] = v4u{0u, 0u, 0u, 0u};
+            if (k < 8 * R && (two || (k & 7) < 4)) wq[q] = W[4 * (steps * (k >> 3) + s) + (k & 7)];
+        }
+    };
+    load(s0 + 2 * turn);
+    for (int64_t k = 0; k < turns; ++k) {
+        const int buf = static_cast<int>(k & 1);
+#pragma unroll
+        for (int t = 0; t < 2 * TT; ++t) rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
+#pragma unroll
+        for (int q = 0; q < WQ; ++q) {
+            const int e = static_cast<int>(threadIdx.x) + kThreads * q;
+            if (e < 8 * R) wrow[buf][e >> 3][e & 7] = wq[q];
+        }
+        // this line of W is there, and everybody has read the one that the next turn overwrites
+        __syncthreads();
+        turn = turn + 1 < turns ? turn + 1 : 0;
+        if (k + 1 < turns) load(s0 + 2 * turn);
+        v4u xv[2][TT], wv[2][RT];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+#pragma unroll
+            for (int r = 0; r < RT; ++r) wv[u][r] = wrow[buf][16 * r + c < R ? 16 * r + c : R - 1][4 * u + g];
+#pragma unroll
+            for (int t = 0; t < TT; ++t) xv[u][t] = rows[w][16 * t + c][4 * u + g];
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) sums.step(wv[u], xv[u]);
+    }
+    sums.finish(c);
+    v4f* dst = reinterpret_cast<v4f*>(part) + (blockIdx.y * B + first) * S4;
+    sums.each(g, c, [&](int t, int q, v4f& v) {
+        if (first + t < B) dst[t * S4 + q] = v;
+    });
 }
 
 // ---------------------------------------------------------------------------
@@ -897,6 +1005,7 @@ struct PreShape {
 };
 
 struct GateLaunch {
+    bool wide;                   // pre_gate_wide_kernel
     int tt, waves;               // 16-token tiles and waves of a block
     int64_t tiles, splits, per;  // blocks over tokens, shares of the row, steps per share
 };
@@ -919,10 +1028,17 @@ constexpr int gate_waves(int tiles) { return tiles == 1 ? 16 : tiles == 2 ? (N =
 
 GateLaunch gate_launch(const PreShape& s, int n) {
     GateLaunch l;
+    l.wide = s.B > (n == 4 ? 20480 : 2048);
     l.tt = s.B <= 16 ? 1 : s.B <= (n == 4 ? 512 : 64) ? 2 : 4;
     l.waves = n == 4 ? gate_waves<4>(l.tt) : gate_waves<8>(l.tt);
+    int64_t lines = l.waves;  // at least, of a share
+    if (l.wide) {
+        l.waves = n == 4 ? gate_wide_waves<4>() : gate_wide_waves<8>();
+        l.tt *= l.waves;
+        lines = 4;
+    }
     l.tiles = cdiv(s.B, 16 * l.tt);
-    const int64_t most = cdiv(s.steps, 2 * l.waves), cap = l.tiles <= 4 ? 32 : 16;
+    const int64_t most = cdiv(s.steps, 2 * lines), cap = l.tiles <= 4 ? 32 : 16;
     int64_t want = cdiv(kGateWant, l.waves * l.tiles);
     if (want > most) want = most;
     if (want > cap) want = cap;
@@ -992,7 +1108,8 @@ int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float*
                    void* U, float* h, float* H, float* q, float* rms, float* part, hipStream_t stream) {
     const GateLaunch l = gate_launch(s, N);
     const v4u *x = static_cast<const v4u*>(X), *w = static_cast<const v4u*>(W);
-    auto gate = l.tt == 1   ? pre_gate_kernel<DX, N, 1, gate_waves<N>(1)>
+    auto gate = l.wide      ? pre_gate_wide_kernel<DX, N>
+                : l.tt == 1 ? pre_gate_kernel<DX, N, 1, gate_waves<N>(1)>
                 : l.tt == 2 ? pre_gate_kernel<DX, N, 2, gate_waves<N>(2)> : pre_gate_kernel<DX, N, 4, gate_waves<N>(4)>;
     launch_kernel(gate, dim3(static_cast<unsigned>(l.tiles), static_cast<unsigned>(l.splits)), dim3(64 * l.waves), 0,
                   stream, x, w, part, s.B, s.steps, l.per);

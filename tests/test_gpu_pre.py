@@ -57,6 +57,15 @@ def test_many_tokens(n, dtype):
     check(*inputs(n, 20011, 64, dtype, 7), 1e-6, f"n={n} many tokens {dtype}")
 
 
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n,B,C", [(4, 20481, 72), (4, 21000, 40), (8, 2049, 72), (8, 2500, 264), (8, 2304, 8)])
+def test_blocks_of_many_tokens(n, B, C, dtype):
+    """Waves with 64 tokens each that share W's lines: rows of odd numbers of 64-byte steps, blocks
+    whose last waves have no tokens, shares of the row."""
+    C = C if dtype == BF16 else C // 2
+    check(*inputs(n, B, C, dtype, 43), 1e-6, f"n={n} B={B} C={C} {dtype}")
+
+
 @pytest.mark.parametrize("scale,eps", [(1e-4, 1e-6), (1e-4, 0.0), (300.0, 1e-6), (1.0, 0.5)])
 def test_scales(scale, eps):
     check(*inputs(4, 50, 256, F32, 3, scale), eps, f"scale {scale}, eps {eps}")
