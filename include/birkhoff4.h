@@ -303,7 +303,7 @@ int birkhoff8_mix_bwd_ex(const float* P, const void* X, const void* dY, int x_dt
  * q, rms [B][N], [B] fp32 outputs: q and r, which the backward needs.
  * work   workspace of work_bytes >= birkhoff4_pre_work(B, C, x_dtype, 0) bytes, in use until the
  *        call's work on `stream` has ended; its contents before and after mean nothing.
- * C      > 0, a multiple of 8 for BF16 or 4 for F32, at most 2^22 (BIRKHOFF4_ERR_CHANNELS, _SIZE);
+ * C      > 0, a multiple of 8 for BF16 or 4 for F32, at most 2^20 (BIRKHOFF4_ERR_CHANNELS, _SIZE);
  *        B at most 2^26.
  * A token with a NaN or infinite value has NaN (or infinite) outputs; the others are not touched
  * by it. The result does not depend on timing: no atomics, fixed orders of sums. */

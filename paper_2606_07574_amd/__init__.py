@@ -552,6 +552,13 @@ def _graph(*inputs: torch.Tensor) -> bool:
     return torch.is_grad_enabled() and any(t.requires_grad for t in inputs)
 
 
+def _whole(t: torch.Tensor) -> torch.Tensor:
+    """t, or a copy where it is strided or begins off the 16 bytes that the kernels count on (a
+    parameter that is a piece of a flat buffer)."""
+    t = t.contiguous()
+    return t.clone() if t.data_ptr() % 16 else t
+
+
 def _dense(t: torch.Tensor, name: str, shape, dtype: torch.dtype, like: torch.Tensor) -> None:
     if t.dtype == dtype and t.device == like.device and t.shape == shape and t.is_contiguous() and t.is_cuda:
         return
@@ -626,14 +633,14 @@ class PreFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, X, W, alpha, bias, eps=DEFAULT_EPS):
         ctx.set_materialize_grads(False)
-        Xc, W, alpha, bias = X.contiguous(), W.contiguous(), alpha.contiguous(), bias.contiguous()
+        Xc, W, alpha, bias = _whole(X), _whole(W), _whole(alpha), _whole(bias)
         U, h, H, q, rms = pre_fwd(Xc, W, alpha, bias, eps)
         ctx.save_for_backward(Xc, W, alpha, bias, q, rms)
         return U, h, H, Xc.view_as(Xc)
 
     @staticmethod
     def backward(ctx, dU, dh, dH, dX):
-        grads = [None if g is None else g.contiguous() for g in (dU, dh, dH, dX)]
+        grads = [None if g is None else _whole(g) for g in (dU, dh, dH, dX)]
         return (*pre_bwd(*ctx.saved_tensors, *grads), None)
 
 
@@ -642,8 +649,8 @@ def pre(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tenso
     given; give it to what uses the streams next, and their gradient costs no pass of its own."""
     if _graph(X, W, alpha, bias):
         return PreFn.apply(X, W, alpha, bias, eps)
-    X = X.contiguous()
-    return (*pre_fwd(X, W.contiguous(), alpha.contiguous(), bias.contiguous(), eps)[:3], X)
+    X = _whole(X)
+    return (*pre_fwd(X, _whole(W), _whole(alpha), _whole(bias), eps)[:3], X)
 
 
 def _written(lead, n: int, C: int, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: float,
@@ -723,8 +730,8 @@ class PostFn(torch.autograd.Function):
 
     @staticmethod
     def forward(ctx, H, X, h, Z, p=0.0, rng=None, tol=DEFAULT_TOL, max_iter=DEFAULT_MAX_ITER):
-        X, h, Z = X.contiguous(), h.contiguous(), Z.contiguous()
-        Y, P, _, _ = post_fwd(H.contiguous(), X, h, Z, p, rng, tol, max_iter)
+        X, h, Z = _whole(X), _whole(h), _whole(Z)
+        Y, P, _, _ = post_fwd(_whole(H), X, h, Z, p, rng, tol, max_iter)
         # rng is saved too: changed in place before the backward, it raises there
         ctx.save_for_backward(P, X, h, Z, rng)
         ctx.p, ctx.h_dtype = p, H.dtype
@@ -733,7 +740,7 @@ class PostFn(torch.autograd.Function):
     @staticmethod
     def backward(ctx, dY):
         P, X, h, Z, rng = ctx.saved_tensors
-        dX, dH, dh, dZ = _post_bwd(P, X, h, Z, dY.contiguous(), ctx.p, rng, ctx.h_dtype)
+        dX, dH, dh, dZ = _post_bwd(P, X, h, Z, _whole(dY), ctx.p, rng, ctx.h_dtype)
         return dH, dX, dh, dZ, None, None, None, None
 
 
@@ -742,7 +749,7 @@ def post(H: torch.Tensor, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: 
     """post_fwd under autograd: Y alone, with gradients for H, X, h and Z."""
     if _graph(H, X, h, Z):
         return PostFn.apply(H, X, h, Z, p, rng, tol, max_iter)
-    return post_fwd(H.contiguous(), X.contiguous(), h.contiguous(), Z.contiguous(), p, rng, tol, max_iter)[0]
+    return post_fwd(_whole(H), _whole(X), _whole(h), _whole(Z), p, rng, tol, max_iter)[0]
 
 
 def connect(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, branch, p: float = 0.0,

@@ -422,7 +422,8 @@ __global__ __launch_bounds__(64 * kReadWaves) void pre_read_kernel(const float* 
 // Tokens are padded to whole stages of 32 (Bp), whose G, h^pre and s are zero, for the products
 // below. `share` waves of the block take four consecutive tokens, one after the other, sharing
 // their columns; the first of these waves forms G. A block leaves one row of sums for dbias and
-// dalpha.
+// dalpha. Bound: HBM; many short blocks that cover whole tokens stream best (2^15 tokens of 4 x 4096
+// bf16 212 us, 6.3 TB/s; a resident grid that loops 254, a wave per token 236).
 constexpr int kTokenStep = 32;  // tokens of a stage of the products over tokens
 constexpr int kHalf = 16;
 constexpr int kDotWaves = 8;
@@ -529,8 +530,7 @@ template <int DX, int N>
 __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
     const v4u* __restrict__ X, const v4u* __restrict__ dU, const float* __restrict__ Q, const float* __restrict__ rms,
     const float* __restrict__ alpha, const float* __restrict__ bias, const float* __restrict__ dh,
-    const float* __restrict__ dH, Stage<DX, N>* __restrict__ G,
-    float* __restrict__ sums, int64_t B, int64_t Bp, int64_t nc, float inv_k, int share) {
+    const float* __restrict__ dH, Stage<DX, N>* __restrict__ G, float* __restrict__ sums, int64_t B, int64_t Bp, int64_t nc, float inv_k, int share) {
     constexpr int R = Gates<N>::rows, S = Gates<N>::stride, P = Stage<DX, N>::rows, J = (P + 63) / 64;
     __shared__ float dots[kDotWaves][N];
     __shared__ float total[kDotWaves][S];
@@ -625,9 +625,9 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 // ---------------------------------------------------------------------------
 // Backward: dX and partial sums of dW
 // ---------------------------------------------------------------------------
-// Wave w of a block takes stream w's channels CW chunk .. + CW, CE of them per lane (lane l: group
-// g = l / 16, channels CE (l % 16) .. + CE), over the stages of 32 tokens of its share, in halves of
-// 16 of which lane group g has tokens 4 g .. 4 g + 3. The same registers serve everything:
+// A wave takes CW channels of a stream, CE of them per lane (lane l: group g = l / 16, channels CE
+// (l % 16) .. + CE), over the stages of 32 tokens of its share, in halves of 16 of which lane group g
+// has tokens 4 g .. 4 g + 3. The same registers serve everything:
 //  * dW: tile of 16 rows of W (G transposed, tokens along k) times the tokens' values, one product
 //    per channel c of the lanes: column l % 16 is channel CE (l % 16) + c, and k runs over the
 //    stage's tokens as the lanes hold them, four of each half.
@@ -636,6 +636,12 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 // W and X are exact in bf16, sums are fp32. W's rows stay in LDS or registers throughout; a stage of
 // G is copied to LDS once for all waves of a block, a stage ahead, and a half's streams are loaded
 // while the other half is worked on.
+//
+// Bound: HBM, by the width of the rows' pieces. A copy (two arrays read, one written) by waves that
+// take 128, 256 or 512 bytes of each row reaches 5.0, 5.5 and 6.5 TB/s here, so a block's waves take
+// neighbouring pieces, 512 bytes together, of one or two streams: 2^15 tokens of 4 x 4096 bf16 648 -> 578 us
+// (6.1 TB/s), 2^13 of 8 x 4096 388 -> 350 (4.9 TB/s). Loading a whole stage ahead (n = 4 with
+// 128-byte pieces, 681 us) or leaving the offsets' arithmetic out of the loop (664) did not help.
 template <int DX, int N>
 struct Back {
     // n = 8: half as many channels, as the sums of 5 row tiles fill the registers
@@ -679,7 +685,7 @@ __device__ __forceinline__ float channel(const Words<WORDS>& r, int c) {
         return __uint_as_float(r.v[c]);
 }
 
-// bf16 channel c of eight (four) rows, in order.
+// bf16 channel c of two (eight) rows, in order.
 template <int WORDS>
 __device__ __forceinline__ uint32_t column_pair(const Words<WORDS>& a, const Words<WORDS>& b, int c) {
     // selector bytes 0..3: second operand, 4..7: first
@@ -706,11 +712,10 @@ struct BackPlan {
 };
 
 template <int DX, int N>
-__global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_kernel(const void* __restrict__ X, const void* __restrict__ W,
-                                                             const void* __restrict__ dU, const void* __restrict__ E,
-                                                             const Stage<DX, N>* __restrict__ G, void* __restrict__ dX,
-                                                             float* __restrict__ dWp, int64_t B, int64_t stages,
-                                                             int64_t C) {
+__global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_kernel(
+    const void* __restrict__ X, const void* __restrict__ W, const void* __restrict__ dU, const void* __restrict__ E,
+    const Stage<DX, N>* __restrict__ G, void* __restrict__ dX, float* __restrict__ dWp, int64_t B, int64_t stages,
+    int64_t C) {
     using St = Stage<DX, N>;
     constexpr bool H16 = St::H16;
     constexpr int R = St::R, RT = St::RT, KS = St::KS;
@@ -1072,7 +1077,9 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
     const int64_t steps = l.Bp / kTokenStep;
     int64_t shares = kBackWaves / (n * l.chunks);
     if (shares < 1) shares = 1;
-    l.token_shares = shares < steps ? shares : steps;
+    if (shares > steps) shares = steps;
+    // the fewest shares whose longest is no longer
+    l.token_shares = steps ? cdiv(steps, cdiv(steps, shares)) : 0;
     int64_t at = 0;
     auto take = [&](int64_t floats) {
         const int64_t was = at;

@@ -221,6 +221,24 @@ def test_strided_inputs():
         assert torch.equal(a, b)
 
 
+def test_flat_parameters():
+    """Parameters that are pieces of one flat buffer, off the kernels' 16 bytes, under autograd; the
+    calls without it refuse them."""
+    (X, W, alpha, bias), grads = grad_inputs(4, (20,), 64, F32, 45)
+    ref = torch.autograd.grad(b4.pre(X, W, alpha, bias), (X, W, alpha, bias), grads)
+    flat = torch.cat([t.detach().flatten() for t in (alpha, bias, W)]).requires_grad_()
+    a, b, w = flat[:3], flat[3:27], flat[27:].view(24, 256)
+    outs = b4.pre(X, w, a, b)
+    got = torch.autograd.grad(outs, (X, flat), grads)
+    assert torch.equal(got[0], ref[0])
+    assert torch.equal(got[1], torch.cat([ref[2], ref[3], ref[1].flatten()]))
+    with torch.no_grad():
+        for x, y in zip(b4.pre(X, w, a, b), outs):
+            assert torch.equal(x, y)
+        with pytest.raises(b4.Birkhoff4Error, match="aligned"):
+            b4.pre_fwd(X, W, a, b)
+
+
 @pytest.mark.parametrize("n", [4, 8])
 def test_differences(n):
     """The gradient against central differences of the forward along random directions, fp32. The
