@@ -959,9 +959,10 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
     }
 }
 
-// The shares' sums added in order: dW, and in the grid's last blocks dbias and dalpha, sixteen
-// entries a block.
+// The shares' sums added in a fixed order: dW, four threads to 16 bytes of the fp32 sums, and in the
+// grid's last blocks dbias and dalpha, sixteen entries a block.
 constexpr int kJoinBlock = 1024;
+constexpr int kJoinQuads = kJoinBlock / 4;
 
 template <int N, bool DW16>
 __global__ __launch_bounds__(kJoinBlock) void pre_join_kernel(const v4f* __restrict__ dWp, const float* __restrict__ sums,
@@ -970,14 +971,26 @@ __global__ __launch_bounds__(kJoinBlock) void pre_join_kernel(const v4f* __restr
                                                               int64_t rows, unsigned wblocks) {
     constexpr int R = Gates<N>::rows, S = Gates<N>::stride;
     if (blockIdx.x < wblocks) {
-        for (int64_t q = static_cast<int64_t>(blockIdx.x) * kJoinBlock + threadIdx.x; q < quads;
-             q += static_cast<int64_t>(wblocks) * kJoinBlock) {
+        __shared__ v4f quarter[3][kJoinQuads];
+        const int own = threadIdx.x % kJoinQuads, part = threadIdx.x / kJoinQuads;
+        for (int64_t base = static_cast<int64_t>(blockIdx.x) * kJoinQuads; base < quads;
+             base += static_cast<int64_t>(wblocks) * kJoinQuads) {  // uniform over the block
+            const int64_t q = base + own;
             v4f v = {0.f, 0.f, 0.f, 0.f};
-            for (int k = 0; k < shares; ++k) v += dWp[k * quads + q];
-            if constexpr (DW16)
-                static_cast<uint2*>(dW)[q] = uint2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
-            else
-                static_cast<v4f*>(dW)[q] = v;
+            if (q < quads) {
+#pragma unroll 4
+                for (int k = part; k < shares; k += 4) v += dWp[k * quads + q];
+            }
+            if (part > 0) quarter[part - 1][own] = v;
+            __syncthreads();
+            if (part == 0 && q < quads) {
+                v = (v + quarter[0][own]) + (quarter[1][own] + quarter[2][own]);
+                if constexpr (DW16)
+                    static_cast<uint2*>(dW)[q] = uint2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
+                else
+                    static_cast<v4f*>(dW)[q] = v;
+            }
+            __syncthreads();
         }
         return;
     }
@@ -986,7 +999,7 @@ __global__ __launch_bounds__(kJoinBlock) void pre_join_kernel(const v4f* __restr
     const int j = 16 * static_cast<int>(blockIdx.x - wblocks) + c;
     float v = 0.f;
     if (j < S)
-#pragma unroll 8
+#pragma unroll 16
         for (int64_t k = part; k < rows; k += kJoinBlock / 16) v += sums[k * S + j];
     red[part][c] = v;
     __syncthreads();
@@ -1148,7 +1161,7 @@ int launch_pre_bwd(const PreShape& s, const void* X, const void* W, const float*
     }
     // without tokens the sums are empty: zeros
     const int64_t quads = Gates<N>::rows * N * s.C / 4;
-    const int64_t want = cdiv(quads, kJoinBlock);
+    const int64_t want = cdiv(quads, kJoinQuads);
     const unsigned wblocks = static_cast<unsigned>(want < 4096 ? want : 4096);
     launch_kernel((pre_join_kernel<N, DX == BIRKHOFF4_BF16>), dim3(wblocks + (Gates<N>::stride + 15) / 16),
                   dim3(kJoinBlock), 0, stream, reinterpret_cast<const v4f*>(at(l.dw)), at(l.sums), dW, dalpha, dbias,
