@@ -29,6 +29,7 @@ import ctypes
 import os
 
 import torch
+from torch.autograd.function import once_differentiable
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libbirkhoff4.so")
@@ -639,6 +640,7 @@ class PreFn(torch.autograd.Function):
         return U, h, H, Xc.view_as(Xc)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dU, dh, dH, dX):
         grads = [None if g is None else _whole(g) for g in (dU, dh, dH, dX)]
         return (*pre_bwd(*ctx.saved_tensors, *grads), None)
@@ -646,7 +648,8 @@ class PreFn(torch.autograd.Function):
 
 def pre(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, eps: float = DEFAULT_EPS):
     """pre_fwd with gradients for X, W, alpha and bias: (U, h, H, X). The X returned is the X
-    given; give it to what uses the streams next, and their gradient costs no pass of its own."""
+    given; give it to what uses the streams next, and their gradient costs no pass of its own.
+    Like post, it has no second derivatives: a backward of its backward raises."""
     if _graph(X, W, alpha, bias):
         return PreFn.apply(X, W, alpha, bias, eps)
     X = _whole(X)
@@ -738,6 +741,7 @@ class PostFn(torch.autograd.Function):
         return Y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dY):
         P, X, h, Z, rng = ctx.saved_tensors
         dX, dH, dh, dZ = _post_bwd(P, X, h, Z, _whole(dY), ctx.p, rng, ctx.h_dtype)
@@ -746,7 +750,8 @@ class PostFn(torch.autograd.Function):
 
 def post(H: torch.Tensor, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: float = 0.0,
          rng: torch.Tensor | None = None, tol: float = DEFAULT_TOL, max_iter: int = DEFAULT_MAX_ITER) -> torch.Tensor:
-    """post_fwd under autograd: Y alone, with gradients for H, X, h and Z."""
+    """post_fwd under autograd: Y alone, with gradients for H, X, h and Z. The backward draws the
+    mask again from rng: give each call of a step its own, and change it after the backward."""
     if _graph(H, X, h, Z):
         return PostFn.apply(H, X, h, Z, p, rng, tol, max_iter)
     return post_fwd(_whole(H), _whole(X), _whole(h), _whole(Z), p, rng, tol, max_iter)[0]

@@ -327,3 +327,18 @@ def test_far_tokens(n):
     dX2 = b4.pre_bwd(X, W, alpha, bias, q, rms, dZ, dh, dH, dX)[0]
     (r, *_), (e, *_) = pre_back_ref(ref, n, dZ[cut], dh[cut], dH[cut], dX[cut])
     within(dX2[cut], r, e, "dX of pre")
+
+
+def test_no_second_derivatives():
+    """A gradient taken with create_graph is right, and its own derivative is refused, not taken as zero."""
+    g = torch.Generator(device="cuda").manual_seed(27)
+    X = torch.randn(5, 4, 64, device="cuda", generator=g, requires_grad=True)
+    W = torch.randn(24, 256, device="cuda", generator=g) / 16
+    alpha, bias = torch.ones(3, device="cuda"), torch.zeros(24, device="cuda")
+    U, h, H, Xs = b4.pre(X, W, alpha, bias)
+    for out in (U, b4.post(H.detach(), X, h.detach(), U.detach())):
+        once, = torch.autograd.grad(out.square().sum(), X, create_graph=True, retain_graph=True)
+        plain, = torch.autograd.grad(out.square().sum(), X, retain_graph=True)
+        assert torch.equal(once, plain)
+        with pytest.raises(RuntimeError, match="differentiable"):
+            once.square().sum().backward()
