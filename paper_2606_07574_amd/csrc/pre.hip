@@ -199,12 +199,8 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
     load(next);
     for (int64_t k = 0; k < turns; ++k) {
         const int64_t s = next;
-#pragma unroll
-        for (int t = 0; t < 2 * TT; ++t) lds.rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
-        turn = turn + 1 < turns ? turn + 1 : 0;
-        next = s0 + 2 * GW * turn + 2 * w;
-        if (k + 1 < turns) load(next);
         v4u xv[2][TT], wv[2][RT];
+        // W's lines before the next streams' (loads come back in order): a wait for them is for them alone
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
 #pragma unroll
@@ -213,9 +209,16 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
 #pragma unroll
                 for (int r = 0; r < RT; ++r) wv[u][r] = wr[r][4 * (s + u)];
             }
+        }
+#pragma unroll
+        for (int t = 0; t < 2 * TT; ++t) lds.rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
+        turn = turn + 1 < turns ? turn + 1 : 0;
+        next = s0 + 2 * GW * turn + 2 * w;
+        if (k + 1 < turns) load(next);
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
 #pragma unroll
             for (int t = 0; t < TT; ++t) xv[u][t] = lds.rows[w][16 * t + c][4 * u + g];
-        }
 #pragma unroll
         for (int u = 0; u < 2; ++u) sums.step(wv[u], xv[u]);
     }
