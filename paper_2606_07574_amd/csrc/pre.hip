@@ -159,13 +159,26 @@ __device__ __forceinline__ void load_lines(v4u (&xr)[2 * TT], const char* p, con
     }
 }
 
+// A block's tile of tokens and share of the row. Workgroups go to the eight XCDs in turn; each XCD
+// gets neighbouring pairs, tiles first, so that its L2 holds the part of W of its shares (forward of 8 K
+// tokens of 8 x 4096 bf16, 5.2 MB of W, 237 -> 204 us, of 32 K of 4 x 4096 414 -> 396).
+struct GatePlace {
+    int64_t tile;
+    int64_t share;
+};
+
+__device__ __forceinline__ GatePlace gate_place(uint32_t tiles, uint32_t per_xcd) {
+    const uint32_t k = (blockIdx.x & 7) * per_xcd + (blockIdx.x >> 3);
+    return {k % tiles, k / tiles};
+}
+
 // A block's GW waves share its 16 TT tokens and take the lines of its share of the row in turn; their
 // sums are added in LDS, the upper half of the waves to the lower.
 template <int DX, int N, int TT, int GW>
 __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(const v4u* __restrict__ X,
                                                                       const v4u* __restrict__ W,
                                                                       float* __restrict__ part, int64_t B, int64_t steps,
-                                                                      int64_t per) {
+                                                                      int64_t per, uint32_t tiles, uint32_t per_xcd) {
     constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4;
     // 128 bytes of a row and 16 that keep the lanes that read one chunk of sixteen rows on different banks
     __shared__ union {
@@ -174,8 +187,10 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
     } lds;
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const int64_t first = static_cast<int64_t>(blockIdx.x) * 16 * TT;
-    const int64_t s0 = blockIdx.y * per, s1 = s0 + per < steps ? s0 + per : steps;
+    const GatePlace at = gate_place(tiles, per_xcd);
+    const int64_t first = at.tile * 16 * TT;
+    const int64_t s0 = at.share * per, s1 = s0 + per < steps ? s0 + per : steps;
+    if (s0 >= s1) return;  // the whole block
     const char* base = reinterpret_cast<const char*>(X) + 64 * steps * first;
     uint32_t off[2 * TT];
     line_offsets<TT>(off, lane, 64 * steps, B - 1 - first);
@@ -234,7 +249,7 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
         __syncthreads();
     }
     if (w == 0) {
-        v4f* dst = reinterpret_cast<v4f*>(part) + (blockIdx.y * B + first) * S4;
+        v4f* dst = reinterpret_cast<v4f*>(part) + (at.share * B + first) * S4;
         sums.each(g, c, [&](int t, int q, v4f& v) {
             if (first + t < B) dst[t * S4 + q] = v;
         });
@@ -243,9 +258,9 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
 
 // Many tokens: a block's waves have 64 tokens each and go along the row together, so that a line of
 // W is brought to LDS once for all of them. With n = 4 from 20 K tokens on, eight waves: 32 K tokens of
-// 4 x 4096 bf16 forward 443 -> 418 us (8 K tokens 105 and 108, 16 K about 220 and 233); with n = 8,
-// whose W is as much as the streams of 80 tokens, from 2 K on, four: 8000 tokens of 8 x 1024 fp32 223 ->
-// 176.
+// 4 x 4096 bf16 forward 443 -> 418 us (8 K tokens 106 and 108, 16 K 194 and 197, 20000 of 4 x 512 44
+// and 57); with n = 8, whose W is as much as the streams of 80 tokens, from 2 K on, four: 8000 tokens of
+// 8 x 1024 fp32 223 -> 176 (2000 of 8 x 4096 bf16 74 and 80).
 template <int N>
 constexpr int gate_wide_waves() { return N == 4 ? 8 : 4; }
 
@@ -254,15 +269,18 @@ __global__ __launch_bounds__((64 * gate_wide_waves<N>()), 2) void pre_gate_wide_
                                                                                        const v4u* __restrict__ W,
                                                                                        float* __restrict__ part,
                                                                                        int64_t B, int64_t steps,
-                                                                                       int64_t per) {
+                                                                                       int64_t per, uint32_t tiles,
+                                                                                       uint32_t per_xcd) {
     constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4, TT = 4, GW = gate_wide_waves<N>();
     constexpr int kThreads = 64 * GW, WQ = (8 * R + kThreads - 1) / kThreads;
     __shared__ v4u rows[GW][16 * TT][9];
     __shared__ v4u wrow[2][R][9];
     const int lane = threadIdx.x & 63, g = lane >> 4, c = lane & 15;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
-    const int64_t first = (static_cast<int64_t>(blockIdx.x) * GW + w) * 16 * TT;
-    const int64_t s0 = blockIdx.y * per, s1 = s0 + per < steps ? s0 + per : steps;
+    const GatePlace at = gate_place(tiles, per_xcd);
+    const int64_t first = (at.tile * GW + w) * 16 * TT;
+    const int64_t s0 = at.share * per, s1 = s0 + per < steps ? s0 + per : steps;
+    if (s0 >= s1) return;  // the whole block
     const int64_t start = first < B ? first : B - 1;  // a wave without tokens goes along on the last one's values
     const char* base = reinterpret_cast<const char*>(X) + 64 * steps * start;
     uint32_t off[2 * TT];
@@ -308,7 +326,7 @@ __global__ __launch_bounds__((64 * gate_wide_waves<N>()), 2) void pre_gate_wide_
         for (int u = 0; u < 2; ++u) sums.step(wv[u], xv[u]);
     }
     sums.finish(c);
-    v4f* dst = reinterpret_cast<v4f*>(part) + (blockIdx.y * B + first) * S4;
+    v4f* dst = reinterpret_cast<v4f*>(part) + (at.share * B + first) * S4;
     sums.each(g, c, [&](int t, int q, v4f& v) {
         if (first + t < B) dst[t * S4 + q] = v;
     });
@@ -1134,8 +1152,9 @@ int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float*
     auto gate = l.wide      ? pre_gate_wide_kernel<DX, N>
                 : l.tt == 1 ? pre_gate_kernel<DX, N, 1, gate_waves<N>(1)>
                 : l.tt == 2 ? pre_gate_kernel<DX, N, 2, gate_waves<N>(2)> : pre_gate_kernel<DX, N, 4, gate_waves<N>(4)>;
-    launch_kernel(gate, dim3(static_cast<unsigned>(l.tiles), static_cast<unsigned>(l.splits)), dim3(64 * l.waves), 0,
-                  stream, x, w, part, s.B, s.steps, l.per);
+    const uint32_t tiles = static_cast<uint32_t>(l.tiles), per_xcd = static_cast<uint32_t>(cdiv(l.tiles * l.splits, 8));
+    launch_kernel(gate, dim3(8 * per_xcd), dim3(64 * l.waves), 0, stream, x, w, part, s.B, s.steps, l.per, tiles,
+                  per_xcd);
     const int L = s.nc <= 8 ? 8 : s.nc <= 16 ? 16 : s.nc <= 32 ? 32 : 64;
     auto read = L == 8 ? pre_read_kernel<DX, N, 8> : L == 16 ? pre_read_kernel<DX, N, 16>
                 : L == 32 ? pre_read_kernel<DX, N, 32> : pre_read_kernel<DX, N, 64>;
