@@ -469,37 +469,50 @@ __device__ __forceinline__ float wave_sum(float x) {
 }
 
 // A stage of G in the operands' layouts, with the tokens' h^pre and s: written by pre_dot_kernel,
-// copied to LDS as it is by pre_back_kernel. bf16: G as the sum of two bf16 values (the upper 16
-// bits, and the rest rounded), 2^-16 off at most, since one alone (2^-8) would be as coarse as the
-// result's own rounding. Operand rows past the last row of W are zeros.
+// copied to LDS as it is by pre_back_kernel. bf16: G as the sum of three bf16 values, which hold all
+// 24 bits of it, so that the products are those of fp32: with two (2^-16 of G) five in a thousand values
+// of dW were rounded to the other neighbour than fp32 products round them to, with three one.
+// Operand rows past the last row of W are zeros.
 template <int DX, int N>
 struct Stage {
     static constexpr bool H16 = DX == BIRKHOFF4_BF16;
     static constexpr int R = Gates<N>::rows, RT = Gates<N>::tiles, KS = H16 ? Gates<N>::ksteps : R / 4;
-    static constexpr int parts = H16 ? 2 : 1;  // upper and lower bf16 values
+    static constexpr int parts = H16 ? 3 : 1;  // bf16 values of one of G
     static constexpr int rows = H16 ? 32 * KS : 16 * RT;  // rows that have a place
+    // n = 8: the last step has 16 rows, so that two parts fit one operand of 32 (and the third one with zeros)
+    static constexpr bool paired = H16 && R % 32 == 16;
     using T = std::conditional_t<H16, uint16_t, float>;
     static constexpr int KE = H16 ? 8 : KS;  // values per lane of a dX operand
-    static constexpr int KO = H16 ? KS : 1;  // dX operands per half
-    alignas(16) T w[parts][RT][2][64][4];    // dW: lane (g, j): row j's tokens 4 g .. + 3 of each half
-    alignas(16) T x[2][parts][KO][64][KE];   // dX: by halves; lane (g, t): token t's rows KE g .. of the operand
+    static constexpr int KO = H16 ? parts * KS - paired : 1;  // dX operands per half
+    alignas(16) T w[parts][RT][2][64][4];  // dW: lane (g, j): row j's tokens 4 g .. + 3 of each half
+    alignas(16) T x[2][KO][64][KE];        // dX: by halves; lane (g, t): token t's rows of the operand's group g
     alignas(16) float coef[N + 1][kTokenStep];
+
+    // Place among a half's groups of dX operands (four to an operand) of rows 8 octet .. + 7 of a part.
+    static __device__ __forceinline__ int group(int part, int octet) {
+        if (paired && octet >= 4 * (KS - 1)) return 4 * parts * (KS - 1) + 2 * part + octet - 4 * (KS - 1);
+        return 4 * (parts * (octet >> 2) + part) + (octet & 3);
+    }
 };
 
-// Eight fp32 values as two bf16 ones each: the upper half of the bits (no rounding, so a large
-// value does not overflow) and the rest, rounded (nothing where the value is not finite).
+// fp32 values as three bf16 ones each, by truncation: the upper eight bits of the significand (no
+// rounding, so a large value does not overflow), the next eight and the last eight. Exact, but for
+// what lies below fp32's smallest normal value; nothing past the first where it is not finite.
 template <int NV>
-__device__ __forceinline__ void split_bf16(const float (&v)[NV], uint32_t (&hi)[NV / 2], uint32_t (&lo)[NV / 2]) {
+__device__ __forceinline__ void split_bf16(const float (&v)[NV], uint32_t (&p)[3][NV / 2]) {
     float rest[NV];
 #pragma unroll
-    for (int k = 0; k < NV; ++k) {
-        const float up = __uint_as_float(__float_as_uint(v[k]) & 0xffff0000u);
-        rest[k] = __builtin_fabsf(v[k]) < __builtin_inff() ? v[k] - up : 0.f;
-    }
+    for (int k = 0; k < NV; ++k) rest[k] = v[k];
 #pragma unroll
-    for (int k = 0; k < NV / 2; ++k) {
-        hi[k] = __builtin_amdgcn_perm(__float_as_uint(v[2 * k + 1]), __float_as_uint(v[2 * k]), 0x07060302u);
-        lo[k] = pack_bf16(rest[2 * k], rest[2 * k + 1]);
+    for (int q = 0; q < 3; ++q) {
+#pragma unroll
+        for (int k = 0; k < NV / 2; ++k)
+            p[q][k] = __builtin_amdgcn_perm(__float_as_uint(rest[2 * k + 1]), __float_as_uint(rest[2 * k]), 0x07060302u);
+#pragma unroll
+        for (int k = 0; k < NV; ++k) {
+            const float up = __uint_as_float(__float_as_uint(rest[k]) & 0xffff0000u);
+            rest[k] = __builtin_fabsf(rest[k]) < __builtin_inff() ? rest[k] - up : 0.f;
+        }
     }
 }
 
@@ -514,10 +527,11 @@ __device__ __forceinline__ void store_stage(Stage<DX, N>& to, const float (&row)
         const float v[4] = {row[0][j], row[1][j], row[2][j], row[3][j]};
         const int at = 16 * g + (j & 15);
         if constexpr (St::H16) {
-            uint32_t hi[2], lo[2];
-            split_bf16<4>(v, hi, lo);
-            *reinterpret_cast<uint2*>(to.w[0][j >> 4][half][at]) = uint2{hi[0], hi[1]};
-            *reinterpret_cast<uint2*>(to.w[1][j >> 4][half][at]) = uint2{lo[0], lo[1]};
+            uint32_t p[St::parts][2];
+            split_bf16<4>(v, p);
+#pragma unroll
+            for (int q = 0; q < St::parts; ++q)
+                *reinterpret_cast<uint2*>(to.w[q][j >> 4][half][at]) = uint2{p[q][0], p[q][1]};
         } else {
             *reinterpret_cast<v4f*>(to.w[0][j >> 4][half][at]) = v4f{v[0], v[1], v[2], v[3]};
         }
@@ -526,18 +540,25 @@ __device__ __forceinline__ void store_stage(Stage<DX, N>& to, const float (&row)
         const int k = lane & 3, j8 = lane >> 2;
         if (j8 < St::rows / 8) {
             float v[8];
-            uint32_t hi[4], lo[4];
+            uint32_t p[St::parts][4];
 #pragma unroll
             for (int q = 0; q < 8; ++q) v[q] = row[k][8 * j8 + q];
-            split_bf16<8>(v, hi, lo);
-            const int at = 16 * (j8 & 3) + (t & 15) + k;
-            *reinterpret_cast<v4u*>(to.x[half][0][j8 >> 2][at]) = v4u{hi[0], hi[1], hi[2], hi[3]};
-            *reinterpret_cast<v4u*>(to.x[half][1][j8 >> 2][at]) = v4u{lo[0], lo[1], lo[2], lo[3]};
+            split_bf16<8>(v, p);
+            auto put = [&](int group, int q) {
+                *reinterpret_cast<v4u*>(to.x[half][group >> 2][16 * (group & 3) + (t & 15) + k]) =
+                    v4u{p[q][0], p[q][1], p[q][2], p[q][3]};
+            };
+            if (St::paired && 8 * j8 >= St::R) {  // the last operand's two groups of zeros
+                put(4 * St::KO - 2 + (j8 & 1), 0);
+            } else {
+#pragma unroll
+                for (int q = 0; q < St::parts; ++q) put(St::group(q, j8), q);
+            }
         }
     } else {
         for (int q = lane; q < 2 * St::R; q += 64) {  // pairs of rows
             const int k = q / (St::R / 2), j = 2 * (q % (St::R / 2));
-            *reinterpret_cast<f32x2*>(&to.x[half][0][0][16 * (j / St::KS) + (t & 15) + k][j % St::KS]) =
+            *reinterpret_cast<f32x2*>(&to.x[half][0][16 * (j / St::KS) + (t & 15) + k][j % St::KS]) =
                 f32x2{row[k][j], row[k][j + 1]};
         }
     }
@@ -747,8 +768,9 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
     constexpr bool kLds = BackPlan<DX, N>::w_lds;
     using Row = Words<WO>;
     __shared__ St lds[NS];
-    // [operand][channel][lane]: of bf16 eight rows, of fp32 one
-    __shared__ std::conditional_t<H16, v4u, float> wlds[kLds ? NW : 1][kLds ? KS : 1][CE][64];
+    // [channel][four lane groups an operand][lane of the group]: of bf16 eight rows, of fp32 one
+    constexpr int WG = 4 * KS - 2 * St::paired;
+    __shared__ std::conditional_t<H16, v4u, float> wlds[kLds ? NW : 1][kLds ? CE : 1][WG][16];
     const int lane = threadIdx.x & 63, g = lane >> 4, c16 = lane & 15;
     const int ww = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     constexpr int ADJ = BackPlan<DX, N>::adj;
@@ -824,15 +846,17 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
 
     // W's rows: operand of the dX products, for each channel c of the lane
     std::conditional_t<H16, v4u, float> wreg[kLds ? 1 : KS][CE];
+    // the lane's group of operand k: where two parts of G share it, both halves of the lanes have the same rows
+    auto group = [&](int k) { return St::paired && k == KS - 1 ? g & 1 : g; };
     auto keep = [&](int k, int c, auto v) {
         if constexpr (kLds)
-            wlds[ww][k][c][lane] = v;
+            wlds[ww][c][4 * k + group(k)][c16] = v;
         else
             wreg[k][c] = v;
     };
     auto wop = [&](int k, int c) {
         if constexpr (kLds)
-            return wlds[ww][k][c][lane];
+            return wlds[ww][c][4 * k + group(k)][c16];
         else
             return wreg[k][c];
     };
@@ -842,7 +866,7 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
             Words<WO> rows[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) {  // past the last row: that row, which meets zeros of G
-                const int row = 32 * k + 8 * g + j;
+                const int row = 32 * k + 8 * group(k) + j;
                 rows[j] = load_words<WO>(W, (K * (row < R ? row : R - 1) + w * C + at) * SZ);
             }
 #pragma unroll
@@ -873,7 +897,7 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int p = 0; p < 2; ++p) {
+                for (int p = 0; p < St::parts; ++p) {
                     const v2u a0 = *reinterpret_cast<const v2u*>(s.w[p][r][0][lane]);
                     const v2u a1 = *reinterpret_cast<const v2u*>(s.w[p][r][1][lane]);
                     const v4u a = {a0.x, a0.y, a1.x, a1.y};
@@ -903,19 +927,23 @@ __global__ __launch_bounds__((64 * BackPlan<DX, N>::waves), 2) void pre_back_ker
         if constexpr (H16) {
 #pragma unroll
             for (int k = 0; k < KS; ++k) {
-                const v4u hi = *reinterpret_cast<const v4u*>(s.x[hf][0][k][lane]);
-                const v4u lo = *reinterpret_cast<const v4u*>(s.x[hf][St::parts - 1][k][lane]);
+                constexpr int NP = St::parts;
+                const int np = St::paired && k == KS - 1 ? NP - 1 : NP;
+                v4u a[NP];
+#pragma unroll
+                for (int p = 0; p < np; ++p) a[p] = *reinterpret_cast<const v4u*>(s.x[hf][NP * k + p][lane]);
 #pragma unroll
                 for (int c = 0; c < CE; ++c) {
                     const v4u b = wop(k, c);
-                    d[c] = mfma_bf16(lo, b, mfma_bf16(hi, b, d[c]));
+#pragma unroll
+                    for (int p = 0; p < np; ++p) d[c] = mfma_bf16(a[p], b, d[c]);
                 }
             }
         } else {
 #pragma unroll
             for (int k = 0; k < KS; ++k)
 #pragma unroll
-                for (int c = 0; c < CE; ++c) d[c] = mfma_f32(s.x[hf][0][0][lane][k], wop(k, c), d[c]);
+                for (int c = 0; c < CE; ++c) d[c] = mfma_f32(s.x[hf][0][lane][k], wop(k, c), d[c]);
         }
         uint32_t off[4];
         rows_of(t0, off, K);

@@ -327,3 +327,47 @@ def test_refusals():
             b4.pre_bwd(X, W, alpha, bias, ok[3], ok[4], *bad)
     with pytest.raises(ValueError):
         b4.pre_bwd(X, W, alpha, bias, ok[3][:5], ok[4], *grads)
+
+
+def pieces(v):
+    """fp32 values as three bf16 ones that add up to them: the upper eight bits of the significand,
+    the next eight and the last eight, so that each is exact."""
+    upper = lambda t: (t.view(torch.int32) & -65536).view(F32)
+    hi = upper(v)
+    mid = upper(v - hi)
+    return hi, mid, v - hi - mid
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 8])
+def test_gradient_of_products_is_whole(n, dtype):
+    """G, the gradient of the products, enters dX = G W and dW = G^T X with all the 24 bits of its
+    fp32 values, also where the streams are bf16: with r = alpha = 1 and q = 0 it is dH, W = 1 (X = 1)
+    makes the product dH itself, and what takes its upper 16 bits away leaves the last eight, of
+    which every sum on the way is a whole fp32 value. One row of W a token, so that nothing else
+    is added."""
+    N, C, M = n * n + 2 * n, 72, n * n
+    g = torch.Generator(device="cuda").manual_seed(47)
+    v = (1 + torch.rand(M, device="cuda", generator=g)) * 2.0 ** torch.randint(-9, 9, (M,), device="cuda", generator=g)
+    hi, mid, lo = pieces(v)
+    assert torch.equal(hi + mid + lo, v) and torch.equal(lo.bfloat16().float(), lo) and (lo != 0).any()
+    alpha, bias = torch.ones(3, device="cuda"), torch.zeros(N, device="cuda")
+    bias[:n] = 300.0  # h^pre = 1, and no gradient through it
+    one = torch.ones(N, n * C, device="cuda").to(dtype)
+    wide = lambda t, *shape: t.reshape(-1, *(1 for _ in shape)).expand(-1, *shape).to(dtype).contiguous()
+
+    def back(X, rows, dU, E):
+        B = len(X)
+        q, rms = torch.zeros(B, N, device="cuda"), torch.ones(B, device="cuda")
+        return b4.pre_bwd(X, one, alpha, bias, q, rms, dU, None, rows.view(B, n, n).contiguous(), E)
+
+    # token t's dH has entry t alone
+    X = torch.randn(M, n, C, device="cuda", generator=g).to(dtype)
+    dX = back(X, torch.diag(v), wide(-mid, C), wide(-hi, n, C))[0]
+    assert torch.equal(dX.float(), lo[:, None, None].expand_as(dX))
+    # three tokens an entry: the value, and its upper pieces taken away
+    rows = torch.zeros(3 * M, M, device="cuda")
+    for k, t in enumerate((v, -hi, -mid)):
+        rows[torch.arange(M) * 3 + k, torch.arange(M)] = t
+    dW = back(torch.ones(3 * M, n, C, device="cuda").to(dtype), rows, None, None)[1]
+    assert torch.equal(dW[2 * n:].float(), lo[:, None].expand(-1, n * C)) and (dW[:2 * n] == 0).all()
