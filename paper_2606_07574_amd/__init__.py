@@ -29,6 +29,7 @@ import ctypes
 import os
 
 import torch
+from torch.autograd import forward_ad
 from torch.autograd.function import once_differentiable
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -549,7 +550,11 @@ def _params(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.T
 
 def _graph(*inputs: torch.Tensor) -> bool:
     """Whether autograd records what is computed from these. Where it does not, the calls leave its
-    functions out (a layer for one token without gradients: 53 us on the host with them, 31 without)."""
+    functions out (a layer for one token without gradients: 53 us on the host with them, 31 without).
+    Within a level of forward-mode derivatives they do not: a tensor with a tangent needs no gradient,
+    and the functions, which have no forward-mode derivative, refuse it."""
+    if forward_ad._current_level >= 0:
+        return True
     return torch.is_grad_enabled() and any(t.requires_grad for t in inputs)
 
 
@@ -649,7 +654,8 @@ class PreFn(torch.autograd.Function):
 def pre(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, eps: float = DEFAULT_EPS):
     """pre_fwd with gradients for X, W, alpha and bias: (U, h, H, X). The X returned is the X
     given; give it to what uses the streams next, and their gradient costs no pass of its own.
-    Like post, it has no second derivatives: a backward of its backward raises."""
+    Like post, it has no second and no forward-mode derivatives: a backward of its backward raises, and
+    so does an input with a tangent."""
     if _graph(X, W, alpha, bias):
         return PreFn.apply(X, W, alpha, bias, eps)
     X = _whole(X)
