@@ -351,8 +351,10 @@ __global__ __launch_bounds__(64 * kReadWaves) void pre_read_kernel(const float* 
     const int lane = threadIdx.x & 63;
     const int w = __builtin_amdgcn_readfirstlane(static_cast<int>(threadIdx.x >> 6));
     const int W = blockDim.x >> 6;
-    // blocks from the last token back: the last ones that the products read are still in the cache
-    const int64_t t0 = (gridDim.x - 1 - static_cast<int64_t>(blockIdx.x)) * TW;
+    // blocks from the last token back: the last ones that the products read are still in the cache. With more
+    // of them than one dimension of a grid takes, they lie along z too
+    const int64_t block = static_cast<int64_t>(blockIdx.z) * gridDim.x + blockIdx.x;
+    const int64_t t0 = (static_cast<int64_t>(gridDim.z) * gridDim.x - 1 - block) * TW;
     const int64_t tok = t0 + lane / L;
     const int64_t first = L == 64 ? 64 * (static_cast<int64_t>(blockIdx.y) * W + w) : 0;  // this wave's column
     const int64_t col = first + lane % L;
@@ -1160,7 +1162,10 @@ BackLaunch back_launch(const PreShape& s, int n, bool bf16) {
     return l;
 }
 
-constexpr int64_t kPreMaxTokens = int64_t(1) << 26;  // a launch's lanes over tokens stay 32-bit
+// The dot kernel has 16 lanes a token up to 64 chunks of a row and 128 at most (above 256 chunks, of
+// which memory does not hold 2^25 tokens): below a launch's 2^32 lanes. The read splits its grid.
+constexpr int64_t kPreMaxTokens = int64_t(1) << 26;
+constexpr int64_t kMaxLanes = int64_t(1) << 31;  // along one dimension of a grid
 constexpr int64_t kPreMaxValues = int64_t(1) << 46;
 constexpr int64_t kPreMaxChannels = int64_t(1) << 20;  // 64 tokens lie within 32-bit offsets
 
@@ -1192,7 +1197,9 @@ int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float*
     auto read = L == 8 ? pre_read_kernel<DX, N, 8> : L == 16 ? pre_read_kernel<DX, N, 16>
                 : L == 32 ? pre_read_kernel<DX, N, 32> : pre_read_kernel<DX, N, 64>;
     const int64_t cols = cdiv(s.nc, L), shares = cdiv(cols, kReadWaves), waves = cdiv(cols, shares);
-    launch_kernel(read, dim3(static_cast<unsigned>(cdiv(s.B, 64 / L)), static_cast<unsigned>(shares)),
+    const int64_t blocks = cdiv(s.B, 64 / L), layers = cdiv(64 * waves * blocks, kMaxLanes);
+    launch_kernel(read, dim3(static_cast<unsigned>(cdiv(blocks, layers)), static_cast<unsigned>(shares),
+                             static_cast<unsigned>(layers)),
                   dim3(static_cast<unsigned>(64 * waves)), 0, stream, part, x, alpha, bias, eps,
                   static_cast<float>(1.0 / (static_cast<double>(N) * s.C)), static_cast<v4u*>(U), h, H, q, rms, s.B, s.nc,
                   static_cast<int>(l.splits));

@@ -131,3 +131,13 @@ def test_philox_reference():
     assert philox((f, f, f, f), (f, f)) == [0x408F276D, 0x41C83B0E, 0xA20BC7C6, 0x6D5451FD]
     assert philox((0x243F6A88, 0x85A308D3, 0x13198A2E, 0x03707344), (0xA4093822, 0x299F31D0)) == \
         [0xD16CFE09, 0x94FDCCEB, 0x5001E420, 0x24126EA1]
+
+
+def test_widest_rows():
+    """C up to 2^20, in every call."""
+    for n in (4, 8):
+        work = getattr(b4.lib(), f"birkhoff{n}_pre_work")
+        for dt, e in ((b4.BF16, 8), (b4.F32, 4)):
+            for backward in (0, 1):
+                assert work(3, 1 << 20, dt, backward) > 0 and work(3, (1 << 20) + e, dt, backward) == SIZE
+                assert work(1 << 26, 64, dt, backward) > 0 and work((1 << 26) + 1, 64, dt, backward) == SIZE

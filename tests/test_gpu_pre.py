@@ -371,3 +371,30 @@ def test_gradient_of_products_is_whole(n, dtype):
         rows[torch.arange(M) * 3 + k, torch.arange(M)] = t
     dW = back(torch.ones(3 * M, n, C, device="cuda").to(dtype), rows, None, None)[1]
     assert torch.equal(dW[2 * n:].float(), lo[:, None].expand(-1, n * C)) and (dW[:2 * n] == 0).all()
+
+
+def test_most_lanes():
+    """Tokens times lanes a token past 2^32, which one dimension of a grid does not take."""
+    n, B, C, part = 4, 1 << 25, 520, 1 << 19  # 65 chunks a row: two waves a token
+    torch.cuda.empty_cache()
+    free = torch.cuda.mem_get_info()[0]
+    if free < 205 << 30:
+        pytest.skip(f"needs 190 GiB of GPU memory, {free >> 30} are free")
+    some, W, alpha, bias, _ = inputs(n, part, C, BF16, 49)
+    X = torch.empty(B, n, C, dtype=BF16, device="cuda")
+    X.view(B // part, *some.shape)[:] = some
+    got = dict(zip(("U", "h", "H", "q", "rms"), b4.pre_fwd(X, W, alpha, bias)))
+    torch.cuda.synchronize()
+    for cut in (slice(0, 40), slice(B // 2 - 20, B // 2 + 20), slice(B - 40, B)):
+        out, err, _ = pre_ref(X[cut], W, alpha, bias, 1e-6)
+        for k in out:
+            within(got[k][cut], out[k], err[k], f"{k} of tokens {cut.start}..")
+    del X
+    # every part's tokens are the first one's, up to the order of their sums: a bf16 step, an ulp's few of q
+    for k, (tol, least) in dict(U=(2.0 ** -6, 1e-4), rms=(1e-6, 0.0), h=(1e-5, 1e-5)).items():
+        parts = got[k].view(B // part, part, -1)
+        ref = parts[0].float()
+        for p in parts[1:]:
+            assert ((p.float() - ref).abs() <= tol * ref.abs() + least).all(), k
+    del got, parts, p, ref
+    torch.cuda.empty_cache()  # the other tests', and other programs'
