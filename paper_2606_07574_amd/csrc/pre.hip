@@ -225,8 +225,10 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
                 for (int r = 0; r < RT; ++r) wv[u][r] = wr[r][4 * (s + u)];
             }
         }
+        __builtin_amdgcn_wave_barrier();  // the last turn's reads of the wave's lines come before, this one's after
 #pragma unroll
         for (int t = 0; t < 2 * TT; ++t) lds.rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
+        __builtin_amdgcn_wave_barrier();
         turn = turn + 1 < turns ? turn + 1 : 0;
         next = s0 + 2 * GW * turn + 2 * w;
         if (k + 1 < turns) load(next);
@@ -303,6 +305,7 @@ __global__ __launch_bounds__((64 * gate_wide_waves<N>()), 2) void pre_gate_wide_
     load(s0 + 2 * turn);
     for (int64_t k = 0; k < turns; ++k) {
         const int buf = static_cast<int>(k & 1);
+        __builtin_amdgcn_wave_barrier();  // the last turn's reads of the wave's lines come before
 #pragma unroll
         for (int t = 0; t < 2 * TT; ++t) rows[w][8 * t + (lane >> 3)][lane & 7] = xr[t];
 #pragma unroll
@@ -647,6 +650,7 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
             if (lane == 0) row[w][k][P + N] = s * r * inv_k;
         }
     }
+    __builtin_amdgcn_wave_barrier();  // lanes read what others of the wave have written
     if (part == 0 && t0 < Bp) store_stage<DX, N>(G[t0 / kTokenStep], row[w], static_cast<int>(t0 % kTokenStep), lane);
     // a row of sums for the block: dl's, then the three groups' dl q
 #pragma unroll
