@@ -398,3 +398,58 @@ def test_most_lanes():
             assert ((p.float() - ref).abs() <= tol * ref.abs() + least).all(), k
     del got, parts, p, ref
     torch.cuda.empty_cache()  # the other tests', and other programs'
+
+
+# rows of more than 512 chunks: several blocks a token in the forward's sum, several turns of a wave in the
+# backward's dots; the widest ones leave the backward's products one share of the tokens (n C > 2048 waves'
+# pieces), or are as wide as a row may be
+WIDE = [(1, 4104), (33, 4104), (1, 8200), (33, 8200), (2049, 4104), (33, 16640), (33, 33288)]
+
+
+@pytest.mark.parametrize("dtype", DTYPES, ids=["f32", "bf16"])
+@pytest.mark.parametrize("n", [4, 8])
+@pytest.mark.parametrize("B,C", WIDE)
+def test_wide_rows(n, B, C, dtype):
+    C = C if dtype == BF16 else C // 2
+    check(*inputs(n, B, C, dtype, 51), 1e-6, f"n={n} B={B} C={C} {dtype}")
+
+
+@pytest.mark.parametrize("n,B,dtype", [(4, 3, BF16), (4, 65, F32), (8, 2, BF16)])
+def test_widest_rows(n, B, dtype):
+    """C = 2^20, the largest; 64 fp32 tokens' offsets are then next to what 32 bits hold."""
+    check(*inputs(n, B, 1 << 20, dtype, 53), 1e-6, f"n={n} B={B} C=2^20 {dtype}")
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("n", [4, 8])
+def test_padding_tokens(n):
+    """The tokens that fill the last stage of 32 count nothing in dW, whatever the last token holds:
+    with q and rms given and G finite, an infinite value of the last token makes its column of dW
+    infinite with the sign of G; read again for the padding, times its G of zero, it would make it
+    NaN. (Nothing of dU's row goes through the value: dU is not given.)"""
+    N, C, B = n * n + 2 * n, 40, 33
+    X, W, alpha, bias, grads = inputs(n, B, C, F32, 55)
+    q, rms = b4.pre_fwd(X, W, alpha, bias)[3:]
+    clean = b4.pre_bwd(X, W, alpha, bias, q, rms, None, *grads[1:])[1]
+    bad = X.clone()
+    bad[B - 1, n - 1, 5] = float("inf")
+    dX, dW, _, _ = b4.pre_bwd(bad, W, alpha, bias, q, rms, None, *grads[1:])
+    col = torch.arange(n * C, device="cuda") == (n - 1) * C + 5
+    assert torch.equal(dW[:, ~col], clean[:, ~col])
+    # dH's rows: G = r alpha dH is not zero
+    sign = torch.sign(alpha[2] * grads[2][B - 1].flatten())
+    assert torch.equal(dW[2 * n:, col].flatten(), sign * float("inf"))
+    assert torch.isfinite(dX[:B - 1]).all()
+
+
+def test_gradient_of_one_token_stays_there():
+    """A NaN in one token's gradient of the streams goes into that token's dX, and nowhere else."""
+    X, W, alpha, bias, grads = inputs(4, 33, 64, BF16, 57)
+    q, rms = b4.pre_fwd(X, W, alpha, bias)[3:]
+    clean = b4.pre_bwd(X, W, alpha, bias, q, rms, *grads)
+    E = grads[3].clone()
+    E[32] = float("nan")
+    dX, *others = b4.pre_bwd(X, W, alpha, bias, q, rms, *grads[:3], E)
+    assert dX[32].isnan().all() and torch.equal(dX[:32], clean[0][:32])
+    for a, b in zip(others, clean[1:]):
+        assert torch.equal(a, b)
