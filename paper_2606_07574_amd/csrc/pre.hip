@@ -71,7 +71,7 @@ __device__ __forceinline__ float row_scale(const float* __restrict__ alpha, int 
 // matrix rate is nearer to what HBM delivers). A wave loads whole lines, eight lanes a row, and takes
 // them to the operands' layout (a lane row's chunk) through LDS of its own while the next are on
 // the way: loaded in that layout, sixteen rows of 64 bytes at a time, 32 K tokens of 4 x 4096 bf16 took
-// 225 us instead of 195. The shares' sums are added by the reader, in order: no atomics, so a
+// 249 us instead of 195. The shares' sums are added by the reader, in order: no atomics, so a
 // token's result does not depend on timing.
 template <int DX, int N, int TT>
 struct GateSums {  // of a wave's 16 TT tokens: lane (g, c) has rows 16 r + 4 g .. + 3 of token 16 t + c
@@ -161,7 +161,8 @@ __device__ __forceinline__ void load_lines(v4u (&xr)[2 * TT], const char* p, con
 
 // A block's tile of tokens and share of the row. Workgroups go to the eight XCDs in turn; each XCD
 // gets neighbouring pairs, tiles first, so that its L2 holds the part of W of its shares (forward of 8 K
-// tokens of 8 x 4096 bf16, 5.2 MB of W, 237 -> 204 us, of 32 K of 4 x 4096 414 -> 396).
+// tokens of 8 x 4096 bf16, 5.2 MB of W, 211 -> 202 us, with W's loads behind the streams' 237 -> 204; n = 4, whose
+// W an L2 holds whole: 16 K tokens of 4 x 4096 194 -> 190, 2^15 of 4 x 2048 188 -> 204).
 struct GatePlace {
     int64_t tile;
     int64_t share;
@@ -199,7 +200,8 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
     for (int r = 0; r < RT; ++r) wr[r] = W + 4 * steps * (16 * r + c < R ? 16 * r + c : R - 1) + g;
     GateSums<DX, N, TT> sums;
     sums.clear();
-    // blocks begin at different places of the row: begun together, 249 us instead of 235 at 32 K tokens of 4 x 4096
+    // blocks begin at different places of the row: begun together, forward of 16 K tokens of 4 x 4096 bf16 212 us
+    // instead of 190, 2^15 390 instead of 383
     const int64_t turns = (s1 - s0 + 2 * GW - 1) / (2 * GW);
     int64_t turn = (blockIdx.x >> 3) % turns, next = s0 + 2 * GW * turn + 2 * w;
     v4u xr[2 * TT];
@@ -258,22 +260,22 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
     }
 }
 
-// Many tokens: a block's waves have 64 tokens each and go along the row together, so that a line of
-// W is brought to LDS once for all of them. With n = 4 from 20 K tokens on, eight waves: 32 K tokens of
-// 4 x 4096 bf16 forward 443 -> 418 us (8 K tokens 106 and 108, 16 K 194 and 197, 20000 of 4 x 512 44
-// and 57); with n = 8, whose W is as much as the streams of 80 tokens, from 2 K on, four: 8000 tokens of
-// 8 x 1024 fp32 223 -> 176 (2000 of 8 x 4096 bf16 74 and 80).
-template <int N>
-constexpr int gate_wide_waves() { return N == 4 ? 8 : 4; }
+// Many tokens with n = 8, whose W is as much as the streams of 80 tokens: a block's waves have 64 tokens
+// each and go along the row together, so that a line of W is brought to LDS once for all of them. From
+// 2 K tokens on; whole forward in us, without it in brackets: 2049 tokens of 8 x 512 bf16 29 (32), 2049 of 8 x
+// 4096 81 (83), 3000 of 8 x 4096 101 (117), 6000 166 (209), 32 K 790 (996), 8000 of 8 x 1024 fp32 178 (228); slower
+// at few of the sizes tried (4096 of 8 x 512 37 (33), 2500 of 8 x 4096 fp32 272 (252)). With n = 4 such a form,
+// of eight waves, was slower at all widths from 128 channels on (20481 tokens of 4 x 4096 297 and 256, 2^15 403
+// and 388, 65537 of 4 x 512 137 and 120; 10^6 of 4 x 8 189 and 228) and is not there.
+constexpr int kGateWideWaves = 4;
 
-template <int DX, int N>
-__global__ __launch_bounds__((64 * gate_wide_waves<N>()), 2) void pre_gate_wide_kernel(const v4u* __restrict__ X,
-                                                                                       const v4u* __restrict__ W,
-                                                                                       float* __restrict__ part,
-                                                                                       int64_t B, int64_t steps,
-                                                                                       int64_t per, uint32_t tiles,
-                                                                                       uint32_t per_xcd) {
-    constexpr int RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4, TT = 4, GW = gate_wide_waves<N>();
+template <int DX>
+__global__ __launch_bounds__(64 * kGateWideWaves, 2) void pre_gate_wide_kernel(const v4u* __restrict__ X,
+                                                                               const v4u* __restrict__ W,
+                                                                               float* __restrict__ part, int64_t B,
+                                                                               int64_t steps, int64_t per, uint32_t tiles,
+                                                                               uint32_t per_xcd) {
+    constexpr int N = 8, RT = Gates<N>::tiles, R = Gates<N>::rows, S4 = Gates<N>::stride / 4, TT = 4, GW = kGateWideWaves;
     constexpr int kThreads = 64 * GW, WQ = (8 * R + kThreads - 1) / kThreads;
     __shared__ v4u rows[GW][16 * TT][9];
     __shared__ v4u wrow[2][R][9];
@@ -475,8 +477,9 @@ __device__ __forceinline__ float wave_sum(float x) {
 
 // A stage of G in the operands' layouts, with the tokens' h^pre and s: written by pre_dot_kernel,
 // copied to LDS as it is by pre_back_kernel. bf16: G as the sum of three bf16 values, which hold all
-// 24 bits of it, so that the products are those of fp32: with two (2^-16 of G) five in a thousand values
-// of dW were rounded to the other neighbour than fp32 products round them to, with three one.
+// 24 bits of it, so that the products are those of fp32: 0.07 % of dW's values are not the exact result
+// rounded to bf16 (2^15 tokens of 4 x 4096; torch's fp32 products 0.2 %), with two (2^-16 of G) it was 0.45 %.
+// It costs 1 % of an autograd step there, 3 % of one of 8 K tokens of 8 x 4096.
 // Operand rows past the last row of W are zeros.
 template <int DX, int N>
 struct Stage {
@@ -1083,7 +1086,7 @@ struct PreShape {
 };
 
 struct GateLaunch {
-    bool wide;                   // pre_gate_wide_kernel
+    bool wide;                   // pre_gate_wide_kernel (n = 8)
     int tt, waves;               // 16-token tiles and waves of a block
     int64_t tiles, splits, per;  // blocks over tokens, shares of the row, steps per share
 };
@@ -1093,8 +1096,8 @@ struct GateLaunch {
 //  * n = 4 up to 512 two tiles and 16 waves: 96 tokens of 4 x 4096 11.5, four tiles and 4 waves 12.4; 300
 //    13.8 and 14.8; 600 23 and 19.3. n = 8 up to 64 two tiles and 8 waves (more do not fit the
 //    registers): 32 tokens of 8 x 4096 16.6, four tiles 19.2; 100 of 8 x 2048 18.1 and 17.5.
-//  * else four tiles, each row of W read once for 64 tokens, and 4 waves: 32 K tokens of 4 x 4096
-//    442 (two tiles 488).
+//  * else four tiles, each row of W read once for 64 tokens, and 4 waves: 16 K tokens of 4 x 4096
+//    190 (two tiles 213), 2^15 384 (430), 1023 of 8 x 4096 40 (49).
 //  * shares until 2048 waves (4097 tokens of 4 x 1000 fp32 45.0; 4096 waves 47.6), each wave with a
 //    whole line of every token at least; at most 16, as each costs a read of the sums (600 tokens of 8 x
 //    4096 33.9, with 32 37.3; 1023 of 8 x 2052 fp32 61.7 and 73.3), 32 where there are few blocks
@@ -1106,12 +1109,12 @@ constexpr int gate_waves(int tiles) { return tiles == 1 ? 16 : tiles == 2 ? (N =
 
 GateLaunch gate_launch(const PreShape& s, int n) {
     GateLaunch l;
-    l.wide = s.B > (n == 4 ? 20480 : 2048);
+    l.wide = n == 8 && s.B > 2048;
     l.tt = s.B <= 16 ? 1 : s.B <= (n == 4 ? 512 : 64) ? 2 : 4;
     l.waves = n == 4 ? gate_waves<4>(l.tt) : gate_waves<8>(l.tt);
     int64_t lines = l.waves;  // at least, of a share
     if (l.wide) {
-        l.waves = n == 4 ? gate_wide_waves<4>() : gate_wide_waves<8>();
+        l.waves = kGateWideWaves;
         l.tt *= l.waves;
         lines = 4;
     }
@@ -1191,9 +1194,10 @@ int launch_pre_fwd(const PreShape& s, const void* X, const void* W, const float*
                    void* U, float* h, float* H, float* q, float* rms, float* part, hipStream_t stream) {
     const GateLaunch l = gate_launch(s, N);
     const v4u *x = static_cast<const v4u*>(X), *w = static_cast<const v4u*>(W);
-    auto gate = l.wide      ? pre_gate_wide_kernel<DX, N>
-                : l.tt == 1 ? pre_gate_kernel<DX, N, 1, gate_waves<N>(1)>
+    auto gate = l.tt == 1   ? pre_gate_kernel<DX, N, 1, gate_waves<N>(1)>
                 : l.tt == 2 ? pre_gate_kernel<DX, N, 2, gate_waves<N>(2)> : pre_gate_kernel<DX, N, 4, gate_waves<N>(4)>;
+    if constexpr (N == 8)
+        if (l.wide) gate = pre_gate_wide_kernel<DX>;
     const uint32_t tiles = static_cast<uint32_t>(l.tiles), per_xcd = static_cast<uint32_t>(cdiv(l.tiles * l.splits, 8));
     launch_kernel(gate, dim3(8 * per_xcd), dim3(64 * l.waves), 0, stream, x, w, part, s.B, s.steps, l.per, tiles,
                   per_xcd);
