@@ -306,7 +306,8 @@ int birkhoff8_mix_bwd_ex(const float* P, const void* X, const void* dY, int x_dt
  * C      > 0, a multiple of 8 for BF16 or 4 for F32, at most 2^20 (BIRKHOFF4_ERR_CHANNELS, _SIZE);
  *        B at most 2^26.
  * A token with a NaN or infinite value has NaN (or infinite) outputs; the others are not touched
- * by it. The result does not depend on timing: no atomics, fixed orders of sums. */
+ * by it. |v|^2 is an fp32 sum: where it passes fp32's range, r = 0, and where it is 0 with eps = 0, r is
+ * infinite. The result does not depend on timing: no atomics, fixed orders of sums. */
 int birkhoff4_pre_fwd(const void* X, const void* W, int x_dtype, const float* alpha, const float* bias, float eps, void* U,
                       float* h, float* H, float* q, float* rms, void* work, int64_t work_bytes, int64_t B, int64_t C,
                       hipStream_t stream);

@@ -451,7 +451,7 @@ __global__ __launch_bounds__(64 * kReadWaves) void pre_read_kernel(const float* 
 // below. `share` waves of the block take four consecutive tokens, one after the other, sharing
 // their columns; the first of these waves forms G. A block leaves one row of sums for dbias and
 // dalpha. Bound: HBM; many short blocks that cover whole tokens stream best (2^15 tokens of 4 x 4096
-// bf16 212 us, 6.3 TB/s; a resident grid that loops 254, a wave per token 236).
+// bf16 218 us, 6.2 TB/s; a resident grid that loops 254, a wave per token 236).
 constexpr int kTokenStep = 32;  // tokens of a stage of the products over tokens
 constexpr int kHalf = 16;
 constexpr int kDotWaves = 8;
@@ -690,8 +690,8 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 //
 // Bound: HBM, by the width of the rows' pieces. A copy (two arrays read, one written) by waves that
 // take 128, 256 or 512 bytes of each row reaches 5.0, 5.5 and 6.5 TB/s here, so a block's waves take
-// neighbouring pieces, 512 bytes together, of one or two streams: 2^15 tokens of 4 x 4096 bf16 648 -> 578 us
-// (6.1 TB/s), 2^13 of 8 x 4096 388 -> 350 (4.9 TB/s). Loading a whole stage ahead (n = 4 with
+// neighbouring pieces, 512 bytes together, of one or two streams: 2^15 tokens of 4 x 4096 bf16 648 -> 578 us,
+// 2^13 of 8 x 4096 388 -> 350 (with G as three bf16 values instead of two 596, 5.9 TB/s, and 370, 4.7 TB/s). Loading a whole stage ahead (n = 4 with
 // 128-byte pieces, 681 us) or leaving the offsets' arithmetic out of the loop (664) did not help.
 template <int DX, int N>
 struct Back {
@@ -1093,9 +1093,10 @@ struct GateLaunch {
 
 // Tokens of a block and its waves, and shares of the row, us of the whole forward:
 //  * up to 16 tokens one tile and 16 waves: 1 token of 4 x 4096 bf16 8.1, of 8 x 4096 13.7.
-//  * n = 4 up to 512 two tiles and 16 waves: 96 tokens of 4 x 4096 11.5, four tiles and 4 waves 12.4; 300
-//    13.8 and 14.8; 600 23 and 19.3. n = 8 up to 64 two tiles and 8 waves (more do not fit the
-//    registers): 32 tokens of 8 x 4096 16.6, four tiles 19.2; 100 of 8 x 2048 18.1 and 17.5.
+//  * n = 4 up to 512 two tiles and 16 waves: 96 tokens of 4 x 4096 11.4, four tiles and 4 waves 11.8; 300
+//    14.3 and 15.6; 600 19.3 and 18.6, 1000 of 4 x 1024 12.5 and 14.1. n = 8 up to 64 two tiles and 8 waves
+//    (more do not fit the registers): 32 tokens of 8 x 4096 17.0, four tiles 18.4; 64 17.3 and 19.2; 100 of
+//    8 x 2048 15.7 and 16.8, 600 of 8 x 4096 47 and 33.5.
 //  * else four tiles, each row of W read once for 64 tokens, and 4 waves: 16 K tokens of 4 x 4096
 //    190 (two tiles 213), 2^15 384 (430), 1023 of 8 x 4096 40 (49).
 //  * shares until 2048 waves (4097 tokens of 4 x 1000 fp32 45.0; 4096 waves 47.6), each wave with a
