@@ -265,8 +265,9 @@ __global__ __launch_bounds__(64 * GW, GW > 8 ? GW / 4 : 2) void pre_gate_kernel(
 // 2 K tokens on; whole forward in us, without it in brackets: 2049 tokens of 8 x 512 bf16 29 (32), 2049 of 8 x
 // 4096 81 (83), 3000 of 8 x 4096 101 (117), 6000 166 (209), 32 K 790 (996), 8000 of 8 x 1024 fp32 178 (228); slower
 // at few of the sizes tried (4096 of 8 x 512 37 (33), 2500 of 8 x 4096 fp32 272 (252)). With n = 4 such a form,
-// of eight waves, was slower at all widths from 128 channels on (20481 tokens of 4 x 4096 297 and 256, 2^15 403
-// and 388, 65537 of 4 x 512 137 and 120; 10^6 of 4 x 8 189 and 228) and is not there.
+// of eight waves, is not there: it was slower at most sizes (20481 tokens of 4 x 4096 297 (256), 2^15 403 (388),
+// 65537 of 4 x 512 137 (120)) and faster only where its 512-token blocks came out even (2^15 of 4 x 2048 196
+// (206), 2^18 of 4 x 128 128 (139)) or rows were very short (10^6 of 4 x 8 189 (228)).
 constexpr int kGateWideWaves = 4;
 
 template <int DX>
@@ -691,8 +692,9 @@ __global__ __launch_bounds__(64 * kDotWaves) void pre_dot_kernel(
 // Bound: HBM, by the width of the rows' pieces. A copy (two arrays read, one written) by waves that
 // take 128, 256 or 512 bytes of each row reaches 5.0, 5.5 and 6.5 TB/s here, so a block's waves take
 // neighbouring pieces, 512 bytes together, of one or two streams: 2^15 tokens of 4 x 4096 bf16 648 -> 578 us,
-// 2^13 of 8 x 4096 388 -> 350 (with G as three bf16 values instead of two 596, 5.9 TB/s, and 370, 4.7 TB/s). Loading a whole stage ahead (n = 4 with
-// 128-byte pieces, 681 us) or leaving the offsets' arithmetic out of the loop (664) did not help.
+// 2^13 of 8 x 4096 388 -> 350 (with G as three bf16 values instead of two 596, 5.9 TB/s, and 370, 4.7 TB/s).
+// Loading a whole stage ahead (n = 4 with 128-byte pieces, 681 us) or leaving the offsets' arithmetic out
+// of the loop (664) did not help.
 template <int DX, int N>
 struct Back {
     // n = 8: half as many channels, as the sums of 5 row tiles fill the registers
