@@ -50,9 +50,9 @@ enum {
     BIRKHOFF4_ERR_LAUNCH = -10,   /* kernel launch failed (hipGetLastError) */
     BIRKHOFF4_ERR_VARIANT = -11,  /* unknown forward variant */
     BIRKHOFF4_ERR_ETA = -12,      /* eta not positive and finite */
-    BIRKHOFF4_ERR_CHANNELS = -13, /* stream width C negative or not a whole number of 16-byte chunks */
+    BIRKHOFF4_ERR_CHANNELS = -13, /* width C negative, or zero or no whole number of 16-byte chunks where that is needed */
     BIRKHOFF4_ERR_EPS = -14,      /* eps negative, infinite or NaN */
-    BIRKHOFF4_ERR_WORK = -15,     /* the workspace is smaller than birkhoff*_pre_work says */
+    BIRKHOFF4_ERR_WORK = -15,     /* the workspace is smaller than the call's _work says */
     BIRKHOFF4_ERR_DROP = -16      /* dropout probability outside [0, 1) */
 };
 
@@ -366,6 +366,29 @@ int birkhoff8_post_fwd(const void* H, int h_dtype, const void* X, const float* h
 int birkhoff8_post_bwd(const float* P, const void* X, const float* h, const void* Z, const void* dY, int x_dtype, double p,
                        const int64_t* rng, void* dX, void* dZ, float* dh, float* dP, void* dH, int dh_dtype, int64_t B,
                        int64_t C, hipStream_t stream);
+
+/* Layer norm over rows of C values, in front of the layer's branch: with mu the mean of a row x and
+ * s = (mean((x - mu)^2) + eps)^(-1/2),
+ *   y = (x - mu) s weight + bias.
+ *
+ * X      [B][C] in x_dtype (F32 or BF16); any C from 1 to 2^20, B up to 2^31.
+ * weight, bias  [C] in w_dtype (F32 or BF16, whatever x_dtype is); NULL for ones and for zeros.
+ * Y      [B][C] output in x_dtype (bf16 rounded to nearest even once); sums are fp32.
+ * mean, rstd  [B] fp32 outputs mu and s, which the backward needs; NULL where they are not wanted.
+ * eps >= 0 and finite (BIRKHOFF4_ERR_EPS). A row with a NaN or infinite value has NaN outputs; the
+ * others are not touched by it. The arrays begin at 16 bytes, their rows at any value. */
+int birkhoff4_norm_fwd(const void* X, int x_dtype, const void* weight, const void* bias, int w_dtype, float eps, void* Y,
+                       float* mean, float* rstd, int64_t B, int64_t C, hipStream_t stream);
+
+/* Backward of birkhoff4_norm_fwd: from X, weight, mean, rstd and dY [B][C] (x_dtype), writes
+ * dX [B][C] (x_dtype), dweight and dbias [C] (w_dtype), each where it is not NULL. With B = 0 the
+ * sums are written as zeros. work: a workspace of birkhoff4_norm_work(B, C, x_dtype) bytes, needed
+ * where dweight or dbias is; its contents before and after mean nothing. The sums over the rows are
+ * fp32, in an order that the sizes alone decide. */
+int birkhoff4_norm_bwd(const void* X, int x_dtype, const void* weight, int w_dtype, const float* mean, const float* rstd,
+                       const void* dY, void* dX, void* dweight, void* dbias, void* work, int64_t work_bytes, int64_t B,
+                       int64_t C, hipStream_t stream);
+int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype);
 
 /* Human-readable text for a return code (static storage). */
 const char* birkhoff4_strerror(int code);

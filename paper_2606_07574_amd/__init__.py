@@ -22,6 +22,8 @@ a GPU, the calls raise.
     Y, P, _, _ = post_fwd(H, X, h, Z, p, rng); dX, dH, dh, dZ = post_bwd(P, X, h, Z, dY, p, rng)
     Y = post(H, X, h, Z, p, rng)      # autograd-aware: Y = P X + h drop(Z), the branch written back
     Y = connect(X, W, alpha, bias, branch)  # pre, the caller's branch, post: a whole layer's update
+    y, mean, rstd = norm_fwd(x, weight, bias); dx, dw, db = norm_bwd(x, weight, mean, rstd, dy)
+    y = norm(x, weight, bias)         # autograd-aware layer norm; connect(..., norm=(weight, bias)) has it too
 """
 from __future__ import annotations
 
@@ -41,6 +43,7 @@ NOT_CONVERGED, NON_FINITE = -1, -2
 DEFAULT_TOL = 1e-6
 DEFAULT_MAX_ITER = 64
 DEFAULT_EPS = 1e-6
+DEFAULT_NORM_EPS = 1e-5
 
 _lib = None
 
@@ -84,6 +87,8 @@ def _load():
         "birkhoff8_mix_bwd_ex": [vp, vp, vp, i32, vp, vp, vp, i32, i64, i64, st],
         "birkhoff8_mix_fwd": [vp, i32, vp, i32, vp, vp, vp, vp, i64, i64, f32, i32, st],
         "birkhoff8_mix_bwd": [vp, vp, vp, i32, vp, vp, i64, i64, st],
+        "birkhoff4_norm_fwd": [vp, i32, vp, vp, i32, f32, vp, vp, vp, i64, i64, st],
+        "birkhoff4_norm_bwd": [vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, st],
         "birkhoff4_version": [],
     }
     for n in (4, 8):
@@ -99,6 +104,8 @@ def _load():
         fn = getattr(lib, f"birkhoff{n}_pre_work")
         fn.argtypes = [i64, i64, i32, i32]
         fn.restype = i64
+    lib.birkhoff4_norm_work.argtypes = [i64, i64, i32]
+    lib.birkhoff4_norm_work.restype = i64
     lib.birkhoff4_strerror.argtypes = [ctypes.c_int]
     lib.birkhoff4_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -763,13 +770,111 @@ def post(H: torch.Tensor, X: torch.Tensor, h: torch.Tensor, Z: torch.Tensor, p: 
     return post_fwd(_whole(H), _whole(X), _whole(h), _whole(Z), p, rng, tol, max_iter)[0]
 
 
+def _normed(x: torch.Tensor, weight: torch.Tensor | None, bias: torch.Tensor | None):
+    """Checks norm's rows [..., C] and parameters [C] (each may be None); returns (rows, C, the
+    parameters' dtype code)."""
+    if not x.is_cuda:
+        raise Birkhoff4Error("x must be a GPU tensor (no CPU path)")
+    if x.dim() < 1 or x.shape[-1] < 1:
+        raise ValueError(f"x must have shape [..., C] with C >= 1, got {tuple(x.shape)}")
+    if not x.is_contiguous():
+        raise ValueError("x must be contiguous")
+    _dtype_code(x)
+    C = x.shape[-1]
+    code = F32
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            if weight is not None and t.dtype != weight.dtype:
+                raise TypeError(f"weight and bias must have one dtype, got {weight.dtype} and {t.dtype}")
+            code = _dtype_code(t)
+            _dense(t, name, (C,), t.dtype, x)
+    return x.numel() // C, C, code
+
+
+def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+             eps: float = DEFAULT_NORM_EPS):
+    """Layer norm over the last axis, what a branch has in front of it: y = (x - mean) rstd weight + bias
+    with rstd = (mean((x - mean)^2) + eps)^(-1/2).
+
+    x: [..., C] float32 or bfloat16, any C up to 2^20; weight, bias: [C] float32 or bfloat16 (one dtype
+    for both, x's or another) or None for ones and zeros. Returns (y like x, mean [...], rstd [...]),
+    the last two float32, for norm_bwd."""
+    rows, C, code = _normed(x, weight, bias)
+    y = torch.empty_like(x)
+    mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
+    rstd = torch.empty_like(mean)
+    _call("birkhoff4_norm_fwd", x, _ptr(x), _dtype_code(x), _ptr(weight), _ptr(bias), code, float(eps), _ptr(y), _ptr(mean),
+          _ptr(rstd), rows, C)
+    return y, mean, rstd
+
+
+def _norm_bwd(x, weight, code, mean, rstd, dy, want):
+    """(dx, dweight, dbias), each None where `want` does not ask for it; code: the parameters' dtype."""
+    rows, C, _ = _normed(x, weight, None)
+    _dense(dy, "dy", x.shape, x.dtype, x)
+    _dense(mean, "mean", x.shape[:-1], torch.float32, x)
+    _dense(rstd, "rstd", x.shape[:-1], torch.float32, x)
+    params = torch.bfloat16 if code == BF16 else torch.float32
+    dx = torch.empty_like(x) if want[0] else None
+    dw, db = (torch.empty(C, dtype=params, device=x.device) if k else None for k in want[1:])
+    work = None
+    if want[1] or want[2]:
+        size = _load().birkhoff4_norm_work(rows, C, _dtype_code(x))
+        if size < 0:
+            _check(size)
+        work = torch.empty(size, dtype=torch.uint8, device=x.device)
+    _call("birkhoff4_norm_bwd", x, _ptr(x), _dtype_code(x), _ptr(weight), code, _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dx),
+          _ptr(dw), _ptr(db), _ptr(work), 0 if work is None else work.numel(), rows, C)
+    return dx, dw, db
+
+
+def norm_bwd(x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor):
+    """Backward of norm_fwd from its x, weight, mean and rstd, and dy (like x): (dx like x, dweight,
+    dbias [C] of weight's dtype, float32 without one)."""
+    return _norm_bwd(x, weight, F32 if weight is None else _dtype_code(weight), mean, rstd, dy, (True, True, True))
+
+
+class NormFn(torch.autograd.Function):
+    """norm_fwd with gradients for x, weight and bias; the backward is one pass over x and dy."""
+
+    @staticmethod
+    def forward(ctx, x, weight=None, bias=None, eps=DEFAULT_NORM_EPS):
+        x = _whole(x)
+        weight, bias = (None if t is None else _whole(t) for t in (weight, bias))
+        y, mean, rstd = norm_fwd(x, weight, bias, eps)
+        ctx.save_for_backward(x, weight, mean, rstd)
+        ctx.code = _dtype_code(weight if weight is not None else bias) if weight is not None or bias is not None else F32
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        x, weight, mean, rstd = ctx.saved_tensors
+        return (*_norm_bwd(x, weight, ctx.code, mean, rstd, _whole(dy), ctx.needs_input_grad[:3]), None)
+
+
+def norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,
+         eps: float = DEFAULT_NORM_EPS) -> torch.Tensor:
+    """norm_fwd under autograd: y alone, with gradients for x, weight and bias. Like pre and post it has
+    no second and no forward-mode derivatives: both raise."""
+    if _graph(*(t for t in (x, weight, bias) if t is not None)):
+        return NormFn.apply(x, weight, bias, eps)
+    return norm_fwd(_whole(x), *(None if t is None else _whole(t) for t in (weight, bias)), eps)[0]
+
+
 def connect(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.Tensor, branch, p: float = 0.0,
             rng: torch.Tensor | None = None, eps: float = DEFAULT_EPS, tol: float = DEFAULT_TOL,
-            max_iter: int = DEFAULT_MAX_ITER) -> torch.Tensor:
+            max_iter: int = DEFAULT_MAX_ITER, norm: tuple | None = None, norm_eps: float = DEFAULT_NORM_EPS) -> torch.Tensor:
     """A hyper-connection layer around `branch` (Sec. 2.1: x <- H^res x + (H^post)^T F(H^pre x)):
-    pre, Z = branch(U) with U and Z [..., C], post. Under autograd or without."""
+    pre, Z = branch(U) with U and Z [..., C], post. Under autograd or without. norm: (weight, bias) of a
+    layer norm of U in front of the branch (each [C] or None), or None for no norm."""
     U, h, H, X = pre(X, W, alpha, bias, eps)
+    if norm is not None:
+        U = _norm(U, *norm, norm_eps)
     return post(H, X, h, branch(U), p, rng, tol, max_iter)
+
+
+_norm = norm  # connect's argument has its name
 
 
 def version() -> int:
