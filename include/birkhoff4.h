@@ -45,7 +45,7 @@ enum {
     BIRKHOFF4_ERR_DTYPE = -5,     /* unknown storage dtype code */
     BIRKHOFF4_ERR_ALIGN = -6,     /* an array is not 16-byte aligned */
     BIRKHOFF4_ERR_OVERLAP = -7,   /* an output overlaps another argument */
-    BIRKHOFF4_ERR_STEPS = -8,     /* Sinkhorn step count out of range */
+    BIRKHOFF4_ERR_STEPS = -8,     /* step count of Sinkhorn or of the orthogonalisation out of range */
     BIRKHOFF4_ERR_DEVICE = -9,    /* HIP device query failed */
     BIRKHOFF4_ERR_LAUNCH = -10,   /* kernel launch failed (hipGetLastError) */
     BIRKHOFF4_ERR_VARIANT = -11,  /* unknown forward variant */
@@ -389,6 +389,41 @@ int birkhoff4_norm_bwd(const void* X, int x_dtype, const void* weight, int w_dty
                        const void* dY, void* dX, void* dweight, void* dbias, void* work, int64_t work_bytes, int64_t B,
                        int64_t C, hipStream_t stream);
 int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype);
+
+/* Matrices taken towards their nearest orthogonal ones (rows or columns orthonormal, whichever are
+ * fewer) by Newton-Schulz products: X = G / (|G|_F + eps), then for each step k, with A = X X^T
+ * (for rows > cols the same of the transpose),
+ *   X <- a_k X + (b_k A + c_k A^2) X,
+ * which keeps the singular vectors and takes each singular value s to a s + b s^3 + c s^5.
+ *
+ * G      [B][rows][cols] in g_dtype (F32 or BF16); out the same in out_dtype.
+ * coefs  host array of 3 * steps floats a, b, c, read before the call returns; 1 <= steps <= 64
+ *        (BIRKHOFF4_ERR_STEPS). Entries of X, A and b A + c A^2 have to stay below 16 in magnitude,
+ *        as they do where the steps keep the singular values below 2; what does not ends as NaN.
+ * eps    >= 0 and finite (BIRKHOFF4_ERR_EPS). The norm is a 64-bit sum: no finite fp32 matrix is
+ *        too large or too small. A zero matrix with eps > 0 gives zeros; one with a NaN or infinite
+ *        value gives NaN everywhere; the others of the batch are not touched by it.
+ * An fp32 result is what fp32 products give. For a bf16 result the products' factors are rounded to
+ * fp16 (11 bits, a quarter of the rounding of the result itself), their sums are fp32.
+ * work   workspace of birkhoff4_orth_work(B, rows, cols, out_dtype) bytes, 16-byte aligned, in use until
+ *        the call's work on `stream` has ended. The other arrays may begin at any value. No output may
+ *        overlap another argument. rows and cols up to 2^20, the smaller of them up to 2^16, B up to
+ *        2^26; a zero among them is a no-op. The result does not depend on timing. */
+int birkhoff4_orth(const void* G, int g_dtype, void* out, int out_dtype, const float* coefs, int steps, float eps, void* work,
+                   int64_t work_bytes, int64_t B, int64_t rows, int64_t cols, hipStream_t stream);
+
+/* A weight update with momentum along orthogonalised directions, in place:
+ *   M <- momentum M + G,   U = G + momentum M (nesterov != 0) or M,
+ *   W <- (1 - r decay) W - r scale orth(U),   r = lr *lr_at.
+ *
+ * W      [B][rows][cols] in w_dtype (F32 or BF16, rounded to nearest even); M the same in fp32.
+ * lr_at  a float in device memory, read when the work runs (a replayed graph takes what it is by
+ *        then), or NULL for one.
+ * The other arguments as above, with w_dtype for out_dtype. */
+int birkhoff4_orth_step(void* W, int w_dtype, const void* G, int g_dtype, float* M, float momentum, int nesterov, float lr,
+                        const float* lr_at, float decay, float scale, const float* coefs, int steps, float eps, void* work,
+                        int64_t work_bytes, int64_t B, int64_t rows, int64_t cols, hipStream_t stream);
+int64_t birkhoff4_orth_work(int64_t B, int64_t rows, int64_t cols, int out_dtype);
 
 /* Human-readable text for a return code (static storage). */
 const char* birkhoff4_strerror(int code);

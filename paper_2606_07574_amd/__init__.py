@@ -24,10 +24,14 @@ a GPU, the calls raise.
     Y = connect(X, W, alpha, bias, branch)  # pre, the caller's branch, post: a whole layer's update
     y, mean, rstd = norm_fwd(x, weight, bias); dx, dw, db = norm_bwd(x, weight, mean, rstd, dy)
     y = norm(x, weight, bias)         # autograd-aware layer norm; connect(..., norm=(weight, bias)) has it too
+    O = orth(G)                       # matrices towards their nearest orthogonal ones (Newton-Schulz products)
+    orth_step(W, G, M, lr)            # momentum, orth and the write of the weights, in place
 """
 from __future__ import annotations
 
 import ctypes
+import functools
+import math
 import os
 
 import torch
@@ -44,6 +48,10 @@ DEFAULT_TOL = 1e-6
 DEFAULT_MAX_ITER = 64
 DEFAULT_EPS = 1e-6
 DEFAULT_NORM_EPS = 1e-5
+# a, b, c of orth's steps: steep at zero, and singular values from 0.003 on end within 0.68..1.21
+ORTH_COEFS = (3.4445, -4.7750, 2.0315)
+ORTH_STEPS = 5
+DEFAULT_ORTH_EPS = 1e-7
 
 _lib = None
 
@@ -89,6 +97,8 @@ def _load():
         "birkhoff8_mix_bwd": [vp, vp, vp, i32, vp, vp, i64, i64, st],
         "birkhoff4_norm_fwd": [vp, i32, vp, vp, i32, f32, vp, vp, vp, i64, i64, st],
         "birkhoff4_norm_bwd": [vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i64, i64, i64, st],
+        "birkhoff4_orth": [vp, i32, vp, i32, vp, i32, f32, vp, i64, i64, i64, i64, st],
+        "birkhoff4_orth_step": [vp, i32, vp, i32, vp, f32, i32, f32, vp, f32, f32, vp, i32, f32, vp, i64, i64, i64, i64, st],
         "birkhoff4_version": [],
     }
     for n in (4, 8):
@@ -106,6 +116,8 @@ def _load():
         fn.restype = i64
     lib.birkhoff4_norm_work.argtypes = [i64, i64, i32]
     lib.birkhoff4_norm_work.restype = i64
+    lib.birkhoff4_orth_work.argtypes = [i64, i64, i64, i32]
+    lib.birkhoff4_orth_work.restype = i64
     lib.birkhoff4_strerror.argtypes = [ctypes.c_int]
     lib.birkhoff4_strerror.restype = ctypes.c_char_p
     _lib = lib
@@ -875,6 +887,103 @@ def connect(X: torch.Tensor, W: torch.Tensor, alpha: torch.Tensor, bias: torch.T
 
 
 _norm = norm  # connect's argument has its name
+
+
+@functools.lru_cache(maxsize=64)
+def _coefs_array(coefs: tuple, steps: int):
+    if len(coefs) == 3 and not any(isinstance(c, tuple) for c in coefs):
+        coefs = (coefs,) * steps
+    if len(coefs) != steps or any(not isinstance(c, tuple) or len(c) != 3 for c in coefs):
+        raise ValueError(f"coefs must be three numbers or {steps} triples of them")
+    flat = [float(v) for c in coefs for v in c]
+    return (ctypes.c_float * len(flat))(*flat)
+
+
+def _steps(coefs, steps: int):
+    """orth's coefficients as the library takes them: a host array of `steps` triples."""
+    steps = int(steps)
+    if not 1 <= steps <= 64:
+        _check(-8)
+    return _coefs_array(tuple(tuple(c) if isinstance(c, (list, tuple)) else c for c in coefs), steps), steps
+
+
+def _matrices(t: torch.Tensor, name: str):
+    """Checks [..., rows, cols] on the GPU; returns (matrices, rows, cols)."""
+    if not t.is_cuda:
+        raise Birkhoff4Error(f"{name} must be a GPU tensor (no CPU path)")
+    if t.dim() < 2:
+        raise ValueError(f"{name} must have shape [..., rows, cols], got {tuple(t.shape)}")
+    rows, cols = t.shape[-2:]
+    return t.numel() // (rows * cols) if rows and cols else 0, rows, cols
+
+
+def _orth_work(t: torch.Tensor, B: int, rows: int, cols: int) -> torch.Tensor:
+    size = _load().birkhoff4_orth_work(B, rows, cols, _dtype_code(t))
+    if size < 0:
+        _check(size)
+    return torch.empty(size, dtype=torch.uint8, device=t.device)
+
+
+def _recorded(*inputs: torch.Tensor) -> None:
+    if _graph(*inputs) and (any(t.requires_grad for t in inputs) or
+                            any(forward_ad.unpack_dual(t).tangent is not None for t in inputs)):
+        raise RuntimeError("orth and orth_step have no derivative: call them under torch.no_grad() or on detached tensors")
+
+
+def orth(G: torch.Tensor, steps: int = ORTH_STEPS, coefs=ORTH_COEFS, eps: float = DEFAULT_ORTH_EPS) -> torch.Tensor:
+    """Each matrix of G [..., rows, cols] (float32 or bfloat16) taken towards its nearest orthogonal one
+    by Newton-Schulz products: X = G / (|G|_F + eps), then `steps` times, with A = X X^T (for rows > cols
+    the same of the transpose), X <- a X + (b A + c A^2) X. The singular vectors stay, and each singular
+    value s goes to a s + b s^3 + c s^5.
+
+    coefs: (a, b, c), or one such triple for each step; entries of X, A and b A + c A^2 have to stay
+    below 16. Returns a tensor like G; in float32 with what float32 products give, in bfloat16 with
+    products of values rounded to 11 bits. No derivative: an input that autograd records is refused."""
+    _recorded(G)
+    B, rows, cols = _matrices(G, "G")
+    G = G.contiguous()
+    array, steps = _steps(coefs, steps)
+    out = torch.empty_like(G)
+    work = _orth_work(G, B, rows, cols)
+    _call("birkhoff4_orth", G, _ptr(G), _dtype_code(G), _ptr(out), _dtype_code(G), array, steps, float(eps), _ptr(work),
+          work.numel(), B, rows, cols)
+    return out
+
+
+def orth_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float | torch.Tensor, momentum: float = 0.95,
+              nesterov: bool = True, decay: float = 0.0, scale: float | None = None, steps: int = ORTH_STEPS,
+              coefs=ORTH_COEFS, eps: float = DEFAULT_ORTH_EPS) -> None:
+    """One update of the weights W [..., rows, cols] (float32 or bfloat16) from their gradient G (either
+    dtype) along orthogonalised directions, W and the momentum M (float32) in place:
+    M <- momentum M + G, U = G + momentum M (nesterov) or M, W <- (1 - lr decay) W - lr scale orth(U).
+
+    lr: a number, or one float32 on the GPU, read when the work runs (for a captured graph). scale:
+    sqrt(max(1, rows / cols)) by default. Weights stacked along leading axes are updated each by itself.
+    Call it under torch.no_grad() where W is a parameter."""
+    B, rows, cols = _matrices(W, "W")
+    _recorded(W, G, M)
+    code = _dtype_code(W)
+    for t, name, dtype in ((W, "W", W.dtype), (M, "M", torch.float32)):
+        _dense(t, name, W.shape, dtype, W)
+    if not isinstance(G, torch.Tensor) or G.shape != W.shape:
+        raise ValueError(f"G must have the shape of W, {tuple(W.shape)}")
+    G = G.contiguous()
+    _dense(G, "G", W.shape, G.dtype, W)
+    at = None
+    if isinstance(lr, torch.Tensor):
+        if lr.numel() != 1:
+            raise ValueError("lr must be a number or one float32 on the GPU")
+        _dense(lr, "lr", lr.shape, torch.float32, W)
+        at, lr = lr, 1.0
+    array, steps = _steps(coefs, steps)
+    if scale is None:
+        scale = math.sqrt(max(1.0, rows / cols)) if cols else 1.0
+    work = _orth_work(W, B, rows, cols)
+    _call("birkhoff4_orth_step", W, _ptr(W), code, _ptr(G), _dtype_code(G), _ptr(M), float(momentum), int(bool(nesterov)),
+          float(lr), _ptr(at), float(decay), float(scale), array, steps, float(eps), _ptr(work), work.numel(), B, rows, cols)
+    for t in (W, M):  # autograd knows that they have changed
+        if not t.is_inference():
+            torch.autograd.graph.increment_version(t)
 
 
 def version() -> int:

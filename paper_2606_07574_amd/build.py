@@ -10,7 +10,7 @@ import subprocess
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SOURCES = [os.path.join(PKG, "csrc", f) for f in ("birkhoff4.hip", "pre.hip", "norm.hip")]
+SOURCES = [os.path.join(PKG, "csrc", f) for f in ("birkhoff4.hip", "pre.hip", "norm.hip", "orth.hip")]
 INCLUDE = os.path.join(ROOT, "include")
 LIB = os.path.join(PKG, "libbirkhoff4.so")
 ARCH = "gfx950"
