@@ -11,9 +11,15 @@
 // fp16 rounding is `hi` and the fp16 rounding of what is left `lo`: 22 bits for values above 2^-14, and
 // never further off than 2^-37, for values below 16 (singular values stay below 1.3 in the usual steps).
 // Results in fp32 take three products, hi hi + hi lo + lo hi: what fp32 inputs would give (relative error
-// of 512 x 512 after five steps 1.4e-6, in fp32 1.3e-6). Results that are rounded to bf16 take hi hi alone
-// (1.3e-3 there, where the rounding to bf16 is 1.7e-3); a X is added from both pieces all the same, as it
-// is what E X corrects, and the error of fp16 in it would be amplified (1.1e-2 for a matrix of low rank).
+// of 512 x 512 after five steps 1.4e-6, in fp32 1.3e-6). Results that are rounded to bf16 take hi hi alone,
+// and what the rounding to 11 bits would spoil most is kept out of the products:
+//   * a X is added from both pieces: it is what E X corrects, and the steps behind amplify its error (a
+//     matrix of low rank 1.1e-2 off without that, 2e-4 with it);
+//   * the diagonals D of A and F of E, the large entries, whose roundings all go one way where the singular
+//     values are near to each other, are fp32 numbers of their own, and zeros in A and E as stored:
+//     (A^2)_ij = (D_i + D_j) A_ij + (A A)_ij off the diagonal, D_i^2 + (A A)_ii on it, and X <- (a + F_i) X_i + (E X)_i
+//     (a spread 400 x 3200 3.6e-3 off without, 0.45e-3 with them).
+// What is left, 0.2e-3 to 1.1e-3, is less than the result's own rounding to bf16, 1.7e-3.
 //
 // The products are of rows with rows (both operands have the summed index along their rows), so X is kept
 // in both orders.
@@ -209,15 +215,19 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const doubl
 // ---------------------------------------------------------------------------
 enum { GRAM, POLY, NEXT, LAST };
 
-// acc_ij = sum_k P_ik Q_jk in units of kUnit^2, and with src a stored matrix the result
-// keep src_ij + add acc_ij / kUnit, stored as own_ij and as turned_ji (GRAM, POLY: of a symmetric result,
-// whose tiles below the diagonal alone are computed; NEXT: the next X). LAST: the value itself goes to
-// the caller's array.
+// acc_ij = sum_k P_ik Q_jk in units of kUnit^2. Results, stored as own_ij and as turned_ji:
+//   GRAM  A = acc
+//   POLY  E = keep A + add A^2 with A^2 from acc, src = A and its diagonal as above
+//   NEXT  (keep + F_i) src_ij + acc, the next X;  LAST: the same, which goes to the caller's array
+// GRAM and POLY have a symmetric result: its tiles below the diagonal alone are computed.
 struct Product {
     Plane P, Q, src, own, turned;
+    const float* src_diag;  // D (POLY) or F (NEXT, LAST), `side` a matrix
+    float* own_diag;        // D (GRAM) or F (POLY)
     float keep, add;
+    int64_t side;
     int lines;    // of 128 bytes in a row of P and Q
-    int ti, tj;   // tiles
+    int tj;       // tiles along j
 };
 
 // What becomes of the last step's values: out (rows x cols, `tall`: out_ji), or the weights
@@ -315,17 +325,30 @@ __global__ __launch_bounds__(256) void orth_product_kernel(Product g, Result res
                 tile[row * kTilePitch + col] = acc[i][j][r];
             }
     __syncthreads();
-    const float add = g.add / kUnit;
     const int64_t i0 = static_cast<int64_t>(ti) * kTile, j0 = static_cast<int64_t>(tj) * kTile;
+    const float* sd = KIND != GRAM ? g.src_diag + matrix * g.side : nullptr;
+    float* od = KIND == GRAM || KIND == POLY ? g.own_diag + matrix * g.side : nullptr;
 #pragma unroll 1
     for (int task = threadIdx.x; task < kTile * kTile / 8; task += 256) {
         const int r = task / 16, c = 8 * (task % 16);
-        float v[8], s[8];
-        if constexpr (KIND != GRAM) load8<SPLIT>(g.src, matrix, i0 + r, j0 + c, s);
+        const bool diag = (KIND == GRAM || KIND == POLY) && ti == tj && r / 8 == c / 8;
+        float v[8], s[8], di = 0.f;
+        if constexpr (KIND != GRAM) {
+            load8<SPLIT>(g.src, matrix, i0 + r, j0 + c, s);
+            di = sd[i0 + r];
+        }
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
-            v[e] = add * tile[r * kTilePitch + c + e];
-            if constexpr (KIND != GRAM) v[e] = __builtin_fmaf(g.keep, s[e], v[e]);
+            const float t = tile[r * kTilePitch + c + e] / kUnit;
+            if constexpr (KIND == GRAM) v[e] = t;
+            if constexpr (KIND == POLY) v[e] = __builtin_fmaf(__builtin_fmaf(g.add, di + sd[j0 + c + e], g.keep), s[e], g.add * t);
+            if constexpr (KIND == NEXT || KIND == LAST) v[e] = __builtin_fmaf(g.keep + di, s[e], t);
+            if (diag && e == r % 8) {
+                const float one = t / kUnit;
+                if constexpr (KIND == GRAM) od[i0 + r] = one;
+                if constexpr (KIND == POLY) od[i0 + r] = __builtin_fmaf(g.keep, di, g.add * __builtin_fmaf(di, di, one));
+                v[e] = 0.f;
+            }
             tile[r * kTilePitch + c + e] = v[e];
         }
         if constexpr (KIND != LAST) store8<SPLIT>(g.own, matrix, i0 + r, j0 + c, v);
@@ -379,7 +402,7 @@ struct OrthShape {
     int64_t m, n, mp, np;    // smaller and larger side, and with zeros around
     int64_t group;           // matrices at a time
     int64_t parts;           // sums of squares of a matrix
-    int64_t x, xt, lo, a, e, bytes;  // bytes of a stored X, its other order, its lo, A and E, and the workspace
+    int64_t x, xt, lo, a, e, d, bytes;  // bytes of a stored X, its other order, its lo, A, E, a diagonal, and the workspace
 };
 
 int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape* s) {
@@ -399,9 +422,10 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
     s->lo = split ? 0 : s->mp * s->np * 2;
     s->a = s->mp * s->mp * 4;  // hi and lo
     s->e = s->mp * s->mp * size;
+    s->d = s->mp * 4;
     const int64_t quads = (R * C + 4 * kPrepBlock - 1) / (4 * kPrepBlock);
     s->parts = quads < kMostParts ? quads : kMostParts;
-    const int64_t each = 2 * (s->x + s->xt + s->lo) + s->a + s->e + kMostParts * 8;
+    const int64_t each = 2 * (s->x + s->xt + s->lo) + s->a + s->e + 2 * s->d + kMostParts * 8;
     s->group = kGroupBytes / each;
     if (s->group < 1) s->group = 1;
     if (s->group > B) s->group = B;
@@ -438,6 +462,8 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
     Plane a = {take(s.a), nullptr, s.mp * W, s.mp * s.mp * W};
     if (!SPLIT) a.lo = a.hi + s.group * s.mp * s.mp * 2;
     Plane e = {take(s.e), nullptr, s.mp * W, s.mp * s.mp * W};
+    float* da = reinterpret_cast<float*>(take(s.d));
+    float* de = reinterpret_cast<float*>(take(s.d));
     double* sums = reinterpret_cast<double*>(take(kMostParts * 8));
     for (int64_t first = 0; first < s.B; first += s.group) {
         const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
@@ -454,11 +480,12 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
         for (int k = 0; k < call.steps; ++k) {
             const float* c = call.coefs + 3 * k;
             const int now = k & 1;
-            Product g = {x[now], x[now], {}, a, a, 0.f, 1.f, static_cast<int>(s.np * W / 128), tm, tm};
+            const int along = static_cast<int>(s.np * W / 128), across = static_cast<int>(s.mp * W / 128);
+            Product g = {x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, s.mp, along, tm};
             launch_kernel((orth_product_kernel<SPLIT, GRAM, DO>), dim3(half, L), dim3(256), 0, stream, g, res);
-            g = {a, a, a, e, e, c[1], c[2], static_cast<int>(s.mp * W / 128), tm, tm};
+            g = {a, a, a, e, e, da, de, c[1], c[2], s.mp, across, tm};
             launch_kernel((orth_product_kernel<SPLIT, POLY, DO>), dim3(half, L), dim3(256), 0, stream, g, res);
-            g = {e, xt[now], x[now], x[now ^ 1], xt[now ^ 1], c[0], 1.f, static_cast<int>(s.mp * W / 128), tm, tn};
+            g = {e, xt[now], x[now], x[now ^ 1], xt[now ^ 1], de, nullptr, c[0], 0.f, s.mp, across, tn};
             auto last = k + 1 < call.steps ? orth_product_kernel<SPLIT, NEXT, DO> : orth_product_kernel<SPLIT, LAST, DO>;
             launch_kernel(last, dim3(static_cast<unsigned>(tm) * tn, L), dim3(256), 0, stream, g, res);
         }
