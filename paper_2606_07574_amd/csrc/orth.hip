@@ -34,6 +34,7 @@ typedef uint32_t v4u_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t v2u_at2 __attribute__((ext_vector_type(2), aligned(2)));
 
 constexpr float kUnit = 4096.f;  // what values are stored in multiples of 1 / kUnit of
+constexpr int kOrthMaxSteps = 64;
 constexpr int kPad = 128;        // rows and columns of the stored matrices are whole multiples
 
 // A stored matrix: rows of `pitch` bytes. SPLIT: lines of 128 bytes, 32 columns' hi and then their lo;
@@ -387,21 +388,280 @@ __global__ __launch_bounds__(256) void orth_product_kernel(Product g, Result res
 }
 
 // ---------------------------------------------------------------------------
+// Matrices with a side of at most 80
+// ---------------------------------------------------------------------------
+// X after any number of steps is F X with F a polynomial in A = X X^T of the beginning, so the steps can run
+// on m x m values alone: with p = a I + b A + c A^2, F <- p F and A <- p A p (all of them symmetric, and they
+// commute). G is read twice, for the first A and for F X, whatever the steps; the direct form reads X twice a
+// step and launches three kernels for it. An error of A is multiplied by up to a^2 = 12 a step where the
+// singular value is small, so A and F are 64-bit numbers, from products of the inputs without rounding: the
+// result is nearer than fp32 products bring it. The matrix cores' 64-bit rate is the limit of m: its cube
+// runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps), and G G^T of 80 rows
+// takes them half as long as reading fp32 G does. F X is formed in fp32.
+constexpr int kNarrow = 80;
+constexpr int kSlab = 64;            // columns of X taken at a time
+constexpr int kSlabPitch = kSlab + 1;
+
+typedef double v4d __attribute__((ext_vector_type(4)));
+
+__device__ __forceinline__ v4d mfma_f64(double a, double b, v4d c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
+
+// X's rows (16 MT of them, zeros behind the m) and columns j0 .. j0 + 63 of a direction, from the caller's
+// R x C array at `base`: X = U, or for a tall U its transpose. WRITE: renews M on the way.
+template <int DG, bool MOMENTUM, bool WRITE, int MT>
+__device__ __forceinline__ void load_slab(const Source& s, int64_t base, int64_t R, int64_t C, int64_t j0, float* slab) {
+    const bool tall = R > C;
+    const int m = static_cast<int>(tall ? C : R);
+    const int64_t n = tall ? R : C;
+    const int left = static_cast<int>(n - j0 < kSlab ? n - j0 : kSlab);
+    // lines of the array: m rows of 64 values, or 64 rows of m, in pieces of four
+    const int lines = tall ? kSlab : 16 * MT, quads = tall ? 4 * MT : kSlab / 4;
+    const int used = tall ? left : m, width = tall ? m : left;
+    for (int task = threadIdx.x; task < lines * quads; task += blockDim.x) {
+        const int line = task / quads, c = 4 * (task % quads);
+        float v[4] = {0.f, 0.f, 0.f, 0.f};
+        if (line < used && c < width) {
+            const int64_t at = base + (tall ? (j0 + line) * C + c : line * C + j0 + c);
+            float mv[4] = {0.f, 0.f, 0.f, 0.f};
+            const bool whole = c + 4 <= width;
+            if (whole) {
+                load4<DG>(s.G, at, v);
+                if constexpr (MOMENTUM) load4<BIRKHOFF4_F32>(s.M, at, mv);
+            } else {
+#pragma unroll
+                for (int e = 0; e < 3; ++e)
+                    if (c + e < width) {
+                        v[e] = load_value<DG>(s.G, at + e);
+                        if constexpr (MOMENTUM) mv[e] = s.M[at + e];
+                    }
+            }
+            if constexpr (MOMENTUM) {
+                if constexpr (WRITE) {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) mv[e] = __builtin_fmaf(s.momentum, mv[e], v[e]);
+                    if (whole) {
+                        v4u_at4 o;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(mv[e]);
+                        *reinterpret_cast<v4u_at4*>(s.M + at) = o;
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < 3; ++e)
+                            if (c + e < width) s.M[at + e] = mv[e];
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < 4; ++e) v[e] = s.ahead < 0.f ? mv[e] : __builtin_fmaf(s.ahead, mv[e], v[e]);
+            }
+        }
+#pragma unroll
+        for (int e = 0; e < 4; ++e) slab[tall ? (c + e) * kSlabPitch + line : line * kSlabPitch + c + e] = v[e];
+    }
+}
+
+// Tiles of 16 x 16 on and below the diagonal, row by row.
+constexpr int tri(int t) { return t * (t + 1) / 2; }
+
+// Each block's part of U U^T (gridDim.x blocks a matrix), and the momentum's renewal. The block's four
+// waves take every fourth tile each, over all columns of a slab.
+constexpr int kGramBlock = 256;
+
+template <int DG, bool MOMENTUM, int MT>
+__global__ __launch_bounds__(kGramBlock) void orth_narrow_gram_kernel(Source s, double* __restrict__ part, int64_t R, int64_t C,
+                                                                      int64_t first) {
+    constexpr int TILES = tri(MT), OWN = (TILES + 3) / 4;
+    __shared__ float slab[16 * MT * kSlabPitch];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.y, base = (first + matrix) * R * C, n = R > C ? R : C;
+    v4d acc[OWN] = {};
+    int ri[OWN], rj[OWN];  // where a lane reads its rows of a tile's sides
+#pragma unroll
+    for (int q = 0; q < OWN; ++q) {
+        const int t = wave + 4 * q < TILES ? wave + 4 * q : 0;
+        int i = 0;
+        while (tri(i + 1) <= t) ++i;
+        ri[q] = (16 * i + (lane & 15)) * kSlabPitch + (lane >> 4);
+        rj[q] = (16 * (t - tri(i)) + (lane & 15)) * kSlabPitch + (lane >> 4);
+    }
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += static_cast<int64_t>(gridDim.x) * kSlab) {
+        __syncthreads();
+        load_slab<DG, MOMENTUM, true, MT>(s, base, R, C, j0, slab);
+        __syncthreads();
+#pragma unroll 4
+        for (int k = 0; k < kSlab; k += 4)
+#pragma unroll
+            for (int q = 0; q < OWN; ++q)
+                if (wave + 4 * q < TILES)  // uniform over the wave
+                    acc[q] = mfma_f64(slab[ri[q] + k], slab[rj[q] + k], acc[q]);
+    }
+    double* out = part + (matrix * gridDim.x + blockIdx.x) * (TILES * 256);
+#pragma unroll
+    for (int q = 0; q < OWN; ++q)
+        if (wave + 4 * q < TILES)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out[(wave + 4 * q) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)] = acc[q][r];
+}
+
+// The blocks' parts added, 64 entries a block in four parts of the order.
+__global__ __launch_bounds__(256) void orth_narrow_join_kernel(const double* __restrict__ part, double* __restrict__ sum, int parts,
+                                                               int entries) {
+    __shared__ double red[4][64];
+    const int c = threadIdx.x & 63, p = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.y, at = static_cast<int64_t>(blockIdx.x) * 64 + c;
+    double v = 0.0;
+#pragma unroll 8
+    for (int k = p; k < parts; k += 4) v += part[(matrix * parts + k) * entries + at];
+    red[p][c] = v;
+    __syncthreads();
+    if (p == 0) sum[matrix * entries + at] = (v + red[1][c]) + (red[2][c] + red[3][c]);
+}
+
+// F of each matrix from its G G^T: one block a matrix, a wave for each tile. A matrix in LDS is
+// symmetric, so its rows serve as both factors' columns: the lanes of 16 read 16 neighbours.
+constexpr int kPolyBlock = 1024;
+
+struct Coefs {
+    float v[3 * kOrthMaxSteps];
+};
+
+template <int MT>
+__global__ __launch_bounds__(kPolyBlock) void orth_narrow_poly_kernel(const double* __restrict__ sum, float* __restrict__ F,
+                                                                      double* __restrict__ scales, double eps, Coefs coefs, int steps) {
+    constexpr int P = 16 * MT;
+    static_assert(tri(MT) <= kPolyBlock / 64, "a tile a wave");
+    __shared__ double A[P * P], S[P * P], Q[P * P];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.x;
+    int ti = 0;
+    while (tri(ti + 1) <= wave) ++ti;
+    const int tj = wave - tri(ti);
+    const bool mine = wave < tri(MT);  // uniform over the wave
+    const int row = 16 * ti + (lane >> 4), col = 16 * tj + (lane & 15);  // of value r: row + 4 r
+    auto product = [&](const double* M, const double* N) {
+        v4d acc = {};
+        if (mine)
+#pragma unroll 4
+            for (int k = 0; k < P; k += 4)
+                acc = mfma_f64(M[(k + (lane >> 4)) * P + 16 * ti + (lane & 15)], N[(k + (lane >> 4)) * P + 16 * tj + (lane & 15)], acc);
+        return acc;
+    };
+    auto put = [&](double* M, const v4d& v) {
+        if (mine)
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (row + 4 * r >= col) M[(row + 4 * r) * P + col] = M[col * P + row + 4 * r] = v[r];
+    };
+    v4d a = {}, f = {};
+    if (mine)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) a[r] = sum[(matrix * tri(MT) + wave) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)];
+    put(A, a);
+    __syncthreads();
+    double norm = 0.0;
+    for (int k = 0; k < P; ++k) norm += A[k * P + k];
+    norm = __builtin_sqrt(norm);
+    const double scale = norm < __builtin_inf() ? 1.0 / (norm + eps) : __builtin_nan("");
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 4; ++r) a[r] = a[r] * scale * scale;
+    put(A, a);
+    __syncthreads();
+    for (int k = 0; k < steps; ++k) {
+        const double ca = coefs.v[3 * k], cb = coefs.v[3 * k + 1], cc = coefs.v[3 * k + 2];
+        v4d p = product(A, A);
+#pragma unroll
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_fma(cc, p[r], __builtin_fma(cb, a[r], row + 4 * r == col ? ca : 0.0));
+        put(S, p);
+        __syncthreads();
+        const bool last = k + 1 == steps;  // uniform
+        f = k == 0 ? p : product(S, Q);
+        if (!last) a = product(S, A);
+        __syncthreads();
+        if (!last) {
+            put(Q, f);
+            put(A, a);
+            __syncthreads();
+            a = product(S, A);
+            __syncthreads();
+            put(A, a);
+            __syncthreads();
+        }
+    }
+    if (mine)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (row + 4 * r >= col)
+                F[matrix * P * P + (row + 4 * r) * P + col] = F[matrix * P * P + col * P + row + 4 * r] = static_cast<float>(f[r]);
+    if (threadIdx.x == 0) scales[matrix] = scale;
+}
+
+// F X, 64 columns at a time: four waves take 16 each.
+template <int DG, int DO, bool MOMENTUM, int MT>
+__global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const float* __restrict__ F, const double* __restrict__ scales,
+                                                                Result res) {
+    constexpr int P = 16 * MT;
+    __shared__ float slab[P * kSlabPitch];
+    __shared__ float f[P * P];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.y, base = (res.first + matrix) * res.rows * res.cols;
+    const int64_t n = res.tall ? res.rows : res.cols;
+    const int m = static_cast<int>(res.tall ? res.cols : res.rows);
+    for (int k = threadIdx.x; k < P * P; k += 256) f[k] = F[matrix * P * P + k];
+    const double scale = scales[matrix];
+    float rate = res.lr;
+    if (res.update && res.lr_at) rate *= *res.lr_at;
+    const float shrink = 1.f - rate * res.decay, by = rate * res.scale;
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += static_cast<int64_t>(gridDim.x) * kSlab) {
+        __syncthreads();
+        load_slab<DG, MOMENTUM, false, MT>(s, base, res.rows, res.cols, j0, slab);
+        __syncthreads();
+        v4f acc[MT] = {};
+#pragma unroll 4
+        for (int k = 0; k < P; k += 4) {
+            const int at = k + (lane >> 4);
+            const float x = static_cast<float>(slab[at * kSlabPitch + 16 * wave + (lane & 15)] * scale);
+#pragma unroll
+            for (int t = 0; t < MT; ++t)
+                acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[at * P + 16 * t + (lane & 15)], x, acc[t], 0, 0, 0);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) slab[(16 * t + 4 * (lane >> 4) + r) * kSlabPitch + 16 * wave + (lane & 15)] = acc[t][r];
+        __syncthreads();
+        const int left = static_cast<int>(n - j0 < kSlab ? n - j0 : kSlab);
+        const int lines = res.tall ? left : m, width = res.tall ? m : left;
+        for (int task = threadIdx.x; task < lines * width; task += 256) {
+            const int line = task / width, c = task % width;
+            float v = res.tall ? slab[c * kSlabPitch + line] : slab[line * kSlabPitch + c];
+            const int64_t at = base + (res.tall ? (j0 + line) * res.cols + c : line * res.cols + j0 + c);
+            if (res.update) v = __builtin_fmaf(-by, v, shrink * load_value<DO>(res.out, at));
+            if constexpr (DO == BIRKHOFF4_BF16)
+                static_cast<uint16_t*>(res.out)[at] = static_cast<uint16_t>(pack_bf16(v, 0.f));
+            else
+                static_cast<float*>(res.out)[at] = v;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
 // Host side
 // ---------------------------------------------------------------------------
 constexpr int64_t kOrthMaxSide = int64_t(1) << 20;
 constexpr int64_t kOrthMaxSmall = int64_t(1) << 16;  // of the smaller side: every grid stays below 2^32 threads
 constexpr int64_t kOrthMaxValues = int64_t(1) << 46;
 constexpr int64_t kOrthMaxMatrices = int64_t(1) << 26;
-constexpr int kOrthMaxSteps = 64;
 constexpr int64_t kGroupBytes = int64_t(1) << 30;  // of workspace, which matrices are taken together for
 constexpr int kMostParts = 128;
+constexpr int64_t kGramBlocks = 512;
 
 struct OrthShape {
     int64_t B, R, C;         // the caller's matrices
     int64_t m, n, mp, np;    // smaller and larger side, and with zeros around
     int64_t group;           // matrices at a time
-    int64_t parts;           // sums of squares of a matrix
+    int mt;                  // tiles of 16 of a narrow matrix's smaller side, 0 for the others
+    int64_t parts;           // sums of squares of a matrix, or of its blocks' G G^T
     int64_t x, xt, lo, a, e, d, bytes;  // bytes of a stored X, its other order, its lo, A, E, a diagonal, and the workspace
 };
 
@@ -415,6 +675,21 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
     s->m = R < C ? R : C;
     s->n = R < C ? C : R;
     if (s->m > kOrthMaxSmall) return BIRKHOFF4_ERR_SIZE;
+    if (s->m <= kNarrow) {
+        s->mt = static_cast<int>((s->m + 15) / 16);
+        const int64_t slabs = (s->n + kSlab - 1) / kSlab, entries = tri(s->mt) * 256 * 8;
+        s->e = entries;               // the sum of the parts
+        s->x = s->mt * s->mt * 1024;  // F
+        s->group = kGroupBytes / (s->e + s->x + 16);
+        if (s->group > B) s->group = B;
+        if (s->group > 32768) s->group = 32768;
+        s->parts = kGramBlocks / s->group;
+        if (s->parts > slabs) s->parts = slabs;
+        if (s->parts < 1) s->parts = 1;
+        s->a = s->parts > 1 ? s->parts * entries : 0;  // the parts
+        s->bytes = s->group * (s->a + s->e + s->x + 16);
+        return BIRKHOFF4_OK;
+    }
     s->mp = (s->m + kPad - 1) / kPad * kPad;
     s->np = (s->n + kPad - 1) / kPad * kPad;
     const int64_t size = split ? 4 : 2;
@@ -442,8 +717,44 @@ struct OrthCall {
     double eps;
 };
 
+template <int DG, int DO, bool MOMENTUM, int MT>
+int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
+    double* sum = reinterpret_cast<double*>(work);
+    double* scales = reinterpret_cast<double*>(work + s.group * s.e);
+    float* F = reinterpret_cast<float*>(work + s.group * (s.e + 16));
+    double* part = s.parts > 1 ? reinterpret_cast<double*>(work + s.group * (s.e + 16 + s.x)) : sum;
+    Coefs coefs = {};
+    for (int k = 0; k < 3 * call.steps; ++k) coefs.v[k] = call.coefs[k];
+    const int64_t slabs = (s.n + kSlab - 1) / kSlab;
+    for (int64_t first = 0; first < s.B; first += s.group) {
+        const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
+        launch_kernel((orth_narrow_gram_kernel<DG, MOMENTUM, MT>), dim3(static_cast<unsigned>(s.parts), L), dim3(kGramBlock), 0,
+                      stream, call.src, part, s.R, s.C, first);
+        if (s.parts > 1)
+            launch_kernel(orth_narrow_join_kernel, dim3(4 * tri(MT), L), dim3(256), 0, stream, part, sum,
+                          static_cast<int>(s.parts), 256 * tri(MT));
+        launch_kernel((orth_narrow_poly_kernel<MT>), dim3(L), dim3(kPolyBlock), 0, stream, sum, F, scales, call.eps, coefs,
+                      call.steps);
+        Result res = call.res;
+        res.first = first;
+        int64_t blocks = 2 * kGramBlocks / L;
+        if (blocks < 1) blocks = 1;
+        if (blocks > slabs) blocks = slabs;
+        launch_kernel((orth_narrow_apply_kernel<DG, DO, MOMENTUM, MT>), dim3(static_cast<unsigned>(blocks), L), dim3(256), 0,
+                      stream, call.src, F, scales, res);
+    }
+    return launch_status();
+}
+
 template <int DG, int DO, bool MOMENTUM>
 int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
+    switch (s.mt) {
+        case 1: return launch_narrow<DG, DO, MOMENTUM, 1>(s, call, work, stream);
+        case 2: return launch_narrow<DG, DO, MOMENTUM, 2>(s, call, work, stream);
+        case 3: return launch_narrow<DG, DO, MOMENTUM, 3>(s, call, work, stream);
+        case 4: return launch_narrow<DG, DO, MOMENTUM, 4>(s, call, work, stream);
+        case 5: return launch_narrow<DG, DO, MOMENTUM, 5>(s, call, work, stream);
+    }
     constexpr bool SPLIT = DO == BIRKHOFF4_F32;
     constexpr int64_t W = SPLIT ? 4 : 2;
     const bool tall = s.R > s.C;
