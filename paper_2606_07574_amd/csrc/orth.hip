@@ -35,46 +35,53 @@ typedef uint32_t v2u_at2 __attribute__((ext_vector_type(2), aligned(2)));
 
 constexpr float kUnit = 4096.f;  // what values are stored in multiples of 1 / kUnit of
 constexpr int kOrthMaxSteps = 64;
-constexpr int kPad = 128;        // rows and columns of the stored matrices are whole multiples
+constexpr int kPad = 64;         // rows and columns of the stored matrices are whole multiples
 
-// A stored matrix: rows of `pitch` bytes. SPLIT: lines of 128 bytes, 32 columns' hi and then their lo;
-// otherwise hi alone, and lo, where it is kept, in a matrix of its own.
+// A stored matrix: panels of 64 bytes of every row, one row behind the other, so that a tile's rows of one
+// panel are one piece of memory, which goes to LDS as it is. SPLIT: 16 columns' hi and then their lo;
+// otherwise 32 columns' hi, and lo, where it is kept, the same way in a matrix of its own. The 16-byte piece c
+// of row r lies at place c ^ (r / 2 mod 4) of its 64 bytes: eight lanes that read one piece of eight
+// neighbouring rows from LDS find it in eight different places of 128 bytes.
 struct Plane {
     char* hi;
     char* lo;
-    int64_t pitch;   // bytes of a row
+    int64_t rows;    // with zeros around
     int64_t stride;  // bytes from one matrix of the batch to the next
 };
 
+constexpr int panel_cols(bool split) { return split ? 16 : 32; }
+
+// Where the eight columns from `col` (a multiple of eight) on of a row begin; SPLIT: their lo is at that ^ 32.
 template <bool SPLIT>
 __device__ __forceinline__ int64_t place(const Plane& p, int64_t row, int64_t col) {
-    return row * p.pitch + (SPLIT ? (col >> 5) * 128 + (col & 31) * 2 : col * 2);
+    constexpr int N = panel_cols(SPLIT);
+    const int piece = static_cast<int>(col % N / 8);
+    return (col / N * p.rows + row) * 64 + 16 * (piece ^ static_cast<int>(row / 2 & 3));
 }
 
-// Eight columns from `col` (a multiple of eight) on.
-template <bool SPLIT>
-__device__ __forceinline__ void store8(const Plane& p, int64_t matrix, int64_t row, int64_t col, const float v[8]) {
-    h8 hi, lo;
+__device__ __forceinline__ void halves(const float v[8], h8* hi, h8* lo) {
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
-        hi[e] = static_cast<_Float16>(v[e]);
-        lo[e] = static_cast<_Float16>(v[e] - static_cast<float>(hi[e]));
+        (*hi)[e] = static_cast<_Float16>(v[e]);
+        (*lo)[e] = static_cast<_Float16>(v[e] - static_cast<float>((*hi)[e]));
     }
+}
+
+template <bool SPLIT>
+__device__ __forceinline__ void store8(const Plane& p, int64_t matrix, int64_t row, int64_t col, const h8& hi, const h8& lo) {
     const int64_t at = matrix * p.stride + place<SPLIT>(p, row, col);
     *reinterpret_cast<h8*>(p.hi + at) = hi;
     if constexpr (SPLIT)
-        *reinterpret_cast<h8*>(p.hi + at + 64) = lo;
+        *reinterpret_cast<h8*>(p.hi + (at ^ 32)) = lo;
     else if (p.lo)
         *reinterpret_cast<h8*>(p.lo + at) = lo;
 }
 
 template <bool SPLIT>
-__device__ __forceinline__ void load8(const Plane& p, int64_t matrix, int64_t row, int64_t col, float v[8]) {
+__device__ __forceinline__ void load8(const Plane& p, int64_t matrix, int64_t row, int64_t col, h8* hi, h8* lo) {
     const int64_t at = matrix * p.stride + place<SPLIT>(p, row, col);
-    const h8 hi = *reinterpret_cast<const h8*>(p.hi + at);
-    const h8 lo = *reinterpret_cast<const h8*>(SPLIT ? p.hi + at + 64 : p.lo + at);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = static_cast<float>(hi[e]) + static_cast<float>(lo[e]);
+    *hi = *reinterpret_cast<const h8*>(p.hi + at);
+    *lo = *reinterpret_cast<const h8*>(SPLIT ? p.hi + (at ^ 32) : p.lo + at);
 }
 
 // ---------------------------------------------------------------------------
@@ -202,12 +209,15 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const doubl
     for (int k = 0; k < 2; ++k) {
         const int task = threadIdx.x + 256 * k, line = task / 8, at = 8 * (task % 8);
         float v[8];
+        h8 hi, lo;
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[line][at + e];
-        store8<SPLIT>(own, matrix, r0 + line, c0 + at, v);
+        halves(v, &hi, &lo);
+        store8<SPLIT>(own, matrix, r0 + line, c0 + at, hi, lo);
 #pragma unroll
         for (int e = 0; e < 8; ++e) v[e] = tile[at + e][line];
-        store8<SPLIT>(turned, matrix, c0 + line, r0 + at, v);
+        halves(v, &hi, &lo);
+        store8<SPLIT>(turned, matrix, c0 + line, r0 + at, hi, lo);
     }
 }
 
@@ -227,8 +237,8 @@ struct Product {
     float* own_diag;        // D (GRAM) or F (POLY)
     float keep, add;
     int64_t side;
-    int lines;    // of 128 bytes in a row of P and Q
-    int tj;       // tiles along j
+    int panels;             // of P's and Q's rows
+    int tiles, tj;          // of the result, and along j
 };
 
 // What becomes of the last step's values: out (rows x cols, `tall`: out_ji), or the weights
@@ -241,151 +251,292 @@ struct Result {
     const float* lr_at;
 };
 
-constexpr int kTile = 128;
-constexpr int kStage = 2 * kTile * 128;           // bytes of one step of both operands
-constexpr int kTilePitch = kTile + 1;             // floats of a row of the finished tile
-constexpr int kTileBytes = kTile * kTilePitch * 4;
+typedef uint32_t v4u_at2 __attribute__((ext_vector_type(4), aligned(2)));
 
-template <bool SPLIT, int KIND, int DO>
-__global__ __launch_bounds__(256) void orth_product_kernel(Product g, Result res) {
-    static_assert(2 * kStage <= kTileBytes, "the finished tile takes the stages' place");
-    __shared__ __attribute__((aligned(128))) char lds[kTileBytes];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+// Eight neighbouring values of a row of the caller's array, of which the first `n` are there.
+template <int DO>
+__device__ __forceinline__ void put_row(void* out, int64_t at, int64_t n, const float v[8]) {
+    if (n >= 8) {
+        if constexpr (DO == BIRKHOFF4_BF16) {
+            v4u_at2 o;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+            *reinterpret_cast<v4u_at2*>(static_cast<uint16_t*>(out) + at) = o;
+        } else {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                v4u_at4 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(v[4 * h + e]);
+                *reinterpret_cast<v4u_at4*>(static_cast<float*>(out) + at + 4 * h) = o;
+            }
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 7; ++e) {
+        if (e >= n) continue;
+        if constexpr (DO == BIRKHOFF4_BF16)
+            static_cast<uint16_t*>(out)[at + e] = static_cast<uint16_t>(pack_bf16(v[e], 0.f));
+        else
+            static_cast<float*>(out)[at + e] = v[e];
+    }
+}
+
+// A block's four waves have (32 W) x (32 W) of a (64 W) x (64 W) tile each. Four stages of one panel of
+// both operands lie in LDS: while one is multiplied the next one is there and two are on their way, so a
+// load has two stages' time. At the middle of a stage the waves meet: what the next stage reads has come then,
+// and the one before is read by nobody any more, whose place the fourth takes.
+constexpr int kStages = 4;
+constexpr int kTurnPitch = 40;  // fp16 values of a row of 32 on its way to the other order
+
+template <int W>
+constexpr int stage_bytes() { return 2 * 64 * W * 64; }
+
+#define ORTH_WAIT(n) asm volatile("s_waitcnt vmcnt(" #n ")\n\ts_barrier" ::: "memory")
+
+// 2 W reads of LDS (and as many loads), one behind each of the first of N products, so that the matrix
+// cores do not wait for all of them.
+template <int W, int N, bool LOADS>
+__device__ __forceinline__ void mix_reads() {
+    if constexpr (W > 1) {
+#pragma unroll
+        for (int k = 0; k < 2 * W; ++k) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            if constexpr (LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, N - 2 * W, 0);
+    }
+}
+
+template <bool SPLIT, int KIND, int DO, int W>
+__global__ __launch_bounds__(256, W <= 2 ? 2 : 1) void orth_product_kernel(Product g, Result res) {
+    constexpr int T = 64 * W;
+    static_assert(kStages * stage_bytes<W>() >= 4 * 2 * 32 * kTurnPitch * 2, "the turning takes the stages' place");
+    __shared__ __attribute__((aligned(128))) char lds[kStages * stage_bytes<W>()];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t matrix = blockIdx.y;
+    // Blocks go round the eight XCDs: each XCD takes neighbouring tiles, whose rows its L2 holds.
+    const int per = (g.tiles + 7) / 8, tile = blockIdx.x % 8 * per + blockIdx.x / 8;
+    if (tile >= g.tiles) return;  // uniform over the block
     int ti, tj;
     if constexpr (KIND == GRAM || KIND == POLY) {  // row by row below the diagonal
-        const int t = blockIdx.x;
-        ti = static_cast<int>((__builtin_sqrtf(8.f * t + 1.f) - 1.f) * 0.5f);
-        while (ti * (ti + 1) / 2 > t) --ti;
-        while ((ti + 1) * (ti + 2) / 2 <= t) ++ti;
-        tj = t - ti * (ti + 1) / 2;
+        ti = static_cast<int>((__builtin_sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
+        while (ti * (ti + 1) / 2 > tile) --ti;
+        while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
+        tj = tile - ti * (ti + 1) / 2;
     } else {
-        ti = blockIdx.x / g.tj;
-        tj = blockIdx.x % g.tj;
+        ti = tile / g.tj;
+        tj = tile % g.tj;
     }
-    const char* p = g.P.hi + matrix * g.P.stride + static_cast<int64_t>(ti) * kTile * g.P.pitch;
-    const char* q = g.Q.hi + matrix * g.Q.stride + static_cast<int64_t>(tj) * kTile * g.Q.pitch;
-
-    // A step is 128 bytes of 128 rows of both, loaded straight to LDS, eight rows an instruction. The
-    // 16-byte piece c of row r lies at place c ^ (r mod 8) of its 128 bytes, so that the eight lanes that
-    // read one piece of eight rows together find it in eight places.
-    const int row8 = lane / 8, piece = (lane % 8) ^ row8;
-    auto load = [&](int step, int buf) {
+    // Rows behind the stored ones, of a tile that hangs over: others in their place, which nothing is made of.
+    const char *p[W], *q[W];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const int r = 8 * (4 * wave + k);
-            const char* a = p + static_cast<int64_t>(r + row8) * g.P.pitch + static_cast<int64_t>(step) * 128 + 16 * piece;
-            const char* b = q + static_cast<int64_t>(r + row8) * g.Q.pitch + static_cast<int64_t>(step) * 128 + 16 * piece;
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)a,
-                                             (__attribute__((address_space(3))) void*)(lds + buf * kStage + r * 128), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)b,
-                                             (__attribute__((address_space(3))) void*)(lds + buf * kStage + kTile * 128 + r * 128),
-                                             16, 0, 0);
+    for (int k = 0; k < W; ++k) {
+        const int64_t r = 16 * (W * wave + k), ri = ti * static_cast<int64_t>(T) + r, rj = tj * static_cast<int64_t>(T) + r;
+        p[k] = g.P.hi + matrix * g.P.stride + (ri < g.P.rows ? ri : g.P.rows - 16) * 64 + lane * 16;
+        q[k] = g.Q.hi + matrix * g.Q.stride + (rj < g.Q.rows ? rj : g.Q.rows - 16) * 64 + lane * 16;
+    }
+    const int64_t p_panel = g.P.rows * 64, q_panel = g.Q.rows * 64;
+    auto load = [&](int stage) {  // past the last panel: the last one again, into a place that is not read
+        const int64_t at = stage < g.panels ? stage : g.panels - 1;
+        char* to = lds + (stage % kStages) * stage_bytes<W>() + 1024 * W * wave;
+#pragma unroll
+        for (int k = 0; k < W; ++k) {
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p[k] + at * p_panel),
+                                             (__attribute__((address_space(3))) void*)(to + 1024 * k), 16, 0, 0);
+            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(q[k] + at * q_panel),
+                                             (__attribute__((address_space(3))) void*)(to + T * 64 + 1024 * k), 16, 0, 0);
         }
     };
-    // a wave has 64 x 64 of the tile: 2 x 2 products of 32 x 32
-    const int wi = 64 * (wave >> 1), wj = 64 * (wave & 1);
-    v16f acc[2][2] = {};
-    load(0, 0);
-    for (int step = 0; step < g.lines; ++step) {
-        __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0): this step's lines are there
-        __syncthreads();                     // for all waves, and nobody reads the other stage any more
-        const char* at = lds + (step & 1) * kStage;
-        h8 a[2][4], b[2][4];  // pieces 2 c + lane / 32
+    const int wi = 32 * W * (wave >> 1), wj = 32 * W * (wave & 1);
+    const int r32 = lane & 31, h = lane >> 5;
+    const char* own_rows = lds + (wi + r32) * 64;
+    const char* col_rows = lds + (T + wj + r32) * 64;
+    const int swizzle = (r32 >> 1) & 3;
+    // pieces 2 part + h: SPLIT: hi (part 0) or lo of 16 columns; otherwise 16 of 32 columns
+    auto fetch = [&](int stage, int part, h8 (&a)[W], h8 (&b)[W]) {
+        const int at = (stage % kStages) * stage_bytes<W>() + 16 * ((2 * part + h) ^ swizzle);
 #pragma unroll
-        for (int t = 0; t < 2; ++t)
+        for (int k = 0; k < W; ++k) {
+            a[k] = *reinterpret_cast<const h8*>(own_rows + at + 2048 * k);
+            b[k] = *reinterpret_cast<const h8*>(col_rows + at + 2048 * k);
+        }
+    };
+    v16f acc[W][W] = {};
+    auto multiply = [&](const h8 (&a)[W], const h8 (&b)[W]) {
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                const int r = 32 * t + (lane & 31), place = 16 * ((2 * c + (lane >> 5)) ^ (r & 7));
-                a[t][c] = *reinterpret_cast<const h8*>(at + (wi + r) * 128 + place);
-                b[t][c] = *reinterpret_cast<const h8*>(at + (kTile + wj + r) * 128 + place);
-            }
-        if (step + 1 < g.lines) load(step + 1, (step + 1) & 1);
+        for (int i = 0; i < W; ++i)
 #pragma unroll
-        for (int c = 0; c < (SPLIT ? 2 : 4); ++c)
+            for (int j = 0; j < W; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i], b[j], acc[i][j], 0, 0, 0);
+    };
+    auto meet = [&] {  // the next stage is there, one further is on its way: 2 W loads of this wave
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (W == 1) ORTH_WAIT(2);
+        if constexpr (W == 2) ORTH_WAIT(4);
+        if constexpr (W == 3) ORTH_WAIT(6);
+        if constexpr (W == 4) ORTH_WAIT(8);
+        __builtin_amdgcn_sched_barrier(0);  // what was read before is also multiplied before
+    };
+    load(0);
+    load(1);
+    load(2);
+    h8 a0[W], b0[W], a1[W], b1[W];
+    meet();
+    fetch(0, 0, a0, b0);
+#pragma unroll 1
+    for (int stage = 0; stage < g.panels; ++stage) {
+        fetch(stage, 1, a1, b1);
+        multiply(a0, b0);
+        mix_reads<W, W * W, false>();
+        meet();
+        load(stage + 3);
+        if constexpr (SPLIT) {
+            h8 a2[W], b2[W];
+            fetch(stage + 1, 0, a2, b2);
+            multiply(a0, b1);
+            multiply(a1, b0);
+            mix_reads<W, 2 * W * W, true>();
 #pragma unroll
-            for (int i = 0; i < 2; ++i)
-#pragma unroll
-                for (int j = 0; j < 2; ++j) {
-                    acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][c], b[j][c], acc[i][j], 0, 0, 0);
-                    if constexpr (SPLIT) {
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][c], b[j][c + 2], acc[i][j], 0, 0, 0);
-                        acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i][c + 2], b[j][c], acc[i][j], 0, 0, 0);
-                    }
-                }
+            for (int k = 0; k < W; ++k) a0[k] = a2[k], b0[k] = b2[k];
+        } else {
+            fetch(stage + 1, 0, a0, b0);
+            multiply(a1, b1);
+            mix_reads<W, W * W, true>();
+        }
     }
-    __syncthreads();
-    float* tile = reinterpret_cast<float*>(lds);
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                const int row = wi + 32 * i + 8 * (r / 4) + 4 * (lane >> 5) + r % 4, col = wj + 32 * j + (lane & 31);
-                tile[row * kTilePitch + col] = acc[i][j][r];
-            }
-    __syncthreads();
-    const int64_t i0 = static_cast<int64_t>(ti) * kTile, j0 = static_cast<int64_t>(tj) * kTile;
+    ORTH_WAIT(0);
+
+    // A lane has column j of 32 x 32 values, rows 8 g + 4 h + 0..3 of it in acc[4 g ..]: exchanged between the
+    // wave's halves, eight neighbouring rows, which are one piece of row j in the other order. What src adds
+    // is read in that order too. The own order is made of it through LDS.
+    const int64_t ib = static_cast<int64_t>(ti) * T + wi, jb = static_cast<int64_t>(tj) * T + wj;
     const float* sd = KIND != GRAM ? g.src_diag + matrix * g.side : nullptr;
     float* od = KIND == GRAM || KIND == POLY ? g.own_diag + matrix * g.side : nullptr;
-#pragma unroll 1
-    for (int task = threadIdx.x; task < kTile * kTile / 8; task += 256) {
-        const int r = task / 16, c = 8 * (task % 16);
-        const bool diag = (KIND == GRAM || KIND == POLY) && ti == tj && r / 8 == c / 8;
-        float v[8], s[8], di = 0.f;
-        if constexpr (KIND != GRAM) {
-            load8<SPLIT>(g.src, matrix, i0 + r, j0 + c, s);
-            di = sd[i0 + r];
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float t = tile[r * kTilePitch + c + e] / kUnit;
-            if constexpr (KIND == GRAM) v[e] = t;
-            if constexpr (KIND == POLY) v[e] = __builtin_fmaf(__builtin_fmaf(g.add, di + sd[j0 + c + e], g.keep), s[e], g.add * t);
-            if constexpr (KIND == NEXT || KIND == LAST) v[e] = __builtin_fmaf(g.keep + di, s[e], t);
-            if (diag && e == r % 8) {
-                const float one = t / kUnit;
-                if constexpr (KIND == GRAM) od[i0 + r] = one;
-                if constexpr (KIND == POLY) od[i0 + r] = __builtin_fmaf(g.keep, di, g.add * __builtin_fmaf(di, di, one));
-                v[e] = 0.f;
-            }
-            tile[r * kTilePitch + c + e] = v[e];
-        }
-        if constexpr (KIND != LAST) store8<SPLIT>(g.own, matrix, i0 + r, j0 + c, v);
+    _Float16* turn = reinterpret_cast<_Float16*>(lds) + wave * 2 * 32 * kTurnPitch;
+    float shrink = 0.f, by = 0.f;
+    if constexpr (KIND == LAST) {
+        const float rate = res.update && res.lr_at ? res.lr * *res.lr_at : res.lr;
+        shrink = 1.f - rate * res.decay, by = rate * res.scale;
     }
-    if constexpr (KIND == GRAM || KIND == POLY)
-        if (ti == tj) return;
-    __syncthreads();
-    if constexpr (KIND != LAST) {
-#pragma unroll 1
-        for (int task = threadIdx.x; task < kTile * kTile / 8; task += 256) {
-            const int r = task / 16, c = 8 * (task % 16);
-            float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = tile[(c + e) * kTilePitch + r];
-            store8<SPLIT>(g.turned, matrix, j0 + r, i0 + c, v);
+    for (int b = 0; b < W; ++b) {
+        const int64_t j = jb + 32 * b + r32;
+        if (jb + 32 * b >= g.Q.rows) continue;  // uniform over the wave: rows come in whole 64s
+        h8 shi[2 * W], slo[2 * W];
+        float dj = 0.f;
+        if constexpr (KIND != GRAM) {
+#pragma unroll
+            for (int k = 0; k < 2 * W; ++k)
+                if (ib + 16 * k < g.P.rows) load8<SPLIT>(g.src, matrix, j, ib + 16 * k + 8 * h, &shi[k], &slo[k]);
+            if constexpr (KIND == POLY) dj = sd[j];
         }
-    } else {
-        float rate = res.lr;
-        if (res.update && res.lr_at) rate *= *res.lr_at;
-        const float shrink = 1.f - rate * res.decay, by = rate * res.scale;
-        const int64_t r0 = res.tall ? j0 : i0, c0 = res.tall ? i0 : j0;
-        const int64_t base = (res.first + matrix) * res.rows * res.cols;
-#pragma unroll 1
-        for (int task = threadIdx.x; task < kTile * kTile; task += 256) {
-            const int r = task / kTile, c = task % kTile;
-            if (r0 + r >= res.rows || c0 + c >= res.cols) continue;
-            float v = (res.tall ? tile[c * kTilePitch + r] : tile[r * kTilePitch + c]) / kUnit;
-            const int64_t at = base + (r0 + r) * res.cols + c0 + c;
-            if (res.update) v = __builtin_fmaf(-by, v, shrink * load_value<DO>(res.out, at));
-            if constexpr (DO == BIRKHOFF4_BF16)
-                static_cast<uint16_t*>(res.out)[at] = static_cast<uint16_t>(pack_bf16(v, 0.f));
-            else
-                static_cast<float*>(res.out)[at] = v;
+#pragma unroll
+        for (int a = 0; a < W; ++a) {
+            if (ib + 32 * a >= g.P.rows) continue;
+            // Of a symmetric result what lies below the diagonal counts, whatever the tiles: the sum of the
+            // pieces' products is not the same bits with the factors exchanged.
+            const bool above = (KIND == GRAM || KIND == POLY) && ib + 32 * a < jb + 32 * b;
+            const bool across = (KIND == GRAM || KIND == POLY) && ib + 32 * a == jb + 32 * b;
+            if (above) continue;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                const int64_t i = ib + 32 * a + 16 * u + 8 * h;
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[a][b][8 * u + e]),
+                                                                    __float_as_uint(acc[a][b][8 * u + 4 + e]), false, false);
+                    v[e] = __uint_as_float(x[0]) / kUnit;
+                    v[4 + e] = __uint_as_float(x[1]) / kUnit;
+                }
+                if constexpr (KIND != GRAM) {
+                    const v4f d0 = *reinterpret_cast<const v4f*>(sd + i), d1 = *reinterpret_cast<const v4f*>(sd + i + 4);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const float di = e < 4 ? d0[e] : d1[e - 4];
+                        const float s = static_cast<float>(shi[2 * a + u][e]) + static_cast<float>(slo[2 * a + u][e]);
+                        if constexpr (KIND == POLY) {
+                            const float t = v[e];
+                            v[e] = __builtin_fmaf(__builtin_fmaf(g.add, di + dj, g.keep), s, g.add * t);
+                            if (i + e == j) {
+                                od[j] = __builtin_fmaf(g.keep, dj, g.add * __builtin_fmaf(dj, dj, t / kUnit));
+                                v[e] = 0.f;
+                            }
+                        } else {
+                            v[e] = __builtin_fmaf(g.keep + di, s, v[e]);
+                        }
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (i + e == j) {
+                            od[j] = v[e] / kUnit;
+                            v[e] = 0.f;
+                        }
+                }
+                if constexpr (KIND == LAST) {
+                    const int64_t base = (res.first + matrix) * res.rows * res.cols;
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[e] /= kUnit;
+                    if (res.tall) {  // row j, columns i..
+                        const int64_t at = base + j * res.cols + i;
+                        if (j < res.rows && i < res.cols) {
+                            if (res.update) {
+#pragma unroll
+                                for (int e = 0; e < 8; ++e)
+                                    if (i + e < res.cols) v[e] = __builtin_fmaf(-by, v[e], shrink * load_value<DO>(res.out, at + e));
+                            }
+                            put_row<DO>(res.out, at, res.cols - i, v);
+                        }
+                    } else {  // rows i.., column j: neighbouring lanes have neighbours
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            if (i + e >= res.rows || j >= res.cols) continue;
+                            const int64_t at = base + (i + e) * res.cols + j;
+                            if (res.update) v[e] = __builtin_fmaf(-by, v[e], shrink * load_value<DO>(res.out, at));
+                            if constexpr (DO == BIRKHOFF4_BF16)
+                                static_cast<uint16_t*>(res.out)[at] = static_cast<uint16_t>(pack_bf16(v[e], 0.f));
+                            else
+                                static_cast<float*>(res.out)[at] = v[e];
+                        }
+                    }
+                } else {
+                    h8 hi, lo;
+                    halves(v, &hi, &lo);
+                    if (!across) store8<SPLIT>(g.turned, matrix, j, i, hi, lo);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        const int row = 16 * u + 8 * h + e;
+                        if (across && row < r32) continue;
+                        turn[row * kTurnPitch + r32] = hi[e];
+                        if (SPLIT || KIND == GRAM) turn[(32 + row) * kTurnPitch + r32] = lo[e];
+                        if (across) {
+                            turn[r32 * kTurnPitch + row] = hi[e];
+                            if (SPLIT || KIND == GRAM) turn[(32 + r32) * kTurnPitch + row] = lo[e];
+                        }
+                    }
+                }
+            }
+            // the other order: a lane has 16 columns of row i
+            if constexpr (KIND != LAST) {
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const _Float16* from = turn + r32 * kTurnPitch + 16 * h + 8 * u;
+                    const h8 hi = *reinterpret_cast<const h8*>(from);
+                    h8 lo = hi;
+                    if (SPLIT || KIND == GRAM) lo = *reinterpret_cast<const h8*>(from + 32 * kTurnPitch);
+                    store8<SPLIT>(g.own, matrix, ib + 32 * a + r32, jb + 32 * b + 16 * h + 8 * u, hi, lo);
+                }
+                __builtin_amdgcn_wave_barrier();
+            }
         }
     }
 }
+
+#undef ORTH_WAIT
 
 // ---------------------------------------------------------------------------
 // Matrices with a side of at most 80
@@ -695,8 +846,8 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
     const int64_t size = split ? 4 : 2;
     s->x = s->xt = s->mp * s->np * size;
     s->lo = split ? 0 : s->mp * s->np * 2;
-    s->a = s->mp * s->mp * 4;  // hi and lo
-    s->e = s->mp * s->mp * size;
+    s->e = s->mp * s->mp * size;  // E, and A without its lo
+    s->a = s->e + (split ? 0 : s->e);
     s->d = s->mp * 4;
     const int64_t quads = (R * C + 4 * kPrepBlock - 1) / (4 * kPrepBlock);
     s->parts = quads < kMostParts ? quads : kMostParts;
@@ -746,6 +897,38 @@ int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStrea
     return launch_status();
 }
 
+// The tile's side in 64s for `rows` x `cols` values a matrix (`half`: of a symmetric result) and its tiles: what the
+// blocks that follow each other on a compute unit take together, by the cycles of a panel, which are the
+// matrix cores' or LDS's, whichever takes longer: 128 bytes a cycle, each operand read by two waves and
+// written once.
+int choose_tile(bool split, int64_t L, int64_t rows, int64_t cols, bool half, int64_t* tiles, int64_t* tj) {
+    int best = 1;
+    double least = 0.0;
+    for (int w = 1; w <= 4; ++w) {
+        const int64_t t = 64 * w, i = (rows + t - 1) / t, j = (cols + t - 1) / t, n = half ? i * (i + 1) / 2 : i * j;
+        const int together = w <= 2 ? 2 : 1;
+        const double rounds = static_cast<double>((n * L + 256 * together - 1) / (256 * together));
+        const double cores = (split ? 96.0 : 64.0) * w * w, memory = 192.0 * w;
+        const double cost = rounds * together * (cores > memory ? cores : memory);
+        if (w == 1 || cost < least) {
+            least = cost, best = w;
+            *tiles = n, *tj = j;
+        }
+    }
+    return best;
+}
+
+template <bool SPLIT, int KIND, int DO>
+void launch_product(Product g, const Result& res, unsigned L, int64_t rows, int64_t cols, hipStream_t stream) {
+    int64_t tiles = 0, tj = 0;
+    const int w = choose_tile(SPLIT, L, rows, cols, KIND == GRAM || KIND == POLY, &tiles, &tj);
+    g.tiles = static_cast<int>(tiles), g.tj = static_cast<int>(tj);
+    auto kern = w == 1   ? orth_product_kernel<SPLIT, KIND, DO, 1>
+                : w == 2 ? orth_product_kernel<SPLIT, KIND, DO, 2>
+                : w == 3 ? orth_product_kernel<SPLIT, KIND, DO, 3> : orth_product_kernel<SPLIT, KIND, DO, 4>;
+    launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((tiles + 7) / 8)), L), dim3(256), 0, stream, g, res);
+}
+
 template <int DG, int DO, bool MOMENTUM>
 int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
     switch (s.mt) {
@@ -756,7 +939,6 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
         case 5: return launch_narrow<DG, DO, MOMENTUM, 5>(s, call, work, stream);
     }
     constexpr bool SPLIT = DO == BIRKHOFF4_F32;
-    constexpr int64_t W = SPLIT ? 4 : 2;
     const bool tall = s.R > s.C;
     char* at = work;
     auto take = [&](int64_t bytes) {
@@ -766,16 +948,17 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
     };
     Plane x[2], xt[2];
     for (int k = 0; k < 2; ++k) {
-        x[k] = {take(s.x), nullptr, s.np * W, s.x};
-        x[k].lo = take(s.lo);
-        xt[k] = {take(s.xt), nullptr, s.mp * W, s.xt};
+        x[k] = {take(s.x), nullptr, s.mp, s.x};
+        xt[k] = {take(s.xt), nullptr, s.np, s.xt};
+        xt[k].lo = take(s.lo);
     }
-    Plane a = {take(s.a), nullptr, s.mp * W, s.mp * s.mp * W};
-    if (!SPLIT) a.lo = a.hi + s.group * s.mp * s.mp * 2;
-    Plane e = {take(s.e), nullptr, s.mp * W, s.mp * s.mp * W};
+    Plane a = {take(s.e), nullptr, s.mp, s.e};
+    a.lo = take(SPLIT ? 0 : s.e);
+    Plane e = {take(s.e), nullptr, s.mp, s.e};
     float* da = reinterpret_cast<float*>(take(s.d));
     float* de = reinterpret_cast<float*>(take(s.d));
     double* sums = reinterpret_cast<double*>(take(kMostParts * 8));
+    const int along = static_cast<int>(s.np / panel_cols(SPLIT)), across = static_cast<int>(s.mp / panel_cols(SPLIT));
     for (int64_t first = 0; first < s.B; first += s.group) {
         const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
         launch_kernel((orth_prep_kernel<DG, MOMENTUM>), dim3(static_cast<unsigned>(s.parts), L), dim3(kPrepBlock), 0, stream,
@@ -784,21 +967,19 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
         launch_kernel((orth_convert_kernel<DG, MOMENTUM, SPLIT>),
                       dim3(static_cast<unsigned>(Cp / kConvert), static_cast<unsigned>(Rp / kConvert), L), dim3(256), 0, stream,
                       call.src, sums, static_cast<int>(s.parts), call.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0], s.R, s.C, first);
-        const int tm = static_cast<int>(s.mp / kTile), tn = static_cast<int>(s.np / kTile);
-        const unsigned half = static_cast<unsigned>(tm) * (tm + 1) / 2;
         Result res = call.res;
         res.first = first;
         for (int k = 0; k < call.steps; ++k) {
             const float* c = call.coefs + 3 * k;
             const int now = k & 1;
-            const int along = static_cast<int>(s.np * W / 128), across = static_cast<int>(s.mp * W / 128);
-            Product g = {x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, s.mp, along, tm};
-            launch_kernel((orth_product_kernel<SPLIT, GRAM, DO>), dim3(half, L), dim3(256), 0, stream, g, res);
-            g = {a, a, a, e, e, da, de, c[1], c[2], s.mp, across, tm};
-            launch_kernel((orth_product_kernel<SPLIT, POLY, DO>), dim3(half, L), dim3(256), 0, stream, g, res);
-            g = {e, xt[now], x[now], x[now ^ 1], xt[now ^ 1], de, nullptr, c[0], 0.f, s.mp, across, tn};
-            auto last = k + 1 < call.steps ? orth_product_kernel<SPLIT, NEXT, DO> : orth_product_kernel<SPLIT, LAST, DO>;
-            launch_kernel(last, dim3(static_cast<unsigned>(tm) * tn, L), dim3(256), 0, stream, g, res);
+            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, s.mp, along, 0, 0}, res, L, s.mp, s.mp,
+                                            stream);
+            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], s.mp, across, 0, 0}, res, L, s.mp, s.mp, stream);
+            const Product next = {e, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], de, nullptr, c[0], 0.f, s.mp, across, 0, 0};
+            if (k + 1 < call.steps)
+                launch_product<SPLIT, NEXT, DO>(next, res, L, s.mp, s.np, stream);
+            else
+                launch_product<SPLIT, LAST, DO>(next, res, L, s.mp, s.np, stream);
         }
     }
     return launch_status();
