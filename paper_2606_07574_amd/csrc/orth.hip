@@ -40,8 +40,9 @@ constexpr int kPad = 64;         // rows and columns of the stored matrices are 
 // A stored matrix: panels of 64 bytes of every row, one row behind the other, so that a tile's rows of one
 // panel are one piece of memory, which goes to LDS as it is. SPLIT: 16 columns' hi and then their lo;
 // otherwise 32 columns' hi, and lo, where it is kept, the same way in a matrix of its own. The 16-byte piece c
-// of row r lies at place c ^ (r / 2 mod 4) of its 64 bytes: eight lanes that read one piece of eight
-// neighbouring rows from LDS find it in eight different places of 128 bytes.
+// of row r lies at place c ^ (r / 4 mod 4) of its 64 bytes: sixteen lanes that read one piece of sixteen
+// neighbouring rows from LDS find it in sixteen different places of its 256 bytes of banks (with r / 2, which is
+// right for 128, half of the cycles of LDS were conflicts).
 struct Plane {
     char* hi;
     char* lo;
@@ -56,14 +57,20 @@ template <bool SPLIT>
 __device__ __forceinline__ int64_t place(const Plane& p, int64_t row, int64_t col) {
     constexpr int N = panel_cols(SPLIT);
     const int piece = static_cast<int>(col % N / 8);
-    return (col / N * p.rows + row) * 64 + 16 * (piece ^ static_cast<int>(row / 2 & 3));
+    return (col / N * p.rows + row) * 64 + 16 * (piece ^ static_cast<int>(row / 4 & 3));
 }
 
+typedef _Float16 h2 __attribute__((ext_vector_type(2)));
+
+// Eight values as hi and lo: two conversions of a pair each, and the rest by one multiply-add of mixed types.
 __device__ __forceinline__ void halves(const float v[8], h8* hi, h8* lo) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        (*hi)[e] = static_cast<_Float16>(v[e]);
-        (*lo)[e] = static_cast<_Float16>(v[e] - static_cast<float>((*hi)[e]));
+    for (int e = 0; e < 8; e += 2) {
+        const h2 x = __builtin_convertvector((f32x2{v[e], v[e + 1]}), h2);
+        const h2 y = __builtin_convertvector((f32x2{__builtin_fmaf(static_cast<float>(x[0]), -1.f, v[e]),
+                                                    __builtin_fmaf(static_cast<float>(x[1]), -1.f, v[e + 1])}), h2);
+        (*hi)[e] = x[0], (*hi)[e + 1] = x[1];
+        (*lo)[e] = y[0], (*lo)[e + 1] = y[1];
     }
 }
 
@@ -75,13 +82,6 @@ __device__ __forceinline__ void store8(const Plane& p, int64_t matrix, int64_t r
         *reinterpret_cast<h8*>(p.hi + (at ^ 32)) = lo;
     else if (p.lo)
         *reinterpret_cast<h8*>(p.lo + at) = lo;
-}
-
-template <bool SPLIT>
-__device__ __forceinline__ void load8(const Plane& p, int64_t matrix, int64_t row, int64_t col, h8* hi, h8* lo) {
-    const int64_t at = matrix * p.stride + place<SPLIT>(p, row, col);
-    *hi = *reinterpret_cast<const h8*>(p.hi + at);
-    *lo = *reinterpret_cast<const h8*>(SPLIT ? p.hi + (at ^ 32) : p.lo + at);
 }
 
 // ---------------------------------------------------------------------------
@@ -251,30 +251,73 @@ struct Result {
     const float* lr_at;
 };
 
-typedef uint32_t v4u_at2 __attribute__((ext_vector_type(4), aligned(2)));
+// Four waves have (32 W) x (32 W) of a (64 W) x (64 W) tile each; KS groups of four take a KS-th of the panels each and
+// add up at the end. A group's `stages` panels of both operands lie in LDS: while one is multiplied the next
+// one is there and the others are on their way. At the middle of a stage the block's waves meet: what the
+// next stage reads has come then, and the one before is read by nobody any more, whose place the last one
+// takes.
+constexpr int stages(int w) { return w == 3 ? 6 : 5; }
+[[maybe_unused]] constexpr int kRawBuffer = 0x00027000;  // a buffer of bytes, addresses outside of it read as zero
 
-// Eight neighbouring values of a row of the caller's array, of which the first `n` are there.
+template <int W>
+constexpr int stage_bytes() { return 2 * 64 * W * 64; }
+
+// The 32 x 32 parts of a stored matrix from a row and a column on, whole multiples of 32: each is four (without
+// lo: two) pieces of memory of 1 KB, which a wave reads and writes 16 bytes a lane. An image is their copy
+// in LDS: SPLIT: 2 KB of two panels; otherwise 2 KB of hi and of lo.
+template <bool SPLIT>
+struct Parts {
+    char *hi, *lo;
+    int64_t across;  // bytes from 32 columns to the next
+
+    __device__ __forceinline__ Parts(const Plane& p, int64_t matrix, int64_t row, int64_t col) {
+        const int64_t at = matrix * p.stride + (col / panel_cols(SPLIT) * p.rows + row) * 64;
+        hi = p.hi + at;
+        lo = SPLIT ? p.hi + at + p.rows * 64 : p.lo + at;
+        across = p.rows * (SPLIT ? 128 : 64);
+    }
+    // kilobyte k of the part `r` parts down and `c` parts across
+    __device__ __forceinline__ char* kilobyte(int r, int c, int k) const {
+        return (k < 2 ? hi : lo) + c * across + r * 2048 + 1024 * (k & 1);
+    }
+};
+
+// Where the piece of eight columns from `col` (0, 8, 16, 24) on lies in row `row` of an image.
+template <bool SPLIT>
+__device__ __forceinline__ int spot(int row, int col, bool lo) {
+    if constexpr (SPLIT)
+        return 2048 * (col >> 4) + row * 64 + 16 * (((col >> 3 & 1) + (lo ? 2 : 0)) ^ (row >> 2 & 3));
+    else
+        return (lo ? 2048 : 0) + row * 64 + 16 * ((col >> 3) ^ (row >> 2 & 3));
+}
+
+// Four neighbouring values of a row of the caller's array, of which `n` are there.
 template <int DO>
-__device__ __forceinline__ void put_row(void* out, int64_t at, int64_t n, const float v[8]) {
-    if (n >= 8) {
+__device__ __forceinline__ v4f read4(const void* out, int64_t at, int64_t n) {
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n >= 4) {
+        load4<DO>(out, at, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) v[e] = load_value<DO>(out, at + e);
+    }
+    return v4f{v[0], v[1], v[2], v[3]};
+}
+
+template <int DO>
+__device__ __forceinline__ void write4(void* out, int64_t at, int64_t n, const v4f v) {
+    if (n >= 4) {
         if constexpr (DO == BIRKHOFF4_BF16) {
-            v4u_at2 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
-            *reinterpret_cast<v4u_at2*>(static_cast<uint16_t*>(out) + at) = o;
+            *reinterpret_cast<v2u_at2*>(static_cast<uint16_t*>(out) + at) = v2u_at2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
         } else {
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                v4u_at4 o;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(v[4 * h + e]);
-                *reinterpret_cast<v4u_at4*>(static_cast<float*>(out) + at + 4 * h) = o;
-            }
+            *reinterpret_cast<v4u_at4*>(static_cast<float*>(out) + at) =
+                v4u_at4{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
         }
         return;
     }
 #pragma unroll
-    for (int e = 0; e < 7; ++e) {
+    for (int e = 0; e < 3; ++e) {
         if (e >= n) continue;
         if constexpr (DO == BIRKHOFF4_BF16)
             static_cast<uint16_t*>(out)[at + e] = static_cast<uint16_t>(pack_bf16(v[e], 0.f));
@@ -283,39 +326,36 @@ __device__ __forceinline__ void put_row(void* out, int64_t at, int64_t n, const 
     }
 }
 
-// A block's four waves have (32 W) x (32 W) of a (64 W) x (64 W) tile each. Four stages of one panel of
-// both operands lie in LDS: while one is multiplied the next one is there and two are on their way, so a
-// load has two stages' time. At the middle of a stage the waves meet: what the next stage reads has come then,
-// and the one before is read by nobody any more, whose place the fourth takes.
-constexpr int kStages = 4;
-constexpr int kTurnPitch = 40;  // fp16 values of a row of 32 on its way to the other order
-
-template <int W>
-constexpr int stage_bytes() { return 2 * 64 * W * 64; }
-
-#define ORTH_WAIT(n) asm volatile("s_waitcnt vmcnt(" #n ")\n\ts_barrier" ::: "memory")
-
-// 2 W reads of LDS (and as many loads), one behind each of the first of N products, so that the matrix
-// cores do not wait for all of them.
+// Of N products, one ahead of each of 2 W reads of LDS and then, where there are LOADS, of the 2 W loads, so that
+// the matrix cores do not wait for all of them (the loads write LDS, so they are not put before a read).
 template <int W, int N, bool LOADS>
 __device__ __forceinline__ void mix_reads() {
     if constexpr (W > 1) {
+        constexpr int left = N - 2 * W, each = left >= 2 * W ? 1 : left > 0 ? (2 * W + left - 1) / left : 2 * W;
 #pragma unroll
         for (int k = 0; k < 2 * W; ++k) {
             __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
             __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            if constexpr (LOADS) __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
         }
-        __builtin_amdgcn_sched_group_barrier(0x008, N - 2 * W, 0);
+        if constexpr (LOADS) {
+#pragma unroll
+            for (int k = 0; k < 2 * W; k += each) {
+                __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+                __builtin_amdgcn_sched_group_barrier(0x010, each, 0);
+            }
+        }
+        __builtin_amdgcn_sched_group_barrier(0x008, left > 0 ? left : 0, 0);
     }
 }
 
-template <bool SPLIT, int KIND, int DO, int W>
-__global__ __launch_bounds__(256, W <= 2 ? 2 : 1) void orth_product_kernel(Product g, Result res) {
+template <bool SPLIT, int KIND, int DO, int W, int KS>
+__global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_kernel(Product g, Result res) {
     constexpr int T = 64 * W;
-    static_assert(kStages * stage_bytes<W>() >= 4 * 2 * 32 * kTurnPitch * 2, "the turning takes the stages' place");
-    __shared__ __attribute__((aligned(128))) char lds[kStages * stage_bytes<W>()];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    constexpr int S = stages(W), STAGE = stage_bytes<W>();
+    static_assert(KS * S * STAGE >= KS * 4 * W * W * 4096, "the sums take the stages' place");
+    __shared__ __attribute__((aligned(128))) char lds[KS * S * STAGE];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
+    const int group = KS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
     const int64_t matrix = blockIdx.y;
     // Blocks go round the eight XCDs: each XCD takes neighbouring tiles, whose rows its L2 holds.
     const int per = (g.tiles + 7) / 8, tile = blockIdx.x % 8 * per + blockIdx.x / 8;
@@ -327,42 +367,54 @@ __global__ __launch_bounds__(256, W <= 2 ? 2 : 1) void orth_product_kernel(Produ
         while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
         tj = tile - ti * (ti + 1) / 2;
     } else {
-        ti = tile / g.tj;
-        tj = tile % g.tj;
+        // four rows of tiles, column by column: those of an XCD are as many rows as columns, about
+        const int rows = g.tiles / g.tj, band = tile / (4 * g.tj), high = rows - 4 * band < 4 ? rows - 4 * band : 4;
+        const int in = tile - band * 4 * g.tj;
+        ti = 4 * band + in % high;
+        tj = in / high;
     }
     // Rows behind the stored ones, of a tile that hangs over: others in their place, which nothing is made of.
-    const char *p[W], *q[W];
+    int pr[W], qr[W];  // bytes from the panel's first row
 #pragma unroll
     for (int k = 0; k < W; ++k) {
         const int64_t r = 16 * (W * wave + k), ri = ti * static_cast<int64_t>(T) + r, rj = tj * static_cast<int64_t>(T) + r;
-        p[k] = g.P.hi + matrix * g.P.stride + (ri < g.P.rows ? ri : g.P.rows - 16) * 64 + lane * 16;
-        q[k] = g.Q.hi + matrix * g.Q.stride + (rj < g.Q.rows ? rj : g.Q.rows - 16) * 64 + lane * 16;
+        pr[k] = static_cast<int>((ri < g.P.rows ? ri : g.P.rows - 16) * 64);
+        qr[k] = static_cast<int>((rj < g.Q.rows ? rj : g.Q.rows - 16) * 64);
     }
-    const int64_t p_panel = g.P.rows * 64, q_panel = g.Q.rows * 64;
-    auto load = [&](int stage) {  // past the last panel: the last one again, into a place that is not read
-        const int64_t at = stage < g.panels ? stage : g.panels - 1;
-        char* to = lds + (stage % kStages) * stage_bytes<W>() + 1024 * W * wave;
+    [[maybe_unused]] char *const p0 = g.P.hi + matrix * g.P.stride, *const q0 = g.Q.hi + matrix * g.Q.stride;
+    [[maybe_unused]] const int p_panel = static_cast<int>(g.P.rows * 64), q_panel = static_cast<int>(g.Q.rows * 64);
+    [[maybe_unused]] const int lane16 = lane * 16;
+    const int panels = g.panels / KS, begin = panels * group;
+    char* const own = lds + group * (S * STAGE);
+    int asked = begin, room = 1024 * W * wave;  // the next panel and its place
+    auto load = [&] {  // past the last panel: the last one again, into a place that is not read
+#ifdef __HIP_DEVICE_COMPILE__  // the host's compiler has no such buffers
+        const auto pb = __builtin_amdgcn_make_buffer_rsrc(p0 + static_cast<int64_t>(asked) * p_panel, 0, p_panel, kRawBuffer);
+        const auto qb = __builtin_amdgcn_make_buffer_rsrc(q0 + static_cast<int64_t>(asked) * q_panel, 0, q_panel, kRawBuffer);
 #pragma unroll
         for (int k = 0; k < W; ++k) {
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(p[k] + at * p_panel),
-                                             (__attribute__((address_space(3))) void*)(to + 1024 * k), 16, 0, 0);
-            __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)(q[k] + at * q_panel),
-                                             (__attribute__((address_space(3))) void*)(to + T * 64 + 1024 * k), 16, 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(pb, (__attribute__((address_space(3))) void*)(own + room + 1024 * k), 16, lane16,
+                                                     pr[k], 0, 0);
+            __builtin_amdgcn_raw_ptr_buffer_load_lds(qb, (__attribute__((address_space(3))) void*)(own + room + T * 64 + 1024 * k), 16,
+                                                     lane16, qr[k], 0, 0);
         }
+#endif
+        asked = asked + 1 < begin + panels ? asked + 1 : asked;
+        room = room >= (S - 1) * STAGE ? room - (S - 1) * STAGE : room + STAGE;
     };
     const int wi = 32 * W * (wave >> 1), wj = 32 * W * (wave & 1);
     const int r32 = lane & 31, h = lane >> 5;
-    const char* own_rows = lds + (wi + r32) * 64;
-    const char* col_rows = lds + (T + wj + r32) * 64;
-    const int swizzle = (r32 >> 1) & 3;
+    const char* own_rows = own + (wi + r32) * 64;
+    const char* col_rows = own + (T + wj + r32) * 64;
+    const int swizzle = (r32 >> 2) & 3;
     // pieces 2 part + h: SPLIT: hi (part 0) or lo of 16 columns; otherwise 16 of 32 columns
-    auto fetch = [&](int stage, int part, h8 (&a)[W], h8 (&b)[W]) {
-        const int at = (stage % kStages) * stage_bytes<W>() + 16 * ((2 * part + h) ^ swizzle);
+    auto fetch = [&](int from, int part, h8 (&a)[W], h8 (&b)[W]) {
+        const int at = from + 16 * ((2 * part + h) ^ swizzle);
+        a[0] = *reinterpret_cast<const h8*>(own_rows + at);  // in the order in which they are multiplied
 #pragma unroll
-        for (int k = 0; k < W; ++k) {
-            a[k] = *reinterpret_cast<const h8*>(own_rows + at + 2048 * k);
-            b[k] = *reinterpret_cast<const h8*>(col_rows + at + 2048 * k);
-        }
+        for (int k = 0; k < W; ++k) b[k] = *reinterpret_cast<const h8*>(col_rows + at + 2048 * k);
+#pragma unroll
+        for (int k = 1; k < W; ++k) a[k] = *reinterpret_cast<const h8*>(own_rows + at + 2048 * k);
     };
     v16f acc[W][W] = {};
     auto multiply = [&](const h8 (&a)[W], const h8 (&b)[W]) {
@@ -371,172 +423,271 @@ __global__ __launch_bounds__(256, W <= 2 ? 2 : 1) void orth_product_kernel(Produ
 #pragma unroll
             for (int j = 0; j < W; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_f16(a[i], b[j], acc[i][j], 0, 0, 0);
     };
-    auto meet = [&] {  // the next stage is there, one further is on its way: 2 W loads of this wave
+    auto meet = [&] {  // the next stage is there; of those behind it 2 W loads each of this wave are on their way
         __builtin_amdgcn_sched_barrier(0);
-        if constexpr (W == 1) ORTH_WAIT(2);
-        if constexpr (W == 2) ORTH_WAIT(4);
-        if constexpr (W == 3) ORTH_WAIT(6);
-        if constexpr (W == 4) ORTH_WAIT(8);
+        asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"i"((S - 3) * 2 * W) : "memory");
         __builtin_amdgcn_sched_barrier(0);  // what was read before is also multiplied before
     };
-    load(0);
-    load(1);
-    load(2);
+    // What the ends of the 32 x 32 parts need from memory is asked for here: behind the sums, and behind the
+    // stores of the part before (for which a wait for a later load waits too), its latency would be seen each
+    // time (2900 cycles a part).
+    const int64_t ib = static_cast<int64_t>(ti) * T + wi, jb = static_cast<int64_t>(tj) * T + wj;
+    const float* sd = KIND != GRAM ? g.src_diag + matrix * g.side : nullptr;
+    // parts that this group ends: its own half of the columns, or all of them for the first group
+    constexpr bool HALVES = KS == 2 && W == 2;
+    constexpr int ENDS = HALVES ? W : W * W;
+    auto part_a = [&](int k) { return HALVES ? k : k / W; };
+    auto part_b = [&](int k) { return HALVES ? group : k % W; };
+    auto there = [&](int k) {  // uniform over the wave: rows come in whole 64s
+        return ib + 32 * part_a(k) < g.P.rows && jb + 32 * part_b(k) < g.Q.rows &&
+               !((KIND == GRAM || KIND == POLY) && ib + 32 * part_a(k) < jb + 32 * part_b(k));
+    };
+    v4u src[ENDS][4];
+    v4f di[W][2][2];
+    float dj[W];
+    // Places of an image that a lane writes and reads, part by part at constant distances: its pieces of row j
+    // (turned order), and, value by value, column j of rows 8 h .. + 3 and 8 h + 4 .. (own order).
+    const int lane16b = lane * 16;
+    int piece_at[2][2], value_at[2][2];  // [hi, lo][first or second]
+#pragma unroll
+    for (int y = 0; y < 2; ++y)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            piece_at[y][u] = spot<SPLIT>(r32, 16 * u + 8 * h, y == 1);
+            value_at[y][u] = spot<SPLIT>(8 * h + 4 * u, r32 & 24, y == 1) + 2 * (r32 & 7);
+        }
+    auto out_at = [&](int k, int t, int64_t* n) {  // LAST: four values of a row of the caller's array, and how many are there
+        const int64_t i0 = ib + 32 * part_a(k), j0 = jb + 32 * part_b(k);
+        const int64_t row = (res.tall ? j0 : i0) + 8 * t + lane / 8, col = (res.tall ? i0 : j0) + 4 * (lane % 8);
+        *n = row < res.rows ? res.cols - col : 0;
+        return ((res.first + matrix) * res.rows + row) * res.cols + col;
+    };
+    const bool ends = HALVES || group == 0;
+    if constexpr (KIND != GRAM)
+        if (ends) {
+            const Parts<SPLIT> from(g.src, matrix, jb, ib);
+#pragma unroll
+            for (int k = 0; k < ENDS; ++k)
+                if (there(k)) {
+#pragma unroll
+                    for (int u = 0; u < 4; ++u)
+                        src[k][u] = *reinterpret_cast<const v4u*>(from.kilobyte(part_b(k), part_a(k), u) + lane16b);
+                }
+#pragma unroll
+            for (int a = 0; a < W; ++a)
+                if (ib + 32 * a < g.P.rows)
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) di[a][u / 2][u % 2] = *reinterpret_cast<const v4f*>(sd + ib + 32 * a + 16 * (u / 2) + 8 * h + 4 * (u % 2));
+            if constexpr (KIND == POLY)
+#pragma unroll
+                for (int b = 0; b < W; ++b)
+                    if (jb + 32 * b < g.Q.rows) dj[b] = sd[jb + 32 * b + r32];
+        }
+#pragma unroll
+    for (int k = 0; k < S - 1; ++k) load();
     h8 a0[W], b0[W], a1[W], b1[W];
     meet();
     fetch(0, 0, a0, b0);
+    int now = 0;
 #pragma unroll 1
-    for (int stage = 0; stage < g.panels; ++stage) {
-        fetch(stage, 1, a1, b1);
+    for (int stage = 0; stage < panels; ++stage) {
+        fetch(now, 1, a1, b1);
         multiply(a0, b0);
         mix_reads<W, W * W, false>();
         meet();
-        load(stage + 3);
+        now = now == (S - 1) * STAGE ? 0 : now + STAGE;
         if constexpr (SPLIT) {
             h8 a2[W], b2[W];
-            fetch(stage + 1, 0, a2, b2);
+            fetch(now, 0, a2, b2);
+            load();
             multiply(a0, b1);
             multiply(a1, b0);
             mix_reads<W, 2 * W * W, true>();
 #pragma unroll
             for (int k = 0; k < W; ++k) a0[k] = a2[k], b0[k] = b2[k];
         } else {
-            fetch(stage + 1, 0, a0, b0);
+            fetch(now, 0, a0, b0);
+            load();
             multiply(a1, b1);
             mix_reads<W, W * W, true>();
         }
     }
-    ORTH_WAIT(0);
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
 
-    // A lane has column j of 32 x 32 values, rows 8 g + 4 h + 0..3 of it in acc[4 g ..]: exchanged between the
-    // wave's halves, eight neighbouring rows, which are one piece of row j in the other order. What src adds
-    // is read in that order too. The own order is made of it through LDS.
-    const int64_t ib = static_cast<int64_t>(ti) * T + wi, jb = static_cast<int64_t>(tj) * T + wj;
-    const float* sd = KIND != GRAM ? g.src_diag + matrix * g.side : nullptr;
-    float* od = KIND == GRAM || KIND == POLY ? g.own_diag + matrix * g.side : nullptr;
-    _Float16* turn = reinterpret_cast<_Float16*>(lds) + wave * 2 * 32 * kTurnPitch;
-    float shrink = 0.f, by = 0.f;
-    if constexpr (KIND == LAST) {
-        const float rate = res.update && res.lr_at ? res.lr * *res.lr_at : res.lr;
-        shrink = 1.f - rate * res.decay, by = rate * res.scale;
-    }
+    // The groups' sums are added through LDS, in their order; two groups end half of the parts each.
+    auto slot = [&](int of, int q) { return reinterpret_cast<v4f*>(lds) + ((of * 4 + wave) * W * W + q) * 256; };
+    if constexpr (KS > 1) {
 #pragma unroll
-    for (int b = 0; b < W; ++b) {
-        const int64_t j = jb + 32 * b + r32;
-        if (jb + 32 * b >= g.Q.rows) continue;  // uniform over the wave: rows come in whole 64s
-        h8 shi[2 * W], slo[2 * W];
-        float dj = 0.f;
+        for (int q = 0; q < W * W; ++q)
+            if (HALVES ? q % W != group : group > 0)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const v16f& c = acc[q / W][q % W];
+                    slot(group, q)[r * 64 + lane] = v4f{c[4 * r], c[4 * r + 1], c[4 * r + 2], c[4 * r + 3]};
+                }
+        __syncthreads();
+        if (!ends) return;
+#pragma unroll
+        for (int q = 0; q < W * W; ++q)
+            if (!HALVES || q % W == group)
+#pragma unroll
+                for (int of = HALVES ? 0 : 1; of < (HALVES ? 1 : KS); ++of)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        const v4f x = slot(HALVES ? group ^ 1 : of, q)[r * 64 + lane];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[q / W][q % W][4 * r + e] += x[e];
+                    }
+    }
+    float rate = 0.f;
+    v4f old[ENDS][4];
+    if constexpr (KIND == LAST)
+        if (res.update) {
+            rate = res.lr_at ? res.lr * *res.lr_at : res.lr;
+#pragma unroll
+            for (int k = 0; k < ENDS; ++k)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    int64_t n;
+                    const int64_t at = out_at(k, t, &n);
+                    old[k][t] = read4<DO>(res.out, at, n);
+                }
+        }
+    const Parts<SPLIT> to_turned(g.turned, matrix, jb, ib), to_own(g.own, matrix, ib, jb);
+#pragma unroll
+    for (int k = 0; k < ENDS; ++k) {
+        if (!there(k)) continue;
+        // A lane has column j of 32 x 32 values, rows 8 g + 4 h + 0..3 of it in sum[4 g ..]: exchanged between the wave's
+        // halves, eight neighbouring rows, which are one piece of row j in the other order. What src adds is
+        // in that order too. Whatever goes to and comes from memory passes the part's place in LDS, so that
+        // a wave's accesses are whole kilobytes.
+        const int a = part_a(k), b = part_b(k);
+        // a group reads what the other one has put into its own slots
+        char* image = reinterpret_cast<char*>(HALVES ? slot(group, a * W + group) : slot(0, a * W + b));
+        v16f sum;
+        if constexpr (HALVES)
+            sum = group ? acc[a][W - 1] : acc[a][0];
+        else
+            sum = acc[k / W][k % W];
+        float v[2][8];
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(sum[8 * u + e]), __float_as_uint(sum[8 * u + 4 + e]), false, false);
+                v[u][e] = __uint_as_float(x[0]);
+                v[u][4 + e] = __uint_as_float(x[1]);
+            }
+        const bool across = (KIND == GRAM || KIND == POLY) && ib + 32 * a == jb + 32 * b;  // the diagonal
+        float one = 0.f;                                                                  // the product's value on it
+        if constexpr (KIND == GRAM || KIND == POLY)
+            if (across) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) one = 16 * u + 8 * h + e == r32 ? v[u][e] : one;
+                one /= kUnit * kUnit;
+            }
         if constexpr (KIND != GRAM) {
 #pragma unroll
-            for (int k = 0; k < 2 * W; ++k)
-                if (ib + 16 * k < g.P.rows) load8<SPLIT>(g.src, matrix, j, ib + 16 * k + 8 * h, &shi[k], &slo[k]);
-            if constexpr (KIND == POLY) dj = sd[j];
-        }
-#pragma unroll
-        for (int a = 0; a < W; ++a) {
-            if (ib + 32 * a >= g.P.rows) continue;
-            // Of a symmetric result what lies below the diagonal counts, whatever the tiles: the sum of the
-            // pieces' products is not the same bits with the factors exchanged.
-            const bool above = (KIND == GRAM || KIND == POLY) && ib + 32 * a < jb + 32 * b;
-            const bool across = (KIND == GRAM || KIND == POLY) && ib + 32 * a == jb + 32 * b;
-            if (above) continue;
+            for (int u = 0; u < 4; ++u) *reinterpret_cast<v4u*>(image + 1024 * u + lane16b) = src[k][u];
+            __builtin_amdgcn_wave_barrier();
+            const float djk = HALVES ? (group ? dj[W - 1] : dj[0]) : dj[k % W], add = g.add / kUnit;
 #pragma unroll
             for (int u = 0; u < 2; ++u) {
-                const int64_t i = ib + 32 * a + 16 * u + 8 * h;
-                float v[8];
+                const h8 hi = *reinterpret_cast<const h8*>(image + piece_at[0][u]);
+                const h8 lo = *reinterpret_cast<const h8*>(image + piece_at[1][u]);
 #pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(acc[a][b][8 * u + e]),
-                                                                    __float_as_uint(acc[a][b][8 * u + 4 + e]), false, false);
-                    v[e] = __uint_as_float(x[0]) / kUnit;
-                    v[4 + e] = __uint_as_float(x[1]) / kUnit;
-                }
-                if constexpr (KIND != GRAM) {
-                    const v4f d0 = *reinterpret_cast<const v4f*>(sd + i), d1 = *reinterpret_cast<const v4f*>(sd + i + 4);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const float di = e < 4 ? d0[e] : d1[e - 4];
-                        const float s = static_cast<float>(shi[2 * a + u][e]) + static_cast<float>(slo[2 * a + u][e]);
-                        if constexpr (KIND == POLY) {
-                            const float t = v[e];
-                            v[e] = __builtin_fmaf(__builtin_fmaf(g.add, di + dj, g.keep), s, g.add * t);
-                            if (i + e == j) {
-                                od[j] = __builtin_fmaf(g.keep, dj, g.add * __builtin_fmaf(dj, dj, t / kUnit));
-                                v[e] = 0.f;
-                            }
-                        } else {
-                            v[e] = __builtin_fmaf(g.keep + di, s, v[e]);
-                        }
-                    }
-                } else {
-#pragma unroll
-                    for (int e = 0; e < 8; ++e)
-                        if (i + e == j) {
-                            od[j] = v[e] / kUnit;
-                            v[e] = 0.f;
-                        }
-                }
-                if constexpr (KIND == LAST) {
-                    const int64_t base = (res.first + matrix) * res.rows * res.cols;
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) v[e] /= kUnit;
-                    if (res.tall) {  // row j, columns i..
-                        const int64_t at = base + j * res.cols + i;
-                        if (j < res.rows && i < res.cols) {
-                            if (res.update) {
-#pragma unroll
-                                for (int e = 0; e < 8; ++e)
-                                    if (i + e < res.cols) v[e] = __builtin_fmaf(-by, v[e], shrink * load_value<DO>(res.out, at + e));
-                            }
-                            put_row<DO>(res.out, at, res.cols - i, v);
-                        }
-                    } else {  // rows i.., column j: neighbouring lanes have neighbours
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            if (i + e >= res.rows || j >= res.cols) continue;
-                            const int64_t at = base + (i + e) * res.cols + j;
-                            if (res.update) v[e] = __builtin_fmaf(-by, v[e], shrink * load_value<DO>(res.out, at));
-                            if constexpr (DO == BIRKHOFF4_BF16)
-                                static_cast<uint16_t*>(res.out)[at] = static_cast<uint16_t>(pack_bf16(v[e], 0.f));
-                            else
-                                static_cast<float*>(res.out)[at] = v[e];
-                        }
-                    }
-                } else {
-                    h8 hi, lo;
-                    halves(v, &hi, &lo);
-                    if (!across) store8<SPLIT>(g.turned, matrix, j, i, hi, lo);
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) {
-                        const int row = 16 * u + 8 * h + e;
-                        if (across && row < r32) continue;
-                        turn[row * kTurnPitch + r32] = hi[e];
-                        if (SPLIT || KIND == GRAM) turn[(32 + row) * kTurnPitch + r32] = lo[e];
-                        if (across) {
-                            turn[r32 * kTurnPitch + row] = hi[e];
-                            if (SPLIT || KIND == GRAM) turn[(32 + r32) * kTurnPitch + row] = lo[e];
-                        }
-                    }
+                for (int e = 0; e < 8; ++e) {
+                    const float d = di[HALVES ? k : k / W][u][e / 4][e % 4], s = __builtin_fmaf(static_cast<float>(hi[e]), 1.f, static_cast<float>(lo[e]));
+                    if constexpr (KIND == POLY)
+                        v[u][e] = __builtin_fmaf(__builtin_fmaf(g.add, d + djk, g.keep), s, add * v[u][e]);
+                    else
+                        v[u][e] = __builtin_fmaf(g.keep + d, s, v[u][e] / kUnit);
                 }
             }
-            // the other order: a lane has 16 columns of row i
-            if constexpr (KIND != LAST) {
-                __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_wave_barrier();
+            if (KIND == POLY && across) one = __builtin_fmaf(g.keep, djk, g.add * __builtin_fmaf(djk, djk, one));
+        } else {
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const _Float16* from = turn + r32 * kTurnPitch + 16 * h + 8 * u;
-                    const h8 hi = *reinterpret_cast<const h8*>(from);
-                    h8 lo = hi;
-                    if (SPLIT || KIND == GRAM) lo = *reinterpret_cast<const h8*>(from + 32 * kTurnPitch);
-                    store8<SPLIT>(g.own, matrix, ib + 32 * a + r32, jb + 32 * b + 16 * h + 8 * u, hi, lo);
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[u][e] /= kUnit;
+        }
+        if constexpr (KIND == LAST) {
+            // rows of the caller's array in LDS, 128 bytes each, whose 16-byte pieces change places by the row
+            auto at = [&](int row, int col) { return reinterpret_cast<float*>(image + row * 128 + 16 * ((col >> 2) ^ (row & 7)) + 4 * (col & 3)); };
+            const float shrink = 1.f - rate * res.decay, by = rate * res.scale;
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int i = 16 * u + 8 * h + e;
+                    *(res.tall ? at(r32, i) : at(i, r32)) = v[u][e] / kUnit;
                 }
-                __builtin_amdgcn_wave_barrier();
+            __builtin_amdgcn_wave_barrier();
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+                v4f o = *reinterpret_cast<const v4f*>(at(8 * t + lane / 8, 4 * (lane % 8)));
+                if (res.update)
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(-by, o[e], shrink * old[k][t][e]);
+                int64_t n;
+                const int64_t to = out_at(k, t, &n);
+                write4<DO>(res.out, to, n, o);
             }
+        } else {
+            constexpr int TURNED = SPLIT || KIND == GRAM || KIND == NEXT ? 4 : 2, OWN = SPLIT || KIND == GRAM ? 4 : 2;
+            if (across) {  // the diagonal itself lies elsewhere
+                if (r32 / 8 % 2 == h) g.own_diag[matrix * g.side + jb + 32 * b + r32] = one;
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[u][e] = 16 * u + 8 * h + e == r32 ? 0.f : v[u][e];
+            }
+            h8 hi[2], lo[2];
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                halves(v[u], &hi[u], &lo[u]);
+                *reinterpret_cast<h8*>(image + piece_at[0][u]) = hi[u];
+                if (TURNED == 4 || OWN == 4) *reinterpret_cast<h8*>(image + piece_at[1][u]) = lo[u];
+            }
+            __builtin_amdgcn_wave_barrier();
+            auto values = [&](bool all) {
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) {
+                        if (!all && 16 * u + 8 * h + e < r32) continue;
+                        *reinterpret_cast<_Float16*>(image + value_at[0][e / 4] + 1024 * u + 64 * (e % 4)) = hi[u][e];
+                        if (OWN == 4) *reinterpret_cast<_Float16*>(image + value_at[1][e / 4] + 1024 * u + 64 * (e % 4)) = lo[u][e];
+                    }
+            };
+            if (!across) {
+                v4u out[TURNED];
+#pragma unroll
+                for (int u = 0; u < TURNED; ++u) out[u] = *reinterpret_cast<const v4u*>(image + 1024 * u + lane16b);
+#pragma unroll
+                for (int u = 0; u < TURNED; ++u) *reinterpret_cast<v4u*>(to_turned.kilobyte(b, a, u) + lane16b) = out[u];
+                __builtin_amdgcn_wave_barrier();
+                values(true);
+            } else {
+                // Of a symmetric result what lies below the diagonal counts, whatever the tiles (the sum of the
+                // pieces' products is not the same bits with the factors exchanged): above it the turned
+                // order, which is there, has it.
+                values(false);
+            }
+            __builtin_amdgcn_wave_barrier();
+            v4u out[OWN];
+#pragma unroll
+            for (int u = 0; u < OWN; ++u) out[u] = *reinterpret_cast<const v4u*>(image + 1024 * u + lane16b);
+#pragma unroll
+            for (int u = 0; u < OWN; ++u) *reinterpret_cast<v4u*>(to_own.kilobyte(a, b, u) + lane16b) = out[u];
         }
     }
 }
-
-#undef ORTH_WAIT
 
 // ---------------------------------------------------------------------------
 // Matrices with a side of at most 80
@@ -897,36 +1048,53 @@ int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStrea
     return launch_status();
 }
 
-// The tile's side in 64s for `rows` x `cols` values a matrix (`half`: of a symmetric result) and its tiles: what the
-// blocks that follow each other on a compute unit take together, by the cycles of a panel, which are the
-// matrix cores' or LDS's, whichever takes longer: 128 bytes a cycle, each operand read by two waves and
-// written once.
-int choose_tile(bool split, int64_t L, int64_t rows, int64_t cols, bool half, int64_t* tiles, int64_t* tj) {
-    int best = 1;
+// The tile and the groups of a product: the one of least time, by what a block takes for its panels with few and
+// with all compute units busy (us a panel; the matrix cores' clock and L2 are shared) and for its beginning
+// and end, fitted to products of 128 to 4096 rows. Measured (us): (A X) of 2560 x 10240 in fp32 128 x 128 383, in
+// two groups 415, 192 x 192 374, 64 x 64 554; X X^T of it 217, 201, 325, 339, of 1000 x 2565 43, 39, 78, 22; of
+// 4096 x 4096 in bf16 107, 112, 84, 167.
+struct Tile {
+    int w, groups, slots;  // its side in 64s, and how many blocks run at once
+    double few, all, ends;
+};
+constexpr Tile kTiles[2][4] = {
+    {{1, 2, 512, 0.20, 0.46, 4.0}, {2, 1, 512, 0.21, 0.45, 7.0}, {2, 2, 256, 0.33, 0.50, 8.0}, {3, 1, 256, 0.36, 0.62, 8.0}},
+    {{1, 4, 256, 0.40, 0.53, 4.0}, {2, 1, 512, 0.23, 0.55, 6.0}, {2, 2, 256, 0.42, 0.62, 8.0}, {3, 1, 256, 0.44, 0.75, 8.0}}};
+
+int64_t tiles_of(int64_t rows, int64_t cols, bool half, int w, int64_t* tj) {
+    const int64_t t = 64 * w, i = (rows + t - 1) / t, j = (cols + t - 1) / t;
+    *tj = j;
+    return half ? i * (i + 1) / 2 : i * j;
+}
+
+int choose_tile(bool split, bool half, bool last, int64_t L, int64_t rows, int64_t cols, int panels) {
+    int best = 0;
     double least = 0.0;
-    for (int w = 1; w <= 4; ++w) {
-        const int64_t t = 64 * w, i = (rows + t - 1) / t, j = (cols + t - 1) / t, n = half ? i * (i + 1) / 2 : i * j;
-        const int together = w <= 2 ? 2 : 1;
-        const double rounds = static_cast<double>((n * L + 256 * together - 1) / (256 * together));
-        const double cores = (split ? 96.0 : 64.0) * w * w, memory = 192.0 * w;
-        const double cost = rounds * together * (cores > memory ? cores : memory);
-        if (w == 1 || cost < least) {
-            least = cost, best = w;
-            *tiles = n, *tj = j;
-        }
+    for (int k = 0; k < (last ? 3 : 4); ++k) {  // the largest tile's last step would not fit the registers
+        const Tile& t = kTiles[split][k];
+        int64_t tj;
+        const int64_t blocks = L * tiles_of(rows, cols, half, t.w, &tj), rest = blocks % t.slots;
+        auto round = [&](double busy) { return panels / t.groups * (t.few + (t.all - t.few) * busy) + t.ends; };
+        const double cost = blocks / t.slots * round(1.0) + (rest ? round(static_cast<double>(rest) / t.slots) : 0.0);
+        if (k == 0 || cost < least) least = cost, best = k;
     }
     return best;
 }
 
 template <bool SPLIT, int KIND, int DO>
 void launch_product(Product g, const Result& res, unsigned L, int64_t rows, int64_t cols, hipStream_t stream) {
-    int64_t tiles = 0, tj = 0;
-    const int w = choose_tile(SPLIT, L, rows, cols, KIND == GRAM || KIND == POLY, &tiles, &tj);
+    constexpr bool HALF = KIND == GRAM || KIND == POLY;
+    const int k = choose_tile(SPLIT, HALF, KIND == LAST, L, rows, cols, g.panels);
+    const Tile& t = kTiles[SPLIT][k];
+    int64_t tj;
+    const int64_t tiles = tiles_of(rows, cols, HALF, t.w, &tj);
     g.tiles = static_cast<int>(tiles), g.tj = static_cast<int>(tj);
-    auto kern = w == 1   ? orth_product_kernel<SPLIT, KIND, DO, 1>
-                : w == 2 ? orth_product_kernel<SPLIT, KIND, DO, 2>
-                : w == 3 ? orth_product_kernel<SPLIT, KIND, DO, 3> : orth_product_kernel<SPLIT, KIND, DO, 4>;
-    launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((tiles + 7) / 8)), L), dim3(256), 0, stream, g, res);
+    auto kern = k == 0   ? orth_product_kernel<SPLIT, KIND, DO, 1, kTiles[SPLIT][0].groups>
+                : k == 1 ? orth_product_kernel<SPLIT, KIND, DO, 2, 1> : orth_product_kernel<SPLIT, KIND, DO, 2, 2>;
+    if constexpr (KIND != LAST)
+        if (k == 3) kern = orth_product_kernel<SPLIT, KIND, DO, 3, 1>;
+    launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((tiles + 7) / 8)), L), dim3(static_cast<unsigned>(256 * t.groups)), 0, stream, g,
+                  res);
 }
 
 template <int DG, int DO, bool MOMENTUM>

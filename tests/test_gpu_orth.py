@@ -108,17 +108,25 @@ def test_bad_matrices_alone(shape, dtype, bad):
 
 
 def test_batches():
-    """A batch is its matrices one by one, also where the workspace takes a part of it at a time."""
-    for shape in ((37, 33, 100), (3, 140, 200)):
+    """A batch is its matrices one by one, also where the workspace takes a part of it at a time: the same
+    bits in one batch wherever a matrix stands, and within the bound of what it is alone (the number of
+    matrices may choose other tiles, and other orders of sums)."""
+    for shape in ((37, 33, 100), (3, 140, 200), (2, 300, 900)):
         G = matrices(shape, F32, 10)
+        G[-1] = G[0]
         O = b4.orth(G)
-        for k in (0, 1, shape[0] - 1):
-            assert torch.equal(b4.orth(G[k]), O[k])
+        assert torch.equal(O[-1], O[0])
+        ref, bound = orth_ref(G)
+        for k in (0, 1):
+            close(b4.orth(G[k]), ref[k:k + 1], bound[k:k + 1], f"{shape} alone")
     G = matrices((6000, 96, 100), F32, 11, "spread")
     assert b4.lib().birkhoff4_orth_work(6000, 96, 100, b4.F32) <= 1 << 30
+    G[1500] = G[5999] = G[3500].clone()
     O = b4.orth(G)
-    for k in (0, 1500, 3500, 5999):
-        assert torch.equal(b4.orth(G[k]), O[k])
+    ref, bound = orth_ref(G[[0, 1500]])
+    close(O[[0, 1500]], ref, bound, "6000 matrices")
+    assert torch.equal(O[1500], O[3500])
+    close(O[5999:], ref[1:], bound[1:], "the last part")
     assert b4.orth(G[:0]).shape == (0, 96, 100) and b4.orth(G[:, :0]).shape == (6000, 0, 100)
 
 
