@@ -24,6 +24,8 @@
 // The products are of rows with rows (both operands have the summed index along their rows), so X is kept
 // in both orders.
 
+#include <type_traits>
+
 #include "common.h"
 
 namespace {
@@ -699,7 +701,7 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
 // singular value is small, so A and F are 64-bit numbers, from products of the inputs without rounding: the
 // result is nearer than fp32 products bring it. The matrix cores' 64-bit rate is the limit of m: its cube
 // runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps), and G G^T of 80 rows
-// takes them half as long as reading fp32 G does. F X is formed in fp32.
+// takes them half as long as reading fp32 G does.
 constexpr int kNarrow = 80;
 constexpr int kSlab = 64;            // columns of X taken at a time
 constexpr int kSlabPitch = kSlab + 1;
@@ -709,57 +711,67 @@ typedef double v4d __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ v4d mfma_f64(double a, double b, v4d c) { return __builtin_amdgcn_mfma_f64_16x16x4f64(a, b, c, 0, 0, 0); }
 
 // X's rows (16 MT of them, zeros behind the m) and columns j0 .. j0 + 63 of a direction, from the caller's
-// R x C array at `base`: X = U, or for a tall U its transpose. WRITE: renews M on the way.
-template <int DG, bool MOMENTUM, bool WRITE, int MT>
-__device__ __forceinline__ void load_slab(const Source& s, int64_t base, int64_t R, int64_t C, int64_t j0, float* slab) {
-    const bool tall = R > C;
-    const int m = static_cast<int>(tall ? C : R);
-    const int64_t n = tall ? R : C;
-    const int left = static_cast<int>(n - j0 < kSlab ? n - j0 : kSlab);
-    // lines of the array: m rows of 64 values, or 64 rows of m, in pieces of four
-    const int lines = tall ? kSlab : 16 * MT, quads = tall ? 4 * MT : kSlab / 4;
-    const int used = tall ? left : m, width = tall ? m : left;
-    for (int task = threadIdx.x; task < lines * quads; task += blockDim.x) {
-        const int line = task / quads, c = 4 * (task % quads);
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (line < used && c < width) {
-            const int64_t at = base + (tall ? (j0 + line) * C + c : line * C + j0 + c);
-            float mv[4] = {0.f, 0.f, 0.f, 0.f};
-            const bool whole = c + 4 <= width;
-            if (whole) {
-                load4<DG>(s.G, at, v);
-                if constexpr (MOMENTUM) load4<BIRKHOFF4_F32>(s.M, at, mv);
-            } else {
+// R x C array: X = U, or for a tall U its transpose. A thread has MT times four neighbouring values of the
+// array, which it asks for (fetch) long before they go to LDS (put).
+template <int DG, bool MOMENTUM, int MT>
+struct Slab {
+    const Source& s;
+    int64_t base, C, n;
+    int m;
+    bool tall;
+    v4f g[MT], mo[MT];
+
+    __device__ __forceinline__ Slab(const Source& src, int64_t at, int64_t R, int64_t cols)
+        : s(src), base(at), C(cols), n(R > cols ? R : cols), m(static_cast<int>(R > cols ? cols : R)), tall(R > cols) {}
+    // where a thread's q-th four values are: in the array, and their place in the slab; how many are there
+    __device__ __forceinline__ int64_t where(int q, int64_t j0, int64_t* at, int* line, int* c) const {
+        const int left = static_cast<int>(n - j0 < kSlab ? n - j0 : kSlab), task = threadIdx.x + 256 * q;
+        if (tall) {
+            *line = task / (4 * MT), *c = 4 * (task % (4 * MT));
+            *at = base + (j0 + *line) * C + *c;
+            return *line < left ? m - *c : 0;
+        }
+        *line = task / 16, *c = 4 * (task % 16);
+        *at = base + *line * C + j0 + *c;
+        return *line < m ? left - *c : 0;
+    }
+    __device__ __forceinline__ float* value(float* slab, int line, int c) const {
+        return slab + (tall ? c * kSlabPitch + line : line * kSlabPitch + c);
+    }
+    __device__ __forceinline__ void fetch(int64_t j0) {
 #pragma unroll
-                for (int e = 0; e < 3; ++e)
-                    if (c + e < width) {
-                        v[e] = load_value<DG>(s.G, at + e);
-                        if constexpr (MOMENTUM) mv[e] = s.M[at + e];
-                    }
-            }
+        for (int q = 0; q < MT; ++q) {
+            int64_t at = base;
+            int line, c;
+            const int64_t there = j0 < n ? where(q, j0, &at, &line, &c) : 0;
+            g[q] = read4<DG>(s.G, at, there);
+            if constexpr (MOMENTUM) mo[q] = read4<BIRKHOFF4_F32>(s.M, at, there);
+        }
+    }
+    // RENEW: M on the way; SCALED: the values times `scale`
+    template <bool RENEW, bool SCALED>
+    __device__ __forceinline__ void put(int64_t j0, float* slab, double scale) {
+#pragma unroll
+        for (int q = 0; q < MT; ++q) {
+            int64_t at;
+            int line, c;
+            const int64_t there = where(q, j0, &at, &line, &c);
+            v4f u = g[q];
             if constexpr (MOMENTUM) {
-                if constexpr (WRITE) {
+                v4f m2 = mo[q];
+                if constexpr (RENEW) {
 #pragma unroll
-                    for (int e = 0; e < 4; ++e) mv[e] = __builtin_fmaf(s.momentum, mv[e], v[e]);
-                    if (whole) {
-                        v4u_at4 o;
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(mv[e]);
-                        *reinterpret_cast<v4u_at4*>(s.M + at) = o;
-                    } else {
-#pragma unroll
-                        for (int e = 0; e < 3; ++e)
-                            if (c + e < width) s.M[at + e] = mv[e];
-                    }
+                    for (int e = 0; e < 4; ++e) m2[e] = __builtin_fmaf(s.momentum, m2[e], u[e]);
+                    write4<BIRKHOFF4_F32>(s.M, at, there, m2);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = s.ahead < 0.f ? mv[e] : __builtin_fmaf(s.ahead, mv[e], v[e]);
+                for (int e = 0; e < 4; ++e) u[e] = s.ahead < 0.f ? m2[e] : __builtin_fmaf(s.ahead, m2[e], u[e]);
             }
-        }
 #pragma unroll
-        for (int e = 0; e < 4; ++e) slab[tall ? (c + e) * kSlabPitch + line : line * kSlabPitch + c + e] = v[e];
+            for (int e = 0; e < 4; ++e) *value(slab, line, c + e) = SCALED ? static_cast<float>(u[e] * scale) : u[e];
+        }
     }
-}
+};
 
 // Tiles of 16 x 16 on and below the diagonal, row by row.
 constexpr int tri(int t) { return t * (t + 1) / 2; }
@@ -785,10 +797,14 @@ __global__ __launch_bounds__(kGramBlock) void orth_narrow_gram_kernel(Source s, 
         ri[q] = (16 * i + (lane & 15)) * kSlabPitch + (lane >> 4);
         rj[q] = (16 * (t - tri(i)) + (lane & 15)) * kSlabPitch + (lane >> 4);
     }
-    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += static_cast<int64_t>(gridDim.x) * kSlab) {
+    Slab<DG, MOMENTUM, MT> x(s, base, R, C);
+    const int64_t pace = static_cast<int64_t>(gridDim.x) * kSlab;
+    x.fetch(static_cast<int64_t>(blockIdx.x) * kSlab);
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += pace) {
         __syncthreads();
-        load_slab<DG, MOMENTUM, true, MT>(s, base, R, C, j0, slab);
+        x.template put<true, false>(j0, slab, 1.0);
         __syncthreads();
+        x.fetch(j0 + pace);
 #pragma unroll 4
         for (int k = 0; k < kSlab; k += 4)
 #pragma unroll
@@ -804,63 +820,65 @@ __global__ __launch_bounds__(kGramBlock) void orth_narrow_gram_kernel(Source s, 
             for (int r = 0; r < 4; ++r) out[(wave + 4 * q) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)] = acc[q][r];
 }
 
-// The blocks' parts added, 64 entries a block in four parts of the order.
+// The blocks' parts added, 16 entries a block in 16 parts of the order, so that few loads follow one another.
 __global__ __launch_bounds__(256) void orth_narrow_join_kernel(const double* __restrict__ part, double* __restrict__ sum, int parts,
                                                                int entries) {
-    __shared__ double red[4][64];
-    const int c = threadIdx.x & 63, p = threadIdx.x >> 6;
-    const int64_t matrix = blockIdx.y, at = static_cast<int64_t>(blockIdx.x) * 64 + c;
+    __shared__ double red[16][16];
+    const int c = threadIdx.x & 15, p = threadIdx.x >> 4;
+    const int64_t matrix = blockIdx.y, at = static_cast<int64_t>(blockIdx.x) * 16 + c;
     double v = 0.0;
 #pragma unroll 8
-    for (int k = p; k < parts; k += 4) v += part[(matrix * parts + k) * entries + at];
+    for (int k = p; k < parts; k += 16) v += part[(matrix * parts + k) * entries + at];
     red[p][c] = v;
     __syncthreads();
-    if (p == 0) sum[matrix * entries + at] = (v + red[1][c]) + (red[2][c] + red[3][c]);
+    if (p > 0) return;
+    for (int k = 1; k < 16; ++k) v += red[k][c];
+    sum[matrix * entries + at] = v;
 }
 
 // F of each matrix from its G G^T: one block a matrix, a wave for each tile. A matrix in LDS is
 // symmetric, so its rows serve as both factors' columns: the lanes of 16 read 16 neighbours.
-constexpr int kPolyBlock = 1024;
-
 struct Coefs {
     float v[3 * kOrthMaxSteps];
 };
 
 template <int MT>
-__global__ __launch_bounds__(kPolyBlock) void orth_narrow_poly_kernel(const double* __restrict__ sum, float* __restrict__ F,
-                                                                      double* __restrict__ scales, double eps, Coefs coefs, int steps) {
+__global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const double* __restrict__ sum, double* __restrict__ F,
+                                                                        double* __restrict__ scales, double eps, Coefs coefs,
+                                                                        int steps) {
     constexpr int P = 16 * MT;
-    static_assert(tri(MT) <= kPolyBlock / 64, "a tile a wave");
     __shared__ double A[P * P], S[P * P], Q[P * P];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t matrix = blockIdx.x;
     int ti = 0;
     while (tri(ti + 1) <= wave) ++ti;
     const int tj = wave - tri(ti);
-    const bool mine = wave < tri(MT);  // uniform over the wave
     const int row = 16 * ti + (lane >> 4), col = 16 * tj + (lane & 15);  // of value r: row + 4 r
+    const int from_i = (lane >> 4) * P + 16 * ti + (lane & 15), from_j = (lane >> 4) * P + 16 * tj + (lane & 15);
+    // two sums that do not wait for each other
     auto product = [&](const double* M, const double* N) {
-        v4d acc = {};
-        if (mine)
-#pragma unroll 4
-            for (int k = 0; k < P; k += 4)
-                acc = mfma_f64(M[(k + (lane >> 4)) * P + 16 * ti + (lane & 15)], N[(k + (lane >> 4)) * P + 16 * tj + (lane & 15)], acc);
-        return acc;
+        v4d x = {}, y = {};
+#pragma unroll
+        for (int k = 0; k < P; k += 8) {
+            x = mfma_f64(M[k * P + from_i], N[k * P + from_j], x);
+            y = mfma_f64(M[(k + 4) * P + from_i], N[(k + 4) * P + from_j], y);
+        }
+        return x + y;
     };
     auto put = [&](double* M, const v4d& v) {
-        if (mine)
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
-                if (row + 4 * r >= col) M[(row + 4 * r) * P + col] = M[col * P + row + 4 * r] = v[r];
+        for (int r = 0; r < 4; ++r)
+            if (row + 4 * r >= col) M[(row + 4 * r) * P + col] = M[col * P + row + 4 * r] = v[r];
     };
-    v4d a = {}, f = {};
-    if (mine)
+    v4d a, f = {};
 #pragma unroll
-        for (int r = 0; r < 4; ++r) a[r] = sum[(matrix * tri(MT) + wave) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)];
+    for (int r = 0; r < 4; ++r) a[r] = sum[(matrix * tri(MT) + wave) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)];
     put(A, a);
     __syncthreads();
-    double norm = 0.0;
-    for (int k = 0; k < P; ++k) norm += A[k * P + k];
+    double norm = 0.0;  // of the diagonal, the same in every wave
+    for (int k = lane & 15; k < P; k += 16) norm += A[k * P + k];
+#pragma unroll
+    for (int k = 1; k < 16; k *= 2) norm += __shfl_xor(norm, k);
     norm = __builtin_sqrt(norm);
     const double scale = norm < __builtin_inf() ? 1.0 / (norm + eps) : __builtin_nan("");
     __syncthreads();
@@ -873,76 +891,270 @@ __global__ __launch_bounds__(kPolyBlock) void orth_narrow_poly_kernel(const doub
         v4d p = product(A, A);
 #pragma unroll
         for (int r = 0; r < 4; ++r) p[r] = __builtin_fma(cc, p[r], __builtin_fma(cb, a[r], row + 4 * r == col ? ca : 0.0));
+        if (steps == 1) {
+            f = p;
+            break;
+        }
         put(S, p);
         __syncthreads();
         const bool last = k + 1 == steps;  // uniform
         f = k == 0 ? p : product(S, Q);
-        if (!last) a = product(S, A);
+        if (last) break;
+        a = product(S, A);
         __syncthreads();
-        if (!last) {
-            put(Q, f);
-            put(A, a);
-            __syncthreads();
-            a = product(S, A);
-            __syncthreads();
-            put(A, a);
-            __syncthreads();
-        }
+        put(Q, f);
+        put(A, a);
+        __syncthreads();
+        a = product(S, A);
+        __syncthreads();
+        put(A, a);
+        __syncthreads();
     }
-    if (mine)
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (row + 4 * r >= col)
-                F[matrix * P * P + (row + 4 * r) * P + col] = F[matrix * P * P + col * P + row + 4 * r] = static_cast<float>(f[r]);
+    for (int r = 0; r < 4; ++r)
+        if (row + 4 * r >= col)
+            F[matrix * P * P + (row + 4 * r) * P + col] = F[matrix * P * P + col * P + row + 4 * r] = f[r];
     if (threadIdx.x == 0) scales[matrix] = scale;
 }
 
-// F X, 64 columns at a time: four waves take 16 each.
+// F X, 64 columns at a time: four waves take 16 each. F has values of a^5 = 485 where X has small singular values,
+// whose products with the large ones cancel: an fp32 result is formed in 64 bits, or it would be off by 485
+// roundings of X there (one for bf16 in 32).
 template <int DG, int DO, bool MOMENTUM, int MT>
-__global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const float* __restrict__ F, const double* __restrict__ scales,
+__global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const double* __restrict__ F, const double* __restrict__ scales,
                                                                 Result res) {
     constexpr int P = 16 * MT;
+    constexpr bool WIDE = DO == BIRKHOFF4_F32;
+    using Value = std::conditional_t<WIDE, double, float>;
+    using Sums = std::conditional_t<WIDE, v4d, v4f>;
     __shared__ float slab[P * kSlabPitch];
-    __shared__ float f[P * P];
+    __shared__ Value f[P * P];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t matrix = blockIdx.y, base = (res.first + matrix) * res.rows * res.cols;
-    const int64_t n = res.tall ? res.rows : res.cols;
-    const int m = static_cast<int>(res.tall ? res.cols : res.rows);
-    for (int k = threadIdx.x; k < P * P; k += 256) f[k] = F[matrix * P * P + k];
+    const int64_t n = res.tall ? res.rows : res.cols, pace = static_cast<int64_t>(gridDim.x) * kSlab;
+    Slab<DG, MOMENTUM, MT> x(s, base, res.rows, res.cols);
+    x.fetch(static_cast<int64_t>(blockIdx.x) * kSlab);
+    for (int k = threadIdx.x; k < P * P; k += 256) f[k] = static_cast<Value>(F[matrix * P * P + k]);
     const double scale = scales[matrix];
-    float rate = res.lr;
-    if (res.update && res.lr_at) rate *= *res.lr_at;
+    const float rate = res.update && res.lr_at ? res.lr * *res.lr_at : res.lr;
     const float shrink = 1.f - rate * res.decay, by = rate * res.scale;
-    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += static_cast<int64_t>(gridDim.x) * kSlab) {
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += pace) {
         __syncthreads();
-        load_slab<DG, MOMENTUM, false, MT>(s, base, res.rows, res.cols, j0, slab);
+        x.template put<false, !WIDE>(j0, slab, scale);
         __syncthreads();
-        v4f acc[MT] = {};
+        x.fetch(j0 + pace);
+        v4f old[MT];
+        if (res.update)
+#pragma unroll
+            for (int q = 0; q < MT; ++q) {
+                int64_t at;
+                int line, c;
+                const int64_t there = x.where(q, j0, &at, &line, &c);
+                old[q] = read4<DO>(res.out, at, there);
+            }
+        Sums acc[MT] = {};
 #pragma unroll 4
         for (int k = 0; k < P; k += 4) {
             const int at = k + (lane >> 4);
-            const float x = static_cast<float>(slab[at * kSlabPitch + 16 * wave + (lane & 15)] * scale);
+            const Value v = slab[at * kSlabPitch + 16 * wave + (lane & 15)];
 #pragma unroll
-            for (int t = 0; t < MT; ++t)
-                acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(f[at * P + 16 * t + (lane & 15)], x, acc[t], 0, 0, 0);
+            for (int t = 0; t < MT; ++t) {
+                const Value c = f[at * P + 16 * t + (lane & 15)];
+                if constexpr (WIDE)
+                    acc[t] = mfma_f64(c, v, acc[t]);
+                else
+                    acc[t] = __builtin_amdgcn_mfma_f32_16x16x4f32(c, v, acc[t], 0, 0, 0);
+            }
         }
         __syncthreads();
 #pragma unroll
         for (int t = 0; t < MT; ++t)
 #pragma unroll
-            for (int r = 0; r < 4; ++r) slab[(16 * t + 4 * (lane >> 4) + r) * kSlabPitch + 16 * wave + (lane & 15)] = acc[t][r];
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * t + (WIDE ? 4 * r + (lane >> 4) : 4 * (lane >> 4) + r);
+                slab[row * kSlabPitch + 16 * wave + (lane & 15)] = WIDE ? static_cast<float>(acc[t][r] * scale) : acc[t][r];
+            }
         __syncthreads();
-        const int left = static_cast<int>(n - j0 < kSlab ? n - j0 : kSlab);
-        const int lines = res.tall ? left : m, width = res.tall ? m : left;
-        for (int task = threadIdx.x; task < lines * width; task += 256) {
-            const int line = task / width, c = task % width;
-            float v = res.tall ? slab[c * kSlabPitch + line] : slab[line * kSlabPitch + c];
-            const int64_t at = base + (res.tall ? (j0 + line) * res.cols + c : line * res.cols + j0 + c);
-            if (res.update) v = __builtin_fmaf(-by, v, shrink * load_value<DO>(res.out, at));
-            if constexpr (DO == BIRKHOFF4_BF16)
-                static_cast<uint16_t*>(res.out)[at] = static_cast<uint16_t>(pack_bf16(v, 0.f));
-            else
-                static_cast<float*>(res.out)[at] = v;
+#pragma unroll
+        for (int q = 0; q < MT; ++q) {
+            int64_t at;
+            int line, c;
+            const int64_t there = x.where(q, j0, &at, &line, &c);
+            v4f v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[e] = *x.value(slab, line, c + e);
+                if (res.update) v[e] = __builtin_fmaf(-by, v[e], shrink * old[q][e]);
+            }
+            write4<DO>(res.out, at, there, v);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// The same for bf16 matrices with fewer rows than columns, and a bf16 result
+// ---------------------------------------------------------------------------
+// The matrix cores take the values as they lie in memory: eight neighbours of a row are what a lane of a product
+// of rows has, and products of bf16 values are exact in fp32. Their sums over `run` columns, 64 or 256, are fp32 numbers (off
+// by 2^-24 of them at most a few times, at random), the sums of those 64-bit ones: enough for a bf16 result
+// where the steps multiply an error by 12 four times. 32 matrices of 80 x 32768: 668 us in 64-bit products.
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+
+__device__ __forceinline__ v4f mfma_b16(const v4u a, const v4u b, const v4f c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+}
+
+typedef uint32_t v4u_at2 __attribute__((ext_vector_type(4), aligned(2)));
+
+// Eight neighbouring bf16 values, of which `n` are there, zeros behind.
+__device__ __forceinline__ v4u read8(const void* G, int64_t at, int64_t n) {
+    const uint16_t* p = static_cast<const uint16_t*>(G) + at;
+    if (n >= 8) return *reinterpret_cast<const v4u_at2*>(p);
+    v4u v = {0, 0, 0, 0};
+#pragma unroll
+    for (int e = 0; e < 7; ++e)
+        if (e < n) v[e / 2] |= static_cast<uint32_t>(p[e]) << (16 * (e & 1));
+    return v;
+}
+
+template <int MT>
+__global__ __launch_bounds__(256) void orth_narrow16_gram_kernel(const void* __restrict__ G, double* __restrict__ part, int m, int64_t n,
+                                                                 int run, int64_t first) {
+    constexpr int TILES = tri(MT);
+    __shared__ double joint[TILES * 256];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.y, base = (first + matrix) * m * n;
+    const int64_t pace = static_cast<int64_t>(gridDim.x) * 4 * run;
+    v4d acc[TILES] = {};
+    v4u x[2][MT], next[2][MT];
+    auto fetch = [&](int64_t j0) {
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int t = 0; t < MT; ++t) {
+                const int row = 16 * t + (lane & 15);
+                const int64_t j = j0 + 32 * k + 8 * (lane >> 4);
+                next[k][t] = read8(G, base + row * n + j, row < m ? n - j : 0);
+            }
+    };
+    int64_t j0 = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * run;
+    fetch(j0);
+    for (; j0 < n; j0 += pace) {
+        v4f sum[TILES] = {};
+#pragma unroll 1
+        for (int c = 0; c < run; c += 64) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int t = 0; t < MT; ++t) x[k][t] = next[k][t];
+            fetch(c + 64 < run ? j0 + c + 64 : j0 + pace);
+#pragma unroll
+            for (int k = 0; k < 2; ++k)
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int j = 0; j <= i; ++j) sum[tri(i) + j] = mfma_b16(x[k][i], x[k][j], sum[tri(i) + j]);
+        }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) acc[t][r] += static_cast<double>(sum[t][r]);
+    }
+    for (int w = 0; w < 4; ++w) {  // the waves' sums, in their order
+        if (wave == w) {
+#pragma unroll
+            for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    double* at = &joint[t * 256 + (4 * (lane >> 4) + r) * 16 + (lane & 15)];
+                    *at = w == 0 ? acc[t][r] : *at + acc[t][r];
+                }
+        }
+        __syncthreads();
+    }
+    for (int k = threadIdx.x; k < TILES * 256; k += 256) part[(matrix * gridDim.x + blockIdx.x) * (TILES * 256) + k] = joint[k];
+}
+
+// F X with F as three bf16 values, which are all its fp32 bits. A wave has 128 columns: its lanes read 16 bytes of
+// eight rows each, and of eight columns the rows' values are paired for the products, whose results are 16 bytes
+// of a row again.
+template <int MT>
+__global__ __launch_bounds__(256) void orth_narrow16_apply_kernel(const void* __restrict__ G, const double* __restrict__ F,
+                                                                  const double* __restrict__ scales, void* __restrict__ out, int m,
+                                                                  int64_t n, int64_t first) {
+    constexpr int P = 16 * MT, KS = (P + 31) / 32;
+    __shared__ v4u f[MT][KS][3][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.y, base = (first + matrix) * m * n;
+    const double scale = scales[matrix];
+    for (int q = wave; q < MT * KS; q += 4) {
+        const int t = q / KS, k = q % KS, row = 16 * t + (lane & 15), col = 32 * k + 8 * (lane >> 4);
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = col < P ? static_cast<float>(F[matrix * P * P + row * P + col + e] * scale) : 0.f;
+#pragma unroll
+        for (int part = 0; part < 3; ++part) {
+            v4u w;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                w[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+                v[2 * e] -= __uint_as_float(w[e] << 16);
+                v[2 * e + 1] -= __uint_as_float(w[e] & 0xffff0000u);
+            }
+            f[t][k][part][lane] = w;
+        }
+    }
+    __syncthreads();
+    for (int64_t j0 = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * 128; j0 < n; j0 += static_cast<int64_t>(gridDim.x) * 512) {
+        const int64_t j = j0 + 8 * (lane & 15), there = n - j;
+        v4u x[KS][8];
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int r = 0; r < 8; ++r) {
+                const int row = 32 * k + 8 * (lane >> 4) + r;
+                x[k][r] = read8(G, base + row * n + j, row < m ? there : 0);
+            }
+        // column c of the eight rows: halves of the words c / 2, paired
+        auto column = [&](int k, int c) {
+            v4u b;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                b[e] = __builtin_amdgcn_perm(x[k][2 * e + 1][c / 2], x[k][2 * e][c / 2], c & 1 ? 0x07060302u : 0x05040100u);
+            return b;
+        };
+        v4u col[KS][8];
+#pragma unroll
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+            for (int c = 0; c < 8; ++c) col[k][c] = column(k, c);
+#pragma unroll 1
+        for (int t = 0; t < MT; ++t) {
+            v4f acc[8] = {};
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int part = 0; part < 3; ++part) {
+                    const v4u a = f[t][k][part][lane];
+#pragma unroll
+                    for (int c = 0; c < 8; ++c) acc[c] = mfma_b16(a, col[k][c], acc[c]);
+                }
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                const int row = 16 * t + 4 * (lane >> 4) + r;
+                if (row >= m) continue;
+                uint16_t* to = static_cast<uint16_t*>(out) + base + row * n + j;
+                v4u_at2 o;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) o[e] = pack_bf16(acc[2 * e][r], acc[2 * e + 1][r]);
+                if (there >= 8) {
+                    *reinterpret_cast<v4u_at2*>(to) = o;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 7; ++e)
+                        if (e < there) to[e] = static_cast<uint16_t>(o[e / 2] >> (16 * (e & 1)));
+                }
+            }
         }
     }
 }
@@ -981,7 +1193,7 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
         s->mt = static_cast<int>((s->m + 15) / 16);
         const int64_t slabs = (s->n + kSlab - 1) / kSlab, entries = tri(s->mt) * 256 * 8;
         s->e = entries;               // the sum of the parts
-        s->x = s->mt * s->mt * 1024;  // F
+        s->x = s->mt * s->mt * 2048;  // F
         s->group = kGroupBytes / (s->e + s->x + 16);
         if (s->group > B) s->group = B;
         if (s->group > 32768) s->group = 32768;
@@ -1023,27 +1235,40 @@ template <int DG, int DO, bool MOMENTUM, int MT>
 int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
     double* sum = reinterpret_cast<double*>(work);
     double* scales = reinterpret_cast<double*>(work + s.group * s.e);
-    float* F = reinterpret_cast<float*>(work + s.group * (s.e + 16));
-    double* part = s.parts > 1 ? reinterpret_cast<double*>(work + s.group * (s.e + 16 + s.x)) : sum;
+    double* F = reinterpret_cast<double*>(work + s.group * (s.e + 16));
+    const bool rows16 = DG == BIRKHOFF4_BF16 && DO == BIRKHOFF4_BF16 && !MOMENTUM && s.R <= s.C;
+    // long sums where they leave a block for every compute unit
+    const int run = s.group * ((s.n + 1023) / 1024) >= 256 ? 256 : 64;
+    const int64_t most = rows16 ? (s.n + 4 * run - 1) / (4 * run) : s.parts, parts = s.parts < most ? s.parts : most;
+    double* part = parts > 1 ? reinterpret_cast<double*>(work + s.group * (s.e + 16 + s.x)) : sum;
     Coefs coefs = {};
     for (int k = 0; k < 3 * call.steps; ++k) coefs.v[k] = call.coefs[k];
     const int64_t slabs = (s.n + kSlab - 1) / kSlab;
     for (int64_t first = 0; first < s.B; first += s.group) {
         const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
-        launch_kernel((orth_narrow_gram_kernel<DG, MOMENTUM, MT>), dim3(static_cast<unsigned>(s.parts), L), dim3(kGramBlock), 0,
-                      stream, call.src, part, s.R, s.C, first);
-        if (s.parts > 1)
-            launch_kernel(orth_narrow_join_kernel, dim3(4 * tri(MT), L), dim3(256), 0, stream, part, sum,
-                          static_cast<int>(s.parts), 256 * tri(MT));
-        launch_kernel((orth_narrow_poly_kernel<MT>), dim3(L), dim3(kPolyBlock), 0, stream, sum, F, scales, call.eps, coefs,
+        if (rows16)
+            launch_kernel(orth_narrow16_gram_kernel<MT>, dim3(static_cast<unsigned>(parts), L), dim3(256), 0, stream, call.src.G,
+                          part, static_cast<int>(s.m), s.n, run, first);
+        else
+            launch_kernel((orth_narrow_gram_kernel<DG, MOMENTUM, MT>), dim3(static_cast<unsigned>(parts), L), dim3(kGramBlock), 0,
+                          stream, call.src, part, s.R, s.C, first);
+        if (parts > 1)
+            launch_kernel(orth_narrow_join_kernel, dim3(16 * tri(MT), L), dim3(256), 0, stream, part, sum,
+                          static_cast<int>(parts), 256 * tri(MT));
+        launch_kernel((orth_narrow_poly_kernel<MT>), dim3(L), dim3(64 * tri(MT)), 0, stream, sum, F, scales, call.eps, coefs,
                       call.steps);
         Result res = call.res;
         res.first = first;
+        const int64_t turns = rows16 ? (s.n + 511) / 512 : slabs;  // what a block takes at a time
         int64_t blocks = 2 * kGramBlocks / L;
         if (blocks < 1) blocks = 1;
-        if (blocks > slabs) blocks = slabs;
-        launch_kernel((orth_narrow_apply_kernel<DG, DO, MOMENTUM, MT>), dim3(static_cast<unsigned>(blocks), L), dim3(256), 0,
-                      stream, call.src, F, scales, res);
+        if (blocks > turns) blocks = turns;
+        if (rows16)
+            launch_kernel(orth_narrow16_apply_kernel<MT>, dim3(static_cast<unsigned>(blocks), L), dim3(256), 0, stream, call.src.G, F,
+                          scales, res.out, static_cast<int>(s.m), s.n, first);
+        else
+            launch_kernel((orth_narrow_apply_kernel<DG, DO, MOMENTUM, MT>), dim3(static_cast<unsigned>(blocks), L), dim3(256), 0,
+                          stream, call.src, F, scales, res);
     }
     return launch_status();
 }

@@ -38,7 +38,9 @@ def check(G, label, **kw):
 # sides of every tile and of the lines of 32 and 64; tall, wide and square; batches
 SIZES = [(1, 1), (3, 1, 7), (9, 1), (2, 3, 5), (5, 8, 8), (24, 1000), (3, 80, 2056), (2, 500, 24), (79, 81), (81, 79), (80, 80),
          (4, 64, 64), (2, 65, 33), (128, 128), (129, 127), (127, 300), (2, 128, 256), (2, 200, 130), (257, 640), (513, 256),
-         (384, 1001), (7, 96, 160), (1000, 300), (300, 1000), (2, 640, 640), (31, 100, 100), (200, 5000), (1100, 1100)]
+         (384, 1001), (7, 96, 160), (1000, 300), (300, 1000), (2, 640, 640), (31, 100, 100), (200, 5000), (1100, 1100),
+         # runs of 64 and 256 columns and what is left of them, every number of tiles of the narrow ones
+         (16, 700), (3, 33, 1025), (48, 4100), (2, 50, 513), (300, 24, 1000), (40, 64, 8200), (70, 30001), (65000, 2, 3)]
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
@@ -87,10 +89,16 @@ def test_sizes_of_values(shape):
 @pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
 @pytest.mark.parametrize("shape", [(3, 24, 333), (2, 150, 333), (100, 700)], ids=str)
 def test_transpose(shape, dtype):
-    """The transpose's result is the result's transpose, bit for bit; strided inputs are taken."""
+    """The transpose's result is the result's transpose, bit for bit but for narrow bf16 matrices, whose rows
+    are taken as they lie (there half a step of bf16 each, and what fp32 sums differ by); strided inputs are
+    taken."""
     G = matrices(shape, dtype, 8)
     O = b4.orth(G)
-    assert torch.equal(b4.orth(G.transpose(-1, -2)), O.transpose(-1, -2))
+    turned = b4.orth(G.transpose(-1, -2)).transpose(-1, -2)
+    if dtype == F32 or min(shape[-2:]) > 80:
+        assert torch.equal(turned, O)
+    else:
+        assert ((turned.float() - O.float()).abs() <= 2 * 2.0 ** -8 * O.float().abs() + 1e-5).all()
     wide = torch.zeros(*shape[:-1], 2 * shape[-1], dtype=dtype, device="cuda")
     wide[..., ::2] = G
     assert torch.equal(b4.orth(wide[..., ::2]), O)
