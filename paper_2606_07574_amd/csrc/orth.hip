@@ -110,6 +110,41 @@ __device__ __forceinline__ void load4(const void* p, int64_t at, float v[4]) {
     }
 }
 
+// Four neighbouring values of a row of the caller's array, of which `n` are there.
+template <int DO>
+__device__ __forceinline__ v4f read4(const void* out, int64_t at, int64_t n) {
+    float v[4] = {0.f, 0.f, 0.f, 0.f};
+    if (n >= 4) {
+        load4<DO>(out, at, v);
+    } else {
+#pragma unroll
+        for (int e = 0; e < 3; ++e)
+            if (e < n) v[e] = load_value<DO>(out, at + e);
+    }
+    return v4f{v[0], v[1], v[2], v[3]};
+}
+
+template <int DO>
+__device__ __forceinline__ void write4(void* out, int64_t at, int64_t n, const v4f v) {
+    if (n >= 4) {
+        if constexpr (DO == BIRKHOFF4_BF16) {
+            *reinterpret_cast<v2u_at2*>(static_cast<uint16_t*>(out) + at) = v2u_at2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
+        } else {
+            *reinterpret_cast<v4u_at4*>(static_cast<float*>(out) + at) =
+                v4u_at4{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
+        }
+        return;
+    }
+#pragma unroll
+    for (int e = 0; e < 3; ++e) {
+        if (e >= n) continue;
+        if constexpr (DO == BIRKHOFF4_BF16)
+            static_cast<uint16_t*>(out)[at + e] = static_cast<uint16_t>(pack_bf16(v[e], 0.f));
+        else
+            static_cast<float*>(out)[at + e] = v[e];
+    }
+}
+
 // What is orthogonalised: G, or with a momentum M the direction G + ahead M (M renewed already).
 struct Source {
     const void* G;
@@ -134,27 +169,28 @@ __global__ __launch_bounds__(kPrepBlock) void orth_prep_kernel(Source s, double*
         }
         sum = __builtin_fma(static_cast<double>(u), static_cast<double>(u), sum);
     };
-    const int64_t quads = values / 4;
-    for (int64_t q = static_cast<int64_t>(blockIdx.x) * kPrepBlock + threadIdx.x; q < quads;
-         q += static_cast<int64_t>(gridDim.x) * kPrepBlock) {
-        float g[4], m[4] = {0.f, 0.f, 0.f, 0.f};
-        load4<DG>(s.G, base + 4 * q, g);
-        if constexpr (MOMENTUM) load4<BIRKHOFF4_F32>(s.M, base + 4 * q, m);
+    const int64_t quads = (values + 3) / 4, pace = static_cast<int64_t>(gridDim.x) * kPrepBlock;
+    constexpr int N = 4;  // asked for together
+    for (int64_t q0 = static_cast<int64_t>(blockIdx.x) * kPrepBlock + threadIdx.x; q0 < quads; q0 += N * pace) {
+        v4f g[N], m[N];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) take(g[e], &m[e]);
-        if constexpr (MOMENTUM) {
-            v4u_at4 o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) o[e] = __float_as_uint(m[e]);
-            *reinterpret_cast<v4u_at4*>(s.M + base + 4 * q) = o;
+        for (int k = 0; k < N; ++k) {
+            const int64_t q = q0 + k * pace, there = values - 4 * q;
+            g[k] = read4<DG>(s.G, base + 4 * q, there);
+            if constexpr (MOMENTUM) m[k] = read4<BIRKHOFF4_F32>(s.M, base + 4 * q, there);
         }
-    }
-    if (blockIdx.x == 0 && threadIdx.x < values - 4 * quads) {
-        const int64_t at = base + 4 * quads + threadIdx.x;
-        float m = 0.f;
-        if constexpr (MOMENTUM) m = s.M[at];
-        take(load_value<DG>(s.G, at), &m);
-        if constexpr (MOMENTUM) s.M[at] = m;
+#pragma unroll
+        for (int k = 0; k < N; ++k) {
+            const int64_t q = q0 + k * pace, there = values - 4 * q;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {  // zeros where there is nothing
+                float x = MOMENTUM ? m[k][e] : 0.f;
+                take(g[k][e], &x);
+                if constexpr (MOMENTUM) m[k][e] = x;
+            }
+            if constexpr (MOMENTUM)
+                if (there > 0) write4<BIRKHOFF4_F32>(s.M, base + 4 * q, there, m[k]);
+        }
     }
     red[threadIdx.x] = sum;
     for (int half = kPrepBlock / 2; half > 0; half /= 2) {
@@ -172,39 +208,38 @@ template <int DG, bool MOMENTUM, bool SPLIT>
 __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const double* __restrict__ sums, int parts, double eps,
                                                            Plane own, Plane turned, int64_t R, int64_t C, int64_t first) {
     __shared__ float tile[kConvert][kConvert + 1];
+    __shared__ double red[256];
     const int64_t matrix = blockIdx.z, base = (first + matrix) * R * C;
     const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kConvert, c0 = static_cast<int64_t>(blockIdx.x) * kConvert;
-    double norm = 0.0;
-    for (int k = 0; k < parts; ++k) norm += sums[matrix * parts + k];
-    norm = __builtin_sqrt(norm);
-    const double scale = norm < __builtin_inf() ? kUnit / (norm + eps) : __builtin_nan("");
+    constexpr int N = kConvert / 16;
     const int c = 4 * (threadIdx.x % 16);
+    v4f u[N], m[N];
 #pragma unroll
-    for (int k = 0; k < kConvert / 16; ++k) {
+    for (int k = 0; k < N; ++k) {
+        const int64_t row = r0 + threadIdx.x / 16 + 16 * k, at = base + row * C + c0 + c, there = row < R ? C - c0 - c : 0;
+        u[k] = read4<DG>(s.G, at, there);
+        if constexpr (MOMENTUM) m[k] = read4<BIRKHOFF4_F32>(s.M, at, there);
+    }
+    double norm = 0.0;  // the parts in the order of the threads, then pairs
+    for (int k = threadIdx.x; k < parts; k += 256) norm += sums[matrix * parts + k];
+    red[threadIdx.x] = norm;
+    for (int half = 128; half > 0; half /= 2) {
+        __syncthreads();
+        if (threadIdx.x < half) red[threadIdx.x] += red[threadIdx.x + half];
+    }
+    __syncthreads();
+    norm = __builtin_sqrt(red[0]);
+    const double scale = norm < __builtin_inf() ? kUnit / (norm + eps) : __builtin_nan("");
+#pragma unroll
+    for (int k = 0; k < N; ++k) {
         const int r = threadIdx.x / 16 + 16 * k;
-        const int64_t row = r0 + r, col = c0 + c, at = base + row * C + col;
-        float v[4] = {0.f, 0.f, 0.f, 0.f};
-        if (row < R && col < C) {
-            float m[4] = {0.f, 0.f, 0.f, 0.f};
-            if (col + 4 <= C) {
-                load4<DG>(s.G, at, v);
-                if constexpr (MOMENTUM) load4<BIRKHOFF4_F32>(s.M, at, m);
-            } else {
 #pragma unroll
-                for (int e = 0; e < 3; ++e)
-                    if (col + e < C) {
-                        v[e] = load_value<DG>(s.G, at + e);
-                        if constexpr (MOMENTUM) m[e] = s.M[at + e];
-                    }
-            }
-            if constexpr (MOMENTUM)
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = s.ahead < 0.f ? m[e] : __builtin_fmaf(s.ahead, m[e], v[e]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = col + e < C ? static_cast<float>(v[e] * scale) : 0.f;
+        for (int e = 0; e < 4; ++e) {
+            float v = u[k][e];
+            if constexpr (MOMENTUM) v = s.ahead < 0.f ? m[k][e] : __builtin_fmaf(s.ahead, m[k][e], v);
+            // around the values zeros, whatever the scale
+            tile[r][c + e] = r0 + r < R && c0 + c + e < C ? static_cast<float>(v * scale) : 0.f;
         }
-#pragma unroll
-        for (int e = 0; e < 4; ++e) tile[r][c + e] = v[e];
     }
     __syncthreads();
 #pragma unroll
@@ -291,41 +326,6 @@ __device__ __forceinline__ int spot(int row, int col, bool lo) {
         return 2048 * (col >> 4) + row * 64 + 16 * (((col >> 3 & 1) + (lo ? 2 : 0)) ^ (row >> 2 & 3));
     else
         return (lo ? 2048 : 0) + row * 64 + 16 * ((col >> 3) ^ (row >> 2 & 3));
-}
-
-// Four neighbouring values of a row of the caller's array, of which `n` are there.
-template <int DO>
-__device__ __forceinline__ v4f read4(const void* out, int64_t at, int64_t n) {
-    float v[4] = {0.f, 0.f, 0.f, 0.f};
-    if (n >= 4) {
-        load4<DO>(out, at, v);
-    } else {
-#pragma unroll
-        for (int e = 0; e < 3; ++e)
-            if (e < n) v[e] = load_value<DO>(out, at + e);
-    }
-    return v4f{v[0], v[1], v[2], v[3]};
-}
-
-template <int DO>
-__device__ __forceinline__ void write4(void* out, int64_t at, int64_t n, const v4f v) {
-    if (n >= 4) {
-        if constexpr (DO == BIRKHOFF4_BF16) {
-            *reinterpret_cast<v2u_at2*>(static_cast<uint16_t*>(out) + at) = v2u_at2{pack_bf16(v.x, v.y), pack_bf16(v.z, v.w)};
-        } else {
-            *reinterpret_cast<v4u_at4*>(static_cast<float*>(out) + at) =
-                v4u_at4{__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
-        }
-        return;
-    }
-#pragma unroll
-    for (int e = 0; e < 3; ++e) {
-        if (e >= n) continue;
-        if constexpr (DO == BIRKHOFF4_BF16)
-            static_cast<uint16_t*>(out)[at + e] = static_cast<uint16_t>(pack_bf16(v[e], 0.f));
-        else
-            static_cast<float*>(out)[at + e] = v[e];
-    }
 }
 
 // Of N products, one ahead of each of 2 W reads of LDS and then, where there are LOADS, of the 2 W loads, so that
@@ -1167,7 +1167,7 @@ constexpr int64_t kOrthMaxSmall = int64_t(1) << 16;  // of the smaller side: eve
 constexpr int64_t kOrthMaxValues = int64_t(1) << 46;
 constexpr int64_t kOrthMaxMatrices = int64_t(1) << 26;
 constexpr int64_t kGroupBytes = int64_t(1) << 30;  // of workspace, which matrices are taken together for
-constexpr int kMostParts = 128;
+constexpr int kMostParts = 1024;
 constexpr int64_t kGramBlocks = 512;
 
 struct OrthShape {
@@ -1212,8 +1212,8 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
     s->e = s->mp * s->mp * size;  // E, and A without its lo
     s->a = s->e + (split ? 0 : s->e);
     s->d = s->mp * 4;
-    const int64_t quads = (R * C + 4 * kPrepBlock - 1) / (4 * kPrepBlock);
-    s->parts = quads < kMostParts ? quads : kMostParts;
+    const int64_t turns = (R * C + 16 * kPrepBlock - 1) / (16 * kPrepBlock);
+    s->parts = turns < kMostParts ? turns : kMostParts;
     const int64_t each = 2 * (s->x + s->xt + s->lo) + s->a + s->e + 2 * s->d + kMostParts * 8;
     s->group = kGroupBytes / each;
     if (s->group < 1) s->group = 1;
