@@ -812,38 +812,50 @@ def norm_fwd(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Te
     for both, x's or another) or None for ones and zeros. Returns (y like x, mean [...], rstd [...]),
     the last two float32, for norm_bwd."""
     rows, C, code = _normed(x, weight, bias)
+    return _norm_fwd(x, weight, bias, code, rows, C, eps)
+
+
+def _norm_fwd(x, weight, bias, code, rows, C, eps):
     y = torch.empty_like(x)
     mean = torch.empty(x.shape[:-1], dtype=torch.float32, device=x.device)
     rstd = torch.empty_like(mean)
-    _call("birkhoff4_norm_fwd", x, _ptr(x), _dtype_code(x), _ptr(weight), _ptr(bias), code, float(eps), _ptr(y), _ptr(mean),
-          _ptr(rstd), rows, C)
+    _call("birkhoff4_norm_fwd", x, x.data_ptr(), _dtype_code(x), _ptr(weight), _ptr(bias), code, float(eps), y.data_ptr(),
+          mean.data_ptr(), rstd.data_ptr(), rows, C)
     return y, mean, rstd
 
 
+@functools.lru_cache(maxsize=256)
+def _norm_work(rows: int, C: int, code: int) -> int:
+    size = _load().birkhoff4_norm_work(rows, C, code)
+    if size < 0:
+        _check(size)
+    return size
+
+
 def _norm_bwd(x, weight, code, mean, rstd, dy, want):
-    """(dx, dweight, dbias), each None where `want` does not ask for it; code: the parameters' dtype."""
-    rows, C, _ = _normed(x, weight, None)
-    _dense(dy, "dy", x.shape, x.dtype, x)
-    _dense(mean, "mean", x.shape[:-1], torch.float32, x)
-    _dense(rstd, "rstd", x.shape[:-1], torch.float32, x)
+    """(dx, dweight, dbias), each None where `want` does not ask for it; code: the parameters' dtype. What
+    norm_bwd has checked, or what norm_fwd has made."""
+    C, dtype = x.shape[-1], _dtype_code(x)
+    rows = x.numel() // C
     params = torch.bfloat16 if code == BF16 else torch.float32
     dx = torch.empty_like(x) if want[0] else None
-    dw, db = (torch.empty(C, dtype=params, device=x.device) if k else None for k in want[1:])
-    work = None
-    if want[1] or want[2]:
-        size = _load().birkhoff4_norm_work(rows, C, _dtype_code(x))
-        if size < 0:
-            _check(size)
-        work = torch.empty(size, dtype=torch.uint8, device=x.device)
-    _call("birkhoff4_norm_bwd", x, _ptr(x), _dtype_code(x), _ptr(weight), code, _ptr(mean), _ptr(rstd), _ptr(dy), _ptr(dx),
-          _ptr(dw), _ptr(db), _ptr(work), 0 if work is None else work.numel(), rows, C)
+    dw = torch.empty(C, dtype=params, device=x.device) if want[1] else None
+    db = torch.empty(C, dtype=params, device=x.device) if want[2] else None
+    size = _norm_work(rows, C, dtype) if want[1] or want[2] else 0
+    work = torch.empty(size, dtype=torch.uint8, device=x.device) if size else None
+    _call("birkhoff4_norm_bwd", x, x.data_ptr(), dtype, _ptr(weight), code, mean.data_ptr(), rstd.data_ptr(), dy.data_ptr(),
+          _ptr(dx), _ptr(dw), _ptr(db), _ptr(work), size, rows, C)
     return dx, dw, db
 
 
 def norm_bwd(x: torch.Tensor, weight: torch.Tensor | None, mean: torch.Tensor, rstd: torch.Tensor, dy: torch.Tensor):
     """Backward of norm_fwd from its x, weight, mean and rstd, and dy (like x): (dx like x, dweight,
     dbias [C] of weight's dtype, float32 without one)."""
-    return _norm_bwd(x, weight, F32 if weight is None else _dtype_code(weight), mean, rstd, dy, (True, True, True))
+    _, _, code = _normed(x, weight, None)
+    _dense(dy, "dy", x.shape, x.dtype, x)
+    _dense(mean, "mean", x.shape[:-1], torch.float32, x)
+    _dense(rstd, "rstd", x.shape[:-1], torch.float32, x)
+    return _norm_bwd(x, weight, code, mean, rstd, dy, (True, True, True))
 
 
 class NormFn(torch.autograd.Function):
@@ -852,17 +864,18 @@ class NormFn(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, weight=None, bias=None, eps=DEFAULT_NORM_EPS):
         x = _whole(x)
-        weight, bias = (None if t is None else _whole(t) for t in (weight, bias))
-        y, mean, rstd = norm_fwd(x, weight, bias, eps)
+        weight = None if weight is None else _whole(weight)
+        bias = None if bias is None else _whole(bias)
+        rows, C, ctx.code = _normed(x, weight, bias)
+        y, mean, rstd = _norm_fwd(x, weight, bias, ctx.code, rows, C, eps)
         ctx.save_for_backward(x, weight, mean, rstd)
-        ctx.code = _dtype_code(weight if weight is not None else bias) if weight is not None or bias is not None else F32
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         x, weight, mean, rstd = ctx.saved_tensors
-        return (*_norm_bwd(x, weight, ctx.code, mean, rstd, _whole(dy), ctx.needs_input_grad[:3]), None)
+        return (*_norm_bwd(x, weight, ctx.code, mean, rstd, _whole(dy), ctx.needs_input_grad), None)
 
 
 def norm(x: torch.Tensor, weight: torch.Tensor | None = None, bias: torch.Tensor | None = None,

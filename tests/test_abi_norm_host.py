@@ -101,7 +101,8 @@ def test_refusals():
 
 @pytest.mark.parametrize("which", [0, 1, 2])
 def test_tangents_are_refused(which, monkeypatch):
-    monkeypatch.setattr(b4, "norm_fwd", lambda x, *rest: (x, x[:, 0], x[:, 0]))
+    monkeypatch.setattr(b4, "_normed", lambda x, *rest: (3, 8, 0))
+    monkeypatch.setattr(b4, "_norm_fwd", lambda x, *rest: (x, x[:, 0], x[:, 0]))
     args = [torch.randn(3, 8), torch.randn(8), torch.randn(8)]
     with forward_ad.dual_level():
         args[which] = forward_ad.make_dual(args[which], torch.ones_like(args[which]))
