@@ -5,7 +5,7 @@
 //     g = dy w,   dx = s (g - mean g - xh mean(g xh)),   dw = sum over rows of dy xh,   db = sum of dy
 //
 // Both passes are bound by HBM: a row is read once into registers (the backward: x and dy), summed over
-// and written from there. G threads hold a row, eight values each, and keep their columns' w and b
+// and written from there. G threads hold a row, sixteen values each (the backward: eight), and keep their columns' w and b
 // (backward: w and the sums of dw and db) in registers over all rows that their group of threads takes.
 // The variance is the mean of (x - mu)^2 with mu known, so a large common offset costs no digits, and sums
 // are divided by C, not multiplied by its rounded reciprocal: equal values have no spread.
@@ -168,7 +168,9 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*red)[N]) {
 // ---------------------------------------------------------------------------
 // Forward
 // ---------------------------------------------------------------------------
-constexpr int kHeld = 8;  // values of a row that a thread holds
+// Values of a row that a thread holds: 32 K rows of 4096 bf16 97 us with 16 and four blocks of 256 threads a compute unit, 106
+// with 8 and eight blocks, 98 with 32; 8191 of 1023 12.3, 13.7 and 15.9. The backward's sums of dw and db leave room for 8.
+constexpr int kFwdHeld = 16, kFwdBlocks = 4, kHeld = 8;
 constexpr int fwd_threads(int G) { return G > 256 ? G : 256; }
 
 template <int DX, int DW, bool RAGGED, int G>
@@ -176,7 +178,7 @@ __global__ __launch_bounds__(fwd_threads(G)) void norm_fwd_kernel(const void* __
                                                                   const void* __restrict__ bias, float eps, float c,
                                                                   void* __restrict__ Y, float* __restrict__ mean,
                                                                   float* __restrict__ rstd, int64_t B, Row r) {
-    constexpr int E = MixChunk<DX>::E, K = kHeld / E, NT = fwd_threads(G), PER = NT / G;
+    constexpr int E = MixChunk<DX>::E, K = kFwdHeld / E, NT = fwd_threads(G), PER = NT / G;
     __shared__ float red[2][NT / 64][1];
     const int t = threadIdx.x % G;
     float w[K][E], b[K][E];
@@ -509,13 +511,13 @@ int norm_shape(int64_t B, int64_t C, int x_dtype, int w_dtype, NormShape* s) {
     return BIRKHOFF4_OK;
 }
 
-constexpr int64_t kLongRow = 1024 * kHeld;  // values of a row, above which a block's threads do not hold it
-constexpr int64_t kNormBlocks = 256;        // of the backward: one a compute unit
+constexpr int64_t kLongRow = 1024 * kHeld;  // values of a row, above which the backward's threads do not hold it
+constexpr int64_t kNormBlocks = 256;  // of the backward: one a compute unit (two: 32 K rows of 4096 bf16 164 us instead of 154, 4097 of 1000 fp32 15.6 and 12.7)
 
 // Threads that hold a row: the fewest, 16 at least.
-int row_group(int64_t C) {
+int row_group(int64_t C, int held = kHeld) {
     int g = 16;
-    while (g * kHeld < C) g *= 2;
+    while (g * held < C) g *= 2;
     return g;
 }
 
@@ -533,14 +535,14 @@ int launch_norm_fwd(const NormShape& s, const void* X, const void* weight, const
                     float* rstd, int cus, hipStream_t stream) {
     const float c = static_cast<float>(s.r.C);
     auto go = [&](auto kern, int G, int threads) {
-        const int64_t want = (s.B * G + threads - 1) / threads, most = int64_t(cus) * (threads > 256 ? 2 : 8);
+        const int64_t want = (s.B * G + threads - 1) / threads, most = int64_t(cus) * kFwdBlocks * 256 / threads;
         launch_kernel(kern, dim3(static_cast<unsigned>(want < most ? want : most)), dim3(threads), 0, stream, X, weight, bias,
                       eps, c, Y, mean, rstd, s.B, s.r);
         return launch_status();
     };
 #define FWD(G) \
     case G: return go(norm_fwd_kernel<DX, DW, RAGGED, G>, G, fwd_threads(G))
-    switch (s.r.C > kLongRow ? 0 : row_group(s.r.C)) {
+    switch (s.r.C > 1024 * kFwdHeld ? 0 : row_group(s.r.C, kFwdHeld)) {
         FWD(16);
         FWD(32);
         FWD(64);

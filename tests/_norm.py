@@ -1,7 +1,7 @@
 """float64 reference of the layer norm and its gradients, with bounds of the kernels' errors.
 
-u = 2^-24 is fp32's largest relative rounding error. A row's sum is formed by threads that chain eight
-values each (a 1024th of the row where it is longer than 8192), a tree over a wave's 64 lanes and a chain
+u = 2^-24 is fp32's largest relative rounding error. A row's sum is formed by threads that chain sixteen
+values each (a 1024th of the row and a chunk where it is longer than they hold), a tree over a wave's 64 lanes and a chain
 of at most 16 waves; a sum over rows by chains of a 256th of them, then at most 64 groups of a block, 16
 partial sums of a part and 16 parts."""
 import torch
@@ -10,7 +10,7 @@ U = 2.0 ** -24
 
 
 def row_depth(C: int) -> float:
-    return max(8.0, C / 1024 + 8) + 6 + 16
+    return max(16.0, C / 1024 + 8) + 6 + 16
 
 
 def column_depth(B: int, C: int) -> float:

@@ -38,7 +38,8 @@ def check(x, w, b, dy, label, eps=EPS32):
 # not, one row to more rows than the blocks take at once, rows that a block does not hold
 SIZES = [(1, 1), (3, 1), (2, 3), (5, 7), (4, 8), (1, 4096), (70, 16), (2600, 24), (33, 127), (300, 128), (65, 129), (40, 256),
          (301, 257), (17, 1000), (1100, 512), (9, 1023), (2050, 1024), (30, 2052), (600, 513), (600, 2049), (6, 4100), (300, 4097),
-         (5, 8192), (270, 8191), (3, 8193), (2, 20001), (1, 65536)]
+         (5, 8192), (270, 8191), (3, 8193), (2, 20001), (1, 65536), (3, 16384),
+         (2, 16385)]
 
 
 @pytest.mark.parametrize("types", [(F32, F32), (BF16, F32), (BF16, BF16), (F32, BF16)], ids=["f32", "mixed", "bf16", "f32bf16"])
