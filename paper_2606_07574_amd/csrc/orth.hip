@@ -25,6 +25,7 @@
 // in both orders.
 
 #include <type_traits>
+#include <utility>
 
 #include "common.h"
 
@@ -261,18 +262,22 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const doubl
 // ---------------------------------------------------------------------------
 // The products
 // ---------------------------------------------------------------------------
-enum { GRAM, POLY, NEXT, LAST };
+enum { GRAM, POLY, PAIR, NEXT, LAST };
 
 // acc_ij = sum_k P_ik Q_jk in units of kUnit^2. Results, stored as own_ij and as turned_ji:
 //   GRAM  A = acc
 //   POLY  E = keep A + add A^2 with A^2 from acc, src = A and its diagonal as above
-//   NEXT  (keep + F_i) src_ij + acc, the next X;  LAST: the same, which goes to the caller's array
-// GRAM and POLY have a symmetric result: its tiles below the diagonal alone are computed.
+//   PAIR  add M N for symmetric M = P and N = Q that commute: add (D_i N_ij + M_ij D'_j + acc), D and D' theirs
+//   NEXT  add ((keep + F_i) src_ij + acc), the next X;  LAST: the same, which goes to the caller's array
+// All but the last two have a symmetric result: its tiles below the diagonal alone are computed. `plus` is
+// added to the diagonal of POLY's.
 struct Product {
     Plane P, Q, src, own, turned;
-    const float* src_diag;  // D (POLY) or F (NEXT, LAST), `side` a matrix
-    float* own_diag;        // D (GRAM) or F (POLY)
+    const float* src_diag;  // D (POLY, PAIR) or F (NEXT, LAST), `side` a matrix
+    float* own_diag;        // D (GRAM, PAIR) or F (POLY)
     float keep, add;
+    const float* q_diag;    // D' (PAIR)
+    float plus;
     int64_t side;
     int panels;             // of P's and Q's rows
     int tiles, tj;          // of the result, and along j
@@ -353,6 +358,7 @@ __device__ __forceinline__ void mix_reads() {
 template <bool SPLIT, int KIND, int DO, int W, int KS>
 __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_kernel(Product g, Result res) {
     constexpr int T = 64 * W;
+    constexpr bool SYM = KIND == GRAM || KIND == POLY || KIND == PAIR;
     constexpr int S = stages(W), STAGE = stage_bytes<W>();
     static_assert(KS * S * STAGE >= KS * 4 * W * W * 4096, "the sums take the stages' place");
     __shared__ __attribute__((aligned(128))) char lds[KS * S * STAGE];
@@ -363,7 +369,7 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
     const int per = (g.tiles + 7) / 8, tile = blockIdx.x % 8 * per + blockIdx.x / 8;
     if (tile >= g.tiles) return;  // uniform over the block
     int ti, tj;
-    if constexpr (KIND == GRAM || KIND == POLY) {  // row by row below the diagonal
+    if constexpr (SYM) {  // row by row below the diagonal
         ti = static_cast<int>((__builtin_sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
         while (ti * (ti + 1) / 2 > tile) --ti;
         while ((ti + 1) * (ti + 2) / 2 <= tile) ++ti;
@@ -442,9 +448,9 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
     auto part_b = [&](int k) { return HALVES ? group : k % W; };
     auto there = [&](int k) {  // uniform over the wave: rows come in whole 64s
         return ib + 32 * part_a(k) < g.P.rows && jb + 32 * part_b(k) < g.Q.rows &&
-               !((KIND == GRAM || KIND == POLY) && ib + 32 * part_a(k) < jb + 32 * part_b(k));
+               !(SYM && ib + 32 * part_a(k) < jb + 32 * part_b(k));
     };
-    v4u src[ENDS][4];
+    v4u src[ENDS][4], src2[KIND == PAIR ? ENDS : 1][4];
     v4f di[W][2][2];
     float dj[W];
     // Places of an image that a lane writes and reads, part by part at constant distances: its pieces of row j
@@ -474,16 +480,24 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
 #pragma unroll
                     for (int u = 0; u < 4; ++u)
                         src[k][u] = *reinterpret_cast<const v4u*>(from.kilobyte(part_b(k), part_a(k), u) + lane16b);
+                    if constexpr (KIND == PAIR) {
+                        const Parts<SPLIT> other(g.P, matrix, jb, ib);
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            src2[k][u] = *reinterpret_cast<const v4u*>(other.kilobyte(part_b(k), part_a(k), u) + lane16b);
+                    }
                 }
 #pragma unroll
             for (int a = 0; a < W; ++a)
                 if (ib + 32 * a < g.P.rows)
 #pragma unroll
                     for (int u = 0; u < 4; ++u) di[a][u / 2][u % 2] = *reinterpret_cast<const v4f*>(sd + ib + 32 * a + 16 * (u / 2) + 8 * h + 4 * (u % 2));
-            if constexpr (KIND == POLY)
+            if constexpr (KIND == POLY || KIND == PAIR) {
+                const float* qd = KIND == PAIR ? g.q_diag + matrix * g.side : sd;
 #pragma unroll
                 for (int b = 0; b < W; ++b)
-                    if (jb + 32 * b < g.Q.rows) dj[b] = sd[jb + 32 * b + r32];
+                    if (jb + 32 * b < g.Q.rows) dj[b] = qd[jb + 32 * b + r32];
+            }
         }
 #pragma unroll
     for (int k = 0; k < S - 1; ++k) load();
@@ -582,9 +596,9 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
                 v[u][e] = __uint_as_float(x[0]);
                 v[u][4 + e] = __uint_as_float(x[1]);
             }
-        const bool across = (KIND == GRAM || KIND == POLY) && ib + 32 * a == jb + 32 * b;  // the diagonal
+        const bool across = SYM && ib + 32 * a == jb + 32 * b;  // the diagonal
         float one = 0.f;                                                                  // the product's value on it
-        if constexpr (KIND == GRAM || KIND == POLY)
+        if constexpr (SYM)
             if (across) {
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
@@ -593,25 +607,47 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
                 one /= kUnit * kUnit;
             }
         if constexpr (KIND != GRAM) {
+            auto pieces_of = [&](const v4u (&from)[4], float (&to)[2][8]) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) *reinterpret_cast<v4u*>(image + 1024 * u + lane16b) = src[k][u];
-            __builtin_amdgcn_wave_barrier();
+                for (int u = 0; u < 4; ++u) *reinterpret_cast<v4u*>(image + 1024 * u + lane16b) = from[u];
+                __builtin_amdgcn_wave_barrier();
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const h8 hi = *reinterpret_cast<const h8*>(image + piece_at[0][u]);
+                    const h8 lo = *reinterpret_cast<const h8*>(image + piece_at[1][u]);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) to[u][e] = __builtin_fmaf(static_cast<float>(hi[e]), 1.f, static_cast<float>(lo[e]));
+                }
+                __builtin_amdgcn_wave_barrier();
+            };
             const float djk = HALVES ? (group ? dj[W - 1] : dj[0]) : dj[k % W], add = g.add / kUnit;
+            float s[2][8], s2[KIND == PAIR ? 2 : 1][8];
+            pieces_of(src[k], s);
+            if constexpr (KIND == PAIR) pieces_of(src2[k], s2);
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-                const h8 hi = *reinterpret_cast<const h8*>(image + piece_at[0][u]);
-                const h8 lo = *reinterpret_cast<const h8*>(image + piece_at[1][u]);
+            for (int u = 0; u < 2; ++u)
 #pragma unroll
                 for (int e = 0; e < 8; ++e) {
-                    const float d = di[HALVES ? k : k / W][u][e / 4][e % 4], s = __builtin_fmaf(static_cast<float>(hi[e]), 1.f, static_cast<float>(lo[e]));
+                    const float d = di[HALVES ? k : k / W][u][e / 4][e % 4];
                     if constexpr (KIND == POLY)
-                        v[u][e] = __builtin_fmaf(__builtin_fmaf(g.add, d + djk, g.keep), s, add * v[u][e]);
+                        v[u][e] = __builtin_fmaf(__builtin_fmaf(g.add, d + djk, g.keep), s[u][e], add * v[u][e]);
+                    else if constexpr (KIND == PAIR)
+                        v[u][e] = __builtin_fmaf(g.add, __builtin_fmaf(d, s[u][e], djk * s2[u][e]), add * v[u][e]);
                     else
-                        v[u][e] = __builtin_fmaf(g.keep + d, s, v[u][e] / kUnit);
+                        v[u][e] = __builtin_fmaf(g.add * (g.keep + d), s[u][e], add * v[u][e]);
                 }
-            }
-            __builtin_amdgcn_wave_barrier();
-            if (KIND == POLY && across) one = __builtin_fmaf(g.keep, djk, g.add * __builtin_fmaf(djk, djk, one));
+            if (KIND == POLY && across) one = g.plus + __builtin_fmaf(g.keep, djk, g.add * __builtin_fmaf(djk, djk, one));
+            // row i is column j here, and the first factor's diagonal is asked for along i alone
+            if constexpr (KIND == PAIR)
+                if (across) {
+                    float dd = 0.f;
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int e = 0; e < 8; ++e)
+                            dd = 16 * u + 8 * h + e == r32 ? di[HALVES ? k : k / W][u][e / 4][e % 4] : dd;
+                    one = g.add * __builtin_fmaf(dd, djk, one);
+                }
         } else {
 #pragma unroll
             for (int u = 0; u < 2; ++u)
@@ -1176,7 +1212,7 @@ struct OrthShape {
     int64_t group;           // matrices at a time
     int mt;                  // tiles of 16 of a narrow matrix's smaller side, 0 for the others
     int64_t parts;           // sums of squares of a matrix, or of its blocks' G G^T
-    int64_t x, xt, lo, a, e, d, bytes;  // bytes of a stored X, its other order, its lo, A, E, a diagonal, and the workspace
+    int64_t x, xt, lo, a, e, d, more, bytes;  // bytes of a stored X, its other order, its lo, A, E, a diagonal, and the workspace
 };
 
 int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape* s) {
@@ -1211,10 +1247,12 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
     s->lo = split ? 0 : s->mp * s->np * 2;
     s->e = s->mp * s->mp * size;  // E, and A without its lo
     s->a = s->e + (split ? 0 : s->e);
+    // of steps without X: their products, which an update may take (and never does nearer to a square)
+    s->more = split && 4 * s->np >= 5 * s->mp ? 3 * s->e + 3 * s->mp * 4 : 0;
     s->d = s->mp * 4;
     const int64_t turns = (R * C + 16 * kPrepBlock - 1) / (16 * kPrepBlock);
     s->parts = turns < kMostParts ? turns : kMostParts;
-    const int64_t each = 2 * (s->x + s->xt + s->lo) + s->a + s->e + 2 * s->d + kMostParts * 8;
+    const int64_t each = 2 * (s->x + s->xt + s->lo) + s->a + s->e + 2 * s->d + s->more + kMostParts * 8;
     s->group = kGroupBytes / each;
     if (s->group < 1) s->group = 1;
     if (s->group > B) s->group = B;
@@ -1292,10 +1330,10 @@ int64_t tiles_of(int64_t rows, int64_t cols, bool half, int w, int64_t* tj) {
     return half ? i * (i + 1) / 2 : i * j;
 }
 
-int choose_tile(bool split, bool half, bool last, int64_t L, int64_t rows, int64_t cols, int panels) {
+int choose_tile(bool split, bool half, bool last, int64_t L, int64_t rows, int64_t cols, int panels, double* time = nullptr) {
     int best = 0;
     double least = 0.0;
-    for (int k = 0; k < (last ? 3 : 4); ++k) {  // the largest tile's last step would not fit the registers
+    for (int k = 0; k < (last ? 3 : 4); ++k) {  // with more to read at the end the largest tile does not fit the registers
         const Tile& t = kTiles[split][k];
         int64_t tj;
         const int64_t blocks = L * tiles_of(rows, cols, half, t.w, &tj), rest = blocks % t.slots;
@@ -1303,23 +1341,42 @@ int choose_tile(bool split, bool half, bool last, int64_t L, int64_t rows, int64
         const double cost = blocks / t.slots * round(1.0) + (rest ? round(static_cast<double>(rest) / t.slots) : 0.0);
         if (k == 0 || cost < least) least = cost, best = k;
     }
+    if (time) *time = least;
     return best;
 }
 
 template <bool SPLIT, int KIND, int DO>
 void launch_product(Product g, const Result& res, unsigned L, int64_t rows, int64_t cols, hipStream_t stream) {
-    constexpr bool HALF = KIND == GRAM || KIND == POLY;
-    const int k = choose_tile(SPLIT, HALF, KIND == LAST, L, rows, cols, g.panels);
+    constexpr bool HALF = KIND == GRAM || KIND == POLY || KIND == PAIR;
+    const int k = choose_tile(SPLIT, HALF, KIND == LAST || KIND == PAIR, L, rows, cols, g.panels);
     const Tile& t = kTiles[SPLIT][k];
     int64_t tj;
     const int64_t tiles = tiles_of(rows, cols, HALF, t.w, &tj);
     g.tiles = static_cast<int>(tiles), g.tj = static_cast<int>(tj);
     auto kern = k == 0   ? orth_product_kernel<SPLIT, KIND, DO, 1, kTiles[SPLIT][0].groups>
                 : k == 1 ? orth_product_kernel<SPLIT, KIND, DO, 2, 1> : orth_product_kernel<SPLIT, KIND, DO, 2, 2>;
-    if constexpr (KIND != LAST)
+    if constexpr (KIND != LAST && KIND != PAIR)
         if (k == 3) kern = orth_product_kernel<SPLIT, KIND, DO, 3, 1>;
     launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((tiles + 7) / 8)), L), dim3(static_cast<unsigned>(256 * t.groups)), 0, stream, g,
                   res);
+}
+
+// Whether an update's steps are taken two or three at a time without X: X <- q X with q the product of the steps'
+// p = a I + b A + c A^2, and A' = p A p instead of a new X X^T, all of them symmetric and of X's smaller side. For
+// five steps two X X^T and two products with X instead of five, and nine more of the smaller side. An error of A
+// is multiplied by up to a^2 = 12 a step, so A is formed anew after three: a direction is then off by up to 1.6
+// times what it is otherwise (2.3e-6 and 1.0e-6 of 256 x 1024; 2.1e-5, 1.6e-5 and in fp32 1.5e-5 where a
+// few directions are a hundred times the others), which an update's weights do not show, while an
+// orthogonalised matrix would: only updates of fp32 weights take it. 2560 x 10240: 3240 -> 2030 us.
+bool without_x(int64_t mp, int64_t np, int64_t L, int steps) {
+    if (steps < 2) return false;
+    const int runs = (steps + 2) / 3, along = static_cast<int>(np / panel_cols(true)), across = static_cast<int>(mp / panel_cols(true));
+    double gram, poly, next;
+    choose_tile(true, true, false, L, mp, mp, along, &gram);
+    choose_tile(true, true, true, L, mp, mp, across, &poly);
+    choose_tile(true, false, true, L, mp, np, across, &next);
+    // a run of r steps: r polynomials, r - 1 products for q and 2 (r - 1) for A
+    return runs * (gram + next) + (steps + 3 * (steps - runs)) * 1.1 * poly < 0.95 * steps * (gram + poly + next);
 }
 
 template <int DG, int DO, bool MOMENTUM>
@@ -1347,10 +1404,11 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
     }
     Plane a = {take(s.e), nullptr, s.mp, s.e};
     a.lo = take(SPLIT ? 0 : s.e);
-    Plane e = {take(s.e), nullptr, s.mp, s.e};
-    float* da = reinterpret_cast<float*>(take(s.d));
-    float* de = reinterpret_cast<float*>(take(s.d));
+    const Plane e_first = {take(s.e), nullptr, s.mp, s.e};
+    float* const da = reinterpret_cast<float*>(take(s.d));
+    float* const de_first = reinterpret_cast<float*>(take(s.d));
     double* sums = reinterpret_cast<double*>(take(kMostParts * 8));
+    char* const rest = at;  // s.more bytes a matrix
     const int along = static_cast<int>(s.np / panel_cols(SPLIT)), across = static_cast<int>(s.mp / panel_cols(SPLIT));
     for (int64_t first = 0; first < s.B; first += s.group) {
         const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
@@ -1362,17 +1420,80 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
                       call.src, sums, static_cast<int>(s.parts), call.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0], s.R, s.C, first);
         Result res = call.res;
         res.first = first;
+        Plane e = e_first;  // which changes places with others below
+        float* de = de_first;
+        char* free = rest;
+        [[maybe_unused]] auto take_more = [&](int64_t bytes) {
+            char* p = free;
+            free += bytes * s.group;
+            return p;
+        };
+        auto gram = [&](int now) {
+            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0}, res, L,
+                                            s.mp, s.mp, stream);
+        };
+        auto poly = [&](const float* c, float plus) {
+            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0}, res, L, s.mp, s.mp,
+                                            stream);
+        };
+        auto next = [&](int now, const Plane& by, const float* diag, float keep, float add, bool last) {
+            const Product g = {by, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], diag, nullptr, keep, add, nullptr, 0.f, s.mp, across, 0, 0};
+            if (last)
+                launch_product<SPLIT, LAST, DO>(g, res, L, s.mp, s.np, stream);
+            else
+                launch_product<SPLIT, NEXT, DO>(g, res, L, s.mp, s.np, stream);
+        };
+        if constexpr (SPLIT && MOMENTUM) {
+            const int runs = (call.steps + 2) / 3;
+            if (s.more && without_x(s.mp, s.np, L, call.steps)) {
+                // q = p_k .. p_1 of a run and A' = p A p of its steps; a power of two keeps q's entries below 16
+                Plane t = e, q[2] = {e, e};
+                t.hi = take_more(s.e), q[0].hi = take_more(s.e), q[1].hi = take_more(s.e);
+                float* dt = reinterpret_cast<float*>(take_more(s.mp * 4));
+                float* dq[2];
+                for (float*& d : dq) d = reinterpret_cast<float*>(take_more(s.mp * 4));
+                auto pair = [&](const Plane& M, const float* dm, const Plane& N, const float* dn, const Plane& to, float* d, float by) {
+                    launch_product<SPLIT, PAIR, DO>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0}, res, L, s.mp, s.mp,
+                                                    stream);
+                };
+                for (int run = 0, k = 0; run < runs; ++run) {
+                    const int length = (call.steps - k) / (runs - run);  // the shorter ones first
+                    gram(run & 1);
+                    double most = 1.0;
+                    float scale = 1.f;
+                    Plane now = e;
+                    float* dnow = de;
+                    for (int i = 0; i < length; ++i, ++k) {
+                        const float* c = call.coefs + 3 * k;
+                        poly(c, c[0]);
+                        most *= c[0] > 1.f ? c[0] : c[0] < -1.f ? -c[0] : 1.f;
+                        if (i > 0) {
+                            float by = 1.f;
+                            while (scale * by * most > 8.0) by *= 0.5f;
+                            scale *= by;
+                            pair(e, de, now, dnow, q[i & 1], dq[i & 1], by);
+                            now = q[i & 1], dnow = dq[i & 1];
+                        }
+                        if (i + 1 < length) {
+                            pair(e, de, a, da, t, dt, 1.f);
+                            pair(e, de, t, dt, a, da, 1.f);
+                            if (i == 0) {  // the first p is q, and the next p comes elsewhere
+                                std::swap(e.hi, q[0].hi);
+                                std::swap(de, dq[0]);
+                                now = q[0], dnow = dq[0];
+                            }
+                        }
+                    }
+                    next(run & 1, now, dnow, 0.f, 1.f / scale, run + 1 == runs);
+                }
+                continue;
+            }
+        }
         for (int k = 0; k < call.steps; ++k) {
             const float* c = call.coefs + 3 * k;
-            const int now = k & 1;
-            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, s.mp, along, 0, 0}, res, L, s.mp, s.mp,
-                                            stream);
-            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], s.mp, across, 0, 0}, res, L, s.mp, s.mp, stream);
-            const Product next = {e, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], de, nullptr, c[0], 0.f, s.mp, across, 0, 0};
-            if (k + 1 < call.steps)
-                launch_product<SPLIT, NEXT, DO>(next, res, L, s.mp, s.np, stream);
-            else
-                launch_product<SPLIT, LAST, DO>(next, res, L, s.mp, s.np, stream);
+            gram(k & 1);
+            poly(c, 0.f);
+            next(k & 1, e, de, c[0], 1.f, k + 1 == call.steps);
         }
     }
     return launch_status();

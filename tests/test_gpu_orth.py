@@ -194,6 +194,31 @@ def test_step(shape, w_dtype, g_dtype, nesterov):
         assert torch.equal(w2, w) and torch.equal(m2, m)
 
 
+@pytest.mark.parametrize("steps", [2, 3, 4, 5, 7])
+@pytest.mark.parametrize("kind", ["mixed", "spread"])
+def test_step_without_x(steps, kind):
+    """Rectangular fp32 weights, whose steps run on the smaller side's products alone: the direction itself, read off
+    weights of zero. It may be off by 1.6 times what the direct steps are, whose bound has a factor of three."""
+    for shape in ((1280, 6000), (6000, 1280), (2, 1300, 5200)):
+        G, M = matrices(shape, F32, 40 + steps, kind), torch.zeros(shape, device="cuda")
+        W = torch.zeros(shape, device="cuda")
+        b4.orth_step(W, G, M, -1.0, momentum=0.0, scale=1.0, steps=steps)
+        ref, bound = orth_ref(G, steps=steps)
+        close(W, ref, 1.6 * bound, f"{shape} {steps} {kind}")
+
+
+def test_step_groups():
+    """More matrices than the workspace takes at a time, with the steps without X: each as by itself."""
+    shape = (9, 1280, 6000)
+    assert b4.lib().birkhoff4_orth_work(*shape, b4.F32) < b4.lib().birkhoff4_orth_work(1, *shape[1:], b4.F32) * 9
+    G, M, W = matrices(shape, BF16, 50), torch.zeros(shape, device="cuda"), torch.zeros(shape, device="cuda")
+    G[-1] = G[0]
+    b4.orth_step(W, G, M, -1.0, momentum=0.0, scale=1.0)
+    ref, bound = orth_ref(G[[0, 5]].float())
+    close(W[[0, 5]], ref, 1.6 * bound, "first and sixth")
+    close(W[8:], ref[:1], 1.6 * bound[:1], "last")
+
+
 def test_step_pieces():
     """Weights and momenta that begin at any value of a flat buffer; strided gradients."""
     shape = (45, 131)
