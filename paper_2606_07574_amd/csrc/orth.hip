@@ -1321,8 +1321,8 @@ struct Tile {
     double few, all, ends;
 };
 constexpr Tile kTiles[2][4] = {
-    {{1, 2, 512, 0.20, 0.46, 4.0}, {2, 1, 512, 0.21, 0.45, 7.0}, {2, 2, 256, 0.33, 0.50, 8.0}, {3, 1, 256, 0.36, 0.62, 8.0}},
-    {{1, 4, 256, 0.40, 0.53, 4.0}, {2, 1, 512, 0.23, 0.55, 6.0}, {2, 2, 256, 0.42, 0.62, 8.0}, {3, 1, 256, 0.44, 0.75, 8.0}}};
+    {{1, 2, 512, 0.20, 0.46, 4.0}, {2, 1, 512, 0.21, 0.45, 9.0}, {2, 2, 256, 0.33, 0.50, 9.0}, {3, 1, 256, 0.36, 0.62, 12.0}},
+    {{1, 4, 256, 0.40, 0.53, 4.0}, {2, 1, 512, 0.23, 0.55, 8.0}, {2, 2, 256, 0.42, 0.62, 8.5}, {3, 1, 256, 0.44, 0.75, 12.0}}};
 
 int64_t tiles_of(int64_t rows, int64_t cols, bool half, int w, int64_t* tj) {
     const int64_t t = 64 * w, i = (rows + t - 1) / t, j = (cols + t - 1) / t;
