@@ -1346,9 +1346,10 @@ int choose_tile(bool split, bool half, bool last, int64_t L, int64_t rows, int64
 }
 
 template <bool SPLIT, int KIND, int DO>
-void launch_product(Product g, const Result& res, unsigned L, int64_t rows, int64_t cols, hipStream_t stream) {
+void launch_product(Product g, const Result& res, int64_t group, unsigned L, int64_t rows, int64_t cols, hipStream_t stream) {
+    // by the matrices of a full group, so that a batch's last ones are summed like the others
     constexpr bool HALF = KIND == GRAM || KIND == POLY || KIND == PAIR;
-    const int k = choose_tile(SPLIT, HALF, KIND == LAST || KIND == PAIR, L, rows, cols, g.panels);
+    const int k = choose_tile(SPLIT, HALF, KIND == LAST || KIND == PAIR, group, rows, cols, g.panels);
     const Tile& t = kTiles[SPLIT][k];
     int64_t tj;
     const int64_t tiles = tiles_of(rows, cols, HALF, t.w, &tj);
@@ -1429,23 +1430,23 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
             return p;
         };
         auto gram = [&](int now) {
-            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0}, res, L,
+            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0}, res, s.group, L,
                                             s.mp, s.mp, stream);
         };
         auto poly = [&](const float* c, float plus) {
-            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0}, res, L, s.mp, s.mp,
+            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0}, res, s.group, L, s.mp, s.mp,
                                             stream);
         };
         auto next = [&](int now, const Plane& by, const float* diag, float keep, float add, bool last) {
             const Product g = {by, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], diag, nullptr, keep, add, nullptr, 0.f, s.mp, across, 0, 0};
             if (last)
-                launch_product<SPLIT, LAST, DO>(g, res, L, s.mp, s.np, stream);
+                launch_product<SPLIT, LAST, DO>(g, res, s.group, L, s.mp, s.np, stream);
             else
-                launch_product<SPLIT, NEXT, DO>(g, res, L, s.mp, s.np, stream);
+                launch_product<SPLIT, NEXT, DO>(g, res, s.group, L, s.mp, s.np, stream);
         };
         if constexpr (SPLIT && MOMENTUM) {
             const int runs = (call.steps + 2) / 3;
-            if (s.more && without_x(s.mp, s.np, L, call.steps)) {
+            if (s.more && without_x(s.mp, s.np, s.group, call.steps)) {
                 // q = p_k .. p_1 of a run and A' = p A p of its steps; a power of two keeps q's entries below 16
                 Plane t = e, q[2] = {e, e};
                 t.hi = take_more(s.e), q[0].hi = take_more(s.e), q[1].hi = take_more(s.e);
@@ -1453,7 +1454,7 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
                 float* dq[2];
                 for (float*& d : dq) d = reinterpret_cast<float*>(take_more(s.mp * 4));
                 auto pair = [&](const Plane& M, const float* dm, const Plane& N, const float* dn, const Plane& to, float* d, float by) {
-                    launch_product<SPLIT, PAIR, DO>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0}, res, L, s.mp, s.mp,
+                    launch_product<SPLIT, PAIR, DO>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0}, res, s.group, L, s.mp, s.mp,
                                                     stream);
                 };
                 for (int run = 0, k = 0; run < runs; ++run) {

@@ -2,7 +2,7 @@
 
 The kernels' products are of values rounded to fp16 pieces (in units of 2^-12): for fp32 results of two
 pieces each (hi hi + hi lo + lo hi), for bf16 results of one, with fp32 sums; X, A and E = b A + c A^2 are
-kept as two pieces. `model` makes these roundings in torch's operations, in another order of sums. Its
+kept as two pieces, the diagonals of A and E as fp32 numbers outside the products. `model` makes these roundings in torch's operations, in another order of sums. Its
 distance from float64 is what the roundings cost for that matrix; they are random, so the kernels' own may
 be another draw: three times it is allowed (of a Frobenius norm over few values, too). A matrix of very few
 values can be lucky in the model; so one rounding of the terms of a step near s = 1, |a| + |b| + |c| = 10
@@ -28,11 +28,10 @@ def wide(G, eps):
     return X / (torch.linalg.vector_norm(X, dim=(1, 2), keepdim=True) + eps), tall
 
 
-def iterate(X, coefs, product, keep):
+def iterate(X, coefs):
     for a, b, c in coefs:
-        A = keep(product(X, turn(X)))
-        E = keep(b * A + c * product(A, A))
-        X = keep(a * X + product(E, X))
+        A = X @ turn(X)
+        X = a * X + (b * A + c * (A @ A)) @ X
     return X
 
 
@@ -47,13 +46,24 @@ def orth_ref(G, steps=5, coefs=COEFS, eps=1e-7, split=True):
     rounded to its type. split: the products of fp32 results."""
     coefs = triples(coefs, steps)
     X, tall = wide(G, eps)
-    ref = iterate(X, coefs, torch.matmul, lambda M: M)
+    ref = iterate(X, coefs)
 
     def product(M, N):
         (mh, ml), (nh, nl) = pieces(M), pieces(N)
         return mh @ nh + (mh @ nl + ml @ nh) if split else mh @ nh
 
-    model = iterate(X.float(), coefs, product, lambda M: sum(pieces(M)))
+    def apart(M):
+        D = M.diagonal(dim1=1, dim2=2)
+        return D, M - torch.diag_embed(D)
+
+    Y = sum(pieces(X.float()))
+    for a, b, c in coefs:
+        D, R = apart(product(Y, turn(Y)))
+        R = sum(pieces(R))
+        S = product(R, R) + (D[:, :, None] + D[:, None, :]) * R + torch.diag_embed(D * D)
+        F, R = apart(b * (R + torch.diag_embed(D)) + c * S)
+        Y = sum(pieces((a + F)[:, :, None] * Y + product(sum(pieces(R)), Y)))
+    model = Y
     size = torch.linalg.vector_norm(ref, dim=(1, 2))
     terms = max(sum(abs(v) for v in c) for c in coefs)
     bound = 3 * torch.linalg.vector_norm(model.double() - ref, dim=(1, 2)) + terms * (2.0 ** -22 if split else 2.0 ** -11) * size

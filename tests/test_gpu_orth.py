@@ -138,6 +138,24 @@ def test_batches():
     assert b4.orth(G[:0]).shape == (0, 96, 100) and b4.orth(G[:, :0]).shape == (6000, 0, 100)
 
 
+@pytest.mark.parametrize("rows,cols", [(128, 1000), (24, 8200), (8200, 24)])
+def test_far_matrices(rows, cols):
+    """Batches beyond 2^31 values and 2^32 bytes: the last matrix, which is the first one again, has its bits."""
+    B = (1 << 31) // (rows * cols) + 300
+    G = torch.empty(B, rows, cols, dtype=BF16, device="cuda")
+    for k in range(0, B, 2000):
+        G[k:k + 2000] = matrices((rows, cols), BF16, k, "spread")
+    G[-1] = G[0]
+    O = b4.orth(G)
+    assert torch.equal(O[-1], O[0]) and not torch.equal(O[-1], O[-2])
+    ref, bound = orth_ref(G[:1], split=False)
+    close(O[-1:], ref, bound, "last")
+    if rows == 24:
+        M, W = torch.zeros(B, rows, cols, device="cuda"), torch.ones(B, rows, cols, dtype=BF16, device="cuda")
+        b4.orth_step(W, G, M, 0.1)
+        assert torch.equal(W[-1], W[0]) and torch.equal(M[-1], G[0].float()) and not torch.equal(W[-1], W[-2])
+
+
 @pytest.mark.parametrize("shape,dtype", [((3, 17, 45), F32), ((2, 150, 131), BF16), ((131, 150), F32)], ids=str)
 def test_nothing_behind(shape, dtype):
     G = matrices(shape, dtype, 12)
