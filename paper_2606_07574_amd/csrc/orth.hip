@@ -844,9 +844,8 @@ __global__ __launch_bounds__(kGramBlock) void orth_narrow_gram_kernel(Source s, 
 #pragma unroll 4
         for (int k = 0; k < kSlab; k += 4)
 #pragma unroll
-            for (int q = 0; q < OWN; ++q)
-                if (wave + 4 * q < TILES)  // uniform over the wave
-                    acc[q] = mfma_f64(slab[ri[q] + k], slab[rj[q] + k], acc[q]);
+            for (int q = 0; q < OWN; ++q)  // a tile too many is the first one again: a branch here took four times as long
+                acc[q] = mfma_f64(slab[ri[q] + k], slab[rj[q] + k], acc[q]);
     }
     double* out = part + (matrix * gridDim.x + blockIdx.x) * (TILES * 256);
 #pragma unroll
@@ -873,7 +872,10 @@ __global__ __launch_bounds__(256) void orth_narrow_join_kernel(const double* __r
 }
 
 // F of each matrix from its G G^T: one block a matrix, a wave for each tile. A matrix in LDS is
-// symmetric, so its rows serve as both factors' columns: the lanes of 16 read 16 neighbours.
+// symmetric, so its rows serve as both factors' columns: the lanes of 16 read 16 neighbours. Rows are 20 or 52
+// or 84 values apart, 40 banks: what a tile's lanes write across the rows then lies in all banks alike.
+constexpr int poly_pitch(int p) { return p <= 16 ? 20 : p <= 48 ? 52 : 84; }
+
 struct Coefs {
     float v[3 * kOrthMaxSteps];
 };
@@ -882,29 +884,39 @@ template <int MT>
 __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const double* __restrict__ sum, double* __restrict__ F,
                                                                         double* __restrict__ scales, double eps, Coefs coefs,
                                                                         int steps) {
-    constexpr int P = 16 * MT;
-    __shared__ double A[P * P], S[P * P], Q[P * P];
+    constexpr int P = 16 * MT, D = poly_pitch(P);
+    __shared__ double A[P * D], S[P * D], Q[P * D];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t matrix = blockIdx.x;
     int ti = 0;
     while (tri(ti + 1) <= wave) ++ti;
     const int tj = wave - tri(ti);
     const int row = 16 * ti + (lane >> 4), col = 16 * tj + (lane & 15);  // of value r: row + 4 r
-    const int from_i = (lane >> 4) * P + 16 * ti + (lane & 15), from_j = (lane >> 4) * P + 16 * tj + (lane & 15);
-    // two sums that do not wait for each other
+    const int from_i = (lane >> 4) * D + 16 * ti + (lane & 15), from_j = (lane >> 4) * D + 16 * tj + (lane & 15);
+    // M N, and with two second factors both; each as two sums that do not wait for each other
     auto product = [&](const double* M, const double* N) {
         v4d x = {}, y = {};
 #pragma unroll
         for (int k = 0; k < P; k += 8) {
-            x = mfma_f64(M[k * P + from_i], N[k * P + from_j], x);
-            y = mfma_f64(M[(k + 4) * P + from_i], N[(k + 4) * P + from_j], y);
+            x = mfma_f64(M[k * D + from_i], N[k * D + from_j], x);
+            y = mfma_f64(M[(k + 4) * D + from_i], N[(k + 4) * D + from_j], y);
         }
         return x + y;
+    };
+    auto products = [&](const double* M, const double* N, const double* O, v4d* by_n, v4d* by_o) {
+        v4d x = {}, y = {};
+#pragma unroll
+        for (int k = 0; k < P; k += 4) {
+            const double m = M[k * D + from_i];
+            x = mfma_f64(m, N[k * D + from_j], x);
+            y = mfma_f64(m, O[k * D + from_j], y);
+        }
+        *by_n = x, *by_o = y;
     };
     auto put = [&](double* M, const v4d& v) {
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-            if (row + 4 * r >= col) M[(row + 4 * r) * P + col] = M[col * P + row + 4 * r] = v[r];
+            if (row + 4 * r >= col) M[(row + 4 * r) * D + col] = M[col * D + row + 4 * r] = v[r];
     };
     v4d a, f = {};
 #pragma unroll
@@ -912,7 +924,7 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     put(A, a);
     __syncthreads();
     double norm = 0.0;  // of the diagonal, the same in every wave
-    for (int k = lane & 15; k < P; k += 16) norm += A[k * P + k];
+    for (int k = lane & 15; k < P; k += 16) norm += A[k * D + k];
 #pragma unroll
     for (int k = 1; k < 16; k *= 2) norm += __shfl_xor(norm, k);
     norm = __builtin_sqrt(norm);
@@ -934,9 +946,16 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
         put(S, p);
         __syncthreads();
         const bool last = k + 1 == steps;  // uniform
-        f = k == 0 ? p : product(S, Q);
-        if (last) break;
-        a = product(S, A);
+        if (last) {
+            f = product(S, Q);
+            break;
+        }
+        if (k == 0) {
+            f = p;
+            a = product(S, A);
+        } else {
+            products(S, Q, A, &f, &a);
+        }
         __syncthreads();
         put(Q, f);
         put(A, a);
@@ -1298,7 +1317,7 @@ int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStrea
         Result res = call.res;
         res.first = first;
         const int64_t turns = rows16 ? (s.n + 511) / 512 : slabs;  // what a block takes at a time
-        int64_t blocks = 2 * kGramBlocks / L;
+        int64_t blocks = kGramBlocks / L;  // two a compute unit (four: 32 of 80 x 32768 bf16 76 us instead of 69)
         if (blocks < 1) blocks = 1;
         if (blocks > turns) blocks = turns;
         if (rows16)
