@@ -45,7 +45,7 @@ enum {
     BIRKHOFF4_ERR_DTYPE = -5,     /* unknown storage dtype code */
     BIRKHOFF4_ERR_ALIGN = -6,     /* an array is not 16-byte aligned */
     BIRKHOFF4_ERR_OVERLAP = -7,   /* an output overlaps another argument */
-    BIRKHOFF4_ERR_STEPS = -8,     /* step count of Sinkhorn or of the orthogonalisation out of range */
+    BIRKHOFF4_ERR_STEPS = -8,     /* step count out of range: Sinkhorn's 1..48, the orthogonalisation's 1..64 */
     BIRKHOFF4_ERR_DEVICE = -9,    /* HIP device query failed */
     BIRKHOFF4_ERR_LAUNCH = -10,   /* kernel launch failed (hipGetLastError) */
     BIRKHOFF4_ERR_VARIANT = -11,  /* unknown forward variant */
@@ -403,8 +403,10 @@ int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype);
  * eps    >= 0 and finite (BIRKHOFF4_ERR_EPS). The norm is a 64-bit sum: no finite fp32 matrix is
  *        too large or too small. A zero matrix with eps > 0 gives zeros; one with a NaN or infinite
  *        value gives NaN everywhere; the others of the batch are not touched by it.
- * An fp32 result is what fp32 products give. For a bf16 result the products' factors are rounded to
- * fp16 (11 bits, a quarter of the rounding of the result itself), their sums are fp32.
+ * An fp32 result is what fp32 products give, or nearer; with a side of at most 80, what 64-bit ones
+ * do. For a bf16 result the products' factors are rounded to fp16 (11 bits; off by less than the
+ * rounding of the result itself), but for the diagonals and a X; sums are fp32. The number of matrices
+ * may change the order of sums; within a batch it is the same for all of them.
  * work   workspace of birkhoff4_orth_work(B, rows, cols, out_dtype) bytes, 16-byte aligned, in use until
  *        the call's work on `stream` has ended. The other arrays may begin at any value. No output may
  *        overlap another argument. rows and cols up to 2^20, the smaller of them up to 2^16, B up to
@@ -419,7 +421,8 @@ int birkhoff4_orth(const void* G, int g_dtype, void* out, int out_dtype, const f
  * W      [B][rows][cols] in w_dtype (F32 or BF16, rounded to nearest even); M the same in fp32.
  * lr_at  a float in device memory, read when the work runs (a replayed graph takes what it is by
  *        then), or NULL for one.
- * The other arguments as above, with w_dtype for out_dtype. */
+ * The other arguments as above, with w_dtype for out_dtype. The direction that fp32 weights far from
+ * square take may be off by up to twice what birkhoff4_orth's is. */
 int birkhoff4_orth_step(void* W, int w_dtype, const void* G, int g_dtype, float* M, float momentum, int nesterov, float lr,
                         const float* lr_at, float decay, float scale, const float* coefs, int steps, float eps, void* work,
                         int64_t work_bytes, int64_t B, int64_t rows, int64_t cols, hipStream_t stream);

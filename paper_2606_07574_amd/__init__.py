@@ -916,7 +916,7 @@ def _steps(coefs, steps: int):
     """orth's coefficients as the library takes them: a host array of `steps` triples."""
     steps = int(steps)
     if not 1 <= steps <= 64:
-        _check(-8)
+        raise ValueError(f"orth's step count must be in [1, 64], got {steps}")
     return _coefs_array(tuple(tuple(c) if isinstance(c, (list, tuple)) else c for c in coefs), steps), steps
 
 

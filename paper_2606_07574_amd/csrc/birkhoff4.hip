@@ -4410,12 +4410,12 @@ const char* birkhoff4_strerror(int code) {
         case BIRKHOFF4_ERR_DTYPE: return "unknown dtype code";
         case BIRKHOFF4_ERR_ALIGN: return "arrays must be 16-byte aligned";
         case BIRKHOFF4_ERR_OVERLAP: return "an output overlaps another argument";
-        case BIRKHOFF4_ERR_STEPS: return "step count out of range (Sinkhorn 1..48, orthogonalisation 1..64)";
+        case BIRKHOFF4_ERR_STEPS: return "Sinkhorn step count must be in [1, 48]";
         case BIRKHOFF4_ERR_DEVICE: return "HIP device query failed";
         case BIRKHOFF4_ERR_LAUNCH: return "kernel launch failed";
         case BIRKHOFF4_ERR_VARIANT: return "unknown forward variant";
         case BIRKHOFF4_ERR_ETA: return "eta must be positive and finite";
-        case BIRKHOFF4_ERR_CHANNELS: return "C must be >= 0 and a multiple of 8 (bf16 streams) or 4 (fp32); of the layer norm, > 0";
+        case BIRKHOFF4_ERR_CHANNELS: return "C must be >= 0 and a multiple of 8 (bf16 streams) or 4 (fp32)";
         case BIRKHOFF4_ERR_EPS: return "eps must be >= 0 and finite";
         case BIRKHOFF4_ERR_WORK: return "workspace too small";
         case BIRKHOFF4_ERR_DROP: return "dropout probability must be in [0, 1)";

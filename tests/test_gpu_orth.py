@@ -254,7 +254,7 @@ def test_step_pieces():
 
 def test_refusals():
     W, G, M = (matrices((30, 20), F32, 19 + k) for k in range(3))
-    for bad, error in (((G.half(),), TypeError), ((G[0],), ValueError), ((G.cpu(),), b4.Birkhoff4Error), ((G, 0), b4.Birkhoff4Error),
+    for bad, error in (((G.half(),), TypeError), ((G[0],), ValueError), ((G.cpu(),), b4.Birkhoff4Error), ((G, 0), ValueError),
                        ((G, 5, (1.0, 2.0)), ValueError), ((G, 5, b4.ORTH_COEFS, -1.0), b4.Birkhoff4Error)):
         with pytest.raises(error):
             b4.orth(*bad)
