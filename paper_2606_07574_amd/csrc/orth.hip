@@ -741,6 +741,7 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
 constexpr int kNarrow = 80;
 constexpr int kSlab = 64;            // columns of X taken at a time
 constexpr int kSlabPitch = kSlab + 1;
+constexpr double kFar = 0x1p80;      // what bf16 values far from one are multiplied or divided by
 
 typedef double v4d __attribute__((ext_vector_type(4)));
 
@@ -969,7 +970,10 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     for (int r = 0; r < 4; ++r)
         if (row + 4 * r >= col)
             F[matrix * P * P + (row + 4 * r) * P + col] = F[matrix * P * P + col * P + row + 4 * r] = f[r];
-    if (threadIdx.x == 0) scales[matrix] = scale;
+    if (threadIdx.x == 0) {
+        scales[2 * matrix] = scale;
+        scales[2 * matrix + 1] = norm < 0x1p-60 ? kFar : norm > 0x1p60 ? 1.0 / kFar : 1.0;
+    }
 }
 
 // F X, 64 columns at a time: four waves take 16 each. F has values of a^5 = 485 where X has small singular values,
@@ -990,7 +994,7 @@ __global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const 
     Slab<DG, MOMENTUM, MT> x(s, base, res.rows, res.cols);
     x.fetch(static_cast<int64_t>(blockIdx.x) * kSlab);
     for (int k = threadIdx.x; k < P * P; k += 256) f[k] = static_cast<Value>(F[matrix * P * P + k]);
-    const double scale = scales[matrix];
+    const double scale = scales[2 * matrix];
     const float rate = res.update && res.lr_at ? res.lr * *res.lr_at : res.lr;
     const float shrink = 1.f - rate * res.decay, by = rate * res.scale;
     for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += pace) {
@@ -1052,7 +1056,9 @@ __global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const 
 // The matrix cores take the values as they lie in memory: eight neighbours of a row are what a lane of a product
 // of rows has, and products of bf16 values are exact in fp32. Their sums over `run` columns, 64 or 256, are fp32 numbers (off
 // by 2^-24 of them at most a few times, at random), the sums of those 64-bit ones: enough for a bf16 result
-// where the steps multiply an error by 12 four times. 32 matrices of 80 x 32768: 668 us in 64-bit products.
+// where the steps multiply an error by 12 four times. A block whose squares leave fp32's range takes its columns
+// again with values far from it (2^80 times or 2^-80 times them, which is exact). 32 matrices of 80 x 32768 take
+// 45.7 us, 3.7 TB/s (by 64-bit products four times as long).
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ v4f mfma_b16(const v4u a, const v4u b, const v4f c) {
@@ -1072,6 +1078,14 @@ __device__ __forceinline__ v4u read8(const void* G, int64_t at, int64_t n) {
     return v;
 }
 
+// The eight values times `by`, a power of two.
+__device__ __forceinline__ v4u times(const v4u v, float by) {
+    v4u w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = pack_bf16(__uint_as_float(v[e] << 16) * by, __uint_as_float(v[e] & 0xffff0000u) * by);
+    return w;
+}
+
 template <int MT>
 __global__ __launch_bounds__(256) void orth_narrow16_gram_kernel(const void* __restrict__ G, double* __restrict__ part, int m, int64_t n,
                                                                  int run, int64_t first) {
@@ -1080,7 +1094,6 @@ __global__ __launch_bounds__(256) void orth_narrow16_gram_kernel(const void* __r
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t matrix = blockIdx.y, base = (first + matrix) * m * n;
     const int64_t pace = static_cast<int64_t>(gridDim.x) * 4 * run;
-    v4d acc[TILES] = {};
     v4u x[2][MT], next[2][MT];
     auto fetch = [&](int64_t j0) {
 #pragma unroll
@@ -1092,40 +1105,55 @@ __global__ __launch_bounds__(256) void orth_narrow16_gram_kernel(const void* __r
                 next[k][t] = read8(G, base + row * n + j, row < m ? n - j : 0);
             }
     };
-    int64_t j0 = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * run;
-    fetch(j0);
-    for (; j0 < n; j0 += pace) {
-        v4f sum[TILES] = {};
+    auto sums = [&](auto scaled, float by) {
+        v4d acc[TILES] = {};
+        int64_t j0 = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * run;
+        fetch(j0);
+        for (; j0 < n; j0 += pace) {
+            v4f sum[TILES] = {};
 #pragma unroll 1
-        for (int c = 0; c < run; c += 64) {
+            for (int c = 0; c < run; c += 64) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int t = 0; t < MT; ++t) x[k][t] = next[k][t];
-            fetch(c + 64 < run ? j0 + c + 64 : j0 + pace);
+                    for (int t = 0; t < MT; ++t) x[k][t] = decltype(scaled)::value ? times(next[k][t], by) : next[k][t];
+                fetch(c + 64 < run ? j0 + c + 64 : j0 + pace);
 #pragma unroll
-            for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 2; ++k)
 #pragma unroll
-                for (int i = 0; i < MT; ++i)
+                    for (int i = 0; i < MT; ++i)
 #pragma unroll
-                    for (int j = 0; j <= i; ++j) sum[tri(i) + j] = mfma_b16(x[k][i], x[k][j], sum[tri(i) + j]);
-        }
-#pragma unroll
-        for (int t = 0; t < TILES; ++t)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) acc[t][r] += static_cast<double>(sum[t][r]);
-    }
-    for (int w = 0; w < 4; ++w) {  // the waves' sums, in their order
-        if (wave == w) {
+                        for (int j = 0; j <= i; ++j) sum[tri(i) + j] = mfma_b16(x[k][i], x[k][j], sum[tri(i) + j]);
+            }
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
-                    double* at = &joint[t * 256 + (4 * (lane >> 4) + r) * 16 + (lane & 15)];
-                    *at = w == 0 ? acc[t][r] : *at + acc[t][r];
-                }
+                for (int r = 0; r < 4; ++r) acc[t][r] += static_cast<double>(sum[t][r]);
         }
+        const double back = 1.0 / (static_cast<double>(by) * by);
+        for (int w = 0; w < 4; ++w) {  // the waves' sums, in their order
+            if (wave == w) {
+#pragma unroll
+                for (int t = 0; t < TILES; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        double* at = &joint[t * 256 + (4 * (lane >> 4) + r) * 16 + (lane & 15)];
+                        const double v = decltype(scaled)::value ? acc[t][r] * back : acc[t][r];
+                        *at = w == 0 ? v : *at + v;
+                    }
+            }
+            __syncthreads();
+        }
+    };
+    sums(std::false_type{}, 1.f);
+    double squares = 0.0;  // the same in every wave
+    for (int k = lane; k < 16 * MT; k += 64) squares += joint[(tri(k / 16) + k / 16) * 256 + 17 * (k % 16)];
+#pragma unroll
+    for (int k = 1; k < 64; k *= 2) squares += __shfl_xor(squares, k);
+    // below 2^-80 the up to 2^20 products lost under 2^-126 would be more than 2^-26 of it
+    if (!(squares >= 0x1p-80 && squares < __builtin_inf())) {
         __syncthreads();
+        sums(std::true_type{}, static_cast<float>(squares < 0x1p-80 ? kFar : 1.0 / kFar));
     }
     for (int k = threadIdx.x; k < TILES * 256; k += 256) part[(matrix * gridDim.x + blockIdx.x) * (TILES * 256) + k] = joint[k];
 }
@@ -1141,7 +1169,8 @@ __global__ __launch_bounds__(256) void orth_narrow16_apply_kernel(const void* __
     __shared__ v4u f[MT][KS][3][64];
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const int64_t matrix = blockIdx.y, base = (first + matrix) * m * n;
-    const double scale = scales[matrix];
+    const double up = scales[2 * matrix + 1], scale = scales[2 * matrix] / up;
+    const bool far = up != 1.0;  // values that many times, and F less by it
     for (int q = wave; q < MT * KS; q += 4) {
         const int t = q / KS, k = q % KS, row = 16 * t + (lane & 15), col = 32 * k + 8 * (lane >> 4);
         float v[8];
@@ -1170,6 +1199,11 @@ __global__ __launch_bounds__(256) void orth_narrow16_apply_kernel(const void* __
                 const int row = 32 * k + 8 * (lane >> 4) + r;
                 x[k][r] = read8(G, base + row * n + j, row < m ? there : 0);
             }
+        if (far)
+#pragma unroll
+            for (int k = 0; k < KS; ++k)
+#pragma unroll
+                for (int r = 0; r < 8; ++r) x[k][r] = times(x[k][r], static_cast<float>(up));
         // column c of the eight rows: halves of the words c / 2, paired
         auto column = [&](int k, int c) {
             v4u b;
@@ -1399,6 +1433,16 @@ bool without_x(int64_t mp, int64_t np, int64_t L, int steps) {
     return runs * (gram + next) + (steps + 3 * (steps - runs)) * 1.1 * poly < 0.95 * steps * (gram + poly + next);
 }
 
+// The most of |a + b t + c t^2|, t the square of a singular value from 0 to sqrt(2), and at least one. (A larger
+// one that a step leaves below 2 has grown by less than sqrt(2), which the room from 8 to 16 is for.)
+double most_of(const float* c) {
+    auto at = [&](double t) { return __builtin_fabs(c[0] + t * (c[1] + t * static_cast<double>(c[2]))); };
+    double most = 1.0;
+    for (const double t : {0.0, 2.0, c[2] != 0.f ? -0.5 * c[1] / c[2] : 0.0})
+        if (t >= 0.0 && t <= 2.0 && at(t) > most) most = at(t);
+    return most;
+}
+
 template <int DG, int DO, bool MOMENTUM>
 int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
     switch (s.mt) {
@@ -1486,7 +1530,7 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
                     for (int i = 0; i < length; ++i, ++k) {
                         const float* c = call.coefs + 3 * k;
                         poly(c, c[0]);
-                        most *= c[0] > 1.f ? c[0] : c[0] < -1.f ? -c[0] : 1.f;
+                        most *= most_of(c);
                         if (i > 0) {
                             float by = 1.f;
                             while (scale * by * most > 8.0) by *= 0.5f;

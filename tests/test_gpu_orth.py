@@ -83,6 +83,25 @@ def test_sizes_of_values(shape):
     for e in (-100, -20, 40, 120):
         assert torch.equal(b4.orth(G * 2.0 ** e, eps=0.0), O)
     check(G * 1e-7, "against eps", eps=1e-5)
+    check(G * 2.0 ** -126, "below the smallest normal value", eps=0.0)
+    assert (b4.orth(torch.zeros_like(G)) == 0).all()
+
+
+@pytest.mark.parametrize("shape", [(24, 200), (3, 80, 5000), (200, 24), (150, 260)], ids=str)
+def test_sizes_of_bf16_values(shape):
+    """The same of bf16 values, whose squares leave fp32's range at both ends; and a matrix with a part that
+    is far larger, or far smaller, than the rest."""
+    G = matrices(shape, BF16, 7, "spread", 1.0)
+    O = b4.orth(G, eps=0.0)
+    assert O.isfinite().all()
+    for e in (-100, -66, -20, 40, 66, 120):
+        assert torch.equal(b4.orth(G * 2.0 ** e, eps=0.0), O), e
+    check(G * 2.0 ** -126, "below the smallest normal value", eps=0.0)
+    check(G * 2.0 ** -70, "against eps", eps=2.0 ** -66)
+    for e in (-80, 100):
+        part = G.clone()
+        part[..., : shape[-1] // 2] *= 2.0 ** e
+        check(part, f"a half 2^{e} times", eps=0.0)
     assert (b4.orth(torch.zeros_like(G)) == 0).all()
 
 
@@ -223,6 +242,15 @@ def test_step_without_x(steps, kind):
         b4.orth_step(W, G, M, -1.0, momentum=0.0, scale=1.0, steps=steps)
         ref, bound = orth_ref(G, steps=steps)
         close(W, ref, 1.6 * bound, f"{shape} {steps} {kind}")
+
+
+def test_step_growing():
+    """Steps without X whose coefficients are large away from zero, not at it."""
+    shape, coefs = (1280, 6000), ((1.0, 1600.0, 0.0), (1.0, 10.0, 0.0), (1.5, -0.5, 0.0))
+    G, M, W = matrices(shape, F32, 12, "spread"), torch.zeros(shape, device="cuda"), torch.zeros(shape, device="cuda")
+    b4.orth_step(W, G, M, -1.0, momentum=0.0, scale=1.0, steps=3, coefs=coefs)
+    ref, bound = orth_ref(G, steps=3, coefs=coefs)
+    close(W, ref, 1.6 * bound, "growing")
 
 
 def test_step_groups():
