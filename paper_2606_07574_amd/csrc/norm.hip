@@ -32,33 +32,52 @@ __device__ __forceinline__ int chunk_values(const Row& r, int c) {
     return RAGGED && c == r.nc - 1 ? r.rem : E;
 }
 
-// Values of chunk c as stored, zeros past the row's end.
+// Chunk c as it is asked for: the last one of a ragged row as the sixteen bytes that end with the row, so that no
+// load waits for another one (element by element, the wave that has it lost the row ahead: 32 K rows of 4095 bf16
+// forward 170 us and now 117, backward 338 and 186; of 4096, 96 and 150). Rows of less than sixteen bytes come element by element.
 template <int DX, bool RAGGED>
-__device__ __forceinline__ v4u load_chunk(const char* row, const Row& r, int c) {
+__device__ __forceinline__ v4u ask_chunk(const char* row, const Row& r, int c) {
     constexpr int E = MixChunk<DX>::E;
     const char* p = row + 16 * static_cast<int64_t>(c);
+    if (c >= r.nc) return v4u{0, 0, 0, 0};
     if constexpr (!RAGGED) {
-        return c < r.nc ? __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p)) : v4u{0, 0, 0, 0};
+        return __builtin_nontemporal_load(reinterpret_cast<const v4u*>(p));
+    } else if (r.nc > 1) {
+        if (c == r.nc - 1) p -= (E - r.rem) * (16 / E);
+        if constexpr (DX == BIRKHOFF4_BF16)
+            return *reinterpret_cast<const v4u_at2*>(p);
+        else
+            return *reinterpret_cast<const v4u_at4*>(p);
     } else {
         v4u v = {0, 0, 0, 0};
-        const int n = chunk_values<DX, RAGGED>(r, c);
-        if (n == E) {
-            if constexpr (DX == BIRKHOFF4_BF16)
-                v = *reinterpret_cast<const v4u_at2*>(p);
-            else
-                v = *reinterpret_cast<const v4u_at4*>(p);
-        } else if (n > 0) {
 #pragma unroll
-            for (int e = 0; e < E - 1; ++e) {
-                if (e >= n) continue;
-                if constexpr (DX == BIRKHOFF4_BF16)
-                    v[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e & 1));
-                else
-                    v[e] = reinterpret_cast<const uint32_t*>(p)[e];
-            }
+        for (int e = 0; e < E - 1; ++e) {
+            if (e >= r.rem) continue;
+            if constexpr (DX == BIRKHOFF4_BF16)
+                v[e / 2] |= static_cast<uint32_t>(reinterpret_cast<const uint16_t*>(p)[e]) << (16 * (e & 1));
+            else
+                v[e] = reinterpret_cast<const uint32_t*>(p)[e];
         }
         return v;
     }
+}
+
+// Its values, zeros past the row's end.
+template <int DX, bool RAGGED>
+__device__ __forceinline__ v4u chunk_of(v4u v, const Row& r, int c) {
+    constexpr int E = MixChunk<DX>::E;
+    if (RAGGED && r.nc > 1 && c == r.nc - 1 && r.rem < E) {
+        const uint64_t lo = v.x | static_cast<uint64_t>(v.y) << 32, hi = v.z | static_cast<uint64_t>(v.w) << 32;
+        const int bits = (E - r.rem) * (128 / E);
+        const uint64_t a = bits >= 64 ? hi >> (bits - 64) : lo >> bits | hi << (64 - bits), b = bits >= 64 ? 0 : hi >> bits;
+        v = v4u{static_cast<uint32_t>(a), static_cast<uint32_t>(a >> 32), static_cast<uint32_t>(b), static_cast<uint32_t>(b >> 32)};
+    }
+    return v;
+}
+
+template <int DX, bool RAGGED>
+__device__ __forceinline__ v4u load_chunk(const char* row, const Row& r, int c) {
+    return chunk_of<DX, RAGGED>(ask_chunk<DX, RAGGED>(row, r, c), r, c);
 }
 
 template <int DX, bool RAGGED>
@@ -169,7 +188,7 @@ __device__ __forceinline__ void group_sums(float (&v)[N], float (*red)[N]) {
 // Forward
 // ---------------------------------------------------------------------------
 // Values of a row that a thread holds: 32 K rows of 4096 bf16 97 us with 16 and four blocks of 256 threads a compute unit, 106
-// with 8 and eight blocks, 98 with 32; 8191 of 1023 12.3, 13.7 and 15.9. The backward's sums of dw and db leave room for 8.
+// with 8 and eight blocks, 98 with 32; 8191 of 1023 12.3, 13.7 and 15.9 (10.8 since, see ask_chunk). The backward's sums of dw and db leave room for 8.
 constexpr int kFwdHeld = 16, kFwdBlocks = 4, kHeld = 8;
 constexpr int fwd_threads(int G) { return G > 256 ? G : 256; }
 
@@ -193,12 +212,12 @@ __global__ __launch_bounds__(fwd_threads(G)) void norm_fwd_kernel(const void* __
     int64_t row = static_cast<int64_t>(blockIdx.x) * PER + threadIdx.x / G;
     v4u next[K];
 #pragma unroll
-    for (int k = 0; k < K; ++k) next[k] = row < B ? load_chunk<DX, RAGGED>(x + row * pitch, r, t + G * k) : v4u{0, 0, 0, 0};
+    for (int k = 0; k < K; ++k) next[k] = row < B ? ask_chunk<DX, RAGGED>(x + row * pitch, r, t + G * k) : v4u{0, 0, 0, 0};
     for (int64_t base = static_cast<int64_t>(blockIdx.x) * PER; base < B; base += step) {  // uniform over the block
         float v[K][E], sum[1] = {0.f};
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            unpack_chunk<DX>(next[k], v[k]);
+            unpack_chunk<DX>(chunk_of<DX, RAGGED>(next[k], r, t + G * k), v[k]);
 #pragma unroll
             for (int e = 0; e < E; ++e) sum[0] += v[k][e];
         }
@@ -206,7 +225,7 @@ __global__ __launch_bounds__(fwd_threads(G)) void norm_fwd_kernel(const void* __
         row += step;
         if (row < B) {
 #pragma unroll
-            for (int k = 0; k < K; ++k) next[k] = load_chunk<DX, RAGGED>(x + row * pitch, r, t + G * k);
+            for (int k = 0; k < K; ++k) next[k] = ask_chunk<DX, RAGGED>(x + row * pitch, r, t + G * k);
         }
         group_sums<G, NT>(sum, red[0]);
         const float mu = sum[0] / c;
@@ -318,8 +337,8 @@ __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const void* __res
         const bool in = at < B;
 #pragma unroll
         for (int k = 0; k < K; ++k) {
-            nx[k] = in ? load_chunk<DX, RAGGED>(x + at * pitch, r, t + G * k) : v4u{0, 0, 0, 0};
-            ny[k] = in ? load_chunk<DX, RAGGED>(dy + at * pitch, r, t + G * k) : v4u{0, 0, 0, 0};
+            nx[k] = in ? ask_chunk<DX, RAGGED>(x + at * pitch, r, t + G * k) : v4u{0, 0, 0, 0};
+            ny[k] = in ? ask_chunk<DX, RAGGED>(dy + at * pitch, r, t + G * k) : v4u{0, 0, 0, 0};
         }
         nmu = in ? mean[at] : 0.f;
         ns = in ? rstd[at] : 0.f;
@@ -331,7 +350,10 @@ __global__ __launch_bounds__(kBwdThreads) void norm_bwd_kernel(const void* __res
         const float mu = nmu, s = ns;
         const int64_t own = row;
 #pragma unroll
-        for (int k = 0; k < K; ++k) cx[k] = nx[k], cy[k] = ny[k];
+        for (int k = 0; k < K; ++k) {
+            cx[k] = chunk_of<DX, RAGGED>(nx[k], r, t + G * k);
+            cy[k] = chunk_of<DX, RAGGED>(ny[k], r, t + G * k);
+        }
         row += step;
         fetch(row);
         float sum[2] = {0.f, 0.f};  // of g and of g xh
