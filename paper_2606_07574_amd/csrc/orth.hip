@@ -5,7 +5,8 @@
 //     A = X X^T,   E = b A + c A^2,   X <- a X + E X        (a, b, c of each step)
 // An odd polynomial of X: it keeps the singular vectors and moves the singular values, p(s) = a s + b s^3 +
 // c s^5. Every step is three products, 2 m^2 n + 2 m^3 + 2 m^2 n operations, of which the symmetric A and
-// A^2 need one half: bound by the matrix cores but for small m.
+// A^2 need one half: bound by the matrix cores but for small m. 4096 x 4096 in bf16 takes 1.6 ms, 0.86 PFLOP/s of
+// those operations; 2560 x 10240 in fp32 (three times as many, in fp16) 3.2 ms.
 //
 // The products run on the matrix cores in fp16 pieces with fp32 sums. A value x is stored as 2^12 x, whose
 // fp16 rounding is `hi` and the fp16 rounding of what is left `lo`: 22 bits for values above 2^-14, and
@@ -154,7 +155,8 @@ struct Source {
 };
 
 // M <- momentum M + G where there is one, and the sum of squares of each matrix's direction in 64 bits (no
-// finite fp32 matrix leaves its range): gridDim.x partial sums for each of gridDim.y matrices.
+// finite fp32 matrix leaves its range): gridDim.x partial sums for each of gridDim.y matrices. Bound by memory:
+// 10240 x 2560 (bf16 G, fp32 M read and written) 46 us, 5.7 TB/s; four loads of each array in flight.
 constexpr int kPrepBlock = 256;
 
 template <int DG, bool MOMENTUM>
@@ -202,7 +204,9 @@ __global__ __launch_bounds__(kPrepBlock) void orth_prep_kernel(Source s, double*
 }
 
 // The directions R x C over their norms, stored in their own order (own) and the other (turned), with zeros
-// around: 64 x 64 values a block. A NaN or infinity anywhere makes the whole matrix NaN.
+// around: 64 x 64 values a block, turned in LDS (a pitch of 65, so that both directions go over all banks). A NaN
+// or infinity anywhere makes the whole matrix NaN. Bound by memory: 4096 x 4096 bf16 28 us, 4.8 TB/s of 2 + 6 bytes a
+// value (10240 x 2560 with M, in fp32 pieces, 78 us, 4.7 TB/s).
 constexpr int kConvert = 64;
 
 template <int DG, bool MOMENTUM, bool SPLIT>
@@ -298,6 +302,9 @@ struct Result {
 // one is there and the others are on their way. At the middle of a stage the block's waves meet: what the
 // next stage reads has come then, and the one before is read by nobody any more, whose place the last one
 // takes.
+// What bounds it: large products the card's power, which takes the clock to 1.6..2 GHz while the matrix cores are busy two
+// thirds of the cycles: A X of 2560 x 10240 in fp32 376 us, 1.07 PFLOP/s of fp16 products; 4096 x 4096 in bf16 160
+// (0.86), its X X^T 88, half a product. Small ones a block's latency: 12 us of 48 matrices of 128 x 512.
 constexpr int stages(int w) { return w == 3 ? 6 : 5; }
 [[maybe_unused]] constexpr int kRawBuffer = 0x00027000;  // a buffer of bytes, addresses outside of it read as zero
 
@@ -736,8 +743,9 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
 // step and launches three kernels for it. An error of A is multiplied by up to a^2 = 12 a step where the
 // singular value is small, so A and F are 64-bit numbers, from products of the inputs without rounding: the
 // result is nearer than fp32 products bring it. The matrix cores' 64-bit rate is the limit of m: its cube
-// runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps), and G G^T of 80 rows
-// takes them half as long as reading fp32 G does.
+// runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps, of 52 that the kernel takes;
+// m = 24: 12), and G G^T of 80 rows takes them half as long as reading fp32 G does. 24 x 16384 fp32 takes 23 us,
+// 80 x 32768 97 (10 MB twice: 4 at the memory's rate).
 constexpr int kNarrow = 80;
 constexpr int kSlab = 64;            // columns of X taken at a time
 constexpr int kSlabPitch = kSlab + 1;
@@ -978,7 +986,7 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
 
 // F X, 64 columns at a time: four waves take 16 each. F has values of a^5 = 485 where X has small singular values,
 // whose products with the large ones cancel: an fp32 result is formed in 64 bits, or it would be off by 485
-// roundings of X there (one for bf16 in 32).
+// roundings of X there (one for bf16 in 32). 24 x 16384 fp32 4.9 us, which is latency.
 template <int DG, int DO, bool MOMENTUM, int MT>
 __global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const double* __restrict__ F, const double* __restrict__ scales,
                                                                 Result res) {
@@ -1160,7 +1168,7 @@ __global__ __launch_bounds__(256) void orth_narrow16_gram_kernel(const void* __r
 
 // F X with F as three bf16 values, which are all its fp32 bits. A wave has 128 columns: its lanes read 16 bytes of
 // eight rows each, and of eight columns the rows' values are paired for the products, whose results are 16 bytes
-// of a row again.
+// of a row again. 32 matrices of 80 x 32768 69 us, 4.8 TB/s.
 template <int MT>
 __global__ __launch_bounds__(256) void orth_narrow16_apply_kernel(const void* __restrict__ G, const double* __restrict__ F,
                                                                   const double* __restrict__ scales, void* __restrict__ out, int m,
