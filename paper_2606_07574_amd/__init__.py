@@ -908,7 +908,7 @@ def _coefs_array(coefs: tuple, steps: int):
         coefs = (coefs,) * steps
     if len(coefs) != steps or any(not isinstance(c, tuple) or len(c) != 3 for c in coefs):
         raise ValueError(f"coefs must be three numbers or {steps} triples of them")
-    flat = [float(v) for c in coefs for v in c]
+    flat = [v for c in coefs for v in c]
     return (ctypes.c_float * len(flat))(*flat)
 
 
@@ -917,7 +917,8 @@ def _steps(coefs, steps: int):
     steps = int(steps)
     if not 1 <= steps <= 64:
         raise ValueError(f"orth's step count must be in [1, 64], got {steps}")
-    return _coefs_array(tuple(tuple(c) if isinstance(c, (list, tuple)) else c for c in coefs), steps), steps
+    coefs = tuple(tuple(map(float, c)) if isinstance(c, (list, tuple)) else float(c) for c in coefs)
+    return _coefs_array(coefs, steps), steps
 
 
 def _matrices(t: torch.Tensor, name: str):
@@ -974,7 +975,7 @@ def orth_step(W: torch.Tensor, G: torch.Tensor, M: torch.Tensor, lr: float | tor
     sqrt(max(1, rows / cols)) by default. Weights stacked along leading axes are updated each by itself.
     Call it under torch.no_grad() where W is a parameter."""
     B, rows, cols = _matrices(W, "W")
-    _recorded(W, G, M)
+    _recorded(W, G, M, *([lr] if isinstance(lr, torch.Tensor) else []))
     code = _dtype_code(W)
     for t, name, dtype in ((W, "W", W.dtype), (M, "M", torch.float32)):
         _dense(t, name, W.shape, dtype, W)

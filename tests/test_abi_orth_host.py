@@ -130,3 +130,12 @@ def test_refusals():
         with pytest.raises(ValueError, match="step count"):
             b4._steps(COEFS, steps)
     assert math.isclose(b4.ORTH_COEFS[0], COEFS[0])
+
+
+def test_coefficients_are_taken_by_value():
+    """A coefficient that changes between calls, in a tensor that stays, is another coefficient."""
+    c = torch.tensor(2.0)
+    first, _ = b4._steps((c, 0.0, 0.0), 1)
+    c += 1
+    second, _ = b4._steps((c, 0.0, 0.0), 1)
+    assert list(first) == [2.0, 0.0, 0.0] and list(second) == [3.0, 0.0, 0.0]

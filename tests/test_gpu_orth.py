@@ -298,6 +298,8 @@ def test_refusals():
         b4.orth_step(P, G, M, 0.1)
     with torch.no_grad():
         b4.orth_step(P, G, M, 0.1)
+    with pytest.raises(RuntimeError, match="no derivative"):
+        b4.orth_step(W, G, M, torch.tensor(0.1, device="cuda", requires_grad=True))
 
 
 @pytest.mark.parametrize("shape,dtype", [((24, 500), F32), ((2, 200, 140), BF16)], ids=str)
