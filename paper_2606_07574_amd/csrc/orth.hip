@@ -880,10 +880,13 @@ __global__ __launch_bounds__(256) void orth_narrow_join_kernel(const double* __r
     sum[matrix * entries + at] = v;
 }
 
-// F of each matrix from its G G^T: one block a matrix, a wave for each tile. A matrix in LDS is
-// symmetric, so its rows serve as both factors' columns: the lanes of 16 read 16 neighbours. Rows are 20 or 52
-// or 84 values apart, 40 banks: what a tile's lanes write across the rows then lies in all banks alike.
-constexpr int poly_pitch(int p) { return p <= 16 ? 20 : p <= 48 ? 52 : 84; }
+// F of each matrix from its G G^T: one block a matrix, a wave for each 16 x 16 tile on and below the diagonal. What a
+// product leaves in a lane, four values of a column every four rows apart, is also what the next one wants from it: as
+// the second factor as it stands, as the first one, of a symmetric matrix, from the tile across the diagonal. So tiles lie in
+// LDS by lanes, 16 bytes of each in two halves, and a wave puts its own and its transpose.
+constexpr int kTile = 2048;  // bytes
+
+typedef double v2d __attribute__((ext_vector_type(2)));
 
 struct Coefs {
     float v[3 * kOrthMaxSteps];
@@ -893,39 +896,58 @@ template <int MT>
 __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const double* __restrict__ sum, double* __restrict__ F,
                                                                         double* __restrict__ scales, double eps, Coefs coefs,
                                                                         int steps) {
-    constexpr int P = 16 * MT, D = poly_pitch(P);
-    __shared__ double A[P * D], S[P * D], Q[P * D];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr int P = 16 * MT, MATRIX = MT * MT * kTile;
+    constexpr bool ROOM = MT <= 3;  // for what would otherwise take the place of something that is still being read
+    __shared__ __attribute__((aligned(16))) char lds[(ROOM ? 5 : 3) * MATRIX];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t matrix = blockIdx.x;
     int ti = 0;
     while (tri(ti + 1) <= wave) ++ti;
     const int tj = wave - tri(ti);
     const int row = 16 * ti + (lane >> 4), col = 16 * tj + (lane & 15);  // of value r: row + 4 r
-    const int from_i = (lane >> 4) * D + 16 * ti + (lane & 15), from_j = (lane >> 4) * D + 16 * tj + (lane & 15);
-    // M N, and with two second factors both; each as two sums that do not wait for each other
-    auto product = [&](const double* M, const double* N) {
+    char *const A = lds, *const S = lds + MATRIX, *const T = ROOM ? lds + 2 * MATRIX : A, *Q = lds + (ROOM ? 3 : 2) * MATRIX,
+         *free = ROOM ? lds + 4 * MATRIX : Q;
+    auto tile = [&](const char* M, int i, int j) {
+        const char* at = M + (i * MT + j) * kTile + 16 * lane;
+        const v2d x = *reinterpret_cast<const v2d*>(at), y = *reinterpret_cast<const v2d*>(at + kTile / 2);
+        return v4d{x.x, x.y, y.x, y.y};
+    };
+    // M N as two sums that do not wait for each other, and with two second factors both
+    auto product = [&](const char* M, const char* N) {
         v4d x = {}, y = {};
 #pragma unroll
-        for (int k = 0; k < P; k += 8) {
-            x = mfma_f64(M[k * D + from_i], N[k * D + from_j], x);
-            y = mfma_f64(M[(k + 4) * D + from_i], N[(k + 4) * D + from_j], y);
+        for (int k = 0; k < MT; ++k) {
+            const v4d a = tile(M, k, ti), b = tile(N, k, tj);
+            x = mfma_f64(a[0], b[0], x);
+            y = mfma_f64(a[1], b[1], y);
+            x = mfma_f64(a[2], b[2], x);
+            y = mfma_f64(a[3], b[3], y);
         }
         return x + y;
     };
-    auto products = [&](const double* M, const double* N, const double* O, v4d* by_n, v4d* by_o) {
+    auto products = [&](const char* M, const char* N, const char* O, v4d* by_n, v4d* by_o) {
         v4d x = {}, y = {};
 #pragma unroll
-        for (int k = 0; k < P; k += 4) {
-            const double m = M[k * D + from_i];
-            x = mfma_f64(m, N[k * D + from_j], x);
-            y = mfma_f64(m, O[k * D + from_j], y);
+        for (int k = 0; k < MT; ++k) {
+            const v4d a = tile(M, k, ti), b = tile(N, k, tj), c = tile(O, k, tj);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                x = mfma_f64(a[r], b[r], x);
+                y = mfma_f64(a[r], c[r], y);
+            }
         }
         *by_n = x, *by_o = y;
     };
-    auto put = [&](double* M, const v4d& v) {
+    auto put = [&](char* M, const v4d& v) {
+        char* at = M + (ti * MT + tj) * kTile + 16 * lane;
+        *reinterpret_cast<v2d*>(at) = v2d{v[0], v[1]};
+        *reinterpret_cast<v2d*>(at + kTile / 2) = v2d{v[2], v[3]};
+        if (ti != tj) {  // row c of the transpose: value c / 4 of the lanes of c mod 4
+            const int c = lane & 15;
+            char* across = M + (tj * MT + ti) * kTile + kTile / 2 * (c >> 3) + 256 * (c & 3) + 16 * (lane >> 4) + 8 * (c >> 2 & 1);
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
-            if (row + 4 * r >= col) M[(row + 4 * r) * D + col] = M[col * D + row + 4 * r] = v[r];
+            for (int r = 0; r < 4; ++r) *reinterpret_cast<double*>(across + 64 * r) = v[r];
+        }
     };
     v4d a, f = {};
 #pragma unroll
@@ -933,44 +955,48 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     put(A, a);
     __syncthreads();
     double norm = 0.0;  // of the diagonal, the same in every wave
-    for (int k = lane & 15; k < P; k += 16) norm += A[k * D + k];
+    const int c = lane & 15;
+#pragma unroll
+    for (int k = 0; k < MT; ++k)
+        norm += *reinterpret_cast<const double*>(A + k * (MT + 1) * kTile + kTile / 2 * (c >> 3) + 256 * (c & 3) + 16 * c + 8 * (c >> 2 & 1));
 #pragma unroll
     for (int k = 1; k < 16; k *= 2) norm += __shfl_xor(norm, k);
     norm = __builtin_sqrt(norm);
     const double scale = norm < __builtin_inf() ? 1.0 / (norm + eps) : __builtin_nan("");
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 4; ++r) a[r] = a[r] * scale * scale;
-    put(A, a);
-    __syncthreads();
+    a = a * scale * scale;
+    double by = scale * scale;  // what A in LDS lacks
     for (int k = 0; k < steps; ++k) {
         const double ca = coefs.v[3 * k], cb = coefs.v[3 * k + 1], cc = coefs.v[3 * k + 2];
-        v4d p = product(A, A);
+        v4d p = product(A, A), t;
 #pragma unroll
-        for (int r = 0; r < 4; ++r) p[r] = __builtin_fma(cc, p[r], __builtin_fma(cb, a[r], row + 4 * r == col ? ca : 0.0));
+        for (int r = 0; r < 4; ++r) p[r] = __builtin_fma(cc, p[r] * by * by, __builtin_fma(cb, a[r], row + 4 * r == col ? ca : 0.0));
         if (steps == 1) {
             f = p;
             break;
         }
         put(S, p);
         __syncthreads();
-        const bool last = k + 1 == steps;  // uniform
-        if (last) {
+        if (k + 1 == steps) {  // uniform
             f = product(S, Q);
             break;
         }
         if (k == 0) {
             f = p;
-            a = product(S, A);
+            t = product(S, A) * by;
+            by = 1.0;
         } else {
-            products(S, Q, A, &f, &a);
+            products(S, Q, A, &f, &t);
+        }
+        if constexpr (!ROOM) __syncthreads();
+        put(free, f);
+        put(T, t);
+        if constexpr (ROOM) {
+            char* const now = free;
+            free = Q, Q = now;
         }
         __syncthreads();
-        put(Q, f);
-        put(A, a);
-        __syncthreads();
-        a = product(S, A);
-        __syncthreads();
+        a = product(S, T);
+        if constexpr (!ROOM) __syncthreads();
         put(A, a);
         __syncthreads();
     }
