@@ -949,6 +949,9 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
             for (int r = 0; r < 4; ++r) *reinterpret_cast<double*>(across + 64 * r) = v[r];
         }
     };
+    // scalar loads would make the reads of LDS beside them wait, and each other
+    __shared__ double co[3 * kOrthMaxSteps];
+    for (int k = threadIdx.x; k < 3 * steps; k += 64 * tri(MT)) co[k] = coefs.v[k];
     v4d a, f = {};
 #pragma unroll
     for (int r = 0; r < 4; ++r) a[r] = sum[(matrix * tri(MT) + wave) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)];
@@ -966,7 +969,7 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     a = a * scale * scale;
     double by = scale * scale;  // what A in LDS lacks
     for (int k = 0; k < steps; ++k) {
-        const double ca = coefs.v[3 * k], cb = coefs.v[3 * k + 1], cc = coefs.v[3 * k + 2];
+        const double ca = co[3 * k], cb = co[3 * k + 1], cc = co[3 * k + 2];
         v4d p = product(A, A), t;
 #pragma unroll
         for (int r = 0; r < 4; ++r) p[r] = __builtin_fma(cc, p[r] * by * by, __builtin_fma(cb, a[r], row + 4 * r == col ? ca : 0.0));
