@@ -211,11 +211,15 @@ constexpr int kConvert = 64;
 
 template <int DG, bool MOMENTUM, bool SPLIT>
 __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const double* __restrict__ sums, int parts, double eps,
-                                                           Plane own, Plane turned, int64_t R, int64_t C, int64_t first) {
+                                                           Plane own, Plane turned, int64_t R, int64_t C, int64_t first,
+                                                           unsigned matrices, unsigned blocks, unsigned across) {
     __shared__ float tile[kConvert][kConvert + 1];
     __shared__ double red[256];
-    const int64_t matrix = blockIdx.z, base = (first + matrix) * R * C;
-    const int64_t r0 = static_cast<int64_t>(blockIdx.y) * kConvert, c0 = static_cast<int64_t>(blockIdx.x) * kConvert;
+    // `blocks` a matrix, `across` of them along a row; on the XCD that takes the matrix's products, too
+    const unsigned flat = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8, block = flat % blocks;
+    if (flat / blocks >= matrices) return;  // uniform over the block
+    const int64_t matrix = flat / blocks, base = (first + matrix) * R * C;
+    const int64_t r0 = static_cast<int64_t>(block / across) * kConvert, c0 = static_cast<int64_t>(block % across) * kConvert;
     constexpr int N = kConvert / 16;
     const int c = 4 * (threadIdx.x % 16);
     v4f u[N], m[N];
@@ -285,6 +289,7 @@ struct Product {
     int64_t side;
     int panels;             // of P's and Q's rows
     int tiles, tj;          // of the result, and along j
+    int matrices;
 };
 
 // What becomes of the last step's values: out (rows x cols, `tall`: out_ji), or the weights
@@ -371,10 +376,12 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
     __shared__ __attribute__((aligned(128))) char lds[KS * S * STAGE];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) & 3;
     const int group = KS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 8) : 0;
-    const int64_t matrix = blockIdx.y;
-    // Blocks go round the eight XCDs: each XCD takes neighbouring tiles, whose rows its L2 holds.
-    const int per = (g.tiles + 7) / 8, tile = blockIdx.x % 8 * per + blockIdx.x / 8;
-    if (tile >= g.tiles) return;  // uniform over the block
+    // Blocks go round the eight XCDs: each XCD takes neighbouring tiles of neighbouring matrices, whose rows its L2 holds.
+    const unsigned flat = blockIdx.x % 8 * (gridDim.x / 8) + blockIdx.x / 8;
+    const unsigned of = g.matrices > 1 ? flat / static_cast<unsigned>(g.tiles) : 0;
+    const int tile = static_cast<int>(flat - of * g.tiles);
+    const int64_t matrix = of;
+    if (tile >= g.tiles || of >= static_cast<unsigned>(g.matrices)) return;  // uniform over the block
     int ti, tj;
     if constexpr (SYM) {  // row by row below the diagonal
         ti = static_cast<int>((__builtin_sqrtf(8.f * tile + 1.f) - 1.f) * 0.5f);
@@ -1443,12 +1450,12 @@ void launch_product(Product g, const Result& res, int64_t group, unsigned L, int
     const Tile& t = kTiles[SPLIT][k];
     int64_t tj;
     const int64_t tiles = tiles_of(rows, cols, HALF, t.w, &tj);
-    g.tiles = static_cast<int>(tiles), g.tj = static_cast<int>(tj);
+    g.tiles = static_cast<int>(tiles), g.tj = static_cast<int>(tj), g.matrices = static_cast<int>(L);
     auto kern = k == 0   ? orth_product_kernel<SPLIT, KIND, DO, 1, kTiles[SPLIT][0].groups>
                 : k == 1 ? orth_product_kernel<SPLIT, KIND, DO, 2, 1> : orth_product_kernel<SPLIT, KIND, DO, 2, 2>;
     if constexpr (KIND != LAST && KIND != PAIR)
         if (k == 3) kern = orth_product_kernel<SPLIT, KIND, DO, 3, 1>;
-    launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((tiles + 7) / 8)), L), dim3(static_cast<unsigned>(256 * t.groups)), 0, stream, g,
+    launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((L * tiles + 7) / 8))), dim3(static_cast<unsigned>(256 * t.groups)), 0, stream, g,
                   res);
 }
 
@@ -1516,9 +1523,10 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
         launch_kernel((orth_prep_kernel<DG, MOMENTUM>), dim3(static_cast<unsigned>(s.parts), L), dim3(kPrepBlock), 0, stream,
                       call.src, sums, s.R * s.C, first);
         const int64_t Rp = tall ? s.np : s.mp, Cp = tall ? s.mp : s.np;
-        launch_kernel((orth_convert_kernel<DG, MOMENTUM, SPLIT>),
-                      dim3(static_cast<unsigned>(Cp / kConvert), static_cast<unsigned>(Rp / kConvert), L), dim3(256), 0, stream,
-                      call.src, sums, static_cast<int>(s.parts), call.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0], s.R, s.C, first);
+        const int64_t tiles = Cp / kConvert * (Rp / kConvert);
+        launch_kernel((orth_convert_kernel<DG, MOMENTUM, SPLIT>), dim3(static_cast<unsigned>((L * tiles + 7) / 8 * 8)), dim3(256), 0,
+                      stream, call.src, sums, static_cast<int>(s.parts), call.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0], s.R, s.C,
+                      first, L, static_cast<unsigned>(tiles), static_cast<unsigned>(Cp / kConvert));
         Result res = call.res;
         res.first = first;
         Plane e = e_first;  // which changes places with others below
@@ -1530,15 +1538,15 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
             return p;
         };
         auto gram = [&](int now) {
-            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0}, res, s.group, L,
+            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0, 0}, res, s.group, L,
                                             s.mp, s.mp, stream);
         };
         auto poly = [&](const float* c, float plus) {
-            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0}, res, s.group, L, s.mp, s.mp,
+            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
                                             stream);
         };
         auto next = [&](int now, const Plane& by, const float* diag, float keep, float add, bool last) {
-            const Product g = {by, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], diag, nullptr, keep, add, nullptr, 0.f, s.mp, across, 0, 0};
+            const Product g = {by, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], diag, nullptr, keep, add, nullptr, 0.f, s.mp, across, 0, 0, 0};
             if (last)
                 launch_product<SPLIT, LAST, DO>(g, res, s.group, L, s.mp, s.np, stream);
             else
@@ -1554,7 +1562,7 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
                 float* dq[2];
                 for (float*& d : dq) d = reinterpret_cast<float*>(take_more(s.mp * 4));
                 auto pair = [&](const Plane& M, const float* dm, const Plane& N, const float* dn, const Plane& to, float* d, float by) {
-                    launch_product<SPLIT, PAIR, DO>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0}, res, s.group, L, s.mp, s.mp,
+                    launch_product<SPLIT, PAIR, DO>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
                                                     stream);
                 };
                 for (int run = 0, k = 0; run < runs; ++run) {
