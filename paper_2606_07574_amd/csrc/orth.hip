@@ -309,7 +309,7 @@ struct Result {
 // takes.
 // What bounds it: large products the card's power, which takes the clock to 1.6..2 GHz while the matrix cores are busy two
 // thirds of the cycles: A X of 2560 x 10240 in fp32 376 us, 1.07 PFLOP/s of fp16 products; 4096 x 4096 in bf16 160
-// (0.86), its X X^T 88, half a product. Small ones a block's latency: 12 us of 48 matrices of 128 x 512.
+// (0.86), its X X^T 88, half a product. Small ones a block's latency: 5 to 10 us of 48 matrices of 128 x 512.
 constexpr int stages(int w) { return w == 3 ? 6 : 5; }
 [[maybe_unused]] constexpr int kRawBuffer = 0x00027000;  // a buffer of bytes, addresses outside of it read as zero
 
@@ -368,7 +368,7 @@ __device__ __forceinline__ void mix_reads() {
 }
 
 template <bool SPLIT, int KIND, int DO, int W, int KS>
-__global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_kernel(Product g, Result res) {
+__global__ __launch_bounds__(256 * KS, W * KS == 1 ? 4 : W * KS == 2 ? 2 : KS) void orth_product_kernel(Product g, Result res) {
     constexpr int T = 64 * W;
     constexpr bool SYM = KIND == GRAM || KIND == POLY || KIND == PAIR;
     constexpr int S = stages(W), STAGE = stage_bytes<W>();
@@ -751,7 +751,7 @@ __global__ __launch_bounds__(256 * KS, W * KS <= 2 ? 2 : KS) void orth_product_k
 // singular value is small, so A and F are 64-bit numbers, from products of the inputs without rounding: the
 // result is nearer than fp32 products bring it. The matrix cores' 64-bit rate is the limit of m: its cube
 // runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps, of 52 that the kernel takes;
-// m = 24: 12), and G G^T of 80 rows takes them half as long as reading fp32 G does. 24 x 16384 fp32 takes 23 us,
+// m = 24: 10), and G G^T of 80 rows takes them half as long as reading fp32 G does. 24 x 16384 fp32 takes 21 us,
 // 80 x 32768 97 (10 MB twice: 4 at the memory's rate).
 constexpr int kNarrow = 80;
 constexpr int kSlab = 64;            // columns of X taken at a time
@@ -1412,14 +1412,22 @@ int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStrea
 // with all compute units busy (us a panel; the matrix cores' clock and L2 are shared) and for its beginning
 // and end, fitted to products of 128 to 4096 rows. Measured (us): (A X) of 2560 x 10240 in fp32 128 x 128 383, in
 // two groups 415, 192 x 192 374, 64 x 64 554; X X^T of it 217, 201, 325, 339, of 1000 x 2565 43, 39, 78, 22; of
-// 4096 x 4096 in bf16 107, 112, 84, 167.
+// 4096 x 4096 in bf16 107, 112, 84, 167. 64 x 64 in one group is for many small matrices: 100 of 128 x 128 in fp32 183 -> 120
+// for all steps, 48 of 128 x 512 in bf16 120 -> 110.
 struct Tile {
     int w, groups, slots;  // its side in 64s, and how many blocks run at once
     double few, all, ends;
 };
-constexpr Tile kTiles[2][4] = {
-    {{1, 2, 512, 0.20, 0.46, 4.0}, {2, 1, 512, 0.21, 0.45, 9.0}, {2, 2, 256, 0.33, 0.50, 9.0}, {3, 1, 256, 0.36, 0.62, 12.0}},
-    {{1, 4, 256, 0.40, 0.53, 4.0}, {2, 1, 512, 0.23, 0.55, 8.0}, {2, 2, 256, 0.42, 0.62, 8.5}, {3, 1, 256, 0.44, 0.75, 12.0}}};
+constexpr Tile kTiles[2][5] = {{{1, 2, 512, 0.20, 0.46, 4.0},
+                              {2, 1, 512, 0.21, 0.45, 9.0},
+                              {2, 2, 256, 0.33, 0.50, 9.0},
+                              {1, 1, 1024, 0.20, 0.46, 4.0},
+                              {3, 1, 256, 0.36, 0.62, 12.0}},
+                             {{1, 4, 256, 0.40, 0.53, 4.0},
+                              {2, 1, 512, 0.23, 0.55, 8.0},
+                              {2, 2, 256, 0.42, 0.62, 8.5},
+                              {1, 1, 1024, 0.25, 0.53, 4.0},
+                              {3, 1, 256, 0.44, 0.75, 12.0}}};
 
 int64_t tiles_of(int64_t rows, int64_t cols, bool half, int w, int64_t* tj) {
     const int64_t t = 64 * w, i = (rows + t - 1) / t, j = (cols + t - 1) / t;
@@ -1430,7 +1438,7 @@ int64_t tiles_of(int64_t rows, int64_t cols, bool half, int w, int64_t* tj) {
 int choose_tile(bool split, bool half, bool last, int64_t L, int64_t rows, int64_t cols, int panels, double* time = nullptr) {
     int best = 0;
     double least = 0.0;
-    for (int k = 0; k < (last ? 3 : 4); ++k) {  // with more to read at the end the largest tile does not fit the registers
+    for (int k = 0; k < (last ? 4 : 5); ++k) {  // with more to read at the end the largest tile does not fit the registers
         const Tile& t = kTiles[split][k];
         int64_t tj;
         const int64_t blocks = L * tiles_of(rows, cols, half, t.w, &tj), rest = blocks % t.slots;
@@ -1452,9 +1460,10 @@ void launch_product(Product g, const Result& res, int64_t group, unsigned L, int
     const int64_t tiles = tiles_of(rows, cols, HALF, t.w, &tj);
     g.tiles = static_cast<int>(tiles), g.tj = static_cast<int>(tj), g.matrices = static_cast<int>(L);
     auto kern = k == 0   ? orth_product_kernel<SPLIT, KIND, DO, 1, kTiles[SPLIT][0].groups>
-                : k == 1 ? orth_product_kernel<SPLIT, KIND, DO, 2, 1> : orth_product_kernel<SPLIT, KIND, DO, 2, 2>;
+                : k == 1 ? orth_product_kernel<SPLIT, KIND, DO, 2, 1>
+                : k == 2 ? orth_product_kernel<SPLIT, KIND, DO, 2, 2> : orth_product_kernel<SPLIT, KIND, DO, 1, 1>;
     if constexpr (KIND != LAST && KIND != PAIR)
-        if (k == 3) kern = orth_product_kernel<SPLIT, KIND, DO, 3, 1>;
+        if (k == 4) kern = orth_product_kernel<SPLIT, KIND, DO, 3, 1>;
     launch_kernel(kern, dim3(static_cast<unsigned>(8 * ((L * tiles + 7) / 8))), dim3(static_cast<unsigned>(256 * t.groups)), 0, stream, g,
                   res);
 }
