@@ -1102,7 +1102,7 @@ __global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const 
 // by 2^-24 of them at most a few times, at random), the sums of those 64-bit ones: enough for a bf16 result
 // where the steps multiply an error by 12 four times. A block whose squares leave fp32's range takes its columns
 // again with values far from it (2^80 times or 2^-80 times them, which is exact). 32 matrices of 80 x 32768 take
-// 45.7 us, 3.7 TB/s (by 64-bit products four times as long).
+// 36 us, 4.7 TB/s (by 64-bit products four times as long; with registers for one wave a SIMD 47).
 typedef __bf16 b8 __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ v4f mfma_b16(const v4u a, const v4u b, const v4f c) {
@@ -1131,43 +1131,54 @@ __device__ __forceinline__ v4u times(const v4u v, float by) {
 }
 
 template <int MT>
-__global__ __launch_bounds__(256) void orth_narrow16_gram_kernel(const void* __restrict__ G, double* __restrict__ part, int m, int64_t n,
+__global__ __launch_bounds__(256, 2) void orth_narrow16_gram_kernel(const void* __restrict__ G, double* __restrict__ part, int m, int64_t n,
                                                                  int run, int64_t first) {
     constexpr int TILES = tri(MT);
     __shared__ double joint[TILES * 256];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int64_t matrix = blockIdx.y, base = (first + matrix) * m * n;
     const int64_t pace = static_cast<int64_t>(gridDim.x) * 4 * run;
-    v4u x[2][MT], next[2][MT];
-    auto fetch = [&](int64_t j0) {
+    v4u x[2][MT];  // 64 columns: each half is asked for again as soon as it has been multiplied
+    const uint32_t own = static_cast<uint32_t>(((lane & 15) * n + 8 * (lane >> 4)) * 2);
+    const bool there = 16 * (MT - 1) + (lane & 15) < m;  // rows behind the last one are zeros
+    auto fetch = [&](int k, int64_t j0) {
+        const int64_t j = j0 + 32 * k;  // uniform over the wave
+        const char* g = static_cast<const char*>(G) + 2 * (base + j);
+        if (j + 32 <= n) {
 #pragma unroll
-        for (int k = 0; k < 2; ++k)
+            for (int t = 0; t < MT; ++t)
+                x[k][t] = t + 1 < MT || there ? v4u(*reinterpret_cast<const v4u_at2*>(g + 32 * t * n + own)) : v4u{0, 0, 0, 0};
+        } else {
 #pragma unroll
             for (int t = 0; t < MT; ++t) {
                 const int row = 16 * t + (lane & 15);
-                const int64_t j = j0 + 32 * k + 8 * (lane >> 4);
-                next[k][t] = read8(G, base + row * n + j, row < m ? n - j : 0);
+                x[k][t] = read8(G, base + row * n + j + 8 * (lane >> 4), row < m ? n - j - 8 * (lane >> 4) : 0);
             }
+        }
     };
     auto sums = [&](auto scaled, float by) {
         v4d acc[TILES] = {};
         int64_t j0 = (static_cast<int64_t>(blockIdx.x) * 4 + wave) * run;
-        fetch(j0);
+        fetch(0, j0);
+        fetch(1, j0);
         for (; j0 < n; j0 += pace) {
             v4f sum[TILES] = {};
 #pragma unroll 1
             for (int c = 0; c < run; c += 64) {
+                const int64_t j1 = c + 64 < run ? j0 + c + 64 : j0 + pace;
 #pragma unroll
-                for (int k = 0; k < 2; ++k)
+                for (int k = 0; k < 2; ++k) {
+                    if constexpr (decltype(scaled)::value)
 #pragma unroll
-                    for (int t = 0; t < MT; ++t) x[k][t] = decltype(scaled)::value ? times(next[k][t], by) : next[k][t];
-                fetch(c + 64 < run ? j0 + c + 64 : j0 + pace);
-#pragma unroll
-                for (int k = 0; k < 2; ++k)
+                        for (int t = 0; t < MT; ++t) x[k][t] = times(x[k][t], by);
 #pragma unroll
                     for (int i = 0; i < MT; ++i)
 #pragma unroll
                         for (int j = 0; j <= i; ++j) sum[tri(i) + j] = mfma_b16(x[k][i], x[k][j], sum[tri(i) + j]);
+                    __builtin_amdgcn_sched_barrier(0);  // or both halves would need registers twice
+                    fetch(k, j1);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
             }
 #pragma unroll
             for (int t = 0; t < TILES; ++t)
