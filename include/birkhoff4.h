@@ -403,7 +403,7 @@ int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype);
  * eps    >= 0 and finite (BIRKHOFF4_ERR_EPS). The norm is a 64-bit sum: no finite fp32 matrix is
  *        too large or too small. A zero matrix with eps > 0 gives zeros; one with a NaN or infinite
  *        value gives NaN everywhere; the others of the batch are not touched by it.
- * An fp32 result is what fp32 products give, or nearer; with a side of at most 80, what 64-bit ones
+ * An fp32 result is about what fp32 products give; with a side of at most 80, what 64-bit ones
  * do. For a bf16 result the products' factors are rounded to fp16 (11 bits; off by less than the
  * rounding of the result itself), but for the diagonals and a X; sums are fp32. The number of matrices
  * may change the order of sums; within a batch it is the same for all of them.
