@@ -545,7 +545,9 @@ int row_group(int64_t C, int held = kHeld) {
     return g;
 }
 
+// Rows of sums that the backward writes and the join reads, none without rows.
 int64_t bwd_blocks(const NormShape& s) {
+    if (s.B == 0) return 0;
     if (s.r.C > kLongRow) {  // shares of the rows
         const int64_t want = 2048 / ((s.r.C + 255) / 256);
         return want < 1 ? 1 : want < s.B ? want : s.B;
@@ -653,7 +655,7 @@ int birkhoff4_norm_fwd(const void* X, int x_dtype, const void* weight, const voi
 int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype) {
     NormShape s;
     if (int e = norm_shape(B, C, x_dtype, BIRKHOFF4_F32, &s)) return e;
-    return B == 0 ? 0 : bwd_blocks(s) * 2 * C * 4;
+    return bwd_blocks(s) * 2 * C * 4;
 }
 
 int birkhoff4_norm_bwd(const void* X, int x_dtype, const void* weight, int w_dtype, const float* mean, const float* rstd,
@@ -664,7 +666,7 @@ int birkhoff4_norm_bwd(const void* X, int x_dtype, const void* weight, int w_dty
     const bool sums = dweight || dbias;
     if (B == 0 && !sums) return BIRKHOFF4_OK;
     if (B > 0 && (!X || !mean || !rstd || !dY || (sums && !work))) return BIRKHOFF4_ERR_NULL;
-    const int64_t need = sums && B > 0 ? bwd_blocks(s) * 2 * C * 4 : 0;
+    const int64_t need = sums ? bwd_blocks(s) * 2 * C * 4 : 0;
     if (work_bytes < need) return BIRKHOFF4_ERR_WORK;
     const void* all[] = {X, weight, mean, rstd, dY, dX, dweight, dbias, work};
     for (const void* p : all)
