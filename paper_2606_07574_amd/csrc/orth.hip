@@ -754,6 +754,18 @@ __global__ __launch_bounds__(256 * KS, W * KS == 1 ? 4 : W * KS == 2 ? 2 : KS) v
 // runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps, of 52 that the kernel takes;
 // m = 24: 10), and G G^T of 80 rows takes them half as long as reading fp32 G does. 24 x 16384 fp32 takes 21 us,
 // 80 x 32768 97 (10 MB twice: 4 at the memory's rate).
+//
+// Errors grow with the product g of the steps' largest |p| (for singular values up to sqrt(2), below): A's by g^2, and a
+// rounding between F's large and small directions by g^3, which five of the usual steps (g = 485) leave at 2^-26.
+// Where g is larger, an eigenvalue that should be zero, of either sign, would run away. There (DEEP):
+//   * A and F are made symmetric in every bit: their errors grow by g and g^2 then;
+//   * the first steps, to g = 64, are taken as above, then A is formed anew from F G, whose small values are 64 times as large;
+//   * from then on A <- p A p + shift I with a shift that is above what the step can have rounded: A stays positive definite, its eigenvalues stay where p keeps them, and F stays below
+//     64 / sqrt(2 P^1.5 2^-53) = 2^28. Singular values under 2^-26 of the norm stay behind what 64 bits would make of them (in fp32
+//     products they are lost among the roundings).
+//   * F X is formed in 64 bits whatever the result's type: F's large values meet zeros.
+// 24 x 1024 in fp32 of rank one: 2.5e-8 off after ten steps and 1.2e-5 after 64 (rows that are equal in pairs: 2.5e-8 and
+// 2.7e-6), where fp32 products are 1e-2 and 1 off (2e-6 and 4e-6).
 constexpr int kNarrow = 80;
 constexpr int kSlab = 64;            // columns of X taken at a time
 constexpr int kSlabPitch = kSlab + 1;
@@ -888,6 +900,63 @@ __global__ __launch_bounds__(256) void orth_narrow_join_kernel(const double* __r
     sum[matrix * entries + at] = v;
 }
 
+// Each block's part of Y Y^T for Y = F X, formed a slab at a time: four waves take 16 columns each of Y, and then the tiles
+// of Y Y^T as above. M is renewed already.
+template <int DG, bool MOMENTUM, int MT>
+__global__ __launch_bounds__(kGramBlock) void orth_narrow_again_kernel(Source s, const double* __restrict__ F,
+                                                                       const double* __restrict__ scales, double* __restrict__ part,
+                                                                       int64_t R, int64_t C, int64_t first) {
+    constexpr int P = 16 * MT, TILES = tri(MT), OWN = (TILES + 3) / 4;
+    __shared__ float slab[P * kSlabPitch];
+    __shared__ double f[P * P], y[P * kSlabPitch];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int64_t matrix = blockIdx.y, base = (first + matrix) * R * C, n = R > C ? R : C;
+    v4d acc[OWN] = {};
+    int ri[OWN], rj[OWN];
+#pragma unroll
+    for (int q = 0; q < OWN; ++q) {
+        const int t = wave + 4 * q < TILES ? wave + 4 * q : 0;
+        int i = 0;
+        while (tri(i + 1) <= t) ++i;
+        ri[q] = (16 * i + (lane & 15)) * kSlabPitch + (lane >> 4);
+        rj[q] = (16 * (t - tri(i)) + (lane & 15)) * kSlabPitch + (lane >> 4);
+    }
+    Slab<DG, MOMENTUM, MT> x(s, base, R, C);
+    const int64_t pace = static_cast<int64_t>(gridDim.x) * kSlab;
+    x.fetch(static_cast<int64_t>(blockIdx.x) * kSlab);
+    for (int k = threadIdx.x; k < P * P; k += kGramBlock) f[k] = F[matrix * P * P + k];
+    const double scale = scales[2 * matrix];
+    for (int64_t j0 = static_cast<int64_t>(blockIdx.x) * kSlab; j0 < n; j0 += pace) {
+        __syncthreads();
+        x.template put<false, false>(j0, slab, 1.0);
+        __syncthreads();
+        x.fetch(j0 + pace);
+        v4d z[MT] = {};
+#pragma unroll 4
+        for (int k = 0; k < P; k += 4) {
+            const int at = k + (lane >> 4);
+            const double v = slab[at * kSlabPitch + 16 * wave + (lane & 15)];
+#pragma unroll
+            for (int t = 0; t < MT; ++t) z[t] = mfma_f64(f[at * P + 16 * t + (lane & 15)], v, z[t]);
+        }
+#pragma unroll
+        for (int t = 0; t < MT; ++t)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) y[(16 * t + 4 * r + (lane >> 4)) * kSlabPitch + 16 * wave + (lane & 15)] = z[t][r] * scale;
+        __syncthreads();
+#pragma unroll 4
+        for (int k = 0; k < kSlab; k += 4)
+#pragma unroll
+            for (int q = 0; q < OWN; ++q) acc[q] = mfma_f64(y[ri[q] + k], y[rj[q] + k], acc[q]);
+    }
+    double* out = part + (matrix * gridDim.x + blockIdx.x) * (TILES * 256);
+#pragma unroll
+    for (int q = 0; q < OWN; ++q)
+        if (wave + 4 * q < TILES)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) out[(wave + 4 * q) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)] = acc[q][r];
+}
+
 // F of each matrix from its G G^T: one block a matrix, a wave for each 16 x 16 tile on and below the diagonal. What a
 // product leaves in a lane, four values of a column every four rows apart, is also what the next one wants from it: as
 // the second factor as it stands, as the first one, of a symmetric matrix, from the tile across the diagonal. So tiles lie in
@@ -900,10 +969,16 @@ struct Coefs {
     float v[3 * kOrthMaxSteps];
 };
 
-template <int MT>
+// A is of F X for the F that is there (`again`), or of G. Shifts in units of A's trace: of A at the beginning, and after each step.
+struct DeepCoefs : Coefs {
+    float first, shift[kOrthMaxSteps];
+    bool again;
+};
+
+template <int MT, bool DEEP>
 __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const double* __restrict__ sum, double* __restrict__ F,
-                                                                        double* __restrict__ scales, double eps, Coefs coefs,
-                                                                        int steps) {
+                                                                        double* __restrict__ scales, double eps,
+                                                                        std::conditional_t<DEEP, DeepCoefs, Coefs> coefs, int steps) {
     constexpr int P = 16 * MT, MATRIX = MT * MT * kTile;
     constexpr bool ROOM = MT <= 3;  // for what would otherwise take the place of something that is still being read
     __shared__ __attribute__((aligned(16))) char lds[(ROOM ? 5 : 3) * MATRIX];
@@ -948,11 +1023,20 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     };
     auto put = [&](char* M, const v4d& v) {
         char* at = M + (ti * MT + tj) * kTile + 16 * lane;
+        // row c of the transpose: value c / 4 of the lanes of c mod 4
+        const int c = lane & 15;
+        char* across = M + (tj * MT + ti) * kTile + kTile / 2 * (c >> 3) + 256 * (c & 3) + 16 * (lane >> 4) + 8 * (c >> 2 & 1);
+        if (DEEP && ti == tj) {  // what lies below the diagonal, on both sides of it
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (row + 4 * r >= col) *reinterpret_cast<double*>(at + kTile / 2 * (r >> 1) + 8 * (r & 1)) = v[r];
+                if (row + 4 * r > col) *reinterpret_cast<double*>(across + 64 * r) = v[r];
+            }
+            return;
+        }
         *reinterpret_cast<v2d*>(at) = v2d{v[0], v[1]};
         *reinterpret_cast<v2d*>(at + kTile / 2) = v2d{v[2], v[3]};
-        if (ti != tj) {  // row c of the transpose: value c / 4 of the lanes of c mod 4
-            const int c = lane & 15;
-            char* across = M + (tj * MT + ti) * kTile + kTile / 2 * (c >> 3) + 256 * (c & 3) + 16 * (lane >> 4) + 8 * (c >> 2 & 1);
+        if (ti != tj) {
 #pragma unroll
             for (int r = 0; r < 4; ++r) *reinterpret_cast<double*>(across + 64 * r) = v[r];
         }
@@ -965,23 +1049,55 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     for (int r = 0; r < 4; ++r) a[r] = sum[(matrix * tri(MT) + wave) * 256 + (4 * r + (lane >> 4)) * 16 + (lane & 15)];
     put(A, a);
     __syncthreads();
-    double norm = 0.0;  // of the diagonal, the same in every wave
-    const int c = lane & 15;
+    auto trace = [&] {  // of what lies in A's place, the same in every wave
+        double x = 0.0;
+        const int c = lane & 15;
 #pragma unroll
-    for (int k = 0; k < MT; ++k)
-        norm += *reinterpret_cast<const double*>(A + k * (MT + 1) * kTile + kTile / 2 * (c >> 3) + 256 * (c & 3) + 16 * c + 8 * (c >> 2 & 1));
+        for (int k = 0; k < MT; ++k)
+            x += *reinterpret_cast<const double*>(A + k * (MT + 1) * kTile + kTile / 2 * (c >> 3) + 256 * (c & 3) + 16 * c + 8 * (c >> 2 & 1));
 #pragma unroll
-    for (int k = 1; k < 16; k *= 2) norm += __shfl_xor(norm, k);
+        for (int k = 1; k < 16; k *= 2) x += __shfl_xor(x, k);
+        return x;
+    };
+    auto shifted = [&](const v4d& v, double by) {
+        v4d x = v;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = row + 4 * r == col ? x[r] + by : x[r];
+        return x;
+    };
+    double norm = trace();
+    bool fresh = true;  // F is the identity still
+    if constexpr (DEEP) fresh = !coefs.again;
+    const double square = norm;
     norm = __builtin_sqrt(norm);
-    const double scale = norm < __builtin_inf() ? 1.0 / (norm + eps) : __builtin_nan("");
+    double scale = norm < __builtin_inf() ? 1.0 / (norm + eps) : __builtin_nan("");
+    if (!fresh) scale = 1.0;
     a = a * scale * scale;
     double by = scale * scale;  // what A in LDS lacks
+    if constexpr (DEEP) {
+        a = shifted(a, coefs.first * (square * scale * scale));
+        __syncthreads();
+        put(A, a);
+        if (!fresh) {
+            v4d q;
+#pragma unroll
+            for (int r = 0; r < 4; ++r) q[r] = F[matrix * P * P + (row + 4 * r) * P + col];
+            put(Q, q);
+        }
+        __syncthreads();
+        by = 1.0;
+    }
     for (int k = 0; k < steps; ++k) {
         const double ca = co[3 * k], cb = co[3 * k + 1], cc = co[3 * k + 2];
+        double shift = 0.0;
+        if constexpr (DEEP) {
+            a = tile(A, ti, tj);  // the same on both sides of the diagonal
+            shift = coefs.shift[k] * trace();
+        }
         v4d p = product(A, A), t;
 #pragma unroll
         for (int r = 0; r < 4; ++r) p[r] = __builtin_fma(cc, p[r] * by * by, __builtin_fma(cb, a[r], row + 4 * r == col ? ca : 0.0));
-        if (steps == 1) {
+        if (fresh && steps == 1) {
             f = p;
             break;
         }
@@ -991,7 +1107,7 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
             f = product(S, Q);
             break;
         }
-        if (k == 0) {
+        if (fresh && k == 0) {
             f = p;
             t = product(S, A) * by;
             by = 1.0;
@@ -1007,6 +1123,7 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
         }
         __syncthreads();
         a = product(S, T);
+        if constexpr (DEEP) a = shifted(a, shift);
         if constexpr (!ROOM) __syncthreads();
         put(A, a);
         __syncthreads();
@@ -1015,7 +1132,7 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
     for (int r = 0; r < 4; ++r)
         if (row + 4 * r >= col)
             F[matrix * P * P + (row + 4 * r) * P + col] = F[matrix * P * P + col * P + row + 4 * r] = f[r];
-    if (threadIdx.x == 0) {
+    if (fresh && threadIdx.x == 0) {
         scales[2 * matrix] = scale;
         scales[2 * matrix + 1] = norm < 0x1p-60 ? kFar : norm > 0x1p60 ? 1.0 / kFar : 1.0;
     }
@@ -1023,12 +1140,11 @@ __global__ __launch_bounds__(64 * tri(MT)) void orth_narrow_poly_kernel(const do
 
 // F X, 64 columns at a time: four waves take 16 each. F has values of a^5 = 485 where X has small singular values,
 // whose products with the large ones cancel: an fp32 result is formed in 64 bits, or it would be off by 485
-// roundings of X there (one for bf16 in 32). 24 x 16384 fp32 4.9 us, which is latency.
-template <int DG, int DO, bool MOMENTUM, int MT>
+// roundings of X there (one for bf16 in 32, but for the larger F of many steps). 24 x 16384 fp32 4.9 us, which is latency.
+template <int DG, int DO, bool MOMENTUM, int MT, bool WIDE>
 __global__ __launch_bounds__(256) void orth_narrow_apply_kernel(Source s, const double* __restrict__ F, const double* __restrict__ scales,
                                                                 Result res) {
     constexpr int P = 16 * MT;
-    constexpr bool WIDE = DO == BIRKHOFF4_F32;
     using Value = std::conditional_t<WIDE, double, float>;
     using Sums = std::conditional_t<WIDE, v4d, v4f>;
     __shared__ float slab[P * kSlabPitch];
@@ -1378,12 +1494,34 @@ struct OrthCall {
     double eps;
 };
 
+// The most of |a + b t + c t^2|, t the square of a singular value from 0 to sqrt(2), and at least one. (A larger
+// one that a step leaves below 2 has grown by less than sqrt(2), which the room from 8 to 16 is for.)
+double most_of(const float* c) {
+    auto at = [&](double t) { return __builtin_fabs(c[0] + t * (c[1] + t * static_cast<double>(c[2]))); };
+    double most = 1.0;
+    for (const double t : {0.0, 2.0, c[2] != 0.f ? -0.5 * c[1] / c[2] : 0.0})
+        if (t >= 0.0 && t <= 2.0 && at(t) > most) most = at(t);
+    return most;
+}
+
+// What the steps of a narrow matrix may multiply a value by, where they are taken in one run, and in the first run of more.
+// (Five of the usual steps have 485. 24 x 1024 of rank one in fp32: eight of them in one run are 3e-5 off, ten 5e-2.)
+constexpr double kNarrowGrowth = 512.0, kNarrowFirst = 64.0;
+
 template <int DG, int DO, bool MOMENTUM, int MT>
 int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
+    constexpr bool WIDE = DO == BIRKHOFF4_F32;
     double* sum = reinterpret_cast<double*>(work);
     double* scales = reinterpret_cast<double*>(work + s.group * s.e);
     double* F = reinterpret_cast<double*>(work + s.group * (s.e + 16));
-    const bool rows16 = DG == BIRKHOFF4_BF16 && DO == BIRKHOFF4_BF16 && !MOMENTUM && s.R <= s.C;
+    double growth = 1.0;
+    int begin = 0;  // steps of the first run
+    for (int k = 0; k < call.steps; ++k) {
+        growth *= most_of(call.coefs + 3 * k);
+        if (growth <= kNarrowFirst && begin == k) begin = k + 1;
+    }
+    const bool deep = !(growth <= kNarrowGrowth);
+    const bool rows16 = DG == BIRKHOFF4_BF16 && DO == BIRKHOFF4_BF16 && !MOMENTUM && s.R <= s.C && !deep;
     // long sums where they leave a block for every compute unit
     const int run = s.group * ((s.n + 1023) / 1024) >= 256 ? 256 : 64;
     const int64_t most = rows16 ? (s.n + 4 * run - 1) / (4 * run) : s.parts, parts = s.parts < most ? s.parts : most;
@@ -1391,31 +1529,60 @@ int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStrea
     Coefs coefs = {};
     for (int k = 0; k < 3 * call.steps; ++k) coefs.v[k] = call.coefs[k];
     const int64_t slabs = (s.n + kSlab - 1) / kSlab;
+    DeepCoefs start = {coefs}, rest = {};
+    if (deep) {
+        // A's entries are sums of that many products, one after the other. A step is two products of P terms and p itself,
+        // of matrices of which |p| may be as large as `most`, and whose Frobenius norms are up to sqrt(P) times their largest value.
+        constexpr double P = 16 * MT;
+        rest.first = static_cast<float>(((slabs + parts - 1) / parts * kSlab + parts / 16 + 32) * 0x1p-53);
+        for (int k = begin; k < call.steps; ++k) {
+            const double p = most_of(call.coefs + 3 * k);
+            for (int e = 0; e < 3; ++e) rest.v[3 * (k - begin) + e] = call.coefs[3 * k + e];
+            rest.shift[k - begin] = static_cast<float>(2.0 * P * __builtin_sqrt(P) * 0x1p-53 * p * p);
+        }
+        rest.again = begin > 0;
+    }
     for (int64_t first = 0; first < s.B; first += s.group) {
         const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
+        auto join = [&] {
+            if (parts > 1)
+                launch_kernel(orth_narrow_join_kernel, dim3(16 * tri(MT), L), dim3(256), 0, stream, part, sum,
+                              static_cast<int>(parts), 256 * tri(MT));
+        };
         if (rows16)
             launch_kernel(orth_narrow16_gram_kernel<MT>, dim3(static_cast<unsigned>(parts), L), dim3(256), 0, stream, call.src.G,
                           part, static_cast<int>(s.m), s.n, run, first);
         else
             launch_kernel((orth_narrow_gram_kernel<DG, MOMENTUM, MT>), dim3(static_cast<unsigned>(parts), L), dim3(kGramBlock), 0,
                           stream, call.src, part, s.R, s.C, first);
-        if (parts > 1)
-            launch_kernel(orth_narrow_join_kernel, dim3(16 * tri(MT), L), dim3(256), 0, stream, part, sum,
-                          static_cast<int>(parts), 256 * tri(MT));
-        launch_kernel((orth_narrow_poly_kernel<MT>), dim3(L), dim3(64 * tri(MT)), 0, stream, sum, F, scales, call.eps, coefs,
-                      call.steps);
+        join();
+        if (!deep) {
+            launch_kernel((orth_narrow_poly_kernel<MT, false>), dim3(L), dim3(64 * tri(MT)), 0, stream, sum, F, scales, call.eps, coefs,
+                          call.steps);
+        } else {
+            if (begin > 0) {
+                launch_kernel((orth_narrow_poly_kernel<MT, true>), dim3(L), dim3(64 * tri(MT)), 0, stream, sum, F, scales, call.eps,
+                              start, begin);
+                launch_kernel((orth_narrow_again_kernel<DG, MOMENTUM, MT>), dim3(static_cast<unsigned>(parts), L), dim3(kGramBlock), 0,
+                              stream, call.src, F, scales, part, s.R, s.C, first);
+                join();
+            }
+            launch_kernel((orth_narrow_poly_kernel<MT, true>), dim3(L), dim3(64 * tri(MT)), 0, stream, sum, F, scales, call.eps, rest,
+                          call.steps - begin);
+        }
         Result res = call.res;
         res.first = first;
         const int64_t turns = rows16 ? (s.n + 511) / 512 : slabs;  // what a block takes at a time
         int64_t blocks = kGramBlocks / L;  // two a compute unit (four: 32 of 80 x 32768 bf16 76 us instead of 69)
         if (blocks < 1) blocks = 1;
         if (blocks > turns) blocks = turns;
-        if (rows16)
+        if (rows16) {
             launch_kernel(orth_narrow16_apply_kernel<MT>, dim3(static_cast<unsigned>(blocks), L), dim3(256), 0, stream, call.src.G, F,
                           scales, res.out, static_cast<int>(s.m), s.n, first);
-        else
-            launch_kernel((orth_narrow_apply_kernel<DG, DO, MOMENTUM, MT>), dim3(static_cast<unsigned>(blocks), L), dim3(256), 0,
-                          stream, call.src, F, scales, res);
+        } else {
+            auto kern = deep ? orth_narrow_apply_kernel<DG, DO, MOMENTUM, MT, true> : orth_narrow_apply_kernel<DG, DO, MOMENTUM, MT, WIDE>;
+            launch_kernel(kern, dim3(static_cast<unsigned>(blocks), L), dim3(256), 0, stream, call.src, F, scales, res);
+        }
     }
     return launch_status();
 }
@@ -1496,16 +1663,6 @@ bool without_x(int64_t mp, int64_t np, int64_t L, int steps) {
     choose_tile(true, false, true, L, mp, np, across, &next);
     // a run of r steps: r polynomials, r - 1 products for q and 2 (r - 1) for A
     return runs * (gram + next) + (steps + 3 * (steps - runs)) * 1.1 * poly < 0.95 * steps * (gram + poly + next);
-}
-
-// The most of |a + b t + c t^2|, t the square of a singular value from 0 to sqrt(2), and at least one. (A larger
-// one that a step leaves below 2 has grown by less than sqrt(2), which the room from 8 to 16 is for.)
-double most_of(const float* c) {
-    auto at = [&](double t) { return __builtin_fabs(c[0] + t * (c[1] + t * static_cast<double>(c[2]))); };
-    double most = 1.0;
-    for (const double t : {0.0, 2.0, c[2] != 0.f ? -0.5 * c[1] / c[2] : 0.0})
-        if (t >= 0.0 && t <= 2.0 && at(t) > most) most = at(t);
-    return most;
 }
 
 template <int DG, int DO, bool MOMENTUM>
