@@ -404,9 +404,12 @@ int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype);
  *        too large or too small. A zero matrix with eps > 0 gives zeros; one with a NaN or infinite
  *        value gives NaN everywhere; the others of the batch are not touched by it.
  * An fp32 result is about what fp32 products give; with a side of at most 80, what 64-bit ones
- * do (where the steps' largest |a + b t + c t^2| for t from 0 to 2 multiply to more than 512, as
- * six of the usual steps do: of singular values above 2^-26 of |G|_F). For a bf16 result the products' factors are rounded to fp16 (11 bits; off by less than the
- * rounding of the result itself), but for the diagonals and a X; sums are fp32. The number of matrices
+ * do. For a bf16 result the products' factors are rounded to fp16 (11 bits), but for the diagonals
+ * and a X; sums are fp32: off by less than the rounding of the result itself, by up to three times
+ * it for matrices of low rank. Steps whose largest |a + b t + c t^2|, t from 0 to 2, multiply to
+ * more than 512 (as six of the usual ones do) make more of small values: a bf16 result's factors
+ * are then those of an fp32 one, and with a side of at most 80 singular values under 2^-26 of
+ * |G|_F stay behind what 64 bits would make of them. The number of matrices
  * may change the order of sums; within a batch it is the same for all of them.
  * work   workspace of birkhoff4_orth_work(B, rows, cols, out_dtype) bytes, 16-byte aligned, in use until
  *        the call's work on `stream` has ended. The other arrays may begin at any value. No output may

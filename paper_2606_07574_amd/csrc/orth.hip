@@ -20,7 +20,8 @@
 //     values are near to each other, are fp32 numbers of their own, and zeros in A and E as stored:
 //     (A^2)_ij = (D_i + D_j) A_ij + (A A)_ij off the diagonal, D_i^2 + (A A)_ii on it, and X <- (a + F_i) X_i + (E X)_i
 //     (a spread 400 x 3200 3.6e-3 off without, 0.45e-3 with them).
-// What is left, 0.2e-3 to 1.1e-3, is less than the result's own rounding to bf16, 1.7e-3.
+// What is left, 0.2e-3 to 1.1e-3, is less than the result's own rounding to bf16, 1.7e-3; of low rank it is up to 4.7e-3 (81 x
+// 81 of rank one). More than five of the usual steps would make more of it, and take two pieces (kMostGrowth).
 //
 // The products are of rows with rows (both operands have the summed index along their rows), so X is kept
 // in both orders.
@@ -1440,6 +1441,8 @@ struct OrthShape {
     int64_t x, xt, lo, a, e, d, more, bytes;  // bytes of a stored X, its other order, its lo, A, E, a diagonal, and the workspace
 };
 
+// split: products of two pieces each, which fp32 results have and bf16 ones of many steps. What those take of the
+// workspace is a bf16 result's, and one matrix's at least.
 int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape* s) {
     if (B < 0 || R < 0 || C < 0 || B > kOrthMaxMatrices || R > kOrthMaxSide || C > kOrthMaxSide) return BIRKHOFF4_ERR_SIZE;
     if (!dtype_ok(dtype)) return BIRKHOFF4_ERR_DTYPE;
@@ -1467,22 +1470,29 @@ int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape
     }
     s->mp = (s->m + kPad - 1) / kPad * kPad;
     s->np = (s->n + kPad - 1) / kPad * kPad;
-    const int64_t size = split ? 4 : 2;
-    s->x = s->xt = s->mp * s->np * size;
-    s->lo = split ? 0 : s->mp * s->np * 2;
-    s->e = s->mp * s->mp * size;  // E, and A without its lo
-    s->a = s->e + (split ? 0 : s->e);
-    // of steps without X: their products, which an update may take (and never does nearer to a square)
-    s->more = split && 4 * s->np >= 5 * s->mp ? 3 * s->e + 3 * s->mp * 4 : 0;
     s->d = s->mp * 4;
+    auto each = [&](bool pieces) {  // bytes of one matrix
+        const int64_t size = pieces ? 4 : 2;
+        s->x = s->xt = s->mp * s->np * size;
+        s->lo = pieces ? 0 : s->mp * s->np * 2;
+        s->e = s->mp * s->mp * size;  // E, and A without its lo
+        s->a = s->e + (pieces ? 0 : s->e);
+        // of steps without X: their products, which an update may take (and never does nearer to a square)
+        s->more = dtype == BIRKHOFF4_F32 && 4 * s->np >= 5 * s->mp ? 3 * s->e + 3 * s->mp * 4 : 0;
+        return 2 * (s->x + s->xt + s->lo) + s->a + s->e + 2 * s->d + s->more + kMostParts * 8;
+    };
     const int64_t turns = (R * C + 16 * kPrepBlock - 1) / (16 * kPrepBlock);
     s->parts = turns < kMostParts ? turns : kMostParts;
-    const int64_t each = 2 * (s->x + s->xt + s->lo) + s->a + s->e + 2 * s->d + s->more + kMostParts * 8;
-    s->group = kGroupBytes / each;
-    if (s->group < 1) s->group = 1;
-    if (s->group > B) s->group = B;
-    if (s->group > 32768) s->group = 32768;
-    s->bytes = s->group * each;
+    auto fit = [&](int64_t bytes, int64_t one) {
+        int64_t group = bytes / one;
+        if (group < 1) group = 1;
+        if (group > B) group = B;
+        return group > 32768 ? 32768 : group;
+    };
+    const int64_t pieces = each(true), usual = each(dtype == BIRKHOFF4_F32);
+    s->group = fit(kGroupBytes, usual);
+    s->bytes = s->group * usual > pieces ? s->group * usual : pieces;
+    if (split) s->group = fit(s->bytes, each(true));
     return BIRKHOFF4_OK;
 }
 
@@ -1492,6 +1502,7 @@ struct OrthCall {
     const float* coefs;
     int steps;
     double eps;
+    bool deep;  // more growth than kMostGrowth
 };
 
 // The most of |a + b t + c t^2|, t the square of a singular value from 0 to sqrt(2), and at least one. (A larger
@@ -1504,9 +1515,19 @@ double most_of(const float* c) {
     return most;
 }
 
-// What the steps of a narrow matrix may multiply a value by, where they are taken in one run, and in the first run of more.
-// (Five of the usual steps have 485. 24 x 1024 of rank one in fp32: eight of them in one run are 3e-5 off, ten 5e-2.)
-constexpr double kNarrowGrowth = 512.0, kNarrowFirst = 64.0;
+// What the steps may multiply a small value by (five of the usual ones have 485) where
+//   * those of a narrow matrix are taken in one run (24 x 1024 of rank one in fp32: eight of them are 3e-5 off, ten 5e-2);
+//   * a bf16 result's products are of one piece each, whose roundings grow by as much: of 1280 x 6000 with singular values
+//     from 1 to 1e-7, five are 1.7e-3 off, which is the result's own rounding, and eight would be 5.9e-3; of 150 x 260 of
+//     rank one 2.3e-3 and 4.2e-2.
+constexpr double kMostGrowth = 512.0;
+constexpr double kNarrowFirst = 64.0;  // in the first run of more
+
+double growth_of(const float* coefs, int steps) {
+    double growth = 1.0;
+    for (int k = 0; k < steps; ++k) growth *= most_of(coefs + 3 * k);
+    return growth;
+}
 
 template <int DG, int DO, bool MOMENTUM, int MT>
 int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
@@ -1514,13 +1535,9 @@ int launch_narrow(const OrthShape& s, const OrthCall& call, char* work, hipStrea
     double* sum = reinterpret_cast<double*>(work);
     double* scales = reinterpret_cast<double*>(work + s.group * s.e);
     double* F = reinterpret_cast<double*>(work + s.group * (s.e + 16));
-    double growth = 1.0;
+    const bool deep = call.deep;
     int begin = 0;  // steps of the first run
-    for (int k = 0; k < call.steps; ++k) {
-        growth *= most_of(call.coefs + 3 * k);
-        if (growth <= kNarrowFirst && begin == k) begin = k + 1;
-    }
-    const bool deep = !(growth <= kNarrowGrowth);
+    while (begin < call.steps && growth_of(call.coefs, begin + 1) <= kNarrowFirst) ++begin;
     const bool rows16 = DG == BIRKHOFF4_BF16 && DO == BIRKHOFF4_BF16 && !MOMENTUM && s.R <= s.C && !deep;
     // long sums where they leave a block for every compute unit
     const int run = s.group * ((s.n + 1023) / 1024) >= 256 ? 256 : 64;
@@ -1665,16 +1682,9 @@ bool without_x(int64_t mp, int64_t np, int64_t L, int steps) {
     return runs * (gram + next) + (steps + 3 * (steps - runs)) * 1.1 * poly < 0.95 * steps * (gram + poly + next);
 }
 
-template <int DG, int DO, bool MOMENTUM>
-int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
-    switch (s.mt) {
-        case 1: return launch_narrow<DG, DO, MOMENTUM, 1>(s, call, work, stream);
-        case 2: return launch_narrow<DG, DO, MOMENTUM, 2>(s, call, work, stream);
-        case 3: return launch_narrow<DG, DO, MOMENTUM, 3>(s, call, work, stream);
-        case 4: return launch_narrow<DG, DO, MOMENTUM, 4>(s, call, work, stream);
-        case 5: return launch_narrow<DG, DO, MOMENTUM, 5>(s, call, work, stream);
-    }
-    constexpr bool SPLIT = DO == BIRKHOFF4_F32;
+template <int DG, int DO, bool MOMENTUM, bool SPLIT>
+int launch_large(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
+    constexpr int KEPT = SPLIT ? BIRKHOFF4_F32 : BIRKHOFF4_BF16;  // the type that products which are not the last go by
     const bool tall = s.R > s.C;
     char* at = work;
     auto take = [&](int64_t bytes) {
@@ -1716,11 +1726,11 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
             return p;
         };
         auto gram = [&](int now) {
-            launch_product<SPLIT, GRAM, DO>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0, 0}, res, s.group, L,
+            launch_product<SPLIT, GRAM, KEPT>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0, 0}, res, s.group, L,
                                             s.mp, s.mp, stream);
         };
         auto poly = [&](const float* c, float plus) {
-            launch_product<SPLIT, POLY, DO>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
+            launch_product<SPLIT, POLY, KEPT>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
                                             stream);
         };
         auto next = [&](int now, const Plane& by, const float* diag, float keep, float add, bool last) {
@@ -1728,9 +1738,9 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
             if (last)
                 launch_product<SPLIT, LAST, DO>(g, res, s.group, L, s.mp, s.np, stream);
             else
-                launch_product<SPLIT, NEXT, DO>(g, res, s.group, L, s.mp, s.np, stream);
+                launch_product<SPLIT, NEXT, KEPT>(g, res, s.group, L, s.mp, s.np, stream);
         };
-        if constexpr (SPLIT && MOMENTUM) {
+        if constexpr (SPLIT && MOMENTUM && DO == BIRKHOFF4_F32) {
             const int runs = (call.steps + 2) / 3;
             if (s.more && without_x(s.mp, s.np, s.group, call.steps)) {
                 // q = p_k .. p_1 of a run and A' = p A p of its steps; a power of two keeps q's entries below 16
@@ -1740,7 +1750,7 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
                 float* dq[2];
                 for (float*& d : dq) d = reinterpret_cast<float*>(take_more(s.mp * 4));
                 auto pair = [&](const Plane& M, const float* dm, const Plane& N, const float* dn, const Plane& to, float* d, float by) {
-                    launch_product<SPLIT, PAIR, DO>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
+                    launch_product<SPLIT, PAIR, KEPT>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
                                                     stream);
                 };
                 for (int run = 0, k = 0; run < runs; ++run) {
@@ -1786,9 +1796,23 @@ int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_
     return launch_status();
 }
 
+template <int DG, int DO, bool MOMENTUM>
+int launch_orth(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
+    switch (s.mt) {
+        case 1: return launch_narrow<DG, DO, MOMENTUM, 1>(s, call, work, stream);
+        case 2: return launch_narrow<DG, DO, MOMENTUM, 2>(s, call, work, stream);
+        case 3: return launch_narrow<DG, DO, MOMENTUM, 3>(s, call, work, stream);
+        case 4: return launch_narrow<DG, DO, MOMENTUM, 4>(s, call, work, stream);
+        case 5: return launch_narrow<DG, DO, MOMENTUM, 5>(s, call, work, stream);
+    }
+    if constexpr (DO == BIRKHOFF4_BF16)
+        if (!call.deep) return launch_large<DG, DO, MOMENTUM, false>(s, call, work, stream);
+    return launch_large<DG, DO, MOMENTUM, true>(s, call, work, stream);
+}
+
 int64_t orth_work(int64_t B, int64_t R, int64_t C, int dtype) {
     OrthShape s;
-    if (int e = orth_shape(B, R, C, dtype, dtype == BIRKHOFF4_F32, &s)) return e;
+    if (int e = orth_shape(B, R, C, dtype, false, &s)) return e;
     return s.bytes;
 }
 
@@ -1796,8 +1820,9 @@ int64_t orth_work(int64_t B, int64_t R, int64_t C, int dtype) {
 int orth_call(const void* G, int g_dtype, float* M, float momentum, float ahead, void* out, int o_dtype, bool update, float lr,
               const float* lr_at, float decay, float scale, const float* coefs, int steps, float eps, void* work,
               int64_t work_bytes, int64_t B, int64_t R, int64_t C, hipStream_t stream) {
+    const bool known = coefs && steps >= 1 && steps <= kOrthMaxSteps, deep = known && !(growth_of(coefs, steps) <= kMostGrowth);
     OrthShape s;
-    if (int e = orth_shape(B, R, C, o_dtype, o_dtype == BIRKHOFF4_F32, &s)) return e;
+    if (int e = orth_shape(B, R, C, o_dtype, o_dtype == BIRKHOFF4_F32 || deep, &s)) return e;
     if (!dtype_ok(g_dtype)) return BIRKHOFF4_ERR_DTYPE;
     if (steps < 1 || steps > kOrthMaxSteps) return BIRKHOFF4_ERR_STEPS;
     if (!(eps >= 0.f && eps < __builtin_inff())) return BIRKHOFF4_ERR_EPS;
@@ -1813,7 +1838,7 @@ int orth_call(const void* G, int g_dtype, float* M, float momentum, float ahead,
     const Span ins[] = {{G, values * dtype_bytes(g_dtype)}, {lr_at, 4}};
     const Span outs[] = {{out, values * dtype_bytes(o_dtype)}, {M, values * 4}, {work, static_cast<size_t>(s.bytes)}};
     if (!disjoint(outs, 3, ins, 2)) return BIRKHOFF4_ERR_OVERLAP;
-    const OrthCall call = {{G, M, momentum, ahead}, {out, R, C, 0, R > C, update, lr, decay, scale, lr_at}, coefs, steps, eps};
+    const OrthCall call = {{G, M, momentum, ahead}, {out, R, C, 0, R > C, update, lr, decay, scale, lr_at}, coefs, steps, eps, deep};
     constexpr int F = BIRKHOFF4_F32, H = BIRKHOFF4_BF16;
     auto pick = [&](auto plain, auto with) { return update ? with : plain; };
     auto launch = g_dtype == H ? (o_dtype == H ? pick(launch_orth<H, H, false>, launch_orth<H, H, true>)

@@ -6,7 +6,7 @@ import torch
 
 import paper_2606_07574_amd as b4
 from tests._orth import COEFS, close, orth_ref, turn
-from tests._orth_rank import CUBIC, PAIRS, dependent, dependent_ref, fades
+from tests._orth_rank import CUBIC, PAIRS, carried, dependent, dependent_ref, fades
 
 pytestmark = pytest.mark.gpu
 
@@ -121,3 +121,47 @@ def test_captured():
         assert torch.equal(O, eager)
         O.fill_(float("nan"))
     close(eager, ref, narrow_bound(ref, 24, 25), "captured")
+
+
+def ordinary(shape, dtype, kind, seed):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    L, m, n = shape
+    normal = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    if kind == "spread":
+        return normal(*shape).to(dtype)
+    return (torch.matmul(normal(L, m, 8) * torch.exp(-0.3 * torch.arange(8, device="cuda")), normal(L, 8, n))).to(dtype)
+
+
+LARGE = [(kind, steps, coefs) for kind in ("spread", "low", "fades") for steps, coefs in ((6, COEFS), (8, COEFS), (10, COEFS), (25, CUBIC))]
+LARGE += [("spread", 64, COEFS), ("spread", 60, CUBIC), ("fades", 25, COEFS), ("fades", 64, COEFS), ("fades", 12, PAIRS * 6)]
+
+
+@pytest.mark.parametrize("kind,steps,coefs", LARGE, ids=[f"{k}-{run_id((s, c))}" for k, s, c in LARGE])
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(1, 150, 260), (2, 300, 140), (1, 1024, 1100)], ids=str)
+def test_many_steps_of_large_matrices(shape, dtype, kind, steps, coefs):
+    """No further off than products of two fp16 pieces each take it, whatever the result's type."""
+    if kind == "fades":
+        G = fades(min(shape[1:]), max(shape[1:]), dtype, 5, 1e-6)
+        G = turn(G) if shape[1] > shape[2] else G
+    else:
+        G = ordinary(shape, dtype, kind, 5)
+    label = f"{shape} {dtype} {kind} {run_id((steps, coefs))}"
+    print(label, flush=True)
+    ref, bound = orth_ref(G, steps, coefs, 0.0)
+    bound = bound + carried(G, steps, coefs)
+    close(b4.orth(G, steps, coefs, 0.0), ref, bound, label)
+    W, M = torch.zeros_like(G), torch.zeros(G.shape, device="cuda")
+    b4.orth_step(W, G, M, -1.0, 0.0, False, scale=1.0, steps=steps, coefs=coefs, eps=0.0)
+    close(W, ref, bound, label + " update")
+
+
+def test_many_steps_in_parts():
+    """A batch of which the workspace takes a part at a time: the same bits wherever a matrix stands."""
+    G = ordinary((2600, 100, 300), BF16, "spread", 6)
+    G[2599] = G[1300] = G[0]
+    O = b4.orth(G, 8)
+    ref, bound = orth_ref(G[:1], 8)
+    close(O[:1], ref, bound, "first")
+    assert torch.equal(O[0], O[1300])
+    close(O[2599:], ref, bound, "last")
