@@ -420,7 +420,8 @@ int birkhoff4_orth(const void* G, int g_dtype, void* out, int out_dtype, const f
 
 /* A weight update with momentum along orthogonalised directions, in place:
  *   M <- momentum M + G,   U = G + momentum M (nesterov != 0) or M,
- *   W <- (1 - r decay) W - r scale orth(U),   r = lr *lr_at.
+ *   W <- (1 - r decay) W - r scale orth(U),   r = lr *lr_at,
+ * for any momentum (of either sign).
  *
  * W      [B][rows][cols] in w_dtype (F32 or BF16, rounded to nearest even); M the same in fp32.
  * lr_at  a float in device memory, read when the work runs (a replayed graph takes what it is by

@@ -148,11 +148,14 @@ __device__ __forceinline__ void write4(void* out, int64_t at, int64_t n, const v
     }
 }
 
-// What is orthogonalised: G, or with a momentum M the direction G + ahead M (M renewed already).
+// What is orthogonalised: G, or with M, which is renewed before it, the direction G + momentum M or M.
 struct Source {
     const void* G;
     float* M;
-    float momentum, ahead;
+    float momentum;
+    bool nesterov;
+
+    __device__ __forceinline__ float direction(float g, float m) const { return nesterov ? __builtin_fmaf(momentum, m, g) : m; }
 };
 
 // M <- momentum M + G where there is one, and the sum of squares of each matrix's direction in 64 bits (no
@@ -169,7 +172,7 @@ __global__ __launch_bounds__(kPrepBlock) void orth_prep_kernel(Source s, double*
         float u = g;
         if constexpr (MOMENTUM) {
             *m = __builtin_fmaf(s.momentum, *m, g);
-            u = s.ahead < 0.f ? *m : __builtin_fmaf(s.ahead, *m, g);
+            u = s.direction(g, *m);
         }
         sum = __builtin_fma(static_cast<double>(u), static_cast<double>(u), sum);
     };
@@ -247,7 +250,7 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const doubl
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             float v = u[k][e];
-            if constexpr (MOMENTUM) v = s.ahead < 0.f ? m[k][e] : __builtin_fmaf(s.ahead, m[k][e], v);
+            if constexpr (MOMENTUM) v = s.direction(v, m[k][e]);
             // around the values zeros, whatever the scale
             tile[r][c + e] = r0 + r < R && c0 + c + e < C ? static_cast<float>(v * scale) : 0.f;
         }
@@ -831,7 +834,7 @@ struct Slab {
                     write4<BIRKHOFF4_F32>(s.M, at, there, m2);
                 }
 #pragma unroll
-                for (int e = 0; e < 4; ++e) u[e] = s.ahead < 0.f ? m2[e] : __builtin_fmaf(s.ahead, m2[e], u[e]);
+                for (int e = 0; e < 4; ++e) u[e] = s.direction(u[e], m2[e]);
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) *value(slab, line, c + e) = SCALED ? static_cast<float>(u[e] * scale) : u[e];
@@ -1817,7 +1820,7 @@ int64_t orth_work(int64_t B, int64_t R, int64_t C, int dtype) {
 }
 
 // The checks that both calls share, and the launches. `out`: what is written, W or the result.
-int orth_call(const void* G, int g_dtype, float* M, float momentum, float ahead, void* out, int o_dtype, bool update, float lr,
+int orth_call(const void* G, int g_dtype, float* M, float momentum, bool nesterov, void* out, int o_dtype, bool update, float lr,
               const float* lr_at, float decay, float scale, const float* coefs, int steps, float eps, void* work,
               int64_t work_bytes, int64_t B, int64_t R, int64_t C, hipStream_t stream) {
     const bool known = coefs && steps >= 1 && steps <= kOrthMaxSteps, deep = known && !(growth_of(coefs, steps) <= kMostGrowth);
@@ -1838,7 +1841,7 @@ int orth_call(const void* G, int g_dtype, float* M, float momentum, float ahead,
     const Span ins[] = {{G, values * dtype_bytes(g_dtype)}, {lr_at, 4}};
     const Span outs[] = {{out, values * dtype_bytes(o_dtype)}, {M, values * 4}, {work, static_cast<size_t>(s.bytes)}};
     if (!disjoint(outs, 3, ins, 2)) return BIRKHOFF4_ERR_OVERLAP;
-    const OrthCall call = {{G, M, momentum, ahead}, {out, R, C, 0, R > C, update, lr, decay, scale, lr_at}, coefs, steps, eps, deep};
+    const OrthCall call = {{G, M, momentum, nesterov}, {out, R, C, 0, R > C, update, lr, decay, scale, lr_at}, coefs, steps, eps, deep};
     constexpr int F = BIRKHOFF4_F32, H = BIRKHOFF4_BF16;
     auto pick = [&](auto plain, auto with) { return update ? with : plain; };
     auto launch = g_dtype == H ? (o_dtype == H ? pick(launch_orth<H, H, false>, launch_orth<H, H, true>)
@@ -1856,14 +1859,14 @@ int64_t birkhoff4_orth_work(int64_t B, int64_t rows, int64_t cols, int out_dtype
 
 int birkhoff4_orth(const void* G, int g_dtype, void* out, int out_dtype, const float* coefs, int steps, float eps, void* work,
                    int64_t work_bytes, int64_t B, int64_t rows, int64_t cols, hipStream_t stream) {
-    return orth_call(G, g_dtype, nullptr, 0.f, 0.f, out, out_dtype, false, 1.f, nullptr, 0.f, 1.f, coefs, steps, eps, work,
+    return orth_call(G, g_dtype, nullptr, 0.f, false, out, out_dtype, false, 1.f, nullptr, 0.f, 1.f, coefs, steps, eps, work,
                      work_bytes, B, rows, cols, stream);
 }
 
 int birkhoff4_orth_step(void* W, int w_dtype, const void* G, int g_dtype, float* M, float momentum, int nesterov, float lr,
                         const float* lr_at, float decay, float scale, const float* coefs, int steps, float eps, void* work,
                         int64_t work_bytes, int64_t B, int64_t rows, int64_t cols, hipStream_t stream) {
-    return orth_call(G, g_dtype, M, momentum, nesterov ? momentum : -1.f, W, w_dtype, true, lr, lr_at, decay, scale, coefs, steps,
+    return orth_call(G, g_dtype, M, momentum, nesterov != 0, W, w_dtype, true, lr, lr_at, decay, scale, coefs, steps,
                      eps, work, work_bytes, B, rows, cols, stream);
 }
 
