@@ -1,4 +1,4 @@
-"""What the library would launch, without a GPU: in a process of its own the library is loaded behind stand-ins for the
+"""What the library holds and would launch, without a GPU: in a process of its own the library is loaded behind stand-ins for the
 few functions of the HIP runtime that it calls, which write down each kernel's name, grid, block and first arguments
 and run nothing."""
 import json
@@ -22,6 +22,8 @@ void __hipRegisterFunction(void** m, const void* f, char* device, const char* na
                            void* block, void* grid, int* size) {
     (void)m, (void)device, (void)limit, (void)tid, (void)bid, (void)block, (void)grid, (void)size;
     if (count < 4096) known[count].f = f, known[count++].name = name;
+    printf("kernel %s\n", name);
+    fflush(stdout);
 }
 int hipStreamGetDevice(void* stream, int* device) { (void)stream; *device = 0; return 0; }
 int hipDeviceGetAttribute(int* value, int attribute, int device) { (void)attribute, (void)device; *value = 256; return 0; }
@@ -52,9 +54,13 @@ for line in sys.stdin:
 """
 
 
-def launches(calls, folder):
-    """calls: (function, kinds of its arguments: p(ointer), i(nt), l(ong), f(loat), c(oefficients), arguments). For each
-    (its code, [(kernel, template arguments, grid x, grid y, block, first argument, second one as an int)])."""
+def split(name):
+    """(kernel, its template's numbers) of a mangled name."""
+    kernel, values = re.match(r"_ZN12_GLOBAL__N_1\d+([a-z_0-9]+?_kernel)(?:I((?:L[bi]\d+E)+)E)?", name).groups()
+    return kernel, tuple(int(v) for v in re.findall(r"L[bi](\d+)E", values or ""))
+
+
+def run(calls, folder):
     source, stub = os.path.join(folder, "standin.c"), os.path.join(folder, "libstandin.so")
     with open(source, "w") as f:
         f.write(STANDIN)
@@ -62,16 +68,24 @@ def launches(calls, folder):
     run = subprocess.run([sys.executable, "-c", DRIVER, stub, build.LIB], input="\n".join(json.dumps(c) for c in calls), text=True,
                          capture_output=True, timeout=300)
     assert run.returncode == 0, run.stderr
+    return [line.split() for line in run.stdout.splitlines()]
+
+
+def kernels(folder):
+    """All kernels of the library."""
+    return {split(words[1]) for words in run([], folder) if words[0] == "kernel"}
+
+
+def launches(calls, folder):
+    """calls: (function, kinds of its arguments: p(ointer), i(nt), l(ong), f(loat), c(oefficients), arguments). For each
+    (its code, [(kernel, its template's numbers, grid x, grid y, block, first argument, second one as an int)])."""
     found, now = [], []
-    for line in run.stdout.splitlines():
-        word, *rest = line.split()
+    for word, *rest in run(calls, folder):
         if word == "done":
             found.append((int(rest[0]), now))
             now = []
-            continue
-        name, gx, gy, _, block, first, second = rest
-        kernel, values = re.match(r"_ZN12_GLOBAL__N_1\d+([a-z_0-9]+?_kernel)(?:I((?:L[bi]\d+E)+)E)?", name).groups()
-        values = tuple(int(v) for v in re.findall(r"L[bi](\d+)E", values or ""))
-        now.append((kernel, values, int(gx), int(gy), int(block), int(first), int(second)))
+        elif word == "launch":
+            name, gx, gy, _, block, first, second = rest
+            now.append((*split(name), int(gx), int(gy), int(block), int(first), int(second)))
     assert len(found) == len(calls)
     return found
