@@ -376,7 +376,10 @@ int birkhoff8_post_bwd(const float* P, const void* X, const float* h, const void
  * Y      [B][C] output in x_dtype (bf16 rounded to nearest even once); sums are fp32.
  * mean, rstd  [B] fp32 outputs mu and s, which the backward needs; NULL where they are not wanted.
  * eps >= 0 and finite (BIRKHOFF4_ERR_EPS). A row with a NaN or infinite value has NaN outputs; the
- * others are not touched by it. The arrays begin at 16 bytes, their rows at any value. */
+ * others are not touched by it. A row whose squares (x - mu)^2 add up past fp32's range (deviations
+ * of 1.8e19 / sqrt(C) and more) gets s = 0, so y = bias and dX = 0; one whose sum passes it NaN.
+ * Subnormal numbers count as zero: with eps = 0 a row of equal values, or of deviations below 1e-19,
+ * has NaN or infinite outputs. The arrays begin at 16 bytes, their rows at any value. */
 int birkhoff4_norm_fwd(const void* X, int x_dtype, const void* weight, const void* bias, int w_dtype, float eps, void* Y,
                        float* mean, float* rstd, int64_t B, int64_t C, hipStream_t stream);
 
@@ -384,7 +387,8 @@ int birkhoff4_norm_fwd(const void* X, int x_dtype, const void* weight, const voi
  * dX [B][C] (x_dtype), dweight and dbias [C] (w_dtype), each where it is not NULL. With B = 0 the
  * sums are written as zeros. work: a workspace of birkhoff4_norm_work(B, C, x_dtype) bytes, needed
  * where dweight or dbias is; its contents before and after mean nothing. The sums over the rows are
- * fp32, in an order that the sizes alone decide. */
+ * fp32, in an order that the sizes alone decide: up to 256 blocks' (for C > 8192, shares') own sums,
+ * one row behind the other, and then the sums of these. */
 int birkhoff4_norm_bwd(const void* X, int x_dtype, const void* weight, int w_dtype, const float* mean, const float* rstd,
                        const void* dY, void* dX, void* dweight, void* dbias, void* work, int64_t work_bytes, int64_t B,
                        int64_t C, hipStream_t stream);
