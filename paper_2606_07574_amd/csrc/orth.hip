@@ -754,8 +754,8 @@ __global__ __launch_bounds__(256 * KS, W * KS == 1 ? 4 : W * KS == 2 ? 2 : KS) v
 // commute). G is read twice, for the first A and for F X, whatever the steps; the direct form reads X twice a
 // step and launches three kernels for it. An error of A is multiplied by up to a^2 = 12 a step where the
 // singular value is small, so A and F are 64-bit numbers, from products of the inputs without rounding: the
-// result is nearer than fp32 products bring it. The matrix cores' 64-bit rate is the limit of m: its cube
-// runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps, of 52 that the kernel takes;
+// result is nearer than fp32 products bring it. LDS is the limit of m: three matrices of 5 x 5 tiles are 150 KB of it. The
+// cube of m runs on one compute unit a matrix (m = 80: 36 us of the matrix cores for five steps, of 52 that the kernel takes;
 // m = 24: 10), and G G^T of 80 rows takes them half as long as reading fp32 G does. 24 x 16384 fp32 takes 21 us,
 // 80 x 32768 97 (10 MB twice: 4 at the memory's rate).
 //
@@ -1670,10 +1670,12 @@ void launch_product(Product g, const Result& res, int64_t group, unsigned L, int
 // Whether an update's steps are taken two or three at a time without X: X <- q X with q the product of the steps'
 // p = a I + b A + c A^2, and A' = p A p instead of a new X X^T, all of them symmetric and of X's smaller side. For
 // five steps two X X^T and two products with X instead of five, and nine more of the smaller side. An error of A
-// is multiplied by up to a^2 = 12 a step, so A is formed anew after three: a direction is then off by up to 1.6
-// times what it is otherwise (2.3e-6 and 1.0e-6 of 256 x 1024; 2.1e-5, 1.6e-5 and in fp32 1.5e-5 where a
-// few directions are a hundred times the others), which an update's weights do not show, while an
-// orthogonalised matrix would: only updates of fp32 weights take it. 2560 x 10240: 3240 -> 2030 us.
+// is multiplied by up to a^2 = 12 a step, so A is formed anew after three. Directions off,
+// with X every step, without it, and in fp32 products: 2560 x 10240 of eight strong directions among weak ones after five
+// steps 1.6e-6, 6.5e-6 and 2.7e-6, after eight, whose runs are the worst of 2 to 12, 3.4e-6, 3.8e-5 and 1.1e-5; with independent
+// values after five 1.7e-6, 6.8e-7 and 6e-6; of singular values from 1 to 1e-7 after five 5e-6, 2e-5 and 8e-6. An update's
+// weights, of which they are a few hundredths, hardly show that, while an orthogonalised matrix would: only updates of fp32 weights
+// take it. 2560 x 10240: 3240 -> 2030 us.
 bool without_x(int64_t mp, int64_t np, int64_t L, int steps) {
     if (steps < 2) return false;
     const int runs = (steps + 2) / 3, along = static_cast<int>(np / panel_cols(true)), across = static_cast<int>(mp / panel_cols(true));
