@@ -952,7 +952,7 @@ def orth(G: torch.Tensor, steps: int = ORTH_STEPS, coefs=ORTH_COEFS, eps: float 
 
     coefs: (a, b, c), or one such triple for each step; entries of X, A and b A + c A^2 have to stay
     below 16. Returns a tensor like G; in float32 with what float32 products give, in bfloat16 with
-    products of values rounded to 11 bits (for more than five of the usual steps to 22). No derivative: an input that autograd records is refused."""
+    products of values rounded to 11 bits (to 22 in the steps before the last five). No derivative: an input that autograd records is refused."""
     _recorded(G)
     B, rows, cols = _matrices(G, "G")
     G = G.contiguous()

@@ -21,7 +21,8 @@
 //     (A^2)_ij = (D_i + D_j) A_ij + (A A)_ij off the diagonal, D_i^2 + (A A)_ii on it, and X <- (a + F_i) X_i + (E X)_i
 //     (a spread 400 x 3200 3.6e-3 off without, 0.45e-3 with them).
 // What is left, 0.2e-3 to 1.1e-3, is less than the result's own rounding to bf16, 1.7e-3; of low rank it is up to 4.7e-3 (81 x
-// 81 of rank one). More than five of the usual steps would make more of it, and take two pieces (kMostGrowth).
+// 81 of rank one). More than five of the usual steps would make more of it; the first of them take two pieces
+// (kMostGrowth).
 //
 // The products are of rows with rows (both operands have the summed index along their rows), so X is kept
 // in both orders.
@@ -269,6 +270,16 @@ __global__ __launch_bounds__(256) void orth_convert_kernel(Source s, const doubl
         for (int e = 0; e < 8; ++e) v[e] = tile[at + e][line];
         halves(v, &hi, &lo);
         store8<SPLIT>(turned, matrix, c0 + line, r0 + at, hi, lo);
+    }
+}
+
+// A matrix stored in pieces of 16 columns' hi and lo, into 32 columns' hi (and lo, where it is kept) of another place.
+__global__ __launch_bounds__(256) void orth_apart_kernel(Plane from, Plane to, int64_t cols) {
+    const int64_t matrix = blockIdx.y, pieces = from.rows * (cols / 8);
+    for (int64_t k = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x; k < pieces; k += static_cast<int64_t>(gridDim.x) * 256) {
+        const int64_t row = k / 2 % from.rows, col = k / 2 / from.rows * 16 + k % 2 * 8;
+        const int64_t at = matrix * from.stride + place<true>(from, row, col);
+        store8<false>(to, matrix, row, col, *reinterpret_cast<const h8*>(from.hi + at), *reinterpret_cast<const h8*>(from.hi + (at ^ 32)));
     }
 }
 
@@ -1444,8 +1455,8 @@ struct OrthShape {
     int64_t x, xt, lo, a, e, d, more, bytes;  // bytes of a stored X, its other order, its lo, A, E, a diagonal, and the workspace
 };
 
-// split: products of two pieces each, which fp32 results have and bf16 ones of many steps. What those take of the
-// workspace is a bf16 result's, and one matrix's at least.
+// split: products of two pieces each, which fp32 results have and the first steps of many for bf16 ones. What those take of
+// the workspace is a bf16 result's, and one matrix's at least.
 int orth_shape(int64_t B, int64_t R, int64_t C, int dtype, bool split, OrthShape* s) {
     if (B < 0 || R < 0 || C < 0 || B > kOrthMaxMatrices || R > kOrthMaxSide || C > kOrthMaxSide) return BIRKHOFF4_ERR_SIZE;
     if (!dtype_ok(dtype)) return BIRKHOFF4_ERR_DTYPE;
@@ -1522,7 +1533,8 @@ double most_of(const float* c) {
 //   * those of a narrow matrix are taken in one run (24 x 1024 of rank one in fp32: eight of them are 3e-5 off, ten 5e-2);
 //   * a bf16 result's products are of one piece each, whose roundings grow by as much: of 1280 x 6000 with singular values
 //     from 1 to 1e-7, five are 1.7e-3 off, which is the result's own rounding, and eight would be 5.9e-3; of 150 x 260 of
-//     rank one 2.3e-3 and 4.2e-2.
+//     rank one 2.3e-3 and 4.2e-2. The steps in front of the last ones take two pieces: 4096 x 4096 725 us each instead
+//     of 325.
 constexpr double kMostGrowth = 512.0;
 constexpr double kNarrowFirst = 64.0;  // in the first run of more
 
@@ -1687,9 +1699,18 @@ bool without_x(int64_t mp, int64_t np, int64_t L, int steps) {
     return runs * (gram + next) + (steps + 3 * (steps - runs)) * 1.1 * poly < 0.95 * steps * (gram + poly + next);
 }
 
-template <int DG, int DO, bool MOMENTUM, bool SPLIT>
+// The stored matrices of one form: X and its other order of this step and the next one's, A and E.
+struct Stored {
+    Plane x[2], xt[2], a, e;
+};
+
+// TWO: products of two pieces, of all steps for fp32 results, of all but the last ones for bf16 results. (The roundings of
+// those that follow grow by kMostGrowth at most: five of the usual steps.)
+template <int DG, int DO, bool MOMENTUM, bool TWO>
 int launch_large(const OrthShape& s, const OrthCall& call, char* work, hipStream_t stream) {
-    constexpr int KEPT = SPLIT ? BIRKHOFF4_F32 : BIRKHOFF4_BF16;  // the type that products which are not the last go by
+    constexpr std::bool_constant<TWO> begun{};
+    constexpr std::true_type two{};
+    constexpr std::false_type one{};
     const bool tall = s.R > s.C;
     char* at = work;
     auto take = [&](int64_t bytes) {
@@ -1697,32 +1718,39 @@ int launch_large(const OrthShape& s, const OrthCall& call, char* work, hipStream
         at += bytes * s.group;
         return bytes ? p : nullptr;
     };
-    Plane x[2], xt[2];
+    Stored p;
     for (int k = 0; k < 2; ++k) {
-        x[k] = {take(s.x), nullptr, s.mp, s.x};
-        xt[k] = {take(s.xt), nullptr, s.np, s.xt};
-        xt[k].lo = take(s.lo);
+        p.x[k] = {take(s.x), nullptr, s.mp, s.x};
+        p.xt[k] = {take(s.xt), nullptr, s.np, s.xt};
+        p.xt[k].lo = take(s.lo);
     }
-    Plane a = {take(s.e), nullptr, s.mp, s.e};
-    a.lo = take(SPLIT ? 0 : s.e);
-    const Plane e_first = {take(s.e), nullptr, s.mp, s.e};
+    p.a = {take(s.e), nullptr, s.mp, s.e};
+    p.a.lo = take(TWO ? 0 : s.e);
+    p.e = {take(s.e), nullptr, s.mp, s.e};
+    Stored q = p;  // the form of one piece in the same places: half of each, and the lo in the other half
+    if (TWO) q.xt[0].lo = p.xt[0].hi + s.xt / 2, q.xt[1].lo = p.xt[1].hi + s.xt / 2, q.a.lo = p.a.hi + s.e / 2;
     float* const da = reinterpret_cast<float*>(take(s.d));
     float* const de_first = reinterpret_cast<float*>(take(s.d));
     double* sums = reinterpret_cast<double*>(take(kMostParts * 8));
     char* const rest = at;  // s.more bytes a matrix
-    const int along = static_cast<int>(s.np / panel_cols(SPLIT)), across = static_cast<int>(s.mp / panel_cols(SPLIT));
+    int turn = 0;  // the first step of one piece
+    if (DO == BIRKHOFF4_F32) turn = call.steps;
+    else if (TWO)
+        for (turn = call.steps - 1; turn > 0 && growth_of(call.coefs + 3 * (turn - 1), call.steps - turn + 1) <= kMostGrowth;) --turn;
+    auto along = [&](auto split) { return static_cast<int>(s.np / panel_cols(decltype(split)::value)); };
+    auto across = [&](auto split) { return static_cast<int>(s.mp / panel_cols(decltype(split)::value)); };
     for (int64_t first = 0; first < s.B; first += s.group) {
         const unsigned L = static_cast<unsigned>(s.B - first < s.group ? s.B - first : s.group);
         launch_kernel((orth_prep_kernel<DG, MOMENTUM>), dim3(static_cast<unsigned>(s.parts), L), dim3(kPrepBlock), 0, stream,
                       call.src, sums, s.R * s.C, first);
         const int64_t Rp = tall ? s.np : s.mp, Cp = tall ? s.mp : s.np;
         const int64_t tiles = Cp / kConvert * (Rp / kConvert);
-        launch_kernel((orth_convert_kernel<DG, MOMENTUM, SPLIT>), dim3(static_cast<unsigned>((L * tiles + 7) / 8 * 8)), dim3(256), 0,
-                      stream, call.src, sums, static_cast<int>(s.parts), call.eps, tall ? xt[0] : x[0], tall ? x[0] : xt[0], s.R, s.C,
-                      first, L, static_cast<unsigned>(tiles), static_cast<unsigned>(Cp / kConvert));
+        launch_kernel((orth_convert_kernel<DG, MOMENTUM, TWO>), dim3(static_cast<unsigned>((L * tiles + 7) / 8 * 8)), dim3(256), 0,
+                      stream, call.src, sums, static_cast<int>(s.parts), call.eps, tall ? p.xt[0] : p.x[0], tall ? p.x[0] : p.xt[0], s.R,
+                      s.C, first, L, static_cast<unsigned>(tiles), static_cast<unsigned>(Cp / kConvert));
         Result res = call.res;
         res.first = first;
-        Plane e = e_first;  // which changes places with others below
+        Plane e = p.e;  // which changes places with others below
         float* de = de_first;
         char* free = rest;
         [[maybe_unused]] auto take_more = [&](int64_t bytes) {
@@ -1730,44 +1758,47 @@ int launch_large(const OrthShape& s, const OrthCall& call, char* work, hipStream
             free += bytes * s.group;
             return p;
         };
-        auto gram = [&](int now) {
-            launch_product<SPLIT, GRAM, KEPT>({x[now], x[now], {}, a, a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp, along, 0, 0, 0}, res, s.group, L,
-                                            s.mp, s.mp, stream);
+        auto gram = [&](auto split, const Stored& m, int now) {
+            constexpr bool S = decltype(split)::value;
+            launch_product<S, GRAM, S ? BIRKHOFF4_F32 : BIRKHOFF4_BF16>({m.x[now], m.x[now], {}, m.a, m.a, nullptr, da, 0.f, 0.f, nullptr, 0.f, s.mp,
+                                                                         along(split), 0, 0, 0}, res, s.group, L, s.mp, s.mp, stream);
         };
-        auto poly = [&](const float* c, float plus) {
-            launch_product<SPLIT, POLY, KEPT>({a, a, a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
-                                            stream);
+        auto poly = [&](auto split, const Stored& m, const Plane& e, float* de, const float* c, float plus) {
+            constexpr bool S = decltype(split)::value;
+            launch_product<S, POLY, S ? BIRKHOFF4_F32 : BIRKHOFF4_BF16>({m.a, m.a, m.a, e, e, da, de, c[1], c[2], nullptr, plus, s.mp, across(split), 0,
+                                                                         0, 0}, res, s.group, L, s.mp, s.mp, stream);
         };
-        auto next = [&](int now, const Plane& by, const float* diag, float keep, float add, bool last) {
-            const Product g = {by, xt[now], xt[now], x[now ^ 1], xt[now ^ 1], diag, nullptr, keep, add, nullptr, 0.f, s.mp, across, 0, 0, 0};
-            if (last)
-                launch_product<SPLIT, LAST, DO>(g, res, s.group, L, s.mp, s.np, stream);
-            else
-                launch_product<SPLIT, NEXT, KEPT>(g, res, s.group, L, s.mp, s.np, stream);
+        auto next = [&](auto split, const Stored& m, int now, const Plane& by, const float* diag, float keep, float add, bool last) {
+            constexpr bool S = decltype(split)::value;
+            const Product g = {by, m.xt[now], m.xt[now], m.x[now ^ 1], m.xt[now ^ 1], diag, nullptr, keep, add, nullptr, 0.f, s.mp, across(split), 0, 0, 0};
+            if constexpr (S == (DO == BIRKHOFF4_F32))
+                if (last) return launch_product<S, LAST, DO>(g, res, s.group, L, s.mp, s.np, stream);
+            launch_product<S, NEXT, S ? BIRKHOFF4_F32 : BIRKHOFF4_BF16>(g, res, s.group, L, s.mp, s.np, stream);
         };
-        if constexpr (SPLIT && MOMENTUM && DO == BIRKHOFF4_F32) {
+        if constexpr (MOMENTUM && DO == BIRKHOFF4_F32) {
             const int runs = (call.steps + 2) / 3;
             if (s.more && without_x(s.mp, s.np, s.group, call.steps)) {
                 // q = p_k .. p_1 of a run and A' = p A p of its steps; a power of two keeps q's entries below 16
+                const Plane& a = p.a;
                 Plane t = e, q[2] = {e, e};
                 t.hi = take_more(s.e), q[0].hi = take_more(s.e), q[1].hi = take_more(s.e);
                 float* dt = reinterpret_cast<float*>(take_more(s.mp * 4));
                 float* dq[2];
                 for (float*& d : dq) d = reinterpret_cast<float*>(take_more(s.mp * 4));
                 auto pair = [&](const Plane& M, const float* dm, const Plane& N, const float* dn, const Plane& to, float* d, float by) {
-                    launch_product<SPLIT, PAIR, KEPT>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across, 0, 0, 0}, res, s.group, L, s.mp, s.mp,
+                    launch_product<true, PAIR, BIRKHOFF4_F32>({M, N, N, to, to, dm, d, 0.f, by, dn, 0.f, s.mp, across(two), 0, 0, 0}, res, s.group, L, s.mp, s.mp,
                                                     stream);
                 };
                 for (int run = 0, k = 0; run < runs; ++run) {
                     const int length = (call.steps - k) / (runs - run);  // the shorter ones first
-                    gram(run & 1);
+                    gram(two, p, run & 1);
                     double most = 1.0;
                     float scale = 1.f;
                     Plane now = e;
                     float* dnow = de;
                     for (int i = 0; i < length; ++i, ++k) {
                         const float* c = call.coefs + 3 * k;
-                        poly(c, c[0]);
+                        poly(two, p, e, de, c, c[0]);
                         most *= most_of(c);
                         if (i > 0) {
                             float by = 1.f;
@@ -1786,16 +1817,29 @@ int launch_large(const OrthShape& s, const OrthCall& call, char* work, hipStream
                             }
                         }
                     }
-                    next(run & 1, now, dnow, 0.f, 1.f / scale, run + 1 == runs);
+                    next(two, p, run & 1, now, dnow, 0.f, 1.f / scale, run + 1 == runs);
                 }
                 continue;
             }
         }
-        for (int k = 0; k < call.steps; ++k) {
+        int now = 0;
+        auto step = [&](auto split, const Stored& m, int k) {
             const float* c = call.coefs + 3 * k;
-            gram(k & 1);
-            poly(c, 0.f);
-            next(k & 1, e, de, c[0], 1.f, k + 1 == call.steps);
+            gram(split, m, now);
+            poly(split, m, m.e, de, c, 0.f);
+            next(split, m, now, m.e, de, c[0], 1.f, k + 1 == call.steps);
+            now ^= 1;
+        };
+        for (int k = 0; k < turn; ++k) step(begun, p, k);
+        if constexpr (DO == BIRKHOFF4_BF16) {
+            if (TWO) {
+                const int64_t blocks = (s.mp * s.np / 8 + 255) / 256;
+                const dim3 grid(static_cast<unsigned>(blocks < 4096 ? blocks : 4096), L);
+                launch_kernel(orth_apart_kernel, grid, dim3(256), 0, stream, p.x[now], q.x[now ^ 1], s.np);
+                launch_kernel(orth_apart_kernel, grid, dim3(256), 0, stream, p.xt[now], q.xt[now ^ 1], s.mp);
+                now ^= 1;
+            }
+            for (int k = turn; k < call.steps; ++k) step(one, q, k);
         }
     }
     return launch_status();

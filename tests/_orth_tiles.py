@@ -1,7 +1,7 @@
 """Sizes that run every form of the orthogonalisation's product kernel, and bounds that hold tile by tile."""
 import torch
 
-from tests._orth import COEFS, iterate, pieces, turn, wide
+from tests._orth import COEFS, iterate, pieces, triples, turn, wide
 
 F32, BF16 = torch.float32, torch.bfloat16
 
@@ -29,19 +29,39 @@ def sums(values, edge=32):
     return values
 
 
-def rounded(X, steps, split):
-    """The steps with the stated roundings, as in tests/_orth.py: products of one or two fp16 pieces, the diagonals apart."""
-    def product(M, N):
-        (mh, ml), (nh, nl) = pieces(M), pieces(N)
-        return mh @ nh + (mh @ nl + ml @ nh) if split else mh @ nh
+def growth(c):
+    """The most of |a + b t + c t^2| for t from 0 to 2, and at least one."""
+    a, b, c = c
+    at = [0.0, 2.0] + ([-0.5 * b / c] if c and 0 <= -0.5 * b / c <= 2 else [])
+    return max(1.0, *(abs(a + b * t + c * t * t) for t in at))
 
+
+def pairs_of(steps, coefs, dtype):
+    """How many of the steps, from the first one on, take products of two fp16 pieces: all for fp32 results; for bf16 ones
+    those in front of the last that multiply to 512 at most (and of the last one)."""
+    if dtype == F32:
+        return steps
+    coefs = triples(coefs, steps)
+    begin, product = steps - 1, growth(coefs[-1])
+    while begin > 0 and product * growth(coefs[begin - 1]) <= 512:
+        begin -= 1
+        product *= growth(coefs[begin])
+    return begin
+
+
+def rounded(X, steps, coefs, pairs):
+    """The steps with the stated roundings, as in tests/_orth.py: products of two fp16 pieces in the first `pairs` of them and
+    of one in the others, the diagonals apart."""
     def apart(M):
         D = M.diagonal(dim1=1, dim2=2)
         return D, sum(pieces(M - torch.diag_embed(D)))
 
-    a, b, c = COEFS
     Y = sum(pieces(X.float()))
-    for _ in range(steps):
+    for k, (a, b, c) in enumerate(triples(coefs, steps)):
+        def product(M, N):
+            (mh, ml), (nh, nl) = pieces(M), pieces(N)
+            return mh @ nh + (mh @ nl + ml @ nh) if k < pairs else mh @ nh
+
         D, R = apart(product(Y, turn(Y)))
         S = product(R, R) + (D[:, :, None] + D[:, None, :]) * R + torch.diag_embed(D * D)
         F, E = apart(b * (R + torch.diag_embed(D)) + c * S)
@@ -49,17 +69,28 @@ def rounded(X, steps, split):
     return Y.double()
 
 
-def close_tiles(got, G, steps, split, label, times=1.0):
+def rounded_ref(G, steps, coefs, eps=0.0):
+    """As orth_ref: float64's result, and per matrix three times the distance that these roundings take it, and one rounding
+    of a step's terms in two pieces."""
+    X, tall = wide(G, eps)
+    ref = iterate(X, triples(coefs, steps))
+    size = torch.linalg.vector_norm(ref, dim=(1, 2))
+    bound = 3 * torch.linalg.vector_norm(rounded(X, steps, coefs, pairs_of(steps, coefs, G.dtype)) - ref, dim=(1, 2))
+    return turn(ref) if tall else ref, bound + max(sum(abs(v) for v in c) for c in triples(coefs, steps)) * 2.0 ** -22 * size
+
+
+def close_tiles(got, G, steps, label, times=1.0):
     """Each tile's error from float64's steps of a wide G, within what another draw of the roundings makes of it. They are of
     one size all over a matrix of independent values: three times those of `rounded` in this tile and on average (`times`
     that), one rounding of a step's terms as in orth_ref, and half a step of got's type in every value."""
     X, _ = wide(G, 1e-7)
-    ref, model = iterate(X, [COEFS] * steps), rounded(X, steps, split)
+    pairs = pairs_of(steps, COEFS, G.dtype)
+    ref, model = iterate(X, [COEFS] * steps), rounded(X, steps, COEFS, pairs)
     half = {F32: 2.0 ** -24, BF16: 2.0 ** -8}[got.dtype]
     err, size = sums((got.double() - ref) ** 2).sqrt(), sums(ref ** 2).sqrt()
     own, count = sums((model - ref) ** 2), sums(torch.ones_like(ref))
     average = (model - ref).square().mean((1, 2), keepdim=True) * count
-    terms = sum(abs(c) for c in COEFS) * (2.0 ** -22 if split else 2.0 ** -11)
+    terms = sum(abs(c) for c in COEFS) * (2.0 ** -22 if pairs == steps else 2.0 ** -11)
     bound = times * (3 * (own + average).sqrt() + terms * size)
     bound = bound + half * (size + bound)
     worst = (err / bound).max().item()

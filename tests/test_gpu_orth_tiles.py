@@ -17,10 +17,9 @@ def spread(shape, dtype, seed):
 @pytest.mark.parametrize("shape,dtype,steps", ORTH, ids=str)
 def test_products(shape, dtype, steps):
     G = spread(shape, dtype, sum(shape))
-    split = dtype == F32 or steps > 5
     print(shape, dtype, steps, flush=True)
-    close_tiles(b4.orth(G, steps), G, steps, split, "wide")
-    close_tiles(turn(b4.orth(turn(G), steps)), G, steps, split, "tall")
+    close_tiles(b4.orth(G, steps), G, steps, "wide")
+    close_tiles(turn(b4.orth(turn(G), steps)), G, steps, "tall")
 
 
 @pytest.mark.parametrize("shape,dtype,steps", STEP, ids=str)
@@ -32,7 +31,7 @@ def test_products_of_updates(shape, dtype, steps):
         D = turn(G) if tall else G
         W, M = torch.zeros_like(D), torch.zeros_like(D)
         b4.orth_step(W, D, M, -1.0, 0.0, False, scale=1.0, steps=steps)
-        close_tiles(turn(W) if tall else W, G, steps, True, "tall" if tall else "wide", 1.6)
+        close_tiles(turn(W) if tall else W, G, steps, "tall" if tall else "wide", 1.6)
 
 
 @pytest.mark.parametrize("shape,dtype", [((14, 723, 723), BF16), ((1, 1326, 1707), BF16), ((1, 580, 3330), F32), ((52, 140, 524), F32)], ids=str)
@@ -67,7 +66,8 @@ def test_types(m, types, steps):
         array, _ = b4._steps(b4.ORTH_COEFS, steps)
         assert lib.birkhoff4_orth(G.data_ptr(), code(kind), out.data_ptr(), code(result), array, steps, 1e-7, work.data_ptr(), size,
                                   *shape, torch.cuda.current_stream().cuda_stream) == 0
-        ref, bound = orth_ref(G, steps, split=result == F32 or steps > 5)
+        # eight steps of bf16 results: the last five of one piece, where the side is more than 80
+        ref, bound = orth_ref(G, steps, split=result == F32 or (steps > 5 and m <= 80))
         close(out, ref, bound, f"{shape} {types} {steps}")
         W, M = torch.zeros(shape, dtype=result, device="cuda"), torch.zeros(shape, device="cuda")
         b4.orth_step(W, G, M, -1.0, 0.0, True, scale=1.0, steps=steps)
