@@ -410,12 +410,12 @@ int64_t birkhoff4_norm_work(int64_t B, int64_t C, int x_dtype);
  * An fp32 result is about what fp32 products give; with a side of at most 80, what 64-bit ones
  * do. For a bf16 result the products' factors are rounded to fp16 (11 bits), but for the diagonals
  * and a X; sums are fp32: off by less than the rounding of the result itself, by up to three times
- * it for matrices of low rank. Steps whose largest |a + b t + c t^2|, t from 0 to 2, multiply to
- * more than 512 (as six of the usual ones do) make more of small values: for a bf16 result those
- * in front of the last that multiply to 512 take the factors of an fp32 one, and with a side of at
- * most 80 singular values under 2^-26 of |G|_F stay behind what 64 bits would make of them. The
- * number of matrices
- * may change the order of sums; within a batch it is the same for all of them.
+ * it for matrices of low rank or of singular values that fade away. Steps whose largest
+ * |a + b t + c t^2|, t from 0 to 2, multiply to more than 512 (as six of the usual ones do) make
+ * more of small values: for a bf16 result those in front of the last that multiply to 512 take
+ * the factors of an fp32 one, and with a side of at most 80 singular values under 2^-26 of |G|_F
+ * stay behind what 64 bits would make of them. The number of matrices may change the order of
+ * sums; within a batch it is the same for all of them.
  * work   workspace of birkhoff4_orth_work(B, rows, cols, out_dtype) bytes, 16-byte aligned, in use until
  *        the call's work on `stream` has ended. The other arrays may begin at any value. No output may
  *        overlap another argument. rows and cols up to 2^20, the smaller of them up to 2^16, B up to

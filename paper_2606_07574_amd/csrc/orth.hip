@@ -20,7 +20,7 @@
 //     values are near to each other, are fp32 numbers of their own, and zeros in A and E as stored:
 //     (A^2)_ij = (D_i + D_j) A_ij + (A A)_ij off the diagonal, D_i^2 + (A A)_ii on it, and X <- (a + F_i) X_i + (E X)_i
 //     (a spread 400 x 3200 3.6e-3 off without, 0.45e-3 with them).
-// What is left, 0.2e-3 to 1.1e-3, is less than the result's own rounding to bf16, 1.7e-3; of low rank it is up to 4.7e-3 (81 x
+// What is left, 0.2e-3 to 1.1e-3, is less than the result's own rounding to bf16, 1.7e-3; of low rank it is up to 5e-3 (81 x
 // 81 of rank one). More than five of the usual steps would make more of it; the first of them take two pieces
 // (kMostGrowth).
 //
@@ -1532,9 +1532,9 @@ double most_of(const float* c) {
 // What the steps may multiply a small value by (five of the usual ones have 485) where
 //   * those of a narrow matrix are taken in one run (24 x 1024 of rank one in fp32: eight of them are 3e-5 off, ten 5e-2);
 //   * a bf16 result's products are of one piece each, whose roundings grow by as much: of 1280 x 6000 with singular values
-//     from 1 to 1e-7, five are 1.7e-3 off, which is the result's own rounding, and eight would be 5.9e-3; of 150 x 260 of
-//     rank one 2.3e-3 and 4.2e-2. The steps in front of the last ones take two pieces: 4096 x 4096 725 us each instead
-//     of 325.
+//     from 1 to 1e-7, five are 1.7e-3 off, which is the result's own rounding. The steps in front of the last ones take two
+//     pieces, 725 instead of 325 us each of 4096 x 4096: eight of them are 4.0e-3 off (with one piece throughout 5.9e-3) and 25
+//     1.7e-3 (1.3e-2), of 150 x 260 of rank one eight 1.9e-3 (4.2e-2; in fp32 products 4e-3).
 constexpr double kMostGrowth = 512.0;
 constexpr double kNarrowFirst = 64.0;  // in the first run of more
 
