@@ -166,3 +166,13 @@ def test_many_steps_in_parts():
     close(O[:1], ref, bound, "first")
     assert torch.equal(O[0], O[1300])
     close(O[2599:], ref, bound, "last")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16], ids=["f32", "bf16"])
+@pytest.mark.parametrize("shape", [(3, 24, 1000), (2, 500, 40), (1, 100, 700)], ids=str)
+def test_a_steep_first_step(shape, dtype):
+    """A first step that alone multiplies by more than the first run of a narrow matrix takes."""
+    G = ordinary(shape, dtype, "spread", 8)
+    coefs = [(1.0, 60.0, 0.0)] + [CUBIC] * 6
+    ref, bound = orth_ref(G, 7, coefs, 0.0, split=dtype == F32)
+    close(b4.orth(G, 7, coefs, 0.0), ref, bound, f"{shape} {dtype}")
